@@ -236,7 +236,7 @@ def _own_cache(case, max_rows, seed):
     import paper_2312_04916_amd as ee
     n_blocks, max_positions = _pool(case)
     cache = ee.Kv4Cache(1, case.get("heads", 1), case.get("kv_heads", 1), case.get("head_dim", 32), case["block"], n_blocks, case["seqs"],
-                        max_positions, max_rows)
+                        max_positions, max_rows, case.get("dtype", "bf16"))
     cache.free.copy_(_order(n_blocks, seed))
     return cache
 
@@ -408,7 +408,7 @@ def run(s):
         if own:
             c = s["cache"]
             c.append(0, s["k"], s["v"])
-            return c.read(0, s["slots"], s["k"].dtype)
+            return c.read(0, s["slots"])
         _plain_append(s["pool"], s["k"], s["v"], s["slots"])
         return _plain_read(s["pool"], s["slots"], s["k"].dtype)
     if own:
