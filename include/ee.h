@@ -386,6 +386,98 @@ int ee_decode_step_static(ee_model* m, ee_kv_cache* c, int n_seqs, const int32_t
                           const int32_t* tokens, const uint8_t* pending_mask, float threshold, int32_t* next_token,
                           int32_t* exit_layer, float* conf, void* stream);
 
+/* ---------------------------------------------------------------- a paged KV cache held in 4 bits
+ *
+ * Operators of their own next to the decode step above, for programs that keep request lengths on the GPU: K and V of
+ * n_kv_heads heads (n_heads query heads share them, n_heads / n_kv_heads each) lie in blocks of block_tokens positions,
+ * in 4 bits and 8 bits of scale per 32 elements.  A step of such a program is
+ *     ee_kv4_plan    blocks and slots of the step's rows, from the requests' lengths       once
+ *     ee_kv4_append  the rows' K and V into the cache                                      per layer
+ *     ee_kv4_attend  the rows' attention over what their requests hold                     per layer
+ * and nothing in it waits for the GPU, so that it can be captured into a graph.
+ *
+ * The 4 bits: 32 neighbouring elements of one head's vector share a power of two 2^e, e the least integer from -111 to
+ * 125 with max|x| <= 7 * 2^e; each element is held as the nearest of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} * 2^e, a tie going to the
+ * one with the even index, what lies above to 6.  (7 and not 6: up to 7 an element is off by at most one unit, the most that
+ * an element between 4 and 6 can be off as well.)  A group that holds an infinity or a NaN stands for 32 NaN.
+ * A power of two makes every held value exact in bf16: no kernel rounds when it reads the cache.
+ *
+ * Slots: position p of a request lies in slot table[request][p / block_tokens] * block_tokens + p % block_tokens, the same
+ * in every layer.  All the state that outlasts a call is the pool, the table and the stack of free blocks.
+ *
+ * Calls check what the host can see and return the codes above; lengths and slots are on the GPU, where a call that cannot
+ * be served is marked (served, slot -1) and every access stays inside the buffers whatever the lengths are. */
+
+typedef struct {
+    int32_t n_layers, n_heads, n_kv_heads, head_dim; /* head_dim in {32, 64, 128, 256}; n_heads a multiple of n_kv_heads */
+    int32_t dtype;         /* EE_F32 | EE_BF16: of the K, V and Q that go in and of what comes out */
+    int32_t block_tokens;  /* 16, 32, 64, 128 or 256 */
+    int32_t n_blocks;      /* of the pool */
+    int32_t max_seqs;      /* requests: 1 .. EE_KV4_MAX_SEQS */
+    int32_t max_positions; /* of one request: 1 .. 2^20 */
+    int32_t max_rows;      /* of one plan: 1 .. 2^22 */
+} ee_kv4_config;
+enum { EE_KV4_MAX_SEQS = 4096 };
+
+typedef struct ee_kv4 ee_kv4;
+
+/* Where the arrays lie that a plan keeps and writes (device memory, inside dev_state). */
+typedef struct {
+    int32_t* table;       /* [max_seqs][table_stride] block of each request's positions; valid: the first ceil(held / block_tokens) */
+    int32_t* free_blocks; /* [n_blocks] stack: the blocks that no request holds are its first n_blocks - sum ceil(held / block_tokens) */
+    int64_t* slots;       /* [max_rows] slot of each row, -1: none */
+    int32_t* positions;   /* [max_rows] position of each row in its request, -1: none */
+    int32_t* row_seq;     /* [max_rows] request of each row, -1: a row behind the last request's */
+    int32_t* row_start;   /* [max_seqs + 1] first row of each request; [n_seqs] = rows in all */
+    int32_t* served;      /* [max_seqs] 1: as asked, 0: refused (the pool is exhausted, or lengths out of range) */
+    int32_t* held_next;   /* [max_seqs] positions each request holds after the call: end, or held where it was refused */
+    int32_t* n_free;      /* [1] free blocks after the call */
+    int32_t table_stride; /* ceil(max_positions / block_tokens) */
+} ee_kv4_arrays;
+
+/* Sizes of the two device buffers: the pool (every layer's K and V) and the state (table, free blocks, the plan's arrays,
+ * parts that the attention's workgroups hand over). */
+int ee_kv4_bytes(const ee_kv4_config* cfg, size_t* pool_bytes, size_t* state_bytes);
+/* A cache over the caller's buffers.  Enqueues the initialisation of the state on `stream`: every block is free, in order. */
+int ee_kv4_create(const ee_kv4_config* cfg, void* dev_pool, size_t pool_bytes, void* dev_state, size_t state_bytes, void* stream,
+                  ee_kv4** out);
+int ee_kv4_free(ee_kv4* c);
+int ee_kv4_get_arrays(const ee_kv4* c, ee_kv4_arrays* out);
+
+/* Blocks, slots and rows of a step.  Request i (all that hold blocks are in the call: 0 <= i < n_seqs) held dev_held[i]
+ * positions, brings rows for positions dev_start[i] .. dev_end[i]-1 and holds dev_end[i] positions afterwards: a decode step
+ * (start = held, end = held + 1), one that carries deferred tokens (start < held), a prompt (start = 0), a step taken back
+ * (end < held), a request that ends (start = end = 0) or waits (start = end = held).  Rows are packed in the requests' order.
+ *   Blocks that are no longer needed go back on the stack of free blocks, the last request's first and of each request the
+ *   last block first; blocks that are needed come off its top in the requests' order.  So a plan that is taken back leaves the
+ *   stack as it was.  Where the free blocks do not suffice, the requests up to there are served, and behind it those that need
+ *   no block.
+ *   The call is a function of the lengths, the table and the stack: called again with the same lengths it gives the same.
+ * n_rows: rows that the caller has room for (0 <= n_rows <= max_rows of the config); rows beyond the requests' have slot -1, a
+ * request whose rows do not fit is refused.  max_rows_per_seq: most rows that a request brings (a request with more is
+ * refused); the attention's tiles follow from it: give 1 for a plain decode step.
+ * dev_held may be the held_next array of the plan before. */
+int ee_kv4_plan(ee_kv4* c, int n_seqs, const int32_t* dev_held, const int32_t* dev_start, const int32_t* dev_end, int n_rows,
+                int max_rows_per_seq, void* stream);
+
+/* K and V of n_rows rows into the slots dev_slots[n_rows] (NULL: the latest plan's, n_rows at most its).  Element (row, head,
+ * i) of K lies at dev_k[row * k_row_stride + head * k_head_stride + i]; strides in elements.  Rows whose slot is negative or
+ * beyond the pool are skipped.  No slot may occur twice in a call. */
+int ee_kv4_append(ee_kv4* c, int layer, int n_rows, const void* dev_k, int64_t k_row_stride, int64_t k_head_stride,
+                  const void* dev_v, int64_t v_row_stride, int64_t v_head_stride, const int64_t* dev_slots, void* stream);
+
+/* What the slots hold, in the config's dtype (exact): dev_k, dev_v [n_rows][n_kv_heads][head_dim]; either may be NULL.  Rows
+ * whose slot is negative or beyond the pool are zero. */
+int ee_kv4_read(ee_kv4* c, int layer, int n_rows, const int64_t* dev_slots, void* dev_k, void* dev_v, void* stream);
+
+/* Attention of the latest plan's rows over what their requests hold: row at position p sees positions max(0, p - window + 1)
+ * .. p (window 0: all up to p).  scores = q . k * scale (scale > 0; 0: 1 / sqrt(head_dim)), soft-max in fp32, weighted sum of V.
+ * dev_out [n_rows][n_heads][head_dim] contiguous; dev_lse [n_rows][n_heads] fp32 or NULL: log sum exp of the row's scores, with
+ * which results over several caches can be joined.  A row that sees nothing (its request was refused, or it belongs to
+ * none) gets zeros and -inf.  NaN in positions that a row does not see do not reach it. */
+int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride, int64_t q_head_stride, void* dev_out, float* dev_lse,
+                  float scale, int window, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -5,3 +5,4 @@ package only marshals arguments and uses PyTorch for device memory and streams. 
 fallback: importing :mod:`binding` fails loudly when the library has not been built.
 """
 from .binding import *  # noqa: F401,F403
+from .kv4 import Kv4Cache  # noqa: F401

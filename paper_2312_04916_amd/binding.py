@@ -22,7 +22,8 @@ EXPORTS = ["ee_strerror", "ee_last_hip_error", "ee_model_bytes", "ee_model_creat
            "ee_model_load", "ee_model_free", "ee_debug_set_logits", "ee_debug_step_confidences", "ee_debug_plan", "ee_debug_gemm_route", "ee_debug_rows_launch", "ee_debug_kv_past_caches", "ee_profile_begin", "ee_profile_end", "ee_profile_every", "ee_measure_stream_read", "ee_debug_lane_reductions", "ee_kv_cache_bytes", "ee_kv_cache_create",
            "ee_kv_cache_set_refeed", "ee_kv_cache_set_pipeline", "ee_kv_cache_reset", "ee_kv_cache_filled", "ee_kv_cache_pending", "ee_kv_cache_read",
            "ee_kv_cache_flush", "ee_kv_cache_free", "ee_debug_read_hidden", "ee_prefill", "ee_prefill_scored",
-           "ee_decode_step", "ee_decode_step_static"]
+           "ee_decode_step", "ee_decode_step_static",
+           "ee_kv4_bytes", "ee_kv4_create", "ee_kv4_free", "ee_kv4_get_arrays", "ee_kv4_plan", "ee_kv4_append", "ee_kv4_read", "ee_kv4_attend"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libee.so")
@@ -39,6 +40,16 @@ class ee_config(C.Structure):
 EE_EXIT_NO_NORM, EE_TIE_EMBEDDINGS, EE_EXIT_MLP, EE_EXIT_LAYER = 1, 2, 4, 8
 (EE_T_EXIT_MLP_NORM, EE_T_EXIT_WG, EE_T_EXIT_WU, EE_T_EXIT_WD, EE_T_EXIT_ATTN_NORM, EE_T_EXIT_WQ, EE_T_EXIT_WK, EE_T_EXIT_WV,
  EE_T_EXIT_WO) = range(14, 23)
+
+
+class ee_kv4_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_heads", "n_kv_heads", "head_dim", "dtype", "block_tokens", "n_blocks", "max_seqs",
+                                         "max_positions", "max_rows")]
+
+
+class ee_kv4_arrays(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("table", "free_blocks", "slots", "positions", "row_seq", "row_start", "served", "held_next",
+                                          "n_free")] + [("table_stride", C.c_int32)]
 
 
 class EeError(RuntimeError):
@@ -99,6 +110,15 @@ def lib():
         # step 40 us of host time)
         L.ee_decode_step.argtypes = [vp, vp, C.c_int, vp, vp, vp, vp, C.c_float, vp, vp, vp, vp]
         L.ee_decode_step_static.argtypes = L.ee_decode_step.argtypes
+        i32, i64 = C.c_int, C.c_int64
+        L.ee_kv4_bytes.argtypes = [C.POINTER(ee_kv4_config), C.POINTER(sz), C.POINTER(sz)]
+        L.ee_kv4_create.argtypes = [C.POINTER(ee_kv4_config), vp, sz, vp, sz, vp, C.POINTER(vp)]
+        L.ee_kv4_free.argtypes = [vp]
+        L.ee_kv4_get_arrays.argtypes = [vp, C.POINTER(ee_kv4_arrays)]
+        L.ee_kv4_plan.argtypes = [vp, i32, vp, vp, vp, i32, i32, vp]
+        L.ee_kv4_append.argtypes = [vp, i32, i32, vp, i64, i64, vp, i64, i64, vp, vp]
+        L.ee_kv4_read.argtypes = [vp, i32, i32, vp, vp, vp, vp]
+        L.ee_kv4_attend.argtypes = [vp, i32, vp, i64, i64, vp, vp, C.c_float, i32, vp]
         _lib = L
     return _lib
 

@@ -1155,6 +1155,11 @@ int prefill_large(ee_model* m, ee_kv_cache* c, int seq, const int32_t* tokens, i
 
 }  // namespace
 
+int ee::note_hip_error(int status) {
+    g_last_hip = status;
+    return EE_ERR_HIP;
+}
+
 extern "C" {
 
 const char* ee_strerror(int code) {

@@ -51,6 +51,9 @@ struct KvGeom {
 
 enum HeadMode { HEAD_RULE = 0, HEAD_EMIT = 1 };
 
+// Keeps a HIP status for ee_last_hip_error; returns EE_ERR_HIP.
+int note_hip_error(int status);
+
 // The next kernel launched by this thread reports its execution time through the event pair.
 void set_launch_events(hipEvent_t start, hipEvent_t stop);
 

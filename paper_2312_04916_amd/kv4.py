@@ -1,0 +1,144 @@
+"""ctypes binding of the 4-bit paged cache (ee_kv4_* of include/ee.h): argument marshalling, and the torch buffers it works in."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Tuple
+
+import torch
+
+from .binding import EE_BF16, EE_F32, _chk, ee_kv4_arrays, ee_kv4_config, lib
+
+_DTYPES = {EE_BF16: torch.bfloat16, EE_F32: torch.float32}
+_CODES = {torch.bfloat16: EE_BF16, torch.float32: EE_F32, "bf16": EE_BF16, "f32": EE_F32, EE_BF16: EE_BF16, EE_F32: EE_F32}
+
+
+def _raw_stream(stream, index: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+
+
+class Kv4Cache:
+    """Owns the pool, the state (torch, device) and the ee_kv4 handle.
+
+    Arrays of the latest plan, on the device, always at the same place: slots, positions, row_seq [max_rows], row_start
+    [max_seqs + 1], served, held_next [max_seqs], n_free [1]; table [max_seqs][blocks] and free [n_blocks] are the state that
+    outlasts it."""
+
+    def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, block_tokens: int, n_blocks: int, max_seqs: int,
+                 max_positions: int, max_rows: int, dtype="bf16", device="cuda:0", stream=None):
+        self.h = C.c_void_p()
+        if dtype not in _CODES:
+            raise ValueError(f"dtype {dtype}: bf16 or f32")
+        self.cfg = cfg = ee_kv4_config(n_layers, n_heads, n_kv_heads, head_dim, _CODES[dtype], block_tokens, n_blocks, max_seqs, max_positions,
+                                       max_rows)
+        pb, sb = C.c_size_t(), C.c_size_t()
+        _chk(lib().ee_kv4_bytes(C.byref(cfg), C.byref(pb), C.byref(sb)), "ee_kv4_bytes")
+        self.device, self.dtype = torch.device(device), _DTYPES[cfg.dtype]
+        self._index = self.device.index or 0
+        self.pool = torch.empty(pb.value, dtype=torch.uint8, device=self.device)
+        self.state = torch.empty(sb.value, dtype=torch.uint8, device=self.device)
+        _chk(lib().ee_kv4_create(C.byref(cfg), self.pool.data_ptr(), pb.value, self.state.data_ptr(), sb.value, _raw_stream(stream, self._index),
+                                 C.byref(self.h)), "ee_kv4_create")
+        a = ee_kv4_arrays()
+        _chk(lib().ee_kv4_get_arrays(self.h, C.byref(a)), "ee_kv4_get_arrays")
+
+        def view(ptr: int, n: int, dt) -> torch.Tensor:
+            at = ptr - self.state.data_ptr()
+            return self.state[at:at + n * dt.itemsize].view(dt)
+
+        self.table = view(a.table, max_seqs * a.table_stride, torch.int32).view(max_seqs, a.table_stride)
+        self.free = view(a.free_blocks, n_blocks, torch.int32)
+        self.slots = view(a.slots, max_rows, torch.int64)
+        self.positions = view(a.positions, max_rows, torch.int32)
+        self.row_seq = view(a.row_seq, max_rows, torch.int32)
+        self.row_start = view(a.row_start, max_seqs + 1, torch.int32)
+        self.served = view(a.served, max_seqs, torch.int32)
+        self.held_next = view(a.held_next, max_seqs, torch.int32)
+        self.n_free = view(a.n_free, 1, torch.int32)
+        self.n_rows = 0
+        # (calls of the loop over layers: looked up once)
+        L = lib()
+        self._plan, self._append, self._read, self._attend = L.ee_kv4_plan, L.ee_kv4_append, L.ee_kv4_read, L.ee_kv4_attend
+
+    def _lengths(self, t: torch.Tensor, n: int, what: str) -> int:
+        if t.dtype != torch.int32 or t.device != self.device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+            raise ValueError(f"{what}: int32[{n}] on {self.device}, contiguous")
+        return t.data_ptr()
+
+    def _vectors(self, t: torch.Tensor, heads: int, rows: Optional[int], what: str) -> Tuple[int, int, int]:
+        if t.dtype != self.dtype or t.device != self.device or t.dim() != 3:
+            raise ValueError(f"{what}: {self.dtype} [rows][heads][head_dim] on {self.device}")
+        n, h, d = t.shape
+        if h != heads or d != self.cfg.head_dim or (rows is not None and n != rows):
+            raise ValueError(f"{what}: shape {tuple(t.shape)}, expected [{'rows' if rows is None else rows}][{heads}][{self.cfg.head_dim}]")
+        sr, sh, sd = t.stride()
+        if sd != 1:
+            raise ValueError(f"{what}: the elements of a head must be contiguous")
+        return t.data_ptr(), sr, sh
+
+    def plan(self, held: torch.Tensor, start: torch.Tensor, end: torch.Tensor, n_rows: int, max_rows_per_seq: Optional[int] = None,
+             stream=None) -> None:
+        """ee_kv4_plan.  held, start, end: int32[n_seqs] on the device; max_rows_per_seq: n_rows where it is not given."""
+        n = held.shape[0]
+        code = self._plan(self.h, n, self._lengths(held, n, "held"), self._lengths(start, n, "start"), self._lengths(end, n, "end"), n_rows,
+                          n_rows if max_rows_per_seq is None else max_rows_per_seq, _raw_stream(stream, self._index))
+        if code:
+            _chk(code, "ee_kv4_plan")
+        self.n_rows = n_rows
+
+    def _slot_ptr(self, slots: torch.Tensor, rows: int) -> int:
+        if slots.dtype != torch.int64 or slots.device != self.device or slots.shape != (rows,) or not slots.is_contiguous():
+            raise ValueError(f"slots: int64[{rows}] on {self.device}, contiguous")
+        return slots.data_ptr()
+
+    def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, slots: Optional[torch.Tensor] = None, stream=None) -> None:
+        """ee_kv4_append.  k, v: [rows][n_kv_heads][head_dim], any strides of rows and heads; slots: the latest plan's where not
+        given."""
+        rows = k.shape[0]
+        kp, kr, kh = self._vectors(k, self.cfg.n_kv_heads, None, "k")
+        vp, vr, vh = self._vectors(v, self.cfg.n_kv_heads, rows, "v")
+        code = self._append(self.h, layer, rows, kp, kr, kh, vp, vr, vh, None if slots is None else self._slot_ptr(slots, rows),
+                            _raw_stream(stream, self._index))
+        if code:
+            _chk(code, "ee_kv4_append")
+
+    def read(self, layer: int, slots: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """ee_kv4_read -> k, v [rows][n_kv_heads][head_dim]: the values that the slots hold."""
+        rows = slots.shape[0]
+        p = self._slot_ptr(slots, rows)
+        k = torch.empty(rows, self.cfg.n_kv_heads, self.cfg.head_dim, dtype=self.dtype, device=self.device)
+        v = torch.empty_like(k)
+        code = self._read(self.h, layer, rows, p, k.data_ptr(), v.data_ptr(), _raw_stream(stream, self._index))
+        if code:
+            _chk(code, "ee_kv4_read")
+        return k, v
+
+    def attend(self, layer: int, q: torch.Tensor, scale: Optional[float] = None, window: int = 0, lse: bool = False,
+               out: Optional[torch.Tensor] = None, stream=None):
+        """ee_kv4_attend -> [rows][n_heads][head_dim], with lse=True also log sum exp [rows][n_heads].  q: the rows of the latest
+        plan, any strides of rows and heads; scale: 1 / sqrt(head_dim) where not given."""
+        if scale is not None and not scale > 0:
+            raise ValueError("scale: positive")
+        heads, hd = self.cfg.n_heads, self.cfg.head_dim
+        qp, qr, qh = self._vectors(q, heads, self.n_rows, "q")
+        if out is None:
+            out = torch.empty(self.n_rows, heads, hd, dtype=self.dtype, device=self.device)
+        elif out.dtype != self.dtype or out.device != self.device or out.shape != (self.n_rows, heads, hd) or not out.is_contiguous():
+            raise ValueError(f"out: {self.dtype} [{self.n_rows}][{heads}][{hd}] on {self.device}, contiguous")
+        s = torch.empty(self.n_rows, heads, dtype=torch.float32, device=self.device) if lse else None
+        code = self._attend(self.h, layer, qp, qr, qh, out.data_ptr(), s.data_ptr() if lse else None, scale or 0.0, window,
+                            _raw_stream(stream, self._index))
+        if code:
+            _chk(code, "ee_kv4_attend")
+        return (out, s) if lse else out
+
+    def close(self) -> None:
+        if self.h:
+            torch.cuda.synchronize()
+            lib().ee_kv4_free(self.h)
+            self.h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

@@ -153,3 +153,40 @@ def test_step_plan_rejects_bad_state():
     assert L.ee_debug_plan(3, f, -1, 4, 0, 1, None, None, None) == -7   # a flush ends in the last segment
     assert L.ee_debug_plan(0, f, 6, 4, 0, -1, None, None, None) == -7
     assert L.ee_debug_plan(3, None, 6, 4, 0, -1, None, None, None) == -7
+
+
+# ---------------------------------------------------------------- the 4-bit cache (host checks, no GPU)
+
+def test_kv4_configs_and_sizes():
+    L = ee.lib()
+    pb, sb = C.c_size_t(), C.c_size_t()
+
+    def code(**kw):
+        good = dict(n_layers=2, n_heads=8, n_kv_heads=2, head_dim=128, dtype=ee.EE_BF16, block_tokens=64, n_blocks=100, max_seqs=4,
+                    max_positions=1000, max_rows=64)
+        good.update(kw)
+        return L.ee_kv4_bytes(C.byref(ee.ee_kv4_config(**good)), C.byref(pb), C.byref(sb))
+
+    assert code() == 0
+    # 4 bits of each element and 8 of each 32, K and V
+    assert pb.value == 2 * 100 * 64 * 2 * 2 * (128 // 2 + 128 // 32)
+    assert sb.value > 4 * 16 * 4 + 100 * 4 + 64 * 16
+    for bad in (dict(n_layers=0), dict(n_heads=0), dict(n_kv_heads=0), dict(n_kv_heads=3), dict(n_heads=2048), dict(head_dim=96), dict(dtype=2),
+                dict(block_tokens=8), dict(block_tokens=48), dict(block_tokens=512), dict(n_blocks=0), dict(max_seqs=0), dict(max_seqs=4097),
+                dict(max_positions=0), dict(max_positions=(1 << 20) + 1), dict(max_rows=0), dict(max_rows=(1 << 22) + 1)):
+        assert code(**bad) == -1, bad
+    assert L.ee_kv4_bytes(None, None, None) == -7
+
+
+def test_kv4_null_handles_are_refused():
+    L = ee.lib()
+    h = C.c_void_p()
+    cfg = ee.ee_kv4_config(1, 1, 1, 64, ee.EE_BF16, 16, 4, 1, 64, 4)
+    assert L.ee_kv4_create(C.byref(cfg), None, 0, None, 0, None, C.byref(h)) == -7
+    assert L.ee_kv4_create(C.byref(cfg), 256, 1 << 30, 257, 1 << 30, None, C.byref(h)) == -7   # not 256-byte aligned
+    assert L.ee_kv4_create(C.byref(cfg), 256, 1, 256, 1 << 30, None, C.byref(h)) == -2         # too small
+    assert L.ee_kv4_plan(None, 1, None, None, None, 0, 0, None) == -7
+    assert L.ee_kv4_append(None, 0, 1, None, 0, 0, None, 0, 0, None, None) == -7
+    assert L.ee_kv4_read(None, 0, 1, None, None, None, None) == -7
+    assert L.ee_kv4_attend(None, 0, None, 0, 0, None, None, 0.0, 0, None) == -7
+    assert L.ee_kv4_get_arrays(None, None) == -7 and L.ee_kv4_free(None) == -7
