@@ -2,7 +2,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cmath>
 
 #include "ee_kv4.h"
 #include "ee_lanes.h"
@@ -14,6 +13,7 @@ namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -478,10 +478,14 @@ __device__ __forceinline__ uint32_t pair_of(uint32_t w, float unit, int b) {
 }
 
 template <int HD>
-struct TileRegs {
-    uint32_t k[HD / 32], v[HD / 32];
-    uint32_t ks[HD / 128 > 1 ? HD / 128 : 1];  // scales of the lane's key
-    uint32_t vs;                               // of the lane's four keys, in its column's group
+struct KeyRegs {  // of one tile of 16 positions
+    uint32_t w[HD / 32];
+    uint32_t sc[HD / 128 > 1 ? HD / 128 : 1];  // scales of the lane's key
+};
+template <int HD>
+struct ValueRegs {
+    uint32_t w[HD / 32];
+    uint32_t sc;  // of the lane's four keys, in its column's group
 };
 
 template <int N>
@@ -501,15 +505,19 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t (&w)[N]) {
 }
 
 template <int HD>
-__device__ __forceinline__ void load_tile(const char* tile, int lane, TileRegs<HD>& r) {
+__device__ __forceinline__ void load_keys(const char* tile, int lane, KeyRegs<HD>& r) {
     constexpr int LB = HD / 8, G = HD / 32;
-    load_words<G>(tile + lane * LB, r.k);
-    load_words<G>(tile + Kv4Tile::v_codes(HD) + lane * LB, r.v);
-    const char* ks = tile + Kv4Tile::k_scales(HD) + (lane & 15) * G;
-    if constexpr (G == 1) r.ks[0] = *(const uint8_t*)ks;
-    if constexpr (G == 2) r.ks[0] = *(const uint16_t*)ks;
-    if constexpr (G >= 4) load_words<G / 4>(ks, r.ks);
-    r.vs = *(const uint32_t*)(tile + Kv4Tile::v_scales(HD) + (lane & 15) * HD / 512 * 16 + (lane >> 4) * 4);
+    load_words<G>(tile + lane * LB, r.w);
+    const char* sc = tile + Kv4Tile::k_scales(HD) + (lane & 15) * G;
+    if constexpr (G == 1) r.sc[0] = *(const uint8_t*)sc;
+    if constexpr (G == 2) r.sc[0] = *(const uint16_t*)sc;
+    if constexpr (G >= 4) load_words<G / 4>(sc, r.sc);
+}
+template <int HD>
+__device__ __forceinline__ void load_values(const char* tile, int lane, ValueRegs<HD>& r) {
+    constexpr int LB = HD / 8, G = HD / 32;
+    load_words<G>(tile + Kv4Tile::v_codes(HD) + lane * LB, r.w);
+    r.sc = *(const uint32_t*)(tile + Kv4Tile::v_scales(HD) + (lane & 15) * HD / 512 * 16 + (lane >> 4) * 4);
 }
 
 __device__ __forceinline__ float scale_of(const uint32_t* words, int i) {  // byte i as 2^(byte - 127)
@@ -521,12 +529,15 @@ __device__ __forceinline__ uint32_t bytes_255(uint32_t w) {  // 0x80 in every by
     return (x - 0x01010101u) & ~x & 0x80808080u;
 }
 
+// What one workgroup leaves for another one of the same launch, maybe on another XCD.
+__device__ __forceinline__ void hand_over(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float handed(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
 // NT: bf16 terms of an element of Q (1: Q is bf16; 3: fp32, exactly), PT: of a probability.  UNITS: 16 entries each of a tile.
 template <int HD, int NT, int PT, int UNITS, int NW, typename ST>
-__global__ __launch_bounds__(NW * 64) void kv4_attend_kernel(Kv4Attend a) {
+__global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 : 3) : 1) void kv4_attend_kernel(Kv4Attend a) {
     constexpr int G = HD / 32, EPC = HD / 16, M = 16 * UNITS;
-    constexpr int CT = UNITS == 1 ? 4 : 2;  // tiles of 16 positions at a time
-    constexpr int STEPS = KV4_CHUNK / (16 * CT);
+    constexpr int CT = 2, STEPS = KV4_CHUNK / (16 * CT);  // tiles of 16 positions at a time: one contraction of P.V
     constexpr int LDO = HD + 4;
     __shared__ float s_o[NW * 16 * LDO];
     __shared__ float s_m[NW * 16], s_l[NW * 16];
@@ -608,13 +619,10 @@ __global__ __launch_bounds__(NW * 64) void kv4_attend_kernel(Kv4Attend a) {
         return table[t >> a.tiles_shift];
     };
     int blocks = n_it ? blocks_from(0) : 0;
-    auto load = [&](int it, TileRegs<HD>(&r)[CT]) {
-#pragma unroll
-        for (int t = 0; t < CT; ++t) {
-            const int tile = min(tile_at(it, t), last_tile);
-            const int block = __builtin_amdgcn_readlane(blocks, it % AHEAD * CT + t);
-            load_tile<HD>(base + (size_t)block * block_bytes + (size_t)(tile & in_block) * Kv4Tile::bytes(HD), lane, r[t]);
-        }
+    auto tile_addr = [&](int it, int t) {
+        const int tile = min(tile_at(it, t), last_tile);
+        const int block = __builtin_amdgcn_readlane(blocks, it % AHEAD * CT + t);
+        return base + (size_t)block * block_bytes + (size_t)(tile & in_block) * Kv4Tile::bytes(HD);
     };
 
     f32x4 o[UNITS][EPC];
@@ -626,13 +634,20 @@ __global__ __launch_bounds__(NW * 64) void kv4_attend_kernel(Kv4Attend a) {
         for (int j = 0; j < EPC; ++j) o[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    TileRegs<HD> cur[CT], nxt[CT];
-    if (n_it) load(0, cur);
+    // K of the next step is asked for as soon as K of this one has been used, V likewise: one set of registers, and with four
+    // waves per SIMD always about 45 KB on their way to a CU
+    KeyRegs<HD> kr[CT];
+    ValueRegs<HD> vr[CT];
+    const char* at[CT];
+    if (n_it) {
+#pragma unroll
+        for (int t = 0; t < CT; ++t) at[t] = tile_addr(0, t);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) load_keys<HD>(at[t], lane, kr[t]);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) load_values<HD>(at[t], lane, vr[t]);
+    }
     for (int it = 0; it < n_it; ++it) {
-        if (it + 1 < n_it) {
-            if ((it + 1) % AHEAD == 0) blocks = blocks_from(it + 1);
-            load(it + 1, nxt);
-        }
         const int key0 = tile_at(it, 0) * 16;
         // scores: rows = positions, columns = entries
         f32x4 s[UNITS][CT];
@@ -642,22 +657,28 @@ __global__ __launch_bounds__(NW * 64) void kv4_attend_kernel(Kv4Attend a) {
             for (int u = 0; u < UNITS; ++u) s[u][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const float unit = scale_of(cur[t].ks, g);
-                const bf16x8 kf = frag(pair_of<0>(cur[t].k[g], unit), pair_of<1>(cur[t].k[g], unit), pair_of<2>(cur[t].k[g], unit),
-                                       pair_of<3>(cur[t].k[g], unit));
+                const float unit = scale_of(kr[t].sc, g);
+                const bf16x8 kf = frag(pair_of<0>(kr[t].w[g], unit), pair_of<1>(kr[t].w[g], unit), pair_of<2>(kr[t].w[g], unit),
+                                       pair_of<3>(kr[t].w[g], unit));
 #pragma unroll
                 for (int u = 0; u < UNITS; ++u)
 #pragma unroll
                     for (int n = NT - 1; n >= 0; --n) s[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[u][n][g], s[u][t], 0, 0, 0);
             }
         }
-        const int key_lane = key0 + quarter * 4;  // position of s[u][t][i]: key_lane + 16 t + i
-        const bool edge = key0 + 16 * CT > pos_first + 1 || key0 < lo_max;
+        const bool more = it + 1 < n_it;
+        if (more) {
+            if ((it + 1) % AHEAD == 0) blocks = blocks_from(it + 1);
+#pragma unroll
+            for (int t = 0; t < CT; ++t) at[t] = tile_addr(it + 1, t);
+#pragma unroll
+            for (int t = 0; t < CT; ++t) load_keys<HD>(at[t], lane, kr[t]);
+        }
         bool poisoned = false;
-        uint32_t bad[CT];
-        if (edge) {
-            // hidden positions; and of V, what lies behind the last position any entry sees may be anything: a scale of 1 makes it
-            // finite, and its probabilities are zero
+        uint32_t nan_keys[CT] = {};  // bytes 1 where V of the lane's key and group is NaN
+        if (key0 + 16 * CT > pos_first + 1 || key0 < lo_max) {  // some entry does not see all of these positions
+            int key_lane = key0 + quarter * 4;  // position of s[u][t][i]: key_lane + 16 t + i
+            asm volatile("" : "+v"(key_lane));  // (nothing of this branch is worth computing outside of it)
             bool any = false;
 #pragma unroll
             for (int t = 0; t < CT; ++t) {
@@ -668,17 +689,25 @@ __global__ __launch_bounds__(NW * 64) void kv4_attend_kernel(Kv4Attend a) {
                         const int key = key_lane + 16 * t + i;
                         if (key > hi[u] || key < lo[u]) s[u][t][i] = -INFINITY;
                     }
+                // V behind the last position that any entry sees may hold anything: a scale of 1 makes it finite, and its
+                // probabilities are zero
                 uint32_t keep = 0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (key_lane + 16 * t + i <= pos_last) keep |= 255u << (8 * i);
-                cur[t].vs = (cur[t].vs & keep) | (0x7f7f7f7fu & ~keep);
-                bad[t] = bytes_255(cur[t].vs);
-                any |= bad[t] != 0;
+                vr[t].sc = (vr[t].sc & keep) | (0x7f7f7f7fu & ~keep);
+                any |= bytes_255(vr[t].sc) != 0;
             }
             poisoned = __any(any);
+            if (poisoned) {  // NaN in V that not every entry sees: taken out here, put back below
+#pragma unroll
+                for (int t = 0; t < CT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if ((vr[t].sc >> (8 * i) & 255u) == SCALE_NAN) vr[t].sc ^= 128u << (8 * i), nan_keys[t] |= 1u << (8 * i);
+            }
         }
-        bf16x8 pf[UNITS][PT][CT / 2];
+        u32x4 pf[UNITS][PT];
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
             float top = s[u][0][0];
@@ -698,80 +727,75 @@ __global__ __launch_bounds__(NW * 64) void kv4_attend_kernel(Kv4Attend a) {
 #pragma unroll
             for (int t = 0; t < CT; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float p = __builtin_amdgcn_exp2f(fmaf(s[u][t][i], a.scale_log2, -ref));
+                for (int i = 0; i < 4; i += 2) {
+                    f32x2 p;
+                    p[0] = __builtin_amdgcn_exp2f(fmaf(s[u][t][i], a.scale_log2, -ref));
+                    p[1] = __builtin_amdgcn_exp2f(fmaf(s[u][t][i + 1], a.scale_log2, -ref));
                     // (with one term the sum is that of the rounded probabilities, so that the weights add up to one)
-                    if (PT > 1) l[u] += p;
+                    if (PT > 1) l[u] += p[0] + p[1];
 #pragma unroll
                     for (int n = 0; n < PT; ++n) {
-                        const __bf16 h = (__bf16)p;
-                        pf[u][n][t >> 1][(t & 1) * 4 + i] = h;
-                        if (PT == 1) l[u] += (float)h;
-                        p -= (float)h;
+                        const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+                        pf[u][n][t * 2 + (i >> 1)] = h;
+                        const float h0 = __uint_as_float(h << 16), h1 = __uint_as_float(h & 0xffff0000u);
+                        if (PT == 1) l[u] += h0 + h1;
+                        if (n + 1 < PT) p[0] -= h0, p[1] -= h1;
                     }
                 }
+        }
+        // weighted sum: rows = elements (column c of V's layout), columns = entries
+        float u0[4], u1[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u0[i] = scale_of(&vr[0].sc, i), u1[i] = scale_of(&vr[1].sc, i);
+#pragma unroll
+        for (int b = 0; b < EPC / 2; ++b) {
+            uint32_t x0[4], x1[4];  // elements 2b, 2b+1 of the column, at the four keys
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int byte = i * (HD / 32) + b;  // of the lane's codes
+                x0[i] = pair_of(vr[0].w[byte >> 2], u0[i], byte & 3);
+                x1[i] = pair_of(vr[1].w[byte >> 2], u1[i], byte & 3);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t sel = h ? 0x07060302u : 0x05040100u;
+                const bf16x8 vf = frag(__builtin_amdgcn_perm(x0[1], x0[0], sel), __builtin_amdgcn_perm(x0[3], x0[2], sel),
+                                       __builtin_amdgcn_perm(x1[1], x1[0], sel), __builtin_amdgcn_perm(x1[3], x1[2], sel));
+#pragma unroll
+                for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+                    for (int n = PT - 1; n >= 0; --n)
+                        o[u][2 * b + h] =
+                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, pf[u][n]), o[u][2 * b + h], 0, 0, 0);
+            }
+        }
+        if (more) {
+#pragma unroll
+            for (int t = 0; t < CT; ++t) load_values<HD>(at[t], lane, vr[t]);
         }
         if (poisoned) {
             // an entry that sees a position whose group of V is NaN gets NaN there, one that does not sees zero: the product of
             // "is NaN" and "is seen", both 0 or 1, counts them
+            int key_lane = key0 + quarter * 4;
+            asm volatile("" : "+v"(key_lane));
+            bf16x8 is_nan;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) is_nan[e] = (__bf16)(float)(nan_keys[e >> 2] >> (8 * (e & 3)) & 1u);
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
-                f32x4 count = {0.f, 0.f, 0.f, 0.f};
+                bf16x8 seen;
 #pragma unroll
-                for (int t2 = 0; t2 < CT / 2; ++t2) {
-                    bf16x8 is_nan, seen;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int t = 2 * t2 + (e >> 2), key = key_lane + 16 * t + (e & 3);
-                        is_nan[e] = (__bf16)((cur[t].vs >> (8 * (e & 3)) & 255u) == SCALE_NAN ? 1.f : 0.f);
-                        seen[e] = (__bf16)(key <= hi[u] && key >= lo[u] ? 1.f : 0.f);
-                    }
-                    count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(is_nan, seen, count, 0, 0, 0);
+                for (int e = 0; e < 8; ++e) {
+                    const int key = key_lane + 16 * (e >> 2) + (e & 3);
+                    seen[e] = (__bf16)(key <= hi[u] && key >= lo[u] ? 1.f : 0.f);
                 }
+                const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(is_nan, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
                 for (int j = 0; j < EPC; ++j)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (count[i] > 0.f) o[u][j][i] = __builtin_nanf("");
             }
-#pragma unroll
-            for (int t = 0; t < CT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if ((cur[t].vs >> (8 * i) & 255u) == SCALE_NAN) cur[t].vs ^= 128u << (8 * i);  // 127: a scale of 1
-        }
-        // weighted sum: rows = elements (column c of V's layout), columns = entries
-#pragma unroll
-        for (int t2 = 0; t2 < CT / 2; ++t2) {
-            const TileRegs<HD>&v0 = cur[2 * t2], &v1 = cur[2 * t2 + 1];
-            float u0[4], u1[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) u0[i] = scale_of(&v0.vs, i), u1[i] = scale_of(&v1.vs, i);
-#pragma unroll
-            for (int b = 0; b < EPC / 2; ++b) {
-                uint32_t x0[4], x1[4];  // elements 2b, 2b+1 of the column, at the four keys
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int at = i * (HD / 32) + b;  // byte of the lane's codes
-                    x0[i] = pair_of(v0.v[at >> 2], u0[i], at & 3);
-                    x1[i] = pair_of(v1.v[at >> 2], u1[i], at & 3);
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t sel = h ? 0x07060302u : 0x05040100u;
-                    const bf16x8 vf = frag(__builtin_amdgcn_perm(x0[1], x0[0], sel), __builtin_amdgcn_perm(x0[3], x0[2], sel),
-                                           __builtin_amdgcn_perm(x1[1], x1[0], sel), __builtin_amdgcn_perm(x1[3], x1[2], sel));
-#pragma unroll
-                    for (int u = 0; u < UNITS; ++u)
-#pragma unroll
-                        for (int n = PT - 1; n >= 0; --n)
-                            o[u][2 * b + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u][n][t2], o[u][2 * b + h], 0, 0, 0);
-                }
-            }
-        }
-        if (it + 1 < n_it) {
-#pragma unroll
-            for (int t = 0; t < CT; ++t) cur[t] = nxt[t];
         }
     }
 
@@ -817,32 +841,33 @@ __global__ __launch_bounds__(NW * 64) void kv4_attend_kernel(Kv4Attend a) {
             } else {
                 const size_t r = (size_t)w.slot * M + 16 * u + my_row;
 #pragma unroll
-                for (int e = 0; e < EPT; ++e) a.part_o[r * HD + my_d + e] = acc[e];
-                if (my_d == 0) a.part_ml[2 * r] = top, a.part_ml[2 * r + 1] = sum;
+                for (int e = 0; e < EPT; ++e) hand_over(a.part_o + r * HD + my_d + e, acc[e]);
+                if (my_d == 0) hand_over(a.part_ml + 2 * r, top), hand_over(a.part_ml + 2 * r + 1, sum);
             }
         }
     }
     if (n_parts == 1) return;
 
-    // the workgroup that leaves the last part of the item joins them, in their order
+    // the workgroup that leaves the last part of the item joins them, in their order.  The parts go past the caches of this
+    // XCD (agent-scope stores and loads): a release fence instead would write the whole of its L2 back, which cost a launch of
+    // 1024 parts 300 us
     const int slot0 = w.slot - part;
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // each thread's stores have arrived before the workgroup is counted
     __syncthreads();
     if (threadIdx.x == 0) s_last = __hip_atomic_fetch_add(a.arrived + slot0, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     if ((int)s_last != n_parts - 1) return;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     if (threadIdx.x == 0) __hip_atomic_store(a.arrived + slot0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     for (int i = threadIdx.x; i < (f_end - f0) * HD; i += NW * 64) {
         const int r = i / HD, d = i % HD, f = f0 + r;
         float top = -INFINITY, sum = 0.f, acc = 0.f;
-        for (int v = 0; v < n_parts; ++v) top = fmaxf(top, a.part_ml[2 * ((size_t)(slot0 + v) * M + r)]);
+        for (int v = 0; v < n_parts; ++v) top = fmaxf(top, handed(a.part_ml + 2 * ((size_t)(slot0 + v) * M + r)));
         const float ref = top == -INFINITY ? 0.f : top;
         for (int v = 0; v < n_parts; ++v) {
             const size_t at = (size_t)(slot0 + v) * M + r;
-            const float wt = __builtin_amdgcn_exp2f(a.part_ml[2 * at] - ref);
-            sum += wt * a.part_ml[2 * at + 1];
-            acc += wt * a.part_o[at * HD + d];
+            const float wt = __builtin_amdgcn_exp2f(handed(a.part_ml + 2 * at) - ref);
+            sum += wt * handed(a.part_ml + 2 * at + 1);
+            acc += wt * handed(a.part_o + at * HD + d);
         }
         const size_t at = (size_t)(w.row0 + f / a.group) * n_heads + w.head * a.group + f % a.group;
         out[at * HD + d] = (ST)(sum == 0.f ? 0.f : acc / sum);
