@@ -415,7 +415,7 @@ typedef struct {
     int32_t n_blocks;      /* of the pool */
     int32_t max_seqs;      /* requests: 1 .. EE_KV4_MAX_SEQS */
     int32_t max_positions; /* of one request: 1 .. 2^20 */
-    int32_t max_rows;      /* of one plan: 1 .. 2^22 */
+    int32_t max_rows;      /* of one plan: 1 .. 2^20 */
 } ee_kv4_config;
 enum { EE_KV4_MAX_SEQS = 4096 };
 

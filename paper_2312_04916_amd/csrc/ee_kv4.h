@@ -40,10 +40,11 @@ struct Kv4Part {
 struct Kv4Plan {
     const int32_t *held, *start, *end;
     int n_seqs, n_rows, max_rows_per_seq;
-    int block_tokens, n_blocks, table_stride, max_positions;
+    int block_shift, n_blocks, table_stride, max_positions;  // 1 << block_shift positions per block
     ee_kv4_arrays a;
     Kv4Part* parts;
     int32_t* n_parts;
+    uint32_t* arrived;  // workgroups that have read the lengths
     int max_parts;  // room in `parts`
     int group, kv_heads, tile_rows;
     int target_parts;  // a launch is cut so that it has about this many parts
@@ -69,23 +70,24 @@ struct Kv4Attend {
     float scale_log2;  // scale / ln 2
     int window, group, kv_heads;
     int tiles_shift;  // log2(block_tokens / 16)
+    int past_caches;  // K and V are read without keeping them in the caches
     int q_vec;        // rows of q can be read 16 bytes at a time
     float* part_o;    // [slot][tile rows][head_dim]
-    float* part_ml;   // [slot][tile rows][2]
-    uint32_t* arrived;  // [slot] of an item's first part: parts that have been left
+    float *part_ml, *joined_ml;  // [slot][tile rows][2]: of parts; of groups of parts, at the first one's slot
+    uint32_t *arrived, *arrived_groups;  // [slot] of the first part of a group, of an item: parts, groups that have been left
 };
 
-constexpr int KV4_CHUNK = 64;  // positions: what a wave works on at a time, and the grain of the parts
+constexpr int KV4_CHUNK = 32;  // positions: what a wave works on at a time, and the grain of the parts
 
 // Entries of a tile in units of 16 (the columns of a matrix instruction), by the most that a request has.
 int kv4_tile_units(int dtype, int head_dim, int most_flat);
 
 hipError_t launch_kv4_init(int32_t* table, int64_t n_table, int32_t* free_blocks, int n_blocks, uint32_t* arrived, int n_arrived,
-                           hipStream_t s);
-hipError_t launch_kv4_plan(const Kv4Plan& p, int workgroups, hipStream_t s);
+                           uint32_t* counts, hipStream_t s);
+hipError_t launch_kv4_plan(const Kv4Plan& p, int workgroups, int threads, hipStream_t s);
 hipError_t launch_kv4_append(const Kv4Cache& c, int n_rows, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row,
                              int64_t v_head, const int64_t* slots, hipStream_t s);
 hipError_t launch_kv4_read(const Kv4Cache& c, int n_rows, const int64_t* slots, void* k, void* v, hipStream_t s);
-hipError_t launch_kv4_attend(const Kv4Attend& a, int dtype, int head_dim, int units, int grid, hipStream_t s);
+hipError_t launch_kv4_attend(const Kv4Attend& a, int dtype, int head_dim, int units, int waves, int grid, hipStream_t s);
 
 }  // namespace ee

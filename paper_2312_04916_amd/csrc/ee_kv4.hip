@@ -24,11 +24,13 @@ constexpr uint32_t SCALE_MIN = 16, SCALE_MAX = 252;  // 2^-111, 2^125: no held v
 // ------------------------------------------------------------------------------------------------
 // create
 // ------------------------------------------------------------------------------------------------
-__global__ void kv4_init_kernel(int32_t* table, int64_t n_table, int32_t* free_blocks, int n_blocks, uint32_t* arrived, int n_arrived) {
+__global__ void kv4_init_kernel(int32_t* table, int64_t n_table, int32_t* free_blocks, int n_blocks, uint32_t* arrived, int n_arrived,
+                                uint32_t* counts) {
     const int64_t i0 = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
     for (int64_t i = i0; i < n_table; i += step) table[i] = 0;
     for (int64_t i = i0; i < n_blocks; i += step) free_blocks[i] = n_blocks - 1 - (int)i;  // block 0 is on top
     for (int64_t i = i0; i < n_arrived; i += step) arrived[i] = 0;
+    if (i0 < 3) counts[i0] = i0 == 0 ? n_blocks : 0;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -36,36 +38,38 @@ __global__ void kv4_init_kernel(int32_t* table, int64_t n_table, int32_t* free_b
 // ------------------------------------------------------------------------------------------------
 constexpr int PLAN_SEQS = EE_KV4_MAX_SEQS + 1;  // and the rows behind the last request's
 
-// Sums over a workgroup: exclusive prefix of each thread's value, and the total.
-template <int N>
-__device__ void scan_sums(int64_t (&v)[N], int64_t (&total)[N], int64_t (*wave_sums)[N]) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
-    int64_t own[N];
-#pragma unroll
-    for (int k = 0; k < N; ++k) own[k] = v[k];
-    for (int d = 1; d < 64; d <<= 1) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const int64_t o = __shfl_up(v[k], d);
-            if (lane >= d) v[k] += o;
-        }
+// inclusive sums over a wave (over each of its rows of 16 lanes if ROWS), in the lanes' order
+template <bool ROWS = false>
+__device__ __forceinline__ int lanes_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // from the lane 1, 2, 4, 8 before in the row
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    if constexpr (!ROWS) {
+        v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // the last of row 0, 2 to row 1, 3
+        v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // the last of row 1 to rows 2 and 3
     }
-    __syncthreads();  // (wave_sums may still be read from the scan before)
+    return v;
+}
+
+// Sums over a workgroup of up to 16 waves: exclusive prefix of each thread's values, and the totals.  `waves` is used by one
+// call only.
+template <int N>
+__device__ __forceinline__ void scan_sums(int (&v)[N], int (&total)[N], int (*waves)[N]) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = blockDim.x >> 6;
+    int own[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) own[k] = v[k], v[k] = lanes_scan(v[k]);
     if (lane == 63) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) wave_sums[wave][k] = v[k];
+        for (int k = 0; k < N; ++k) waves[wave][k] = v[k];
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        int64_t before = 0, all = 0;
-        for (int w = 0; w < n_waves; ++w) {
-            const int64_t s = wave_sums[w][k];
-            before += w < wave ? s : 0;
-            all += s;
-        }
-        v[k] += before - own[k];
-        total[k] = all;
+        const int sums = lanes_scan<true>(lane < n_waves ? waves[lane][k] : 0);
+        total[k] = __builtin_amdgcn_readlane(sums, 15);
+        v[k] += (wave ? __builtin_amdgcn_readlane(sums, wave - 1) : 0) - own[k];
     }
 }
 
@@ -81,219 +85,179 @@ __device__ __forceinline__ int last_not_above(const int32_t* first, int n, int32
 }
 
 // Every workgroup forms the sums over all requests for itself (a few thousand lengths at most: cheaper than handing them on)
-// and takes its share of the rows, blocks and parts.  What a workgroup reads, no other one writes: a block that one request
-// gives back and another one takes is looked up in the table row of the first, behind what it keeps, which nothing changes.
-// (dev_held == held_next is the one exception, and the launch then has one workgroup.)
+// and takes its share of what has to be written, one thread per row, block and part.  What a workgroup reads, no other one
+// writes: a block that one request gives back and another one takes is looked up in the table row of the first, behind what it
+// keeps, which nothing changes; and held_next, which may be where the lengths are read, is written by the workgroup that is
+// the last to have read them.  All sums fit 32 bits: a request has at most
+// 2^16 blocks, and a thread's rows are counted up to n_rows + 1, at most 2^20 + 1.
+constexpr int SERVED = 1 << 30, BLOCKS = SERVED - 1;  // in s_had
 __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
-    __shared__ int32_t s_row[PLAN_SEQS];   // first row
-    __shared__ int32_t s_take[PLAN_SEQS];  // blocks taken by the requests before; then first part
-    __shared__ int32_t s_give[PLAN_SEQS];  // blocks given back by the requests before; then parts per item << 16 | served
-    __shared__ int64_t s_sums[16][4];
-    const int tid = threadIdx.x, nt = blockDim.x;
-    const int n = p.n_seqs, per = (n + 1 + nt - 1) / nt;
+    __shared__ int32_t s_row[PLAN_SEQS + 1];    // first row
+    __shared__ int32_t s_take[PLAN_SEQS + 1];   // blocks taken by the requests before
+    __shared__ int32_t s_give[PLAN_SEQS + 1];   // blocks given back by the requests before
+    __shared__ int32_t s_start[PLAN_SEQS + 1];  // first row's position
+    __shared__ int32_t s_had[PLAN_SEQS + 1];    // blocks held before, SERVED
+    __shared__ int32_t s_part[PLAN_SEQS + 1];   // first part, of requests and then of the rows behind them
+    __shared__ int32_t s_slot[PLAN_SEQS + 1];   // first slot of parts that are joined
+    __shared__ int s_sums[16][4], s_sums2[16][4], s_sums3[16][2];
+    __shared__ float s_work[16];
+    __shared__ int s_taken[16], s_last;
+    const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 63, wave = tid >> 6;
+    const int n = p.n_seqs, per = (n + nt) / nt;  // requests of a thread, with the one behind the last
     const int i0 = min(n, tid * per), i1 = min(n, i0 + per);
-    const int bt = p.block_tokens;
+    const int most = p.max_positions, bt_shift = p.block_shift, bt = 1 << bt_shift, cap = p.n_rows + 1;
     const bool first_wg = blockIdx.x == 0;
 
-    struct Req {
-        int held, start, end, had, need, rows;
-        bool ok;
-    };
-    auto request = [&](int i) {
-        Req r;
-        r.held = p.held[i], r.start = p.start[i], r.end = p.end[i];
-        const int most = p.max_positions;
-        const bool range = r.start >= 0 && r.start <= r.end && r.end <= most;
-        r.ok = range && r.held >= 0 && r.held <= most && r.end - r.start <= p.max_rows_per_seq;
-        r.rows = range ? r.end - r.start : 0;
-        r.had = (min(max(r.held, 0), most) + bt - 1) / bt;
-        r.need = r.ok ? (r.end + bt - 1) / bt : r.had;
-        return r;
-    };
-
-    // blocks held, given back, asked for; rows
-    int64_t v[4] = {0, 0, 0, 0}, all[4];
+    // lengths; blocks held, given back, asked for; rows
+    int sum[4] = {0, 0, 0, 0}, all[4];
     for (int i = i0; i < i1; ++i) {
-        const Req r = request(i);
-        v[0] += r.had, v[1] += max(r.had - r.need, 0), v[2] += max(r.need - r.had, 0), v[3] += r.rows;
+        const int held = p.held[i], start = p.start[i], end = p.end[i];
+        const bool range = start >= 0 && start <= end && end <= most;
+        const bool ok = range && held >= 0 && held <= most && end - start <= p.max_rows_per_seq;
+        const int had = (min(max(held, 0), most) + bt - 1) >> bt_shift, need = ok ? (end + bt - 1) >> bt_shift : had;
+        const int rows = range ? min(end - start, cap) : 0;
+        s_start[i] = start, s_had[i] = had | (ok ? SERVED : 0), s_take[i] = need, s_row[i] = rows;  // (this thread's, for now)
+        sum[0] += had, sum[1] += max(had - need, 0), sum[2] += max(need - had, 0);
+        sum[3] = min(sum[3] + rows, cap);
     }
-    scan_sums<4>(v, all, s_sums);
-    const int left = (int)max((int64_t)0, p.n_blocks - all[0]);  // free before the call (< 0: the lengths contradict the pool)
-    const int have = left + (int)all[1];
-    const int rows_all = (int)min(all[3], (int64_t)p.n_rows);
-    // a request whose rows do not fit is refused, and gives and takes nothing: only then do the sums have to be formed again
-    // (rows_all is what the caller says it is, unless its lengths are wrong)
+    scan_sums<4>(sum, all, s_sums);
+    const int left = max(0, p.n_blocks - all[0]);  // free before the call (the lengths may contradict the pool)
     const bool clipped = all[3] > p.n_rows;
     if (clipped) {
-        int64_t row = v[3];
-        int64_t w[2] = {0, 0}, all2[4];
+        // rows that do not fit: their requests are refused, and give and take nothing
+        int row = sum[3], again[4] = {0, 0, 0, 0};
         for (int i = i0; i < i1; ++i) {
-            const Req r = request(i);
-            if (row + r.rows <= p.n_rows) w[0] += max(r.had - r.need, 0), w[1] += max(r.need - r.had, 0);
-            row += r.rows;
+            const int rows = s_row[i];
+            if (row + rows > p.n_rows) s_had[i] &= BLOCKS, s_take[i] = s_had[i];
+            const int had = s_had[i] & BLOCKS, need = s_take[i];
+            again[1] += max(had - need, 0), again[2] += max(need - had, 0);
+            row = min(row + rows, cap);
         }
-        int64_t x[4] = {w[0], w[1], 0, 0};
-        scan_sums<4>(x, all2, s_sums);
-        v[1] = x[0], v[2] = x[1];
-        all[1] = all2[0], all[2] = all2[1];
+        int all2[4];
+        scan_sums<4>(again, all2, s_sums2);
+        sum[1] = again[1], sum[2] = again[2], all[1] = all2[1], all[2] = all2[2];
     }
-    const int have_now = clipped ? left + (int)all[1] : have;
+    const int given = all[1], have = left + given, rows_all = min(all[3], p.n_rows);
 
-    // per request: first row, blocks before it, served; and the work of its rows in chunks of positions
-    int64_t work[4] = {0, 0, 0, 0}, work_all[4];
+    // served; the work of the rows in chunks of positions per kv head
+    float work = 0.f;
+    int taken = 0;
     {
-        int64_t give = v[1], take = v[2], row = v[3];
+        int give = sum[1], take = sum[2], row = sum[3];
         for (int i = i0; i < i1; ++i) {
-            Req r = request(i);
-            const bool fits = row + r.rows <= p.n_rows;
-            if (!fits) r.ok = false, r.need = r.had;
-            const int asked = max(r.need - r.had, 0);
-            const bool ok = r.ok && (asked == 0 || take + asked <= have_now);
-            s_row[i] = (int)min(row, (int64_t)p.n_rows);
-            s_take[i] = (int)min(take, (int64_t)have_now);
-            s_give[i] = (int)give;
-            give += max(r.had - r.need, 0), take += asked;
-            const int64_t row_end = row + r.rows;
-            const int64_t tiles = ((min(row_end, (int64_t)p.n_rows) - min(row, (int64_t)p.n_rows)) * p.group + p.tile_rows - 1) / p.tile_rows;
-            if (ok) work[0] += tiles * p.kv_heads * ((r.end + KV4_CHUNK - 1) / KV4_CHUNK);
-            work[1] += asked > 0 && ok ? asked : 0;
-            row = row_end;
-            if (first_wg) {
-                p.a.served[i] = ok ? 1 : 0;
-                p.a.row_start[i] = s_row[i];
+            const int had = s_had[i] & BLOCKS, need = s_take[i], rows = s_row[i], asked = max(need - had, 0);
+            const bool ok = (s_had[i] & SERVED) && (asked == 0 || take + asked <= have);
+            const int row0 = min(row, p.n_rows), row1 = min(row + rows, p.n_rows);
+            s_row[i] = row0, s_take[i] = min(take, have), s_give[i] = give, s_had[i] = had | (ok ? SERVED : 0);
+            give += max(had - need, 0), take += asked, row = min(row + rows, cap);
+            if (ok) {
+                if (asked) taken = take;
+                if (row1 > row0) {
+                    const int tiles = ((row1 - row0) * p.group + p.tile_rows - 1) / p.tile_rows;
+                    work += (float)tiles * (float)((s_start[i] + row1 - row0 + KV4_CHUNK - 1) / KV4_CHUNK);
+                }
             }
+            if (first_wg) p.a.served[i] = ok ? 1 : 0, p.a.row_start[i] = row0;
         }
-        if (tid == 0) s_row[n] = rows_all;
+        if (tid == 0) s_row[n] = rows_all, s_row[n + 1] = p.n_rows, s_give[n] = given;
     }
-    scan_sums<4>(work, work_all, s_sums);  // (its barriers also make s_row, s_take, s_give whole)
-    const int taken = (int)work_all[1];
-    const int chunks_per_part = (int)max((int64_t)p.min_chunks, (work_all[0] + p.target_parts - 1) / p.target_parts);
+    work = wave_sum(work);
+    taken = max(taken, __shfl_xor(taken, 32)), taken = max(taken, __shfl_xor(taken, 16)), taken = max(taken, __shfl_xor(taken, 8));
+    taken = max(taken, __shfl_xor(taken, 4)), taken = max(taken, __shfl_xor(taken, 2)), taken = max(taken, __shfl_xor(taken, 1));
+    if (lane == 0) s_work[wave] = work, s_taken[wave] = taken;
+    __syncthreads();
+    for (int v = 0; v < nt >> 6; ++v) work = v ? work + s_work[v] : s_work[0], taken = max(taken, s_taken[v]);
+    // (1.001: a sum in fp32, and the parts must not come out more than the target)
+    const int per_part = max(p.min_chunks, (int)fminf(1e6f, ceilf(work * (float)p.kv_heads * 1.001f / (float)p.target_parts)));
 
-    auto served_of = [&](int i, const Req& r) {
-        if (!r.ok) return false;
-        const int asked = max(r.need - r.had, 0);
-        // (s_take is capped at the blocks there are: a request behind the cap that asks for any is refused)
-        return asked == 0 || (int64_t)s_take[i] + asked <= have_now;
+    // parts: items (tile of rows, kv head) in the requests' order, each cut alike; the rows behind the last request's are one
+    // more request that sees nothing
+    auto parts_of = [&](int i) {  // of an item
+        const int rows = s_row[i + 1] - s_row[i];
+        if (i == n || rows == 0 || !(s_had[i] & SERVED)) return 1;
+        return ((s_start[i] + rows + KV4_CHUNK - 1) / KV4_CHUNK + per_part - 1) / per_part;
     };
-    auto request_at = [&](int i) {  // as above, with the rows that do not fit
-        Req r = request(i);
-        if (s_row[i] + (int64_t)r.rows > p.n_rows) r.ok = false, r.need = r.had, r.rows = p.n_rows - s_row[i];
-        return r;
-    };
+    auto items_of = [&](int i) { return ((s_row[i + 1] - s_row[i]) * p.group + p.tile_rows - 1) / p.tile_rows * p.kv_heads; };
+    int cnt[2] = {0, 0}, cnt_all[2];
+    const int j0 = min(n + 1, tid * per), j1 = min(n + 1, j0 + per);
+    for (int i = j0; i < j1; ++i) {
+        const int np = parts_of(i), items = items_of(i);
+        cnt[0] += items * np, cnt[1] += np > 1 ? items * np : 0;
+    }
+    scan_sums<2>(cnt, cnt_all, s_sums3);
+    for (int i = j0; i < j1; ++i) {
+        const int np = parts_of(i), items = items_of(i);
+        s_part[i] = cnt[0], s_slot[i] = cnt[1];
+        cnt[0] += items * np, cnt[1] += np > 1 ? items * np : 0;
+    }
+    __syncthreads();
+    const int n_parts = min(cnt_all[0], p.max_parts);
+    if (first_wg && tid == 0) *p.n_parts = n_parts, *p.a.n_free = have - taken, p.a.row_start[n] = rows_all;
+
     // entry `at` of the stack as it stands once everything given back lies on it
     auto stack = [&](int at) {
         if (at < left) return p.a.free_blocks[at];
-        const int back = (int)all[1] - 1 - (at - left);  // in the requests' order, first block first
+        const int back = given - 1 - (at - left);  // in the requests' order, first block first
         const int i = last_not_above(s_give, n, back);
-        const Req r = request_at(i);
-        return p.a.table[(size_t)i * p.table_stride + min(r.need + back - s_give[i], p.table_stride - 1)];
+        const int need = (s_had[i] & BLOCKS) - (s_give[i + 1] - s_give[i]);
+        return p.a.table[(size_t)i * p.table_stride + min(need + back - s_give[i], p.table_stride - 1)];
     };
-
-    const int64_t t0 = (int64_t)blockIdx.x * nt + tid, t_step = (int64_t)gridDim.x * nt;
-    // rows
-    for (int64_t r = t0; r < p.n_rows; r += t_step) {
-        int64_t slot = -1;
-        int pos = -1, seq = -1;
-        if (r < rows_all) {
-            seq = last_not_above(s_row, n, (int)r);
-            const Req q = request_at(seq);
-            if (served_of(seq, q)) {
-                pos = q.start + (int)r - s_row[seq];
-                const int b = pos / bt;
-                const int block = b < q.had ? p.a.table[(size_t)seq * p.table_stride + b] : stack(have_now - 1 - (s_take[seq] + b - q.had));
-                slot = (int64_t)block * bt + pos % bt;
+    const int64_t n_tasks = (int64_t)p.n_rows + taken + given + n_parts;
+    for (int64_t task = (int64_t)blockIdx.x * nt + tid; task < n_tasks; task += (int64_t)gridDim.x * nt) {
+        int64_t t = task;
+        if (t < p.n_rows) {
+            int64_t slot = -1;
+            int pos = -1, seq = -1;
+            if (t < rows_all) {
+                seq = last_not_above(s_row, n, (int)t);
+                const int had = s_had[seq];
+                if (had & SERVED) {
+                    pos = s_start[seq] + (int)t - s_row[seq];
+                    const int b = (pos >> bt_shift) - (had & BLOCKS);
+                    const int block = b < 0 ? p.a.table[(size_t)seq * p.table_stride + (pos >> bt_shift)] : stack(have - 1 - (s_take[seq] + b));
+                    slot = ((int64_t)block << bt_shift) + (pos & (bt - 1));
+                }
             }
+            p.a.slots[t] = slot, p.a.positions[t] = pos, p.a.row_seq[t] = seq;
+            continue;
         }
-        p.a.slots[r] = slot;
-        p.a.positions[r] = pos;
-        p.a.row_seq[r] = seq;
-    }
-    // blocks that are taken (n > 0 here: something was asked for)
-    for (int64_t t = t0; t < taken; t += t_step) {
-        const int i = last_not_above(s_take, n, (int)t);
-        const Req q = request_at(i);
-        const int b = q.had + (int)t - s_take[i];
-        if (b < p.table_stride) p.a.table[(size_t)i * p.table_stride + b] = stack(have_now - 1 - (int)t);
-    }
-    // blocks that are given back
-    for (int64_t t = t0; t < all[1]; t += t_step)
+        t -= p.n_rows;
+        if (t < n_parts) {
+            const int i = last_not_above(s_part, n + 1, (int)t), np = parts_of(i), local = (int)t - s_part[i], item = local / np;
+            const int rows = s_row[i + 1] - s_row[i], tiles = (rows * p.group + p.tile_rows - 1) / p.tile_rows;
+            Kv4Part w;
+            w.seq = i < n && (s_had[i] & SERVED) ? i : -1;
+            w.row0 = s_row[i];
+            w.n_flat = rows * p.group;
+            w.start = i < n ? s_start[i] : 0;
+            w.tile = tiles - 1 - item / p.kv_heads;  // (those that see most come first)
+            w.head = item % p.kv_heads;
+            w.part_of = local % np | np << 16;
+            w.slot = s_slot[i] + local;
+            p.parts[t] = w;
+            continue;
+        }
+        t -= n_parts;
+        if (t < taken) {
+            const int i = last_not_above(s_take, n, (int)t), b = (s_had[i] & BLOCKS) + (int)t - s_take[i];
+            if (b < p.table_stride) p.a.table[(size_t)i * p.table_stride + b] = stack(have - 1 - (int)t);
+            continue;
+        }
+        t -= taken;
         if (left + t < p.n_blocks) p.a.free_blocks[left + t] = stack(left + (int)t);
-    __syncthreads();
+    }
 
-    // parts: items (tile of rows, kv head) in the requests' order, each cut alike; the rows behind the last request's are one
-    // more "request" that sees nothing
-    int64_t cnt[4] = {0, 0, 0, 0}, cnt_all[4];
-    const int j1 = tid * per + per > n ? min(n + 1, tid * per + per) : i1;
-    auto items_of = [&](int i, int& np, bool& sees, Req& r) {
-        int flat;
-        if (i < n) {
-            r = request_at(i);
-            sees = served_of(i, r) && r.rows > 0;
-            flat = r.rows * p.group;
-        } else {
-            sees = false, flat = (p.n_rows - rows_all) * p.group, r.start = 0, r.rows = p.n_rows - rows_all;
+    if (tid == 0) {
+        s_last = 1;
+        if (gridDim.x > 1) {
+            const uint32_t before = __hip_atomic_fetch_add(p.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s_last = before == gridDim.x - 1;
+            if (s_last) __hip_atomic_store(p.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
-        np = sees ? ((r.end + KV4_CHUNK - 1) / KV4_CHUNK + chunks_per_part - 1) / chunks_per_part : 1;
-        return (flat + p.tile_rows - 1) / p.tile_rows * p.kv_heads;
-    };
-    for (int i = min(n + 1, tid * per); i < j1; ++i) {
-        int np;
-        bool sees;
-        Req r;
-        const int items = items_of(i, np, sees, r);
-        cnt[0] += (int64_t)items * np;
-        cnt[1] += np > 1 ? (int64_t)items * np : 0;
-    }
-    scan_sums<4>(cnt, cnt_all, s_sums);
-    for (int i = min(n + 1, tid * per); i < j1; ++i) {  // s_take, s_give: first part, first slot from here on
-        int np;
-        bool sees;
-        Req r;
-        const int items = items_of(i, np, sees, r);
-        const int64_t first = cnt[0], slot = cnt[1];
-        cnt[0] += (int64_t)items * np;
-        cnt[1] += np > 1 ? (int64_t)items * np : 0;
-        // (items_of reads s_take of request i only: this thread's own)
-        s_take[i] = (int)first;
-        s_give[i] = sees ? (int)slot : -1;
-    }
-    if (first_wg && tid == 0) {
-        *p.n_parts = (int)min(cnt_all[0], (int64_t)p.max_parts);
-        *p.a.n_free = have_now - taken;
-        p.a.row_start[n] = rows_all;
     }
     __syncthreads();
-    for (int64_t t = t0; t < min(cnt_all[0], (int64_t)p.max_parts); t += t_step) {
-        const int i = last_not_above(s_take, n + 1, (int)t);
-        Kv4Part w;
-        const int local = (int)t - s_take[i];
-        int np = 1, rows;
-        w.start = 0;
-        if (i < n) {
-            const Req r = request_at(i);
-            rows = r.rows;
-            w.start = r.start;
-            if (s_give[i] >= 0) np = ((r.end + KV4_CHUNK - 1) / KV4_CHUNK + chunks_per_part - 1) / chunks_per_part;
-        } else {
-            rows = p.n_rows - rows_all;
-        }
-        const int item = local / np;
-        w.seq = s_give[i] >= 0 ? i : -1;
-        w.row0 = s_row[i];
-        w.n_flat = rows * p.group;
-        // the tiles that see most come first
-        const int tiles = (w.n_flat + p.tile_rows - 1) / p.tile_rows;
-        w.tile = tiles - 1 - item / p.kv_heads;
-        w.head = item % p.kv_heads;
-        w.part_of = (local % np) | np << 16;
-        w.slot = s_give[i] + local;
-        p.parts[t] = w;
-    }
-    if (first_wg) {
-        // (behind every read of the lengths: dev_held may be this array)
-        __syncthreads();
-        for (int i = i0; i < i1; ++i) p.a.held_next[i] = p.a.served[i] ? p.end[i] : p.held[i];
-    }
+    if (s_last)
+        for (int i = i0; i < i1; ++i) p.a.held_next[i] = s_had[i] & SERVED ? p.end[i] : p.held[i];
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -488,35 +452,36 @@ struct ValueRegs {
     uint32_t sc;  // of the lane's four keys, in its column's group
 };
 
-template <int N>
+// PAST: without keeping the lines in the caches.
+template <bool PAST, int N>
 __device__ __forceinline__ void load_words(const char* p, uint32_t (&w)[N]) {
     if constexpr (N == 1) {
         w[0] = *(const uint32_t*)p;
     } else if constexpr (N == 2) {
-        const u32x2 x = *(const u32x2*)p;
+        const u32x2 x = PAST ? __builtin_nontemporal_load((const u32x2*)p) : *(const u32x2*)p;
         w[0] = x[0], w[1] = x[1];
     } else {
 #pragma unroll
         for (int i = 0; i < N; i += 4) {
-            const u32x4 x = *(const u32x4*)(p + 4 * i);
+            const u32x4 x = PAST ? __builtin_nontemporal_load((const u32x4*)(p + 4 * i)) : *(const u32x4*)(p + 4 * i);
             w[i] = x[0], w[i + 1] = x[1], w[i + 2] = x[2], w[i + 3] = x[3];
         }
     }
 }
 
-template <int HD>
+template <int HD, bool PAST>
 __device__ __forceinline__ void load_keys(const char* tile, int lane, KeyRegs<HD>& r) {
     constexpr int LB = HD / 8, G = HD / 32;
-    load_words<G>(tile + lane * LB, r.w);
+    load_words<PAST, G>(tile + lane * LB, r.w);
     const char* sc = tile + Kv4Tile::k_scales(HD) + (lane & 15) * G;
     if constexpr (G == 1) r.sc[0] = *(const uint8_t*)sc;
     if constexpr (G == 2) r.sc[0] = *(const uint16_t*)sc;
-    if constexpr (G >= 4) load_words<G / 4>(sc, r.sc);
+    if constexpr (G >= 4) load_words<false, G / 4>(sc, r.sc);
 }
-template <int HD>
+template <int HD, bool PAST>
 __device__ __forceinline__ void load_values(const char* tile, int lane, ValueRegs<HD>& r) {
     constexpr int LB = HD / 8, G = HD / 32;
-    load_words<G>(tile + Kv4Tile::v_codes(HD) + lane * LB, r.w);
+    load_words<PAST, G>(tile + Kv4Tile::v_codes(HD) + lane * LB, r.w);
     r.sc = *(const uint32_t*)(tile + Kv4Tile::v_scales(HD) + (lane & 15) * HD / 512 * 16 + (lane >> 4) * 4);
 }
 
@@ -532,9 +497,13 @@ __device__ __forceinline__ uint32_t bytes_255(uint32_t w) {  // 0x80 in every by
 // What one workgroup leaves for another one of the same launch, maybe on another XCD.
 __device__ __forceinline__ void hand_over(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ float handed(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ f32x2 handed2(const float* p) {
+    return __builtin_bit_cast(f32x2, __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+constexpr int FAN_IN = 32;  // parts that are joined at a time
 
 // NT: bf16 terms of an element of Q (1: Q is bf16; 3: fp32, exactly), PT: of a probability.  UNITS: 16 entries each of a tile.
-template <int HD, int NT, int PT, int UNITS, int NW, typename ST>
+template <int HD, int NT, int PT, int UNITS, int NW, bool PAST, typename ST>
 __global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 : 3) : 1) void kv4_attend_kernel(Kv4Attend a) {
     constexpr int G = HD / 32, EPC = HD / 16, M = 16 * UNITS;
     constexpr int CT = 2, STEPS = KV4_CHUNK / (16 * CT);  // tiles of 16 positions at a time: one contraction of P.V
@@ -543,8 +512,8 @@ __global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 :
     __shared__ float s_m[NW * 16], s_l[NW * 16];
     __shared__ uint32_t s_last;
 
+    const Kv4Part w = a.parts[blockIdx.x];  // (there is room for as many as the grid has; asked for together with their number)
     if ((int)blockIdx.x >= *a.n_parts) return;
-    const Kv4Part w = a.parts[blockIdx.x];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const int f0 = w.tile * M, f_end = min(w.n_flat, f0 + M);  // entries
@@ -643,9 +612,9 @@ __global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 :
 #pragma unroll
         for (int t = 0; t < CT; ++t) at[t] = tile_addr(0, t);
 #pragma unroll
-        for (int t = 0; t < CT; ++t) load_keys<HD>(at[t], lane, kr[t]);
+        for (int t = 0; t < CT; ++t) load_keys<HD, PAST>(at[t], lane, kr[t]);
 #pragma unroll
-        for (int t = 0; t < CT; ++t) load_values<HD>(at[t], lane, vr[t]);
+        for (int t = 0; t < CT; ++t) load_values<HD, PAST>(at[t], lane, vr[t]);
     }
     for (int it = 0; it < n_it; ++it) {
         const int key0 = tile_at(it, 0) * 16;
@@ -672,7 +641,7 @@ __global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 :
 #pragma unroll
             for (int t = 0; t < CT; ++t) at[t] = tile_addr(it + 1, t);
 #pragma unroll
-            for (int t = 0; t < CT; ++t) load_keys<HD>(at[t], lane, kr[t]);
+            for (int t = 0; t < CT; ++t) load_keys<HD, PAST>(at[t], lane, kr[t]);
         }
         bool poisoned = false;
         uint32_t nan_keys[CT] = {};  // bytes 1 where V of the lane's key and group is NaN
@@ -771,7 +740,7 @@ __global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 :
         }
         if (more) {
 #pragma unroll
-            for (int t = 0; t < CT; ++t) load_values<HD>(at[t], lane, vr[t]);
+            for (int t = 0; t < CT; ++t) load_values<HD, PAST>(at[t], lane, vr[t]);
         }
         if (poisoned) {
             // an entry that sees a position whose group of V is NaN gets NaN there, one that does not sees zero: the product of
@@ -800,8 +769,8 @@ __global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 :
     }
 
     // join the waves' shares, 16 entries at a time
-    constexpr int EPT = 16 * HD / (NW * 64);  // elements per thread
-    const int e0 = threadIdx.x * EPT, my_row = e0 / HD, my_d = e0 % HD;
+    constexpr int EPT = 16 * HD >= NW * 64 ? 16 * HD / (NW * 64) : 1;  // elements per thread
+    const int my_row = threadIdx.x * EPT / HD, my_d = threadIdx.x * EPT % HD;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
         if (f0 + 16 * u >= f_end) break;
@@ -817,7 +786,7 @@ __global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 :
         }
         __syncthreads();
         const int f = f0 + 16 * u + my_row;
-        if (f < f_end) {
+        if (my_row < 16 && f < f_end) {
             float top = -INFINITY, sum = 0.f, acc[EPT];
 #pragma unroll
             for (int v = 0; v < NW; ++v) top = fmaxf(top, s_m[v * 16 + my_row]);
@@ -848,52 +817,104 @@ __global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 :
     }
     if (n_parts == 1) return;
 
-    // the workgroup that leaves the last part of the item joins them, in their order.  The parts go past the caches of this
-    // XCD (agent-scope stores and loads): a release fence instead would write the whole of its L2 back, which cost a launch of
-    // 1024 parts 300 us
+    // Parts are joined by the workgroup that leaves the last one, in their order; many of them in two levels: first each
+    // FAN_IN neighbours by the last of those, into the first one's place, then these.  The parts go past the caches of this XCD
+    // (agent-scope stores and loads): a release fence instead would write the whole of its L2 back, which cost a launch of 1024
+    // parts 300 us.
     const int slot0 = w.slot - part;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // each thread's stores have arrived before the workgroup is counted
-    __syncthreads();
-    if (threadIdx.x == 0) s_last = __hip_atomic_fetch_add(a.arrived + slot0, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if ((int)s_last != n_parts - 1) return;
-    if (threadIdx.x == 0) __hip_atomic_store(a.arrived + slot0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    for (int i = threadIdx.x; i < (f_end - f0) * HD; i += NW * 64) {
-        const int r = i / HD, d = i % HD, f = f0 + r;
-        float top = -INFINITY, sum = 0.f, acc = 0.f;
-        for (int v = 0; v < n_parts; ++v) top = fmaxf(top, handed(a.part_ml + 2 * ((size_t)(slot0 + v) * M + r)));
-        const float ref = top == -INFINITY ? 0.f : top;
-        for (int v = 0; v < n_parts; ++v) {
-            const size_t at = (size_t)(slot0 + v) * M + r;
-            const float wt = __builtin_amdgcn_exp2f(handed(a.part_ml + 2 * at) - ref);
-            sum += wt * handed(a.part_ml + 2 * at + 1);
-            acc += wt * handed(a.part_o + at * HD + d);
+    auto last_of = [&](uint32_t* counter, int n) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // each thread's stores have arrived before its workgroup is counted
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if ((int)before == n - 1) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s_last = before;
         }
-        const size_t at = (size_t)(w.row0 + f / a.group) * n_heads + w.head * a.group + f % a.group;
-        out[at * HD + d] = (ST)(sum == 0.f ? 0.f : acc / sum);
-        if (a.lse && d == 0) a.lse[at] = (ref + log2f(sum)) * 0.6931471805599453f;
-    }
+        __syncthreads();
+        return (int)s_last == n - 1;
+    };
+    auto join = [&](const float* part_ml, int first, int stride, int n, bool whole) {
+        // one thread per two elements: it asks for eight parts at once, weights and elements, so that a join of few parts is one
+        // trip to memory
+        constexpr int AT_ONCE = 8;
+        for (int i = threadIdx.x; i < (f_end - f0) * (HD / 2); i += NW * 64) {
+            const int r = i / (HD / 2), d = i % (HD / 2) * 2, f = f0 + r;
+            const size_t row = (size_t)first * M + r, step = (size_t)stride * M;
+            float top = -INFINITY, sum = 0.f;
+            f32x2 acc = {0.f, 0.f};
+            for (int v0 = 0; v0 < n; v0 += AT_ONCE) {
+                f32x2 ml[AT_ONCE], x[AT_ONCE];
+#pragma unroll
+                for (int v = 0; v < AT_ONCE; ++v) {
+                    const size_t at = row + step * min(v0 + v, n - 1);
+                    ml[v] = handed2(part_ml + 2 * at);
+                    x[v] = handed2(a.part_o + at * HD + d);
+                }
+                float t = top;
+#pragma unroll
+                for (int v = 0; v < AT_ONCE; ++v) t = fmaxf(t, ml[v][0]);  // (the last part again behind the last)
+                const float ref = t == -INFINITY ? 0.f : t;
+                const float old = __builtin_amdgcn_exp2f(top - ref);
+                sum *= old, acc *= old;
+#pragma unroll
+                for (int v = 0; v < AT_ONCE; ++v) {
+                    if (v0 + v < n) {
+                        const float wt = __builtin_amdgcn_exp2f(ml[v][0] - ref);
+                        sum += wt * ml[v][1], acc += wt * x[v];
+                    }
+                }
+                top = t;
+            }
+            if (whole) {
+                const size_t at = (size_t)(w.row0 + f / a.group) * n_heads + w.head * a.group + f % a.group;
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                out[at * HD + d] = (ST)(acc[0] * inv);
+                out[at * HD + d + 1] = (ST)(acc[1] * inv);
+                if (a.lse && d == 0) a.lse[at] = ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.6931471805599453f;
+            } else {  // elements into the first part's place, which no other thread reads; weights apart, as all of a row's threads read them
+                hand_over(a.part_o + row * HD + d, acc[0]), hand_over(a.part_o + row * HD + d + 1, acc[1]);
+                if (d == 0) hand_over(a.joined_ml + 2 * row, top), hand_over(a.joined_ml + 2 * row + 1, sum);
+            }
+        }
+    };
+    const int groups = (n_parts + FAN_IN - 1) / FAN_IN, group0 = part / FAN_IN * FAN_IN, in_group = min(FAN_IN, n_parts - group0);
+    if (!last_of(a.arrived + slot0 + group0, in_group)) return;
+    join(a.part_ml, slot0 + group0, 1, in_group, groups == 1);
+    if (groups == 1) return;
+    if (!last_of(a.arrived_groups + slot0, groups)) return;
+    join(a.joined_ml, slot0, FAN_IN, groups, true);
 }
 
-template <int HD, int UNITS>
-hipError_t attend_units(const Kv4Attend& a, int dtype, int grid, hipStream_t s) {
-    constexpr int NW = 4;
+template <int HD, int UNITS, int NW>
+hipError_t attend_waves(const Kv4Attend& a, int dtype, int grid, hipStream_t s) {
+    // (tiles of more than 16 entries: a request has several, which read the same K and V)
+    const bool past = UNITS == 1 && a.past_caches;
     if (dtype == EE_BF16)
-        EE_LAUNCH((kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, __bf16>), dim3(grid), dim3(NW * 64), s, a);
+        EE_LAUNCH((past ? kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, UNITS == 1, __bf16>
+                        : kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, false, __bf16>),
+                  dim3(grid), dim3(NW * 64), s, a);
     else if constexpr (UNITS <= 2)
-        EE_LAUNCH((kv4_attend_kernel<HD, 3, 3, UNITS, NW, float>), dim3(grid), dim3(NW * 64), s, a);
+        EE_LAUNCH((past ? kv4_attend_kernel<HD, 3, 3, UNITS, NW, UNITS == 1, float> : kv4_attend_kernel<HD, 3, 3, UNITS, NW, false, float>), dim3(grid),
+                  dim3(NW * 64), s, a);
     else
         return hipErrorInvalidValue;
     return hipGetLastError();
 }
 
+template <int HD, int UNITS>
+hipError_t attend_units(const Kv4Attend& a, int dtype, int waves, int grid, hipStream_t s) {
+    if constexpr (UNITS == 1)
+        if (waves == 8) return attend_waves<HD, 1, 8>(a, dtype, grid, s);
+    return attend_waves<HD, UNITS, 4>(a, dtype, grid, s);
+}
+
 template <int HD>
-hipError_t attend_hd(const Kv4Attend& a, int dtype, int units, int grid, hipStream_t s) {
-    if (units == 1) return attend_units<HD, 1>(a, dtype, grid, s);
+hipError_t attend_hd(const Kv4Attend& a, int dtype, int units, int waves, int grid, hipStream_t s) {
+    if (units == 1) return attend_units<HD, 1>(a, dtype, waves, grid, s);
     if constexpr (HD <= 128)
-        if (units == 2) return attend_units<HD, 2>(a, dtype, grid, s);
+        if (units == 2) return attend_units<HD, 2>(a, dtype, waves, grid, s);
     if constexpr (HD <= 64)
-        if (units == 4) return attend_units<HD, 4>(a, dtype, grid, s);
+        if (units == 4) return attend_units<HD, 4>(a, dtype, waves, grid, s);
     return hipErrorInvalidValue;
 }
 
@@ -938,13 +959,13 @@ int kv4_tile_units(int dtype, int head_dim, int most_flat) {
 }
 
 hipError_t launch_kv4_init(int32_t* table, int64_t n_table, int32_t* free_blocks, int n_blocks, uint32_t* arrived, int n_arrived,
-                           hipStream_t s) {
-    EE_LAUNCH(kv4_init_kernel, dim3(1024), dim3(256), s, table, n_table, free_blocks, n_blocks, arrived, n_arrived);
+                           uint32_t* counts, hipStream_t s) {
+    EE_LAUNCH(kv4_init_kernel, dim3(1024), dim3(256), s, table, n_table, free_blocks, n_blocks, arrived, n_arrived, counts);
     return hipGetLastError();
 }
 
-hipError_t launch_kv4_plan(const Kv4Plan& p, int workgroups, hipStream_t s) {
-    EE_LAUNCH(kv4_plan_kernel, dim3(workgroups), dim3(1024), s, p);
+hipError_t launch_kv4_plan(const Kv4Plan& p, int workgroups, int threads, hipStream_t s) {
+    EE_LAUNCH(kv4_plan_kernel, dim3(workgroups), dim3(threads), s, p);
     return hipGetLastError();
 }
 
@@ -969,13 +990,13 @@ hipError_t launch_kv4_read(const Kv4Cache& c, int n_rows, const int64_t* slots, 
     }
 }
 
-hipError_t launch_kv4_attend(const Kv4Attend& a, int dtype, int head_dim, int units, int grid, hipStream_t s) {
+hipError_t launch_kv4_attend(const Kv4Attend& a, int dtype, int head_dim, int units, int waves, int grid, hipStream_t s) {
     if (grid <= 0) return hipSuccess;
     switch (head_dim) {
-        case 32: return attend_hd<32>(a, dtype, units, grid, s);
-        case 64: return attend_hd<64>(a, dtype, units, grid, s);
-        case 128: return attend_hd<128>(a, dtype, units, grid, s);
-        case 256: return attend_hd<256>(a, dtype, units, grid, s);
+        case 32: return attend_hd<32>(a, dtype, units, waves, grid, s);
+        case 64: return attend_hd<64>(a, dtype, units, waves, grid, s);
+        case 128: return attend_hd<128>(a, dtype, units, waves, grid, s);
+        case 256: return attend_hd<256>(a, dtype, units, waves, grid, s);
         default: return hipErrorInvalidValue;
     }
 }

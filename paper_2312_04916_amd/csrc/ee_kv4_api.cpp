@@ -21,13 +21,25 @@ int check_config(const ee_kv4_config& c) {
     if (c.n_blocks < 1 || c.n_blocks > (1 << 26)) return EE_ERR_CONFIG;
     if (c.max_seqs < 1 || c.max_seqs > EE_KV4_MAX_SEQS) return EE_ERR_CONFIG;
     if (c.max_positions < 1 || c.max_positions > (1 << 20)) return EE_ERR_CONFIG;
-    if (c.max_rows < 1 || c.max_rows > (1 << 22)) return EE_ERR_CONFIG;
+    if (c.max_rows < 1 || c.max_rows > (1 << 20)) return EE_ERR_CONFIG;
     return EE_OK;
 }
 
-// A launch of the attention is cut into about this many parts.
-constexpr int TARGET_PARTS = 1024;
-constexpr int MIN_CHUNKS = 8;  // of a part that is one of several
+// How a launch of the attention is cut: workgroups of `waves` waves, in about `parts` parts of at least `min_chunks` chunks.
+constexpr int TARGET_PARTS = 2048;  // most of any
+struct Cut {
+    int waves, parts, min_chunks;
+};
+Cut cut_of(const ee_kv4_config& c, int n_seqs, int n_rows, int units) {
+    const int items = std::min(n_seqs, n_rows) * c.n_kv_heads;
+    Cut k = {4, 768, 8};
+    if (units == 1 && items < 128) k = {8, 256, 8};
+    return k;
+}
+
+// A pool larger than the last-level cache (256 MB) is not found there again by the next step: keeping what is read only pushes
+// other data out.
+constexpr size_t PAST_CACHES_BYTES = 256u << 20;
 
 int table_stride(const ee_kv4_config& c) { return (c.max_positions + c.block_tokens - 1) / c.block_tokens; }
 size_t layer_bytes(const ee_kv4_config& c) {
@@ -63,13 +75,13 @@ StateLayout state_layout(const ee_kv4_config& c) {
     w.row_start = take(((size_t)c.max_seqs + 1) * 4);
     w.served = take((size_t)c.max_seqs * 4);
     w.held_next = take((size_t)c.max_seqs * 4);
-    w.counts = take(8);  // free blocks, parts
+    w.counts = take(12);  // free blocks, parts, the plan's workgroups that have read the lengths
     w.max_parts = most_parts(c, c.max_seqs, c.max_rows, 16);
     w.parts = take((size_t)w.max_parts * sizeof(Kv4Part));
     w.max_slots = 2 * TARGET_PARTS;
-    w.arrived = take((size_t)w.max_slots * 4);
+    w.arrived = take((size_t)w.max_slots * 8);  // of groups of parts, of items
     const int most = 16 * kv4_tile_units(c.dtype, c.head_dim, 1 << 30);
-    w.part_ml = take((size_t)w.max_slots * most * 8);
+    w.part_ml = take((size_t)w.max_slots * most * 16);  // of parts, of joined ones
     w.part_o = take((size_t)w.max_slots * most * c.head_dim * 4);
     w.total = off;
     return w;
@@ -83,7 +95,7 @@ struct ee_kv4 {
     ee_kv4_config cfg;
     char *pool, *state;
     StateLayout sl;
-    int n_seqs, n_rows, units;  // of the latest plan (n_seqs = 0: none)
+    int n_seqs, n_rows, units, waves;  // of the latest plan (n_seqs = 0: none)
     ee_kv4_arrays arrays;
 };
 
@@ -113,7 +125,7 @@ int ee_kv4_create(const ee_kv4_config* cfg, void* dev_pool, size_t pool_bytes, v
     c->state = (char*)dev_state;
     c->sl = state_layout(*cfg);
     c->n_seqs = c->n_rows = 0;
-    c->units = 1;
+    c->units = 1, c->waves = 4;
     const StateLayout& w = c->sl;
     ee_kv4_arrays& a = c->arrays;
     a.table = (int32_t*)(c->state + w.table);
@@ -127,7 +139,7 @@ int ee_kv4_create(const ee_kv4_config* cfg, void* dev_pool, size_t pool_bytes, v
     a.n_free = (int32_t*)(c->state + w.counts);
     a.table_stride = table_stride(*cfg);
     const int st = hip_status(launch_kv4_init(a.table, (int64_t)cfg->max_seqs * a.table_stride, a.free_blocks, cfg->n_blocks,
-                                              (uint32_t*)(c->state + w.arrived), w.max_slots, (hipStream_t)stream));
+                                              (uint32_t*)(c->state + w.arrived), 2 * w.max_slots, (uint32_t*)a.n_free, (hipStream_t)stream));
     if (st != EE_OK) {
         delete c;
         return st;
@@ -159,22 +171,23 @@ int ee_kv4_plan(ee_kv4* c, int n_seqs, const int32_t* dev_held, const int32_t* d
     Kv4Plan p;
     p.held = dev_held, p.start = dev_start, p.end = dev_end;
     p.n_seqs = n_seqs, p.n_rows = n_rows, p.max_rows_per_seq = most;
-    p.block_tokens = g.block_tokens, p.n_blocks = g.n_blocks, p.table_stride = c->arrays.table_stride, p.max_positions = g.max_positions;
+    p.block_shift = __builtin_ctz((unsigned)g.block_tokens), p.n_blocks = g.n_blocks, p.table_stride = c->arrays.table_stride, p.max_positions = g.max_positions;
     p.a = c->arrays;
     p.parts = (Kv4Part*)(c->state + c->sl.parts);
-    p.n_parts = (int32_t*)(c->state + c->sl.counts) + 1;
+    p.n_parts = c->arrays.n_free + 1;
+    p.arrived = (uint32_t*)c->arrays.n_free + 2;
     p.group = group, p.kv_heads = g.n_kv_heads;
     const int units = kv4_tile_units(g.dtype, g.head_dim, (int)std::min<int64_t>((int64_t)most * group, 1 << 30));
     p.tile_rows = 16 * units;
     p.max_parts = (int)std::min(c->sl.max_parts, most_parts(g, n_seqs, n_rows, p.tile_rows));
-    p.target_parts = TARGET_PARTS, p.min_chunks = MIN_CHUNKS;
-    // (a workgroup that writes held_next must not do so while another one reads it as dev_held)
-    const int32_t* hn = c->arrays.held_next;
-    const bool in_place = dev_held < hn + g.max_seqs && hn < dev_held + n_seqs;
-    const int workgroups = in_place ? 1 : std::min(64, 1 + n_rows / 4096);
-    const int rc = hip_status(launch_kv4_plan(p, workgroups, (hipStream_t)stream));
+    const Cut cut = cut_of(g, n_seqs, n_rows, units);
+    p.target_parts = cut.parts, p.min_chunks = cut.min_chunks;
+    // one thread per row (and part: about as many), a few for the requests; a small step in one small workgroup
+    const bool small = n_seqs < 256 && n_rows <= 256;
+    const int workgroups = small ? 1 : std::min(256, 1 + (n_rows + p.max_parts) / 1024);
+    const int rc = hip_status(launch_kv4_plan(p, workgroups, small ? 256 : 1024, (hipStream_t)stream));
     if (rc != EE_OK) return rc;
-    c->n_seqs = n_seqs, c->n_rows = n_rows, c->units = units;
+    c->n_seqs = n_seqs, c->n_rows = n_rows, c->units = units, c->waves = cut.waves;
     return EE_OK;
 }
 
@@ -228,18 +241,21 @@ int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride,
     a.layer = c->pool + layer_bytes(g) * layer;
     a.table = c->arrays.table, a.table_stride = c->arrays.table_stride;
     a.parts = (const Kv4Part*)(c->state + c->sl.parts);
-    a.n_parts = (const int32_t*)(c->state + c->sl.counts) + 1;
+    a.n_parts = c->arrays.n_free + 1;
     a.q = dev_q, a.q_row = q_row_stride, a.q_head = q_head_stride;
     a.out = dev_out, a.lse = dev_lse;
     a.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt((float)g.head_dim)) * 1.4426950408889634f;
     a.window = window, a.group = g.n_heads / g.n_kv_heads, a.kv_heads = g.n_kv_heads;
     a.tiles_shift = __builtin_ctz((unsigned)g.block_tokens) - 4;
+    a.past_caches = layer_bytes(g) * g.n_layers > PAST_CACHES_BYTES;
     a.q_vec = ((uintptr_t)dev_q & 15) == 0 && (q_row_stride * (int64_t)es) % 16 == 0 && (q_head_stride * (int64_t)es) % 16 == 0;
     a.part_o = (float*)(c->state + c->sl.part_o);
     a.part_ml = (float*)(c->state + c->sl.part_ml);
+    a.joined_ml = a.part_ml + (size_t)c->sl.max_slots * 2 * 16 * kv4_tile_units(g.dtype, g.head_dim, 1 << 30);
     a.arrived = (uint32_t*)(c->state + c->sl.arrived);
+    a.arrived_groups = a.arrived + c->sl.max_slots;
     const int grid = (int)std::min(c->sl.max_parts, most_parts(g, c->n_seqs, c->n_rows, 16 * c->units));
-    return hip_status(launch_kv4_attend(a, g.dtype, g.head_dim, c->units, grid, (hipStream_t)stream));
+    return hip_status(launch_kv4_attend(a, g.dtype, g.head_dim, c->units, c->waves, grid, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -173,7 +173,7 @@ def test_kv4_configs_and_sizes():
     assert sb.value > 4 * 16 * 4 + 100 * 4 + 64 * 16
     for bad in (dict(n_layers=0), dict(n_heads=0), dict(n_kv_heads=0), dict(n_kv_heads=3), dict(n_heads=2048), dict(head_dim=96), dict(dtype=2),
                 dict(block_tokens=8), dict(block_tokens=48), dict(block_tokens=512), dict(n_blocks=0), dict(max_seqs=0), dict(max_seqs=4097),
-                dict(max_positions=0), dict(max_positions=(1 << 20) + 1), dict(max_rows=0), dict(max_rows=(1 << 22) + 1)):
+                dict(max_positions=0), dict(max_positions=(1 << 20) + 1), dict(max_rows=0), dict(max_rows=(1 << 20) + 1)):
         assert code(**bad) == -1, bad
     assert L.ee_kv4_bytes(None, None, None) == -7
 
