@@ -53,7 +53,7 @@ struct Kv4Plan {
 
 struct Kv4Cache {
     char* layer;  // this layer's pool
-    int kv_heads, head_dim, block_tokens, dtype;
+    int kv_heads, head_dim, block_shift, dtype;  // 1 << block_shift positions per block
     int64_t n_slots;
 };
 

@@ -284,73 +284,132 @@ __device__ __forceinline__ void load8(const ST* p, bool vec, float (&x)[8]) {
     for (int e = 0; e < 8; ++e) x[e] = (float)p[e];
 }
 
-__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, false));  // lane ^ 1
-    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, false));  // lane ^ 2
+template <int N>
+__device__ __forceinline__ void store_words(char* p, const uint32_t (&w)[N]) {
+    if constexpr (N == 1) {
+        *(uint32_t*)p = w[0];
+    } else if constexpr (N == 2) {
+        *(u32x2*)p = u32x2{w[0], w[1]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) *(u32x4*)(p + 4 * i) = u32x4{w[i], w[i + 1], w[i + 2], w[i + 3]};
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void store_bytes(char* p, const uint32_t (&b)[N]) {
+    if constexpr (N == 1) {
+        *p = (char)b[0];
+    } else if constexpr (N == 2) {
+        *(uint16_t*)p = (uint16_t)(b[0] | b[1] << 8);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) *(uint32_t*)(p + i) = b[i] | b[i + 1] << 8 | b[i + 2] << 16 | b[i + 3] << 24;
+    }
 }
 
 // tile of a slot's position, and the position in it
 template <int HD>
 __device__ __forceinline__ char* tile_of(const Kv4Cache& c, int64_t slot, int head, int& key) {
-    const int64_t block = slot / c.block_tokens;
-    const int in = (int)(slot % c.block_tokens);
+    const int64_t block = slot >> c.block_shift;
+    const int in = (int)slot & ((1 << c.block_shift) - 1);
     key = in & 15;
-    return c.layer + ((block * c.kv_heads + head) * (c.block_tokens >> 4) + (in >> 4)) * (int64_t)Kv4Tile::bytes(HD);
+    return c.layer + (((block * c.kv_heads + head) << (c.block_shift - 4)) + (in >> 4)) * (int64_t)Kv4Tile::bytes(HD);
 }
 
-// One thread per 8 elements, four threads per group: the largest magnitude by two lane exchanges, the conversion by the
-// hardware's (which rounds to nearest even and saturates).
+// Largest of the four lanes that share a column (lanes i, i + 16, i + 32, i + 48).
+__device__ __forceinline__ uint32_t rows4_umax(uint32_t v) {
+    const lanes_u32x2 a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max(a[0], a[1]);
+    const lanes_u32x2 b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max(b[0], b[1]);
+}
+
+// One wave per 16 rows of one head of K or of V, its lanes as the attention reads a tile: lane (quarter h, row t) has elements
+// 8h .. 8h+7 of every group.  So a group's largest magnitude is two lane swaps away, K of 16 rows that fill a tile is written as one
+// run of 1 KB (head_dim 128) and its scales as one of 64 bytes; the conversion is the hardware's, which rounds to nearest even
+// and saturates.  Rows that follow each other usually lie in one tile, whose lines so come from one workgroup: with the heads
+// of a row together instead, eight XCDs wrote parts of each line (79 us where this takes 49: 40 768 rows of 8 heads of 128 in
+// bf16, 211 MB, which a copy moves in 41).
 template <int HD, typename ST>
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Cache c, int n_rows, const ST* __restrict__ k, int64_t k_row, int64_t k_head,
                                                          const ST* __restrict__ v, int64_t v_row, int64_t v_head, int vec,
                                                          const int64_t* __restrict__ slots) {
-    constexpr int TPV = HD / 8, LB = HD / 8;  // threads per vector, bytes per lane of a tile
-    const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int e8 = (int)(idx % TPV);
-    const int64_t vecs = idx / TPV;
-    const int which = (int)(vecs & 1), head = (int)((vecs >> 1) % c.kv_heads);
-    const int64_t row = (vecs >> 1) / c.kv_heads;
-    if (row >= n_rows) return;  // (whole groups of four lanes: their exchanges stay among themselves)
-    const int64_t slot = slots[row];
-    if (slot < 0 || slot >= c.n_slots) return;
-    float x[8];
-    const ST* src = which ? v + row * v_row + head * v_head : k + row * k_row + head * k_head;
-    load8(src + e8 * 8, (vec >> which) & 1, x);
-    uint32_t top = 0;
+    constexpr int G = HD / 32, LB = HD / 8;
+    const int lane = threadIdx.x & 63, h = lane >> 4;
+    const uint32_t vecs = blockIdx.x * 4u + (threadIdx.x >> 6);
+    const int which = vecs & 1, head = (int)((vecs >> 1) % (uint32_t)c.kv_heads);
+    const int64_t row = (int64_t)((vecs >> 1) / (uint32_t)c.kv_heads) * 16 + (lane & 15);
+    const bool there = row < n_rows;
+    const int64_t slot = there ? slots[row] : -1;
+    float x[G][8] = {};
+    if (there) {
+        const ST* src = (which ? v + row * v_row + head * v_head : k + row * k_row + head * k_head) + h * 8;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-    top = quad_max(top);
-    // the least e with top <= 7 * 2^e = 1.75 * 2^(e+2); biased by 127
-    uint32_t sc = min(max((top >> 23) + ((top & 0x7fffffu) > 0x600000u ? 1u : 0u), SCALE_MIN + 2) - 2, SCALE_MAX);
-    const float unit = __uint_as_float(sc << 23);
-    uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], unit, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], unit, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], unit, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], unit, 3);
-    if (top >= 0x7f800000u) sc = SCALE_NAN;
+        for (int g = 0; g < G; ++g) load8(src + g * 32, (vec >> which) & 1, x[g]);
+    }
+    uint32_t code[G], sc[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[g][e]) & 0x7fffffffu);
+        top = rows4_umax(top);
+        // the least e with top <= 7 * 2^e = 1.75 * 2^(e+2); biased by 127
+        sc[g] = min(max((top >> 23) + ((top & 0x7fffffu) > 0x600000u ? 1u : 0u), SCALE_MIN + 2) - 2, SCALE_MAX);
+        const float unit = __uint_as_float(sc[g] << 23);
+        uint32_t w = 0;
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[g][0], x[g][1], unit, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[g][2], x[g][3], unit, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[g][4], x[g][5], unit, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[g][6], x[g][7], unit, 3);
+        code[g] = w;
+        if (top >= 0x7f800000u) sc[g] = SCALE_NAN;
+    }
+    if (slot < 0 || slot >= c.n_slots) return;
     int key;
     char* tile = tile_of<HD>(c, slot, head, key);
-    const int g = e8 >> 2;
     if (which == 0) {
-        *(uint32_t*)(tile + ((e8 & 3) * 16 + key) * LB + g * 4) = w;
-        if ((e8 & 3) == 0) tile[Kv4Tile::k_scales(HD) + key * (HD / 32) + g] = (char)sc;
+        store_words<G>(tile + (h * 16 + key) * LB, code);
+        if (h == 0) store_bytes<G>(tile + Kv4Tile::k_scales(HD) + key * G, sc);
     } else {
         constexpr int EPC = HD / 16;  // elements per column
-        char* t = tile + Kv4Tile::v_codes(HD) + (key & 3) * (LB / 4);
-        const int col = (key >> 2) * 16 + e8 * 8 / EPC;
-        if constexpr (EPC == 16) *(uint32_t*)(t + col * LB + (e8 & 1) * 4) = w;
-        if constexpr (EPC == 8) *(uint32_t*)(t + col * LB) = w;
-        if constexpr (EPC == 4) {
-            *(uint16_t*)(t + col * LB) = (uint16_t)w;
-            *(uint16_t*)(t + (col + 1) * LB) = (uint16_t)(w >> 16);
-        }
-        if constexpr (EPC == 2) {
+        char* t = tile + Kv4Tile::v_codes(HD) + (key & 3) * (LB / 4) + (key >> 2) * 16 * LB;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) t[(col + b) * LB] = (char)(w >> (8 * b));
+        for (int g = 0; g < G; ++g) {
+            char* at = t + (g * 32 + h * 8) / EPC * LB;
+            if constexpr (EPC == 16) *(uint32_t*)(at + (h & 1) * 4) = code[g];
+            if constexpr (EPC == 8) *(uint32_t*)at = code[g];
+            if constexpr (EPC == 4) {
+                *(uint16_t*)at = (uint16_t)code[g];
+                *(uint16_t*)(at + LB) = (uint16_t)(code[g] >> 16);
+            }
+            if constexpr (EPC == 2) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) at[b * LB] = (char)(code[g] >> (8 * b));
+            }
         }
-        if ((e8 & 3) == 0) tile[Kv4Tile::v_scales(HD) + g * 16 + key] = (char)sc;
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+            if (h == (g & 3)) tile[Kv4Tile::v_scales(HD) + g * 16 + key] = (char)sc[g];
     }
+}
+
+// What a thread of the read-back has: 8 elements of 16 rows of one head of K (of V), then of the next, for the same lines' sake.
+struct Kv4Work {
+    int e8, which, head;
+    int64_t row;
+};
+template <int TPV>
+__device__ __forceinline__ Kv4Work work_of(int kv_heads) {
+    const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t in = (uint32_t)(idx % (16 * TPV)), vec = (uint32_t)(idx / (16 * TPV));
+    Kv4Work w;
+    w.e8 = in % TPV;
+    w.which = vec & 1;
+    w.head = (vec >> 1) % (uint32_t)kv_heads;
+    w.row = (int64_t)((vec >> 1) / (uint32_t)kv_heads) * 16 + in / TPV;
+    return w;
 }
 
 // 8 elements of a word of codes, times their group's scale
@@ -366,40 +425,38 @@ template <int HD, typename ST>
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Cache c, int n_rows, const int64_t* __restrict__ slots, ST* __restrict__ k,
                                                        ST* __restrict__ v) {
     constexpr int TPV = HD / 8, LB = HD / 8;
-    const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int e8 = (int)(idx % TPV);
-    const int64_t vecs = idx / TPV;
-    const int which = (int)(vecs & 1), head = (int)((vecs >> 1) % c.kv_heads);
-    const int64_t row = (vecs >> 1) / c.kv_heads;
+    const Kv4Work w = work_of<TPV>(c.kv_heads);
+    const int e8 = w.e8, which = w.which, head = w.head;
+    const int64_t row = w.row;
     if (row >= n_rows) return;
     ST* dst = which ? v : k;
     if (!dst) return;
     dst += (row * c.kv_heads + head) * HD + e8 * 8;
     const int64_t slot = slots[row];
-    uint32_t w = 0, sc = SCALE_MIN;
+    uint32_t code = 0, sc = SCALE_MIN;
     if (slot >= 0 && slot < c.n_slots) {
         int key;
         const char* tile = tile_of<HD>(c, slot, head, key);
         const int g = e8 >> 2;
         if (which == 0) {
-            w = *(const uint32_t*)(tile + ((e8 & 3) * 16 + key) * LB + g * 4);
+            code = *(const uint32_t*)(tile + ((e8 & 3) * 16 + key) * LB + g * 4);
             sc = (uint8_t)tile[Kv4Tile::k_scales(HD) + key * (HD / 32) + g];
         } else {
             constexpr int EPC = HD / 16;
             const char* t = tile + Kv4Tile::v_codes(HD) + (key & 3) * (LB / 4);
             const int col = (key >> 2) * 16 + e8 * 8 / EPC;
-            if constexpr (EPC == 16) w = *(const uint32_t*)(t + col * LB + (e8 & 1) * 4);
-            if constexpr (EPC == 8) w = *(const uint32_t*)(t + col * LB);
-            if constexpr (EPC == 4) w = *(const uint16_t*)(t + col * LB) | (uint32_t) * (const uint16_t*)(t + (col + 1) * LB) << 16;
+            if constexpr (EPC == 16) code = *(const uint32_t*)(t + col * LB + (e8 & 1) * 4);
+            if constexpr (EPC == 8) code = *(const uint32_t*)(t + col * LB);
+            if constexpr (EPC == 4) code = *(const uint16_t*)(t + col * LB) | (uint32_t) * (const uint16_t*)(t + (col + 1) * LB) << 16;
             if constexpr (EPC == 2) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) w |= (uint32_t)(uint8_t)t[(col + b) * LB] << (8 * b);
+                for (int b = 0; b < 4; ++b) code |= (uint32_t)(uint8_t)t[(col + b) * LB] << (8 * b);
             }
             sc = (uint8_t)tile[Kv4Tile::v_scales(HD) + g * 16 + key];
         }
     }
     bf16x2 x[4];
-    values8(w, sc, x);
+    values8(code, sc, x);
     if (sc == SCALE_NAN) {
         const bf16x2 nan = {(__bf16)__builtin_nanf(""), (__bf16)__builtin_nanf("")};
 #pragma unroll
@@ -927,8 +984,8 @@ hipError_t append_hd(const Kv4Cache& c, int n_rows, const void* k, int64_t k_row
                      const int64_t* slots, hipStream_t s) {
     const int es = c.dtype == EE_BF16 ? 2 : 4;
     const int vec = (aligned16(k, k_row, k_head, es) ? 1 : 0) | (aligned16(v, v_row, v_head, es) ? 2 : 0);
-    const int64_t threads = (int64_t)n_rows * c.kv_heads * 2 * (HD / 8);
-    const dim3 grid((unsigned)((threads + 255) / 256));
+    const int64_t waves = (int64_t)((n_rows + 15) / 16) * c.kv_heads * 2;
+    const dim3 grid((unsigned)((waves + 3) / 4));
     if (c.dtype == EE_BF16)
         EE_LAUNCH((kv4_append_kernel<HD, __bf16>), grid, dim3(256), s, c, n_rows, (const __bf16*)k, k_row, k_head, (const __bf16*)v, v_row, v_head,
                   vec, slots);
@@ -940,7 +997,7 @@ hipError_t append_hd(const Kv4Cache& c, int n_rows, const void* k, int64_t k_row
 
 template <int HD>
 hipError_t read_hd(const Kv4Cache& c, int n_rows, const int64_t* slots, void* k, void* v, hipStream_t s) {
-    const int64_t threads = (int64_t)n_rows * c.kv_heads * 2 * (HD / 8);
+    const int64_t threads = (int64_t)((n_rows + 15) / 16 * 16) * c.kv_heads * 2 * (HD / 8);
     const dim3 grid((unsigned)((threads + 255) / 256));
     if (c.dtype == EE_BF16)
         EE_LAUNCH((kv4_read_kernel<HD, __bf16>), grid, dim3(256), s, c, n_rows, slots, (__bf16*)k, (__bf16*)v);

@@ -182,10 +182,12 @@ int ee_kv4_plan(ee_kv4* c, int n_seqs, const int32_t* dev_held, const int32_t* d
     p.max_parts = (int)std::min(c->sl.max_parts, most_parts(g, n_seqs, n_rows, p.tile_rows));
     const Cut cut = cut_of(g, n_seqs, n_rows, units);
     p.target_parts = cut.parts, p.min_chunks = cut.min_chunks;
-    // one thread per row (and part: about as many), a few for the requests; a small step in one small workgroup
-    const bool small = n_seqs < 256 && n_rows <= 256;
-    const int workgroups = small ? 1 : std::min(256, 1 + (n_rows + p.max_parts) / 1024);
-    const int rc = hip_status(launch_kv4_plan(p, workgroups, small ? 256 : 1024, (hipStream_t)stream));
+    // one thread per row and part, and for blocks that change hands, which only the GPU knows, a sixteenth of the pool; a small
+    // step in one small workgroup
+    const int threads = n_seqs < 256 && n_rows <= 1024 ? 256 : 1024;
+    const int64_t tasks = (int64_t)n_rows + p.max_parts + g.n_blocks / 16;
+    const int workgroups = n_rows + p.max_parts <= 2048 && g.n_blocks <= 4096 && threads == 256 ? 1 : (int)std::min<int64_t>(256, 1 + tasks / threads);
+    const int rc = hip_status(launch_kv4_plan(p, workgroups, threads, (hipStream_t)stream));
     if (rc != EE_OK) return rc;
     c->n_seqs = n_seqs, c->n_rows = n_rows, c->units = units, c->waves = cut.waves;
     return EE_OK;
@@ -201,7 +203,7 @@ static int check_rows(const ee_kv4* c, int layer, int n_rows) {
 static Kv4Cache geometry(const ee_kv4* c, int layer) {
     Kv4Cache k;
     k.layer = c->pool + layer_bytes(c->cfg) * layer;
-    k.kv_heads = c->cfg.n_kv_heads, k.head_dim = c->cfg.head_dim, k.block_tokens = c->cfg.block_tokens, k.dtype = c->cfg.dtype;
+    k.kv_heads = c->cfg.n_kv_heads, k.head_dim = c->cfg.head_dim, k.block_shift = __builtin_ctz((unsigned)c->cfg.block_tokens), k.dtype = c->cfg.dtype;
     k.n_slots = (int64_t)c->cfg.n_blocks * c->cfg.block_tokens;
     return k;
 }

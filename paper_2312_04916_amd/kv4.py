@@ -105,8 +105,7 @@ class Kv4Cache:
         """ee_kv4_read -> k, v [rows][n_kv_heads][head_dim]: the values that the slots hold."""
         rows = slots.shape[0]
         p = self._slot_ptr(slots, rows)
-        k = torch.empty(rows, self.cfg.n_kv_heads, self.cfg.head_dim, dtype=self.dtype, device=self.device)
-        v = torch.empty_like(k)
+        k, v = torch.empty(2, rows, self.cfg.n_kv_heads, self.cfg.head_dim, dtype=self.dtype, device=self.device).unbind()
         code = self._read(self.h, layer, rows, p, k.data_ptr(), v.data_ptr(), _raw_stream(stream, self._index))
         if code:
             _chk(code, "ee_kv4_read")
