@@ -560,10 +560,11 @@ __device__ __forceinline__ f32x2 handed2(const float* p) {
 constexpr int FAN_IN = 32;  // parts that are joined at a time
 
 // NT: bf16 terms of an element of Q (1: Q is bf16; 3: fp32, exactly), PT: of a probability.  UNITS: 16 entries each of a tile.
-template <int HD, int NT, int PT, int UNITS, int NW, bool PAST, typename ST>
-__global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 : 3) : 1) void kv4_attend_kernel(Kv4Attend a) {
+template <int HD, int NT, int PT, int UNITS, int NW, int DEPTH, bool PAST, typename ST>
+__global__ __launch_bounds__(NW * 64, UNITS == 1 && HD <= 128 ? (DEPTH > 1 ? 2 : NT == 1 ? 4 : 3) : 1) void kv4_attend_kernel(Kv4Attend a) {
     constexpr int G = HD / 32, EPC = HD / 16, M = 16 * UNITS;
-    constexpr int CT = 2, STEPS = KV4_CHUNK / (16 * CT);  // tiles of 16 positions at a time: one contraction of P.V
+    constexpr int CT = KV4_CHUNK / 16;  // tiles of 16 positions at a time: one contraction of P.V
+    static_assert(CT == 2, "a contraction has 32 positions");
     constexpr int LDO = HD + 4;
     __shared__ float s_o[NW * 16 * LDO];
     __shared__ float s_m[NW * 16], s_l[NW * 16];
@@ -633,18 +634,17 @@ __global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 :
     const char* base = a.layer + ((size_t)Kv4Tile::bytes(HD) << a.tiles_shift) * w.head;
     const int in_block = (1 << a.tiles_shift) - 1;
 
-    // step `it` of this wave: tiles (c_lo + wave + it / STEPS * NW) * 4 + it % STEPS * CT ...; tiles behind the last one that is
-    // seen repeat it (their positions are hidden)
-    const int my_chunks = max(0, (c_hi - c_lo - wave + NW - 1) / NW);
-    const int n_it = my_chunks * STEPS;
-    auto tile_at = [&](int it, int t) { return (c_lo + wave + it / STEPS * NW) * (KV4_CHUNK / 16) + it % STEPS * CT + t; };
-    // block numbers of the next 64 / CT steps, one per lane
+    // step `it` of this wave: chunk c_lo + wave + it * NW, two tiles; a tile behind the last one that is seen repeats it (its
+    // positions are hidden)
+    const int n_it = max(0, (c_hi - c_lo - wave + NW - 1) / NW);
+    auto tile_at = [&](int it, int t) { return (c_lo + wave + it * NW) * CT + t; };
+    // block numbers of AHEAD steps at a time, one per lane, and those of the next
     constexpr int AHEAD = 64 / CT;
     auto blocks_from = [&](int it) {
         const int t = min(tile_at(it + lane / CT, lane % CT), last_tile);
         return table[t >> a.tiles_shift];
     };
-    int blocks = n_it ? blocks_from(0) : 0;
+    int blocks = n_it ? blocks_from(0) : 0, blocks_next = n_it > AHEAD ? blocks_from(AHEAD) : 0;
     auto tile_addr = [&](int it, int t) {
         const int tile = min(tile_at(it, t), last_tile);
         const int block = __builtin_amdgcn_readlane(blocks, it % AHEAD * CT + t);
@@ -660,20 +660,22 @@ __global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 :
         for (int j = 0; j < EPC; ++j) o[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // K of the next step is asked for as soon as K of this one has been used, V likewise: one set of registers, and with four
-    // waves per SIMD always about 45 KB on their way to a CU
-    KeyRegs<HD> kr[CT];
-    ValueRegs<HD> vr[CT];
+    // K of a step DEPTH ahead is asked for as soon as K of this one has been used, V likewise
+    KeyRegs<HD> key_regs[DEPTH][CT];
+    ValueRegs<HD> value_regs[DEPTH][CT];
     const char* at[CT];
-    if (n_it) {
 #pragma unroll
-        for (int t = 0; t < CT; ++t) at[t] = tile_addr(0, t);
+    for (int i = 0; i < DEPTH; ++i) {
+        if (i < n_it) {
 #pragma unroll
-        for (int t = 0; t < CT; ++t) load_keys<HD, PAST>(at[t], lane, kr[t]);
+            for (int t = 0; t < CT; ++t) at[t] = tile_addr(i, t);
 #pragma unroll
-        for (int t = 0; t < CT; ++t) load_values<HD, PAST>(at[t], lane, vr[t]);
+            for (int t = 0; t < CT; ++t) load_keys<HD, PAST>(at[t], lane, key_regs[i][t]);
+#pragma unroll
+            for (int t = 0; t < CT; ++t) load_values<HD, PAST>(at[t], lane, value_regs[i][t]);
+        }
     }
-    for (int it = 0; it < n_it; ++it) {
+    auto step = [&](const int it, KeyRegs<HD>(&kr)[CT], ValueRegs<HD>(&vr)[CT]) {
         const int key0 = tile_at(it, 0) * 16;
         // scores: rows = positions, columns = entries
         f32x4 s[UNITS][CT];
@@ -692,11 +694,14 @@ __global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 :
                     for (int n = NT - 1; n >= 0; --n) s[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[u][n][g], s[u][t], 0, 0, 0);
             }
         }
-        const bool more = it + 1 < n_it;
+        const bool more = it + DEPTH < n_it;
         if (more) {
-            if ((it + 1) % AHEAD == 0) blocks = blocks_from(it + 1);
+            if ((it + DEPTH) % AHEAD == 0) {
+                blocks = blocks_next;
+                blocks_next = blocks_from(it + DEPTH + AHEAD);
+            }
 #pragma unroll
-            for (int t = 0; t < CT; ++t) at[t] = tile_addr(it + 1, t);
+            for (int t = 0; t < CT; ++t) at[t] = tile_addr(it + DEPTH, t);
 #pragma unroll
             for (int t = 0; t < CT; ++t) load_keys<HD, PAST>(at[t], lane, kr[t]);
         }
@@ -823,6 +828,11 @@ __global__ __launch_bounds__(NW * 64, (UNITS == 1 && HD <= 128) ? (NT == 1 ? 4 :
                         if (count[i] > 0.f) o[u][j][i] = __builtin_nanf("");
             }
         }
+    };
+    for (int it = 0; it < n_it; it += DEPTH) {
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i)
+            if (i == 0 || it + i < n_it) step(it + i, key_regs[i], value_regs[i]);
     }
 
     // join the waves' shares, 16 entries at a time
@@ -946,12 +956,13 @@ template <int HD, int UNITS, int NW>
 hipError_t attend_waves(const Kv4Attend& a, int dtype, int grid, hipStream_t s) {
     // (tiles of more than 16 entries: a request has several, which read the same K and V)
     const bool past = UNITS == 1 && a.past_caches;
+    constexpr int DEPTH = NW == 8 && HD <= 128 ? 2 : 1;
     if (dtype == EE_BF16)
-        EE_LAUNCH((past ? kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, UNITS == 1, __bf16>
-                        : kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, false, __bf16>),
+        EE_LAUNCH((past ? kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, DEPTH, UNITS == 1, __bf16>
+                        : kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, DEPTH, false, __bf16>),
                   dim3(grid), dim3(NW * 64), s, a);
     else if constexpr (UNITS <= 2)
-        EE_LAUNCH((past ? kv4_attend_kernel<HD, 3, 3, UNITS, NW, UNITS == 1, float> : kv4_attend_kernel<HD, 3, 3, UNITS, NW, false, float>), dim3(grid),
+        EE_LAUNCH((past ? kv4_attend_kernel<HD, 3, 3, UNITS, NW, DEPTH, UNITS == 1, float> : kv4_attend_kernel<HD, 3, 3, UNITS, NW, DEPTH, false, float>), dim3(grid),
                   dim3(NW * 64), s, a);
     else
         return hipErrorInvalidValue;

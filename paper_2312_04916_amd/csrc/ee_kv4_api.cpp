@@ -37,9 +37,9 @@ Cut cut_of(const ee_kv4_config& c, int n_seqs, int n_rows, int units) {
     return k;
 }
 
-// A pool larger than the last-level cache (256 MB) is not found there again by the next step: keeping what is read only pushes
-// other data out.
-constexpr size_t PAST_CACHES_BYTES = 256u << 20;
+// A pool of more than half of the last-level cache (256 MB) is not found there again by the next step, which has read weights in
+// between: keeping what is read only pushes other data out.
+constexpr size_t PAST_CACHES_BYTES = 128u << 20;
 
 int table_stride(const ee_kv4_config& c) { return (c.max_positions + c.block_tokens - 1) / c.block_tokens; }
 size_t layer_bytes(const ee_kv4_config& c) {
