@@ -77,6 +77,7 @@ struct Kv4Attend {
     uint32_t *arrived, *arrived_groups;  // [slot] of the first part of a group, of an item: parts, groups that have been left
 };
 
+constexpr int KV4_WIDE = 128;  // entries of the tiles of prompts
 constexpr int KV4_CHUNK = 32;  // positions: what a wave works on at a time, and the grain of the parts
 
 // Entries of a tile in units of 16 (the columns of a matrix instruction), by the most that a request has.

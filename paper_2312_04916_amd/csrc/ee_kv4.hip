@@ -15,6 +15,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -509,41 +510,46 @@ struct ValueRegs {
     uint32_t sc;  // of the lane's four keys, in its column's group
 };
 
+// The pool, as an address that the compiler knows to be global memory (a flat load would also wait for LDS).  An unsigned offset
+// from an address that all lanes share costs no arithmetic.
+#define EE_GLOBAL __attribute__((address_space(1)))
+typedef const EE_GLOBAL char* PoolPtr;
+
 // PAST: without keeping the lines in the caches.
 template <bool PAST, int N>
-__device__ __forceinline__ void load_words(const char* p, uint32_t (&w)[N]) {
+__device__ __forceinline__ void load_words(PoolPtr p, uint32_t (&w)[N]) {
     if constexpr (N == 1) {
-        w[0] = *(const uint32_t*)p;
+        w[0] = *(const EE_GLOBAL uint32_t*)p;
     } else if constexpr (N == 2) {
-        const u32x2 x = PAST ? __builtin_nontemporal_load((const u32x2*)p) : *(const u32x2*)p;
+        const u32x2 x = PAST ? __builtin_nontemporal_load((const EE_GLOBAL u32x2*)p) : *(const EE_GLOBAL u32x2*)p;
         w[0] = x[0], w[1] = x[1];
     } else {
 #pragma unroll
         for (int i = 0; i < N; i += 4) {
-            const u32x4 x = PAST ? __builtin_nontemporal_load((const u32x4*)(p + 4 * i)) : *(const u32x4*)(p + 4 * i);
+            const u32x4 x = PAST ? __builtin_nontemporal_load((const EE_GLOBAL u32x4*)(p + 4 * i)) : *(const EE_GLOBAL u32x4*)(p + 4 * i);
             w[i] = x[0], w[i + 1] = x[1], w[i + 2] = x[2], w[i + 3] = x[3];
         }
     }
 }
 
 template <int HD, bool PAST>
-__device__ __forceinline__ void load_keys(const char* tile, int lane, KeyRegs<HD>& r) {
-    constexpr int LB = HD / 8, G = HD / 32;
+__device__ __forceinline__ void load_keys(PoolPtr tile, uint32_t lane, KeyRegs<HD>& r) {
+    constexpr uint32_t LB = HD / 8, G = HD / 32;
     load_words<PAST, G>(tile + lane * LB, r.w);
-    const char* sc = tile + Kv4Tile::k_scales(HD) + (lane & 15) * G;
-    if constexpr (G == 1) r.sc[0] = *(const uint8_t*)sc;
-    if constexpr (G == 2) r.sc[0] = *(const uint16_t*)sc;
+    PoolPtr sc = tile + Kv4Tile::k_scales(HD) + (lane & 15u) * G;
+    if constexpr (G == 1) r.sc[0] = *(const EE_GLOBAL uint8_t*)sc;
+    if constexpr (G == 2) r.sc[0] = *(const EE_GLOBAL uint16_t*)sc;
     if constexpr (G >= 4) load_words<false, G / 4>(sc, r.sc);
 }
 template <int HD, bool PAST>
-__device__ __forceinline__ void load_values(const char* tile, int lane, ValueRegs<HD>& r) {
-    constexpr int LB = HD / 8, G = HD / 32;
+__device__ __forceinline__ void load_values(PoolPtr tile, uint32_t lane, ValueRegs<HD>& r) {
+    constexpr uint32_t LB = HD / 8, G = HD / 32;
     load_words<PAST, G>(tile + Kv4Tile::v_codes(HD) + lane * LB, r.w);
-    r.sc = *(const uint32_t*)(tile + Kv4Tile::v_scales(HD) + (lane & 15) * HD / 512 * 16 + (lane >> 4) * 4);
+    r.sc = *(const EE_GLOBAL uint32_t*)(tile + Kv4Tile::v_scales(HD) + ((lane & 15u) * HD / 512u * 16u + (lane >> 4) * 4u));
 }
 
-__device__ __forceinline__ float scale_of(const uint32_t* words, int i) {  // byte i as 2^(byte - 127)
-    return __uint_as_float((words[i >> 2] >> (8 * (i & 3)) & 255u) << 23);
+__device__ __forceinline__ float scale_of(uint32_t word, int i) {  // byte i as 2^(byte - 127)
+    return __uint_as_float((word >> (8 * i) & 255u) << 23);
 }
 
 __device__ __forceinline__ uint32_t bytes_255(uint32_t w) {  // 0x80 in every byte of w that is 255 (and maybe above such a one)
@@ -552,16 +558,100 @@ __device__ __forceinline__ uint32_t bytes_255(uint32_t w) {  // 0x80 in every by
 }
 
 // What one workgroup leaves for another one of the same launch, maybe on another XCD.
-__device__ __forceinline__ void hand_over(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ float handed(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void hand_over2(float* p, f32x2 v) {
+    __hip_atomic_store((uint64_t*)p, __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 __device__ __forceinline__ f32x2 handed2(const float* p) {
     return __builtin_bit_cast(f32x2, __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 constexpr int FAN_IN = 32;  // parts that are joined at a time
 
+// rows that see nothing
+template <int HD, typename ST>
+__device__ __forceinline__ void sees_nothing(const Kv4Attend& a, const Kv4Part& w, int f0, int f_end, int threads, ST* out) {
+    for (int i = threadIdx.x; i < (f_end - f0) * HD; i += threads) {
+        const int f = f0 + i / HD;
+        const size_t o = (size_t)(w.row0 + f / a.group) * (a.group * a.kv_heads) + w.head * a.group + f % a.group;
+        out[o * HD + i % HD] = (ST)0.f;
+        if (i % HD == 0 && a.lse) a.lse[o] = -INFINITY;
+    }
+}
+
+// Parts are joined by the workgroup that leaves the last one, in their order; many of them in two levels: first each FAN_IN
+// neighbours by the last of those, into the first one's place, then these.  The parts go past the caches of this XCD (agent-scope
+// stores and loads): a release fence instead would write the whole of its L2 back, which cost a launch of 1024 parts 300 us.
+template <int HD, int THREADS, int M, typename ST>
+__device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w, int f0, int f_end, uint32_t* s_last) {
+    const int n_parts = w.part_of >> 16, part = w.part_of & 0xffff, slot0 = w.slot - part, n_heads = a.group * a.kv_heads;
+    const int groups = (n_parts + FAN_IN - 1) / FAN_IN, group0 = part / FAN_IN * FAN_IN;
+    ST* out = (ST*)a.out;
+    const bool two_levels = groups > 1;
+    int first = slot0 + group0, stride = 1, n = min(FAN_IN, n_parts - group0);
+    uint32_t* counter = a.arrived + first;
+    const float* part_ml = a.part_ml;
+    for (int level = 0;; ++level) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // each thread's stores have arrived before its workgroup is counted
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if ((int)before == n - 1) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            *s_last = before;
+        }
+        __syncthreads();
+        if ((int)*s_last != n - 1) return;
+        const bool whole = level == 1 || !two_levels;
+        // one thread per two elements: it asks for eight parts at once, weights and elements, so that a join of few parts is one
+        // trip to memory
+        constexpr int AT_ONCE = 8;
+        for (int i = threadIdx.x; i < (f_end - f0) * (HD / 2); i += THREADS) {
+            const int r = i / (HD / 2), d = i % (HD / 2) * 2, f = f0 + r;
+            const size_t row = (size_t)first * M + r, step = (size_t)stride * M;
+            float top = -INFINITY, sum = 0.f;
+            f32x2 acc = {0.f, 0.f};
+            for (int v0 = 0; v0 < n; v0 += AT_ONCE) {
+                f32x2 ml[AT_ONCE], x[AT_ONCE];
+#pragma unroll
+                for (int v = 0; v < AT_ONCE; ++v) {
+                    const size_t at = row + step * min(v0 + v, n - 1);
+                    ml[v] = handed2(part_ml + 2 * at);
+                    x[v] = handed2(a.part_o + at * HD + d);
+                }
+                float t = top;
+#pragma unroll
+                for (int v = 0; v < AT_ONCE; ++v) t = fmaxf(t, ml[v][0]);  // (the last part again behind the last)
+                const float ref = t == -INFINITY ? 0.f : t;
+                const float old = __builtin_amdgcn_exp2f(top - ref);
+                sum *= old, acc *= old;
+#pragma unroll
+                for (int v = 0; v < AT_ONCE; ++v) {
+                    if (v0 + v < n) {
+                        const float wt = __builtin_amdgcn_exp2f(ml[v][0] - ref);
+                        sum += wt * ml[v][1], acc += wt * x[v];
+                    }
+                }
+                top = t;
+            }
+            if (whole) {
+                const size_t at = (size_t)(w.row0 + f / a.group) * n_heads + w.head * a.group + f % a.group;
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                out[at * HD + d] = (ST)(acc[0] * inv);
+                out[at * HD + d + 1] = (ST)(acc[1] * inv);
+                if (a.lse && d == 0) a.lse[at] = ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.6931471805599453f;
+            } else {  // elements into the first part's place, which no other thread reads; weights apart, as all of a row's threads read them
+                hand_over2(a.part_o + row * HD + d, acc);
+                if (d == 0) hand_over2(a.joined_ml + 2 * row, f32x2{top, sum});
+            }
+        }
+        if (whole) return;
+        counter = a.arrived_groups + slot0;
+        part_ml = a.joined_ml;
+        first = slot0, stride = FAN_IN, n = groups;
+    }
+}
+
 // NT: bf16 terms of an element of Q (1: Q is bf16; 3: fp32, exactly), PT: of a probability.  UNITS: 16 entries each of a tile.
 template <int HD, int NT, int PT, int UNITS, int NW, int DEPTH, bool PAST, typename ST>
-__global__ __launch_bounds__(NW * 64, UNITS == 1 && HD <= 128 ? (DEPTH > 1 ? 2 : NT == 1 ? 4 : 3) : 1) void kv4_attend_kernel(Kv4Attend a) {
+__global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 : NT == 1 ? 4 : 3) void kv4_attend_kernel(Kv4Attend a) {
     constexpr int G = HD / 32, EPC = HD / 16, M = 16 * UNITS;
     constexpr int CT = KV4_CHUNK / 16;  // tiles of 16 positions at a time: one contraction of P.V
     static_assert(CT == 2, "a contraction has 32 positions");
@@ -578,12 +668,7 @@ __global__ __launch_bounds__(NW * 64, UNITS == 1 && HD <= 128 ? (DEPTH > 1 ? 2 :
     const int n_heads = a.group * a.kv_heads;
     ST* out = (ST*)a.out;
     if (w.seq < 0) {
-        for (int i = threadIdx.x; i < (f_end - f0) * HD; i += NW * 64) {
-            const int f = f0 + i / HD;
-            const size_t o = (size_t)(w.row0 + f / a.group) * n_heads + w.head * a.group + f % a.group;
-            out[o * HD + i % HD] = (ST)0.f;
-            if (i % HD == 0 && a.lse) a.lse[o] = -INFINITY;
-        }
+        sees_nothing<HD>(a, w, f0, f_end, NW * 64, out);
         return;
     }
 
@@ -631,7 +716,7 @@ __global__ __launch_bounds__(NW * 64, UNITS == 1 && HD <= 128 ? (DEPTH > 1 ? 2 :
     const int32_t* table = a.table + (size_t)w.seq * a.table_stride;
     const int last_tile = pos_last >> 4;
     const size_t block_bytes = ((size_t)Kv4Tile::bytes(HD) << a.tiles_shift) * a.kv_heads;
-    const char* base = a.layer + ((size_t)Kv4Tile::bytes(HD) << a.tiles_shift) * w.head;
+    const PoolPtr base = (PoolPtr)a.layer + ((size_t)Kv4Tile::bytes(HD) << a.tiles_shift) * w.head;
     const int in_block = (1 << a.tiles_shift) - 1;
 
     // step `it` of this wave: chunk c_lo + wave + it * NW, two tiles; a tile behind the last one that is seen repeats it (its
@@ -652,7 +737,8 @@ __global__ __launch_bounds__(NW * 64, UNITS == 1 && HD <= 128 ? (DEPTH > 1 ? 2 :
     };
 
     f32x4 o[UNITS][EPC];
-    float m[UNITS], l[UNITS];
+    float m[UNITS], l[UNITS];  // m: the scores' reference, at most `slack` below their maximum (so no probability passes 2^8)
+    const float slack = 8.f / a.scale_log2;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
         m[u] = -INFINITY, l[u] = 0.f;
@@ -663,7 +749,7 @@ __global__ __launch_bounds__(NW * 64, UNITS == 1 && HD <= 128 ? (DEPTH > 1 ? 2 :
     // K of a step DEPTH ahead is asked for as soon as K of this one has been used, V likewise
     KeyRegs<HD> key_regs[DEPTH][CT];
     ValueRegs<HD> value_regs[DEPTH][CT];
-    const char* at[CT];
+    PoolPtr at[CT];
 #pragma unroll
     for (int i = 0; i < DEPTH; ++i) {
         if (i < n_it) {
@@ -685,7 +771,7 @@ __global__ __launch_bounds__(NW * 64, UNITS == 1 && HD <= 128 ? (DEPTH > 1 ? 2 :
             for (int u = 0; u < UNITS; ++u) s[u][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const float unit = scale_of(kr[t].sc, g);
+                const float unit = scale_of(kr[t].sc[g >> 2], g & 3);
                 const bf16x8 kf = frag(pair_of<0>(kr[t].w[g], unit), pair_of<1>(kr[t].w[g], unit), pair_of<2>(kr[t].w[g], unit),
                                        pair_of<3>(kr[t].w[g], unit));
 #pragma unroll
@@ -747,7 +833,7 @@ __global__ __launch_bounds__(NW * 64, UNITS == 1 && HD <= 128 ? (DEPTH > 1 ? 2 :
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, s[u][t][i]);
             top = fmaxf(rows4_max(top), m[u]);
-            if (__any(top > m[u])) {
+            if (__any(top > m[u] + slack)) {
                 const float corr = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[u] - top) * a.scale_log2);
                 l[u] *= corr;
 #pragma unroll
@@ -777,7 +863,7 @@ __global__ __launch_bounds__(NW * 64, UNITS == 1 && HD <= 128 ? (DEPTH > 1 ? 2 :
         // weighted sum: rows = elements (column c of V's layout), columns = entries
         float u0[4], u1[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) u0[i] = scale_of(&vr[0].sc, i), u1[i] = scale_of(&vr[1].sc, i);
+        for (int i = 0; i < 4; ++i) u0[i] = scale_of(vr[0].sc, i), u1[i] = scale_of(vr[1].sc, i);
 #pragma unroll
         for (int b = 0; b < EPC / 2; ++b) {
             uint32_t x0[4], x1[4];  // elements 2b, 2b+1 of the column, at the four keys
@@ -836,7 +922,7 @@ __global__ __launch_bounds__(NW * 64, UNITS == 1 && HD <= 128 ? (DEPTH > 1 ? 2 :
     }
 
     // join the waves' shares, 16 entries at a time
-    constexpr int EPT = 16 * HD >= NW * 64 ? 16 * HD / (NW * 64) : 1;  // elements per thread
+    constexpr int EPT = 16 * HD >= 2 * NW * 64 ? 16 * HD / (NW * 64) : 2;  // elements per thread
     const int my_row = threadIdx.x * EPT / HD, my_d = threadIdx.x * EPT % HD;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
@@ -877,79 +963,281 @@ __global__ __launch_bounds__(NW * 64, UNITS == 1 && HD <= 128 ? (DEPTH > 1 ? 2 :
             } else {
                 const size_t r = (size_t)w.slot * M + 16 * u + my_row;
 #pragma unroll
-                for (int e = 0; e < EPT; ++e) hand_over(a.part_o + r * HD + my_d + e, acc[e]);
-                if (my_d == 0) hand_over(a.part_ml + 2 * r, top), hand_over(a.part_ml + 2 * r + 1, sum);
+                for (int e = 0; e < EPT; e += 2) hand_over2(a.part_o + r * HD + my_d + e, f32x2{acc[e], acc[e + 1]});
+                if (my_d == 0) hand_over2(a.part_ml + 2 * r, f32x2{top, sum});
             }
         }
     }
-    if (n_parts == 1) return;
+    if (n_parts > 1) join_parts<HD, NW * 64, M, ST>(a, w, f0, f_end, &s_last);
+}
 
-    // Parts are joined by the workgroup that leaves the last one, in their order; many of them in two levels: first each
-    // FAN_IN neighbours by the last of those, into the first one's place, then these.  The parts go past the caches of this XCD
-    // (agent-scope stores and loads): a release fence instead would write the whole of its L2 back, which cost a launch of 1024
-    // parts 300 us.
-    const int slot0 = w.slot - part;
-    auto last_of = [&](uint32_t* counter, int n) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // each thread's stores have arrived before its workgroup is counted
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            if ((int)before == n - 1) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            s_last = before;
+// Prompts: 128 entries of a tile, 32 for each of four waves.  The four convert the next 32 positions together, a tile of K or V
+// each, into bf16 in LDS in operand order, while they work on these; so an element is converted once for 128 entries, and
+// 32 x 32 products halve what is read from LDS per operation.  One barrier per 32 positions, two buffers.  Two such groups of
+// waves take every other 32 positions, so that a SIMD has two waves, and join their sums through LDS at the end.
+// Bound by the vector units (soft-max: an exponential, a multiply-add, a maximum, a sum and a conversion per score) about as much
+// as by the matrix units.
+template <int HD>
+__global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
+    constexpr int M = KV4_WIDE, G = HD / 32, EPC = HD / 16, KS = HD / 16, DB = HD / 32, LB = HD / 8;
+    __shared__ u32x4 s_operands[2][2][(KS + 2 * DB) * 64];  // K, V of each group's two steps; at the end the second group's sums
+    __shared__ float s_ml[2][256];
+    __shared__ uint32_t s_scales_of[2][2][2][G * 4];  // of V, if some entry does not see all of the positions
+    __shared__ uint32_t s_nan_of[2][2][2];            // ... and there is a NaN among them
+    static_assert(sizeof(s_operands) >= 4 * 64 * 16 * DB * sizeof(float), "room for the sums");
+    __shared__ uint32_t s_last;
+
+    const Kv4Part w = a.parts[blockIdx.x];
+    if ((int)blockIdx.x >= *a.n_parts) return;
+    const int lane = threadIdx.x & 63, group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3;
+    const int col = lane & 31, half = lane >> 5;
+    const int f0 = w.tile * M, f_end = min(w.n_flat, f0 + M);
+    const int n_heads = a.group * a.kv_heads;
+    __bf16* out = (__bf16*)a.out;
+    if (w.seq < 0) {
+        sees_nothing<HD>(a, w, f0, f_end, 512, out);
+        return;
+    }
+
+    // entry of this lane's column; what the wave's and the workgroup's entries see
+    const int f_wave = f0 + 32 * wave, f = min(f_wave + col, f_end - 1);
+    const int row = f / a.group, head = w.head * a.group + f % a.group;
+    const int hi = w.start + row, lo = a.window ? max(0, hi - a.window + 1) : 0;
+    bf16x8 q[KS];  // elements 16 s + 8 half ..
+    {
+        const __bf16* src = (const __bf16*)a.q + (w.row0 + row) * a.q_row + head * a.q_head + half * 8;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            if (a.q_vec) {
+                q[s] = *(const bf16x8*)(src + s * 16);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) q[s][e] = src[s * 16 + e];
+            }
         }
-        __syncthreads();
-        return (int)s_last == n - 1;
+    }
+    auto first_of = [&](int pos) { return a.window ? max(0, pos - a.window + 1) : 0; };
+    const int pos_first = w.start + f0 / a.group, pos_last = w.start + (f_end - 1) / a.group;
+    const bool idle = f_wave >= f_end;
+    const int wave_first = w.start + min(f_wave, f_end - 1) / a.group, wave_last = w.start + min(f_wave + 31, f_end - 1) / a.group;
+    const int c_first = first_of(pos_first) / KV4_CHUNK, n_chunks = pos_last / KV4_CHUNK + 1 - c_first;
+    const int n_parts = w.part_of >> 16, part = w.part_of & 0xffff;
+    const int c_lo = c_first + (int)((int64_t)n_chunks * part / n_parts), c_hi = c_first + (int)((int64_t)n_chunks * (part + 1) / n_parts);
+
+    // this wave converts tile `tl` of a step's two, of K or of V
+    const int tl = wave & 1, quarter = lane >> 4, t16 = lane & 15;
+    const bool of_v = wave >= 2;
+    const int32_t* table = a.table + (size_t)w.seq * a.table_stride;
+    const int last_tile = pos_last >> 4, in_block = (1 << a.tiles_shift) - 1;
+    const size_t block_bytes = ((size_t)Kv4Tile::bytes(HD) << a.tiles_shift) * a.kv_heads;
+    const PoolPtr base = (PoolPtr)a.layer + ((size_t)Kv4Tile::bytes(HD) << a.tiles_shift) * w.head;
+    auto(&s_buffers)[2][(KS + 2 * DB) * 64] = s_operands[group];
+    auto(&s_scales)[2][2][G * 4] = s_scales_of[group];
+    auto(&s_nan)[2][2] = s_nan_of[group];
+    const int n_it = max(0, (c_hi - c_lo - group + 1) >> 1), n_most = (c_hi - c_lo + 1) >> 1;
+    auto chunk_of = [&](int it) { return c_lo + group + 2 * it; };
+    auto blocks_from = [&](int it) { return table[min(chunk_of(it + lane) * 2 + tl, last_tile) >> a.tiles_shift]; };
+    int blocks = n_it ? blocks_from(0) : 0, blocks_next = n_it > 64 ? blocks_from(64) : 0;
+    uint32_t codes[G], scales;
+    auto load = [&](int it) {
+        if (it && it % 64 == 0) {
+            blocks = blocks_next;
+            blocks_next = blocks_from(it + 64);
+        }
+        const int tile = min(chunk_of(it) * 2 + tl, last_tile);
+        const PoolPtr at = base + (size_t)__builtin_amdgcn_readlane(blocks, it % 64) * block_bytes + (size_t)(tile & in_block) * Kv4Tile::bytes(HD);
+        load_words<false, G>(at + (of_v ? Kv4Tile::v_codes(HD) : 0) + (uint32_t)lane * LB, codes);
+        if (of_v) {
+            scales = *(const EE_GLOBAL uint32_t*)(at + Kv4Tile::v_scales(HD) + (uint32_t)(t16 * EPC / 32 * 16 + quarter * 4));
+        } else {
+            const PoolPtr sc = at + Kv4Tile::k_scales(HD) + (uint32_t)(t16 * G);
+            if constexpr (G == 4) scales = *(const EE_GLOBAL uint32_t*)sc;
+            if constexpr (G == 2) scales = *(const EE_GLOBAL uint16_t*)sc;
+        }
     };
-    auto join = [&](const float* part_ml, int first, int stride, int n, bool whole) {
-        // one thread per two elements: it asks for eight parts at once, weights and elements, so that a join of few parts is one
-        // trip to memory
-        constexpr int AT_ONCE = 8;
-        for (int i = threadIdx.x; i < (f_end - f0) * (HD / 2); i += NW * 64) {
-            const int r = i / (HD / 2), d = i % (HD / 2) * 2, f = f0 + r;
-            const size_t row = (size_t)first * M + r, step = (size_t)stride * M;
-            float top = -INFINITY, sum = 0.f;
-            f32x2 acc = {0.f, 0.f};
-            for (int v0 = 0; v0 < n; v0 += AT_ONCE) {
-                f32x2 ml[AT_ONCE], x[AT_ONCE];
+    auto convert = [&](int it, int buf) {
+        if (of_v) {
+            const int key0 = chunk_of(it) * KV4_CHUNK;
+            if (key0 + KV4_CHUNK > pos_first + 1 || key0 < first_of(pos_last)) {
+                // V behind the last position that any entry sees may hold anything: a scale of 1 makes it finite, and its
+                // probabilities are zero.  NaN that not every entry sees is taken out here and put back by who sees it.
+                const int key = key0 + 16 * tl + quarter * 4;
+                uint32_t keep = 0, nan = 0;
 #pragma unroll
-                for (int v = 0; v < AT_ONCE; ++v) {
-                    const size_t at = row + step * min(v0 + v, n - 1);
-                    ml[v] = handed2(part_ml + 2 * at);
-                    x[v] = handed2(a.part_o + at * HD + d);
+                for (int i = 0; i < 4; ++i) {
+                    if (key + i <= pos_last) keep |= 255u << (8 * i);
+                    if ((scales >> (8 * i) & 255u) == SCALE_NAN) nan |= 255u << (8 * i);
                 }
-                float t = top;
+                nan &= keep;
+                if (t16 * EPC % 32 == 0) s_scales[buf][tl][t16 * EPC / 32 * 4 + quarter] = nan;
+                const bool any = __any(nan != 0);
+                if (lane == 0) s_nan[buf][tl] = any;
+                scales = (scales & keep & ~nan) | (0x7f7f7f7fu & (~keep | nan));
+            }
+            float unit[4];
 #pragma unroll
-                for (int v = 0; v < AT_ONCE; ++v) t = fmaxf(t, ml[v][0]);  // (the last part again behind the last)
-                const float ref = t == -INFINITY ? 0.f : t;
-                const float old = __builtin_amdgcn_exp2f(top - ref);
-                sum *= old, acc *= old;
+            for (int i = 0; i < 4; ++i) unit[i] = scale_of(scales, i);
+            char* dst = (char*)&s_buffers[buf][KS * 64 + (tl * DB * 2 + (quarter & 1)) * 32 + t16] + (quarter >> 1) * 8;
 #pragma unroll
-                for (int v = 0; v < AT_ONCE; ++v) {
-                    if (v0 + v < n) {
-                        const float wt = __builtin_amdgcn_exp2f(ml[v][0] - ref);
-                        sum += wt * ml[v][1], acc += wt * x[v];
+            for (int b = 0; b < EPC / 2; ++b) {
+                uint32_t x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int byte = i * (HD / 32) + b;
+                    x[i] = pair_of(codes[byte >> 2], unit[i], byte & 3);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t sel = h ? 0x07060302u : 0x05040100u;
+                    *(u32x2*)(dst + (b * 64 + h * 16) * 16) = u32x2{__builtin_amdgcn_perm(x[1], x[0], sel), __builtin_amdgcn_perm(x[3], x[2], sel)};
+                }
+            }
+        } else {
+            u32x4* dst = &s_buffers[buf][(quarter & 1) * 32 + tl * 16 + t16];
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const float unit = scale_of(scales, g);
+                dst[(g * 2 + (quarter >> 1)) * 64] = u32x4{pair_of<0>(codes[g], unit), pair_of<1>(codes[g], unit), pair_of<2>(codes[g], unit), pair_of<3>(codes[g], unit)};
+            }
+        }
+    };
+
+    f32x16 o[DB] = {};
+    float m = -INFINITY, l = 0.f;  // m: the scores' reference, at most `slack` below their maximum (so no probability passes 2^8)
+    const float slack = 8.f / a.scale_log2;
+    if (n_it) {
+        load(0);
+        convert(0, 0);
+        if (n_it > 1) load(1);
+    }
+    __syncthreads();
+    for (int it = 0; it < n_most; ++it) {
+        const int buf = it & 1, key0 = chunk_of(it) * KV4_CHUNK;
+        if (it + 1 < n_it) convert(it + 1, buf ^ 1);
+        if (it + 2 < n_it) load(it + 2);
+        if (!idle && it < n_it && key0 <= wave_last && key0 + KV4_CHUNK > first_of(wave_first)) {
+            // scores: rows = positions, columns = entries
+            f32x16 s = {};
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, s_buffers[buf][k * 64 + lane]), q[k], s, 0, 0, 0);
+            // position of s[i]: key0 + 8 (i / 4) + 4 half + i % 4
+            const bool wg_edge = key0 + KV4_CHUNK > pos_first + 1 || key0 < first_of(pos_last);
+            if (key0 + KV4_CHUNK > wave_first + 1 || key0 < first_of(wave_last)) {
+                int key = key0 + 4 * half;
+                asm volatile("" : "+v"(key));
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int k = key + 8 * (i >> 2) + (i & 3);
+                    if (k > hi || k < lo) s[i] = -INFINITY;
+                }
+            }
+            float top = s[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+            float t0, t1;
+            halves_of(top, t0, t1);
+            top = fmaxf(fmaxf(t0, t1), m);
+            if (__any(top > m + slack)) {
+                const float corr = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * a.scale_log2);
+                l *= corr;
+#pragma unroll
+                for (int b = 0; b < DB; ++b) o[b] *= corr;
+                m = top;
+            }
+            const float ref = m == -INFINITY ? 0.f : m * a.scale_log2;
+            u32x4 p[2];  // (one bf16 term; the sum is that of the probabilities before they are rounded)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                f32x2 x;
+                x[0] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, -ref));
+                x[1] = __builtin_amdgcn_exp2f(fmaf(s[i + 1], a.scale_log2, -ref));
+                l += x[0] + x[1];
+                p[i >> 3][(i & 7) >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+            }
+            // weighted sum: rows = elements, columns = entries
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+                    o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, s_buffers[buf][(KS + t * DB + b) * 64 + lane]),
+                                                                   __builtin_bit_cast(bf16x8, p[t]), o[b], 0, 0, 0);
+            if (wg_edge && (s_nan[buf][0] | s_nan[buf][1])) {
+                // as in the kernel above: "is NaN" times "is seen", counted per column of V and entry
+                f32x16 count = {};
+                int key = key0 + 4 * half;
+                asm volatile("" : "+v"(key));
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const uint32_t* sc = &s_scales[buf][t][t16 * EPC / 32 * 4];
+                    bf16x8 is_nan, seen;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int k = key + 16 * t + 8 * (e >> 2) + (e & 3);
+                        is_nan[e] = (__bf16)((sc[half + 2 * (e >> 2)] >> (8 * (e & 3)) & 255u) ? 1.f : 0.f);
+                        seen[e] = (__bf16)(k <= hi && k >= lo ? 1.f : 0.f);
                     }
+                    count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(is_nan, seen, count, 0, 0, 0);
                 }
-                top = t;
-            }
-            if (whole) {
-                const size_t at = (size_t)(w.row0 + f / a.group) * n_heads + w.head * a.group + f % a.group;
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                out[at * HD + d] = (ST)(acc[0] * inv);
-                out[at * HD + d + 1] = (ST)(acc[1] * inv);
-                if (a.lse && d == 0) a.lse[at] = ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.6931471805599453f;
-            } else {  // elements into the first part's place, which no other thread reads; weights apart, as all of a row's threads read them
-                hand_over(a.part_o + row * HD + d, acc[0]), hand_over(a.part_o + row * HD + d + 1, acc[1]);
-                if (d == 0) hand_over(a.joined_ml + 2 * row, top), hand_over(a.joined_ml + 2 * row + 1, sum);
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (count[i] > 0.f) o[b][i] = __builtin_nanf("");
             }
         }
-    };
-    const int groups = (n_parts + FAN_IN - 1) / FAN_IN, group0 = part / FAN_IN * FAN_IN, in_group = min(FAN_IN, n_parts - group0);
-    if (!last_of(a.arrived + slot0 + group0, in_group)) return;
-    join(a.part_ml, slot0 + group0, 1, in_group, groups == 1);
-    if (groups == 1) return;
-    if (!last_of(a.arrived_groups + slot0, groups)) return;
-    join(a.joined_ml, slot0, FAN_IN, groups, true);
+        __syncthreads();
+    }
+
+    // the second group's sums join the first's
+    float* s_sums = (float*)s_operands;
+    if (group) {
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s_sums[((wave * DB + b) * 16 + i) * 64 + lane] = o[b][i];
+        s_ml[0][wave * 64 + lane] = m, s_ml[1][wave * 64 + lane] = l;
+    }
+    __syncthreads();
+    if (!group) {
+        const float m2 = s_ml[0][wave * 64 + lane], top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+        const float w1 = __builtin_amdgcn_exp2f((m - ref) * a.scale_log2), w2 = __builtin_amdgcn_exp2f((m2 - ref) * a.scale_log2);
+        l = l * w1 + s_ml[1][wave * 64 + lane] * w2;
+        m = top;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[b][i] = o[b][i] * w1 + s_sums[((wave * DB + b) * 16 + i) * 64 + lane] * w2;
+    }
+    float l0, l1;
+    halves_of(l, l0, l1);
+    const float sum = l0 + l1;
+    if (!group && f_wave + col < f_end) {
+        const size_t r = (size_t)(w.row0 + row) * n_heads + head, at = (size_t)w.slot * M + 32 * wave + col;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = 8 * (i >> 2) + 4 * half + (i & 3);  // column of V: elements c * EPC ...
+            if (n_parts == 1) {
+                uint32_t x[EPC / 2];
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+                    x[b] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{o[b][i] * inv, o[b][8 + i] * inv}, bf16x2));
+                if constexpr (EPC == 8) *(u32x4*)(out + r * HD + c * EPC) = u32x4{x[0], x[1], x[2], x[3]};
+                if constexpr (EPC == 4) *(u32x2*)(out + r * HD + c * EPC) = u32x2{x[0], x[1]};
+            } else {
+#pragma unroll
+                for (int b = 0; b < DB; ++b) hand_over2(a.part_o + at * HD + c * EPC + 2 * b, f32x2{o[b][i], o[b][8 + i]});
+            }
+        }
+        if (half == 0) {
+            if (n_parts > 1)
+                hand_over2(a.part_ml + 2 * at, f32x2{m * a.scale_log2, sum});
+            else if (a.lse)
+                a.lse[r] = ((m == -INFINITY ? 0.f : m * a.scale_log2) + log2f(sum)) * 0.6931471805599453f;
+        }
+    }
+    if (n_parts > 1) join_parts<HD, 512, M, __bf16>(a, w, f0, f_end, &s_last);
 }
 
 template <int HD, int UNITS, int NW>
@@ -981,7 +1269,13 @@ hipError_t attend_hd(const Kv4Attend& a, int dtype, int units, int waves, int gr
     if (units == 1) return attend_units<HD, 1>(a, dtype, waves, grid, s);
     if constexpr (HD <= 128)
         if (units == 2) return attend_units<HD, 2>(a, dtype, waves, grid, s);
-    if constexpr (HD <= 64)
+    if constexpr (HD == 64 || HD == 128) {
+        if (units == KV4_WIDE / 16 && dtype == EE_BF16) {
+            EE_LAUNCH((kv4_attend_wide_kernel<HD>), dim3(grid), dim3(512), s, a);
+            return hipGetLastError();
+        }
+    }
+    if constexpr (HD == 32)
         if (units == 4) return attend_units<HD, 4>(a, dtype, waves, grid, s);
     return hipErrorInvalidValue;
 }
@@ -1020,6 +1314,7 @@ hipError_t read_hd(const Kv4Cache& c, int n_rows, const int64_t* slots, void* k,
 }  // namespace
 
 int kv4_tile_units(int dtype, int head_dim, int most_flat) {
+    if (dtype == EE_BF16 && (head_dim == 64 || head_dim == 128) && most_flat > 32) return KV4_WIDE / 16;
     const int most = dtype == EE_BF16 ? std::min(4, 256 / head_dim) : std::min(2, 256 / head_dim);  // what a wave's registers hold
     int units = 1;
     while (units < most && 16 * units < most_flat) units *= 2;

@@ -26,15 +26,16 @@ int check_config(const ee_kv4_config& c) {
 }
 
 // How a launch of the attention is cut: workgroups of `waves` waves, in about `parts` parts of at least `min_chunks` chunks.
-constexpr int TARGET_PARTS = 2048;  // most of any
+constexpr int MOST_PARTS = 768;
 struct Cut {
     int waves, parts, min_chunks;
 };
+int most_of_cut(int units) { return units * 16 == KV4_WIDE ? 256 : MOST_PARTS; }
 Cut cut_of(const ee_kv4_config& c, int n_seqs, int n_rows, int units) {
     const int items = std::min(n_seqs, n_rows) * c.n_kv_heads;
-    Cut k = {4, 768, 8};
-    if (units == 1 && items < 128) k = {8, 256, 8};
-    return k;
+    if (units * 16 == KV4_WIDE) return {8, most_of_cut(units), 32};
+    if (units == 1 && items < 128) return {8, 256, 8};
+    return {4, most_of_cut(units), 8};
 }
 
 // A pool of more than half of the last-level cache (256 MB) is not found there again by the next step, which has read weights in
@@ -50,13 +51,14 @@ size_t layer_bytes(const ee_kv4_config& c) {
 // that are not full (one per request that has rows, one behind the last).
 int64_t most_parts(const ee_kv4_config& c, int n_seqs, int n_rows, int tile_rows) {
     const int64_t tiles = (int64_t)n_rows * (c.n_heads / c.n_kv_heads) / tile_rows + std::min(n_seqs, n_rows) + 1;
-    return tiles * c.n_kv_heads + TARGET_PARTS;
+    return tiles * c.n_kv_heads + MOST_PARTS;
 }
 
 struct StateLayout {
     size_t table, free_blocks, slots, positions, row_seq, row_start, served, held_next, counts, parts, arrived, part_ml, part_o, total;
     int64_t max_parts;
-    int max_slots;  // parts of items that are cut: each of these has more than half its full length, so twice the target bounds them
+    int max_slots, part_rows;  // parts of items that are cut, and their rows: each of these has more than half its full length, so
+                               // twice the target bounds them
 };
 
 StateLayout state_layout(const ee_kv4_config& c) {
@@ -78,11 +80,16 @@ StateLayout state_layout(const ee_kv4_config& c) {
     w.counts = take(12);  // free blocks, parts, the plan's workgroups that have read the lengths
     w.max_parts = most_parts(c, c.max_seqs, c.max_rows, 16);
     w.parts = take((size_t)w.max_parts * sizeof(Kv4Part));
-    w.max_slots = 2 * TARGET_PARTS;
+    w.max_slots = 2 * MOST_PARTS;
     w.arrived = take((size_t)w.max_slots * 8);  // of groups of parts, of items
-    const int most = 16 * kv4_tile_units(c.dtype, c.head_dim, 1 << 30);
-    w.part_ml = take((size_t)w.max_slots * most * 16);  // of parts, of joined ones
-    w.part_o = take((size_t)w.max_slots * most * c.head_dim * 4);
+    w.part_rows = 0;
+    const int64_t most_flat = (int64_t)c.max_rows * (c.n_heads / c.n_kv_heads);
+    for (int flat = 16; flat < 512; flat *= 2) {
+        const int units = kv4_tile_units(c.dtype, c.head_dim, (int)std::min<int64_t>(flat, most_flat));
+        w.part_rows = std::max(w.part_rows, 2 * most_of_cut(units) * 16 * units);
+    }
+    w.part_ml = take((size_t)w.part_rows * 16);  // of parts, of joined ones
+    w.part_o = take((size_t)w.part_rows * c.head_dim * 4);
     w.total = off;
     return w;
 }
@@ -253,7 +260,7 @@ int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride,
     a.q_vec = ((uintptr_t)dev_q & 15) == 0 && (q_row_stride * (int64_t)es) % 16 == 0 && (q_head_stride * (int64_t)es) % 16 == 0;
     a.part_o = (float*)(c->state + c->sl.part_o);
     a.part_ml = (float*)(c->state + c->sl.part_ml);
-    a.joined_ml = a.part_ml + (size_t)c->sl.max_slots * 2 * 16 * kv4_tile_units(g.dtype, g.head_dim, 1 << 30);
+    a.joined_ml = a.part_ml + (size_t)c->sl.part_rows * 2;
     a.arrived = (uint32_t*)(c->state + c->sl.arrived);
     a.arrived_groups = a.arrived + c->sl.max_slots;
     const int grid = (int)std::min(c->sl.max_parts, most_parts(g, c->n_seqs, c->n_rows, 16 * c->units));
