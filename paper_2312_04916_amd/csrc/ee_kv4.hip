@@ -1105,22 +1105,36 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     f32x16 o[DB] = {};
     float m = -INFINITY, l = 0.f;  // m: the scores' reference, at most `slack` below their maximum (so no probability passes 2^8)
     const float slack = 8.f / a.scale_log2;
+    // The second group's matrix products come when the first one's vector work does: its scores are formed an interval ahead, so K
+    // is converted two steps ahead there.
+    const int ahead = group && !of_v ? 2 : 1;
     if (n_it) {
         load(0);
         convert(0, 0);
         if (n_it > 1) load(1);
+        if (ahead == 2 && n_it > 1) {
+            convert(1, 1);
+            if (n_it > 2) load(2);
+        }
     }
+    f32x16 s;
+    auto works = [&](int it) {
+        const int key0 = chunk_of(it) * KV4_CHUNK;
+        return !idle && it < n_it && key0 <= wave_last && key0 + KV4_CHUNK > first_of(wave_first);
+    };
+    auto scores = [&](int it) {  // rows = positions, columns = entries
+        s = f32x16{};
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, s_buffers[it & 1][k * 64 + lane]), q[k], s, 0, 0, 0);
+    };
+    __syncthreads();
+    if (group && works(0)) scores(0);
     __syncthreads();
     for (int it = 0; it < n_most; ++it) {
         const int buf = it & 1, key0 = chunk_of(it) * KV4_CHUNK;
-        if (it + 1 < n_it) convert(it + 1, buf ^ 1);
-        if (it + 2 < n_it) load(it + 2);
-        if (!idle && it < n_it && key0 <= wave_last && key0 + KV4_CHUNK > first_of(wave_first)) {
-            // scores: rows = positions, columns = entries
-            f32x16 s = {};
-#pragma unroll
-            for (int k = 0; k < KS; ++k)
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, s_buffers[buf][k * 64 + lane]), q[k], s, 0, 0, 0);
+        if (works(it)) {
+            if (!group) scores(it);
             // position of s[i]: key0 + 8 (i / 4) + 4 half + i % 4
             const bool wg_edge = key0 + KV4_CHUNK > pos_first + 1 || key0 < first_of(pos_last);
             if (key0 + KV4_CHUNK > wave_first + 1 || key0 < first_of(wave_last)) {
@@ -1186,6 +1200,9 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
                         if (count[i] > 0.f) o[b][i] = __builtin_nanf("");
             }
         }
+        if (it + ahead < n_it) convert(it + ahead, (it + ahead) & 1);
+        if (it + ahead + 1 < n_it) load(it + ahead + 1);
+        if (group && works(it + 1)) scores(it + 1);
         __syncthreads();
     }
 
