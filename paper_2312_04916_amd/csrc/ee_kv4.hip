@@ -1036,16 +1036,20 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     auto(&s_nan)[2][2] = s_nan_of[group];
     const int n_it = max(0, (c_hi - c_lo - group + 1) >> 1), n_most = (c_hi - c_lo + 1) >> 1;
     auto chunk_of = [&](int it) { return c_lo + group + 2 * it; };
-    auto blocks_from = [&](int it) { return table[min(chunk_of(it + lane) * 2 + tl, last_tile) >> a.tiles_shift]; };
-    int blocks = n_it ? blocks_from(0) : 0, blocks_next = n_it > 64 ? blocks_from(64) : 0;
+    // where the tiles of 64 steps lie, one per lane, and the block numbers of the 64 behind them
+    auto tile_of_lane = [&](int it) { return min(chunk_of(it + lane) * 2 + tl, last_tile); };
+    auto offsets_of = [&](int it, int block) { return (uint64_t)block * block_bytes + (uint32_t)((tile_of_lane(it) & in_block) * Kv4Tile::bytes(HD)); };
+    uint64_t offsets = 0;
+    int blocks_next = 0;
+    if (n_it) offsets = offsets_of(0, table[tile_of_lane(0) >> a.tiles_shift]), blocks_next = table[tile_of_lane(64) >> a.tiles_shift];
     uint32_t codes[G], scales;
     auto load = [&](int it) {
         if (it && it % 64 == 0) {
-            blocks = blocks_next;
-            blocks_next = blocks_from(it + 64);
+            offsets = offsets_of(it, blocks_next);
+            blocks_next = table[tile_of_lane(it + 64) >> a.tiles_shift];
         }
-        const int tile = min(chunk_of(it) * 2 + tl, last_tile);
-        const PoolPtr at = base + (size_t)__builtin_amdgcn_readlane(blocks, it % 64) * block_bytes + (size_t)(tile & in_block) * Kv4Tile::bytes(HD);
+        const uint32_t lo32 = __builtin_amdgcn_readlane((uint32_t)offsets, it % 64), hi32 = __builtin_amdgcn_readlane((uint32_t)(offsets >> 32), it % 64);
+        const PoolPtr at = base + ((uint64_t)hi32 << 32 | lo32);
         load_words<false, G>(at + (of_v ? Kv4Tile::v_codes(HD) : 0) + (uint32_t)lane * LB, codes);
         if (of_v) {
             scales = *(const EE_GLOBAL uint32_t*)(at + Kv4Tile::v_scales(HD) + (uint32_t)(t16 * EPC / 32 * 16 + quarter * 4));
@@ -1128,6 +1132,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
         for (int k = 0; k < KS; ++k)
             s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, s_buffers[it & 1][k * 64 + lane]), q[k], s, 0, 0, 0);
     };
+    if (group) __builtin_amdgcn_s_setprio(1);  // (the younger waves of each SIMD, which it would serve last)
     __syncthreads();
     if (group && works(0)) scores(0);
     __syncthreads();
