@@ -49,6 +49,7 @@ struct Kv4Plan {
     int group, kv_heads, tile_rows;
     int target_parts;  // a launch is cut so that it has about this many parts
     int min_chunks;    // of a part that is one of several
+    int one_per_cu;    // a CU holds one workgroup of the launch
 };
 
 struct Kv4Cache {
@@ -69,6 +70,7 @@ struct Kv4Attend {
     float* lse;
     float scale_log2;  // scale / ln 2
     int window, group, kv_heads;
+    int min_chunks;  // of a part that is one of several
     int tiles_shift;  // log2(block_tokens / 16)
     int past_caches;  // K and V are read without keeping them in the caches
     int q_vec;        // rows of q can be read 16 bytes at a time

@@ -168,15 +168,17 @@ __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
     if (lane == 0) s_work[wave] = work, s_taken[wave] = taken;
     __syncthreads();
     for (int v = 0; v < nt >> 6; ++v) work = v ? work + s_work[v] : s_work[0], taken = max(taken, s_taken[v]);
-    // (1.001: a sum in fp32, and the parts must not come out more than the target)
-    const int per_part = max(p.min_chunks, (int)fminf(1e6f, ceilf(work * (float)p.kv_heads * 1.001f / (float)p.target_parts)));
+    // chunks of a part: an even share of the work.  Where a CU holds one workgroup, a request is cut into as many parts as it has
+    // shares (more would run after the others have ended); else into one more, so that none is longer than a share.
+    const int per_part = max(p.min_chunks, (int)fminf(1e6f, ceilf(work * (float)p.kv_heads / (float)p.target_parts)));
+    const int round_up = p.one_per_cu ? 0 : per_part - 1;
 
     // parts: items (tile of rows, kv head) in the requests' order, each cut alike; the rows behind the last request's are one
     // more request that sees nothing
     auto parts_of = [&](int i) {  // of an item
         const int rows = s_row[i + 1] - s_row[i];
         if (i == n || rows == 0 || !(s_had[i] & SERVED)) return 1;
-        return ((s_start[i] + rows + KV4_CHUNK - 1) / KV4_CHUNK + per_part - 1) / per_part;
+        return max(1, ((s_start[i] + rows + KV4_CHUNK - 1) / KV4_CHUNK + round_up) / per_part);
     };
     auto items_of = [&](int i) { return ((s_row[i + 1] - s_row[i]) * p.group + p.tile_rows - 1) / p.tile_rows * p.kv_heads; };
     int cnt[2] = {0, 0}, cnt_all[2];
@@ -579,10 +581,11 @@ __device__ __forceinline__ void sees_nothing(const Kv4Attend& a, const Kv4Part& 
 
 // Parts are joined by the workgroup that leaves the last one, in their order; many of them in two levels: first each FAN_IN
 // neighbours by the last of those, into the first one's place, then these.  The parts go past the caches of this XCD (agent-scope
-// stores and loads): a release fence instead would write the whole of its L2 back, which cost a launch of 1024 parts 300 us.
+// stores and loads).  Fences instead act on the whole of its L2: a release cost a launch of 1024 parts 300 us, and an acquire
+// by the workgroups that join alone made a ragged batch's 20 us 37.
 template <int HD, int THREADS, int M, typename ST>
-__device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w, int f0, int f_end, uint32_t* s_last) {
-    const int n_parts = w.part_of >> 16, part = w.part_of & 0xffff, slot0 = w.slot - part, n_heads = a.group * a.kv_heads;
+__device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w, int n_parts, int f0, int f_end, uint32_t* s_last) {
+    const int part = w.part_of & 0xffff, slot0 = w.slot - part, n_heads = a.group * a.kv_heads;
     const int groups = (n_parts + FAN_IN - 1) / FAN_IN, group0 = part / FAN_IN * FAN_IN;
     ST* out = (ST*)a.out;
     const bool two_levels = groups > 1;
@@ -601,8 +604,9 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
         if ((int)*s_last != n - 1) return;
         const bool whole = level == 1 || !two_levels;
         // one thread per two elements: it asks for eight parts at once, weights and elements, so that a join of few parts is one
-        // trip to memory
+        // trip to memory (and for the whole of a prompt's tile four)
         constexpr int AT_ONCE = 8;
+#pragma unroll(M > 64 ? 4 : 1)
         for (int i = threadIdx.x; i < (f_end - f0) * (HD / 2); i += THREADS) {
             const int r = i / (HD / 2), d = i % (HD / 2) * 2, f = f0 + r;
             const size_t row = (size_t)first * M + r, step = (size_t)stride * M;
@@ -612,22 +616,23 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
                 f32x2 ml[AT_ONCE], x[AT_ONCE];
 #pragma unroll
                 for (int v = 0; v < AT_ONCE; ++v) {
-                    const size_t at = row + step * min(v0 + v, n - 1);
-                    ml[v] = handed2(part_ml + 2 * at);
-                    x[v] = handed2(a.part_o + at * HD + d);
+                    ml[v] = f32x2{-INFINITY, 0.f}, x[v] = f32x2{0.f, 0.f};
+                    if (v0 + v < n) {
+                        const size_t at = row + step * (v0 + v);
+                        ml[v] = handed2(part_ml + 2 * at);
+                        x[v] = handed2(a.part_o + at * HD + d);
+                    }
                 }
                 float t = top;
 #pragma unroll
-                for (int v = 0; v < AT_ONCE; ++v) t = fmaxf(t, ml[v][0]);  // (the last part again behind the last)
+                for (int v = 0; v < AT_ONCE; ++v) t = fmaxf(t, ml[v][0]);
                 const float ref = t == -INFINITY ? 0.f : t;
                 const float old = __builtin_amdgcn_exp2f(top - ref);
                 sum *= old, acc *= old;
 #pragma unroll
                 for (int v = 0; v < AT_ONCE; ++v) {
-                    if (v0 + v < n) {
-                        const float wt = __builtin_amdgcn_exp2f(ml[v][0] - ref);
-                        sum += wt * ml[v][1], acc += wt * x[v];
-                    }
+                    const float wt = __builtin_amdgcn_exp2f(ml[v][0] - ref);
+                    sum += wt * ml[v][1], acc += wt * x[v];
                 }
                 top = t;
             }
@@ -710,7 +715,9 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
     const int lo_min = a.window ? max(0, pos_first - a.window + 1) : 0;
     const int lo_max = a.window ? max(0, pos_last - a.window + 1) : 0;
     const int c_first = lo_min / KV4_CHUNK, n_chunks = pos_last / KV4_CHUNK + 1 - c_first;
-    const int n_parts = w.part_of >> 16, part = w.part_of & 0xffff;
+    // (a tile that sees less than the request's last row, because of its rows' positions or the window, needs fewer parts)
+    const int n_parts = min(w.part_of >> 16, max(1, (n_chunks + a.min_chunks - 1) / a.min_chunks)), part = w.part_of & 0xffff;
+    if (part >= n_parts) return;
     const int c_lo = c_first + (int)((int64_t)n_chunks * part / n_parts), c_hi = c_first + (int)((int64_t)n_chunks * (part + 1) / n_parts);
 
     const int32_t* table = a.table + (size_t)w.seq * a.table_stride;
@@ -968,7 +975,7 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
             }
         }
     }
-    if (n_parts > 1) join_parts<HD, NW * 64, M, ST>(a, w, f0, f_end, &s_last);
+    if (n_parts > 1) join_parts<HD, NW * 64, M, ST>(a, w, n_parts, f0, f_end, &s_last);
 }
 
 // Prompts: 128 entries of a tile, 32 for each of four waves.  The four convert the next 32 positions together, a tile of K or V
@@ -1021,7 +1028,9 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     const bool idle = f_wave >= f_end;
     const int wave_first = w.start + min(f_wave, f_end - 1) / a.group, wave_last = w.start + min(f_wave + 31, f_end - 1) / a.group;
     const int c_first = first_of(pos_first) / KV4_CHUNK, n_chunks = pos_last / KV4_CHUNK + 1 - c_first;
-    const int n_parts = w.part_of >> 16, part = w.part_of & 0xffff;
+    // (a tile that sees less than the request's last row, because of its rows' positions or the window, needs fewer parts)
+    const int n_parts = min(w.part_of >> 16, max(1, (n_chunks + a.min_chunks - 1) / a.min_chunks)), part = w.part_of & 0xffff;
+    if (part >= n_parts) return;
     const int c_lo = c_first + (int)((int64_t)n_chunks * part / n_parts), c_hi = c_first + (int)((int64_t)n_chunks * (part + 1) / n_parts);
 
     // this wave converts tile `tl` of a step's two, of K or of V
@@ -1259,7 +1268,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
                 a.lse[r] = ((m == -INFINITY ? 0.f : m * a.scale_log2) + log2f(sum)) * 0.6931471805599453f;
         }
     }
-    if (n_parts > 1) join_parts<HD, 512, M, __bf16>(a, w, f0, f_end, &s_last);
+    if (n_parts > 1) join_parts<HD, 512, M, __bf16>(a, w, n_parts, f0, f_end, &s_last);
 }
 
 template <int HD, int UNITS, int NW>

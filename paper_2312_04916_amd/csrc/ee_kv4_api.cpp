@@ -51,7 +51,7 @@ size_t layer_bytes(const ee_kv4_config& c) {
 // that are not full (one per request that has rows, one behind the last).
 int64_t most_parts(const ee_kv4_config& c, int n_seqs, int n_rows, int tile_rows) {
     const int64_t tiles = (int64_t)n_rows * (c.n_heads / c.n_kv_heads) / tile_rows + std::min(n_seqs, n_rows) + 1;
-    return tiles * c.n_kv_heads + MOST_PARTS;
+    return tiles * c.n_kv_heads + MOST_PARTS + 64;  // (64: the share is formed in fp32)
 }
 
 struct StateLayout {
@@ -80,13 +80,13 @@ StateLayout state_layout(const ee_kv4_config& c) {
     w.counts = take(12);  // free blocks, parts, the plan's workgroups that have read the lengths
     w.max_parts = most_parts(c, c.max_seqs, c.max_rows, 16);
     w.parts = take((size_t)w.max_parts * sizeof(Kv4Part));
-    w.max_slots = 2 * MOST_PARTS;
+    w.max_slots = 2 * MOST_PARTS + 64;
     w.arrived = take((size_t)w.max_slots * 8);  // of groups of parts, of items
     w.part_rows = 0;
     const int64_t most_flat = (int64_t)c.max_rows * (c.n_heads / c.n_kv_heads);
     for (int flat = 16; flat < 512; flat *= 2) {
         const int units = kv4_tile_units(c.dtype, c.head_dim, (int)std::min<int64_t>(flat, most_flat));
-        w.part_rows = std::max(w.part_rows, 2 * most_of_cut(units) * 16 * units);
+        w.part_rows = std::max(w.part_rows, (2 * most_of_cut(units) + 64) * 16 * units);
     }
     w.part_ml = take((size_t)w.part_rows * 16);  // of parts, of joined ones
     w.part_o = take((size_t)w.part_rows * c.head_dim * 4);
@@ -102,7 +102,7 @@ struct ee_kv4 {
     ee_kv4_config cfg;
     char *pool, *state;
     StateLayout sl;
-    int n_seqs, n_rows, units, waves;  // of the latest plan (n_seqs = 0: none)
+    int n_seqs, n_rows, units, waves, min_chunks;  // of the latest plan (n_seqs = 0: none)
     ee_kv4_arrays arrays;
 };
 
@@ -132,7 +132,7 @@ int ee_kv4_create(const ee_kv4_config* cfg, void* dev_pool, size_t pool_bytes, v
     c->state = (char*)dev_state;
     c->sl = state_layout(*cfg);
     c->n_seqs = c->n_rows = 0;
-    c->units = 1, c->waves = 4;
+    c->units = 1, c->waves = 4, c->min_chunks = 8;
     const StateLayout& w = c->sl;
     ee_kv4_arrays& a = c->arrays;
     a.table = (int32_t*)(c->state + w.table);
@@ -188,7 +188,7 @@ int ee_kv4_plan(ee_kv4* c, int n_seqs, const int32_t* dev_held, const int32_t* d
     p.tile_rows = 16 * units;
     p.max_parts = (int)std::min(c->sl.max_parts, most_parts(g, n_seqs, n_rows, p.tile_rows));
     const Cut cut = cut_of(g, n_seqs, n_rows, units);
-    p.target_parts = cut.parts, p.min_chunks = cut.min_chunks;
+    p.target_parts = cut.parts, p.min_chunks = cut.min_chunks, p.one_per_cu = cut.waves == 8;
     // one thread per row and part, and for blocks that change hands, which only the GPU knows, a sixteenth of the pool; a small
     // step in one small workgroup
     const int threads = n_seqs < 256 && n_rows <= 1024 ? 256 : 1024;
@@ -196,7 +196,7 @@ int ee_kv4_plan(ee_kv4* c, int n_seqs, const int32_t* dev_held, const int32_t* d
     const int workgroups = n_rows + p.max_parts <= 2048 && g.n_blocks <= 4096 && threads == 256 ? 1 : (int)std::min<int64_t>(256, 1 + tasks / threads);
     const int rc = hip_status(launch_kv4_plan(p, workgroups, threads, (hipStream_t)stream));
     if (rc != EE_OK) return rc;
-    c->n_seqs = n_seqs, c->n_rows = n_rows, c->units = units, c->waves = cut.waves;
+    c->n_seqs = n_seqs, c->n_rows = n_rows, c->units = units, c->waves = cut.waves, c->min_chunks = cut.min_chunks;
     return EE_OK;
 }
 
@@ -254,7 +254,7 @@ int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride,
     a.q = dev_q, a.q_row = q_row_stride, a.q_head = q_head_stride;
     a.out = dev_out, a.lse = dev_lse;
     a.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt((float)g.head_dim)) * 1.4426950408889634f;
-    a.window = window, a.group = g.n_heads / g.n_kv_heads, a.kv_heads = g.n_kv_heads;
+    a.window = window, a.group = g.n_heads / g.n_kv_heads, a.kv_heads = g.n_kv_heads, a.min_chunks = c->min_chunks;
     a.tiles_shift = __builtin_ctz((unsigned)g.block_tokens) - 4;
     a.past_caches = layer_bytes(g) * g.n_layers > PAST_CACHES_BYTES;
     a.q_vec = ((uintptr_t)dev_q & 15) == 0 && (q_row_stride * (int64_t)es) % 16 == 0 && (q_head_stride * (int64_t)es) % 16 == 0;
