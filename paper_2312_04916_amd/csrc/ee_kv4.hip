@@ -1306,7 +1306,7 @@ hipError_t attend_hd(const Kv4Attend& a, int dtype, int units, int waves, int gr
             return hipGetLastError();
         }
     }
-    if constexpr (HD == 32)
+    if constexpr (HD <= 64)
         if (units == 4) return attend_units<HD, 4>(a, dtype, waves, grid, s);
     return hipErrorInvalidValue;
 }
@@ -1344,8 +1344,11 @@ hipError_t read_hd(const Kv4Cache& c, int n_rows, const int64_t* slots, void* k,
 
 }  // namespace
 
-int kv4_tile_units(int dtype, int head_dim, int most_flat) {
-    if (dtype == EE_BF16 && (head_dim == 64 || head_dim == 128) && most_flat > 32) return KV4_WIDE / 16;
+constexpr int64_t WIDE_ITEMS = 128;
+
+int kv4_tile_units(int dtype, int head_dim, int most_flat, int64_t all_flat) {
+    // wide tiles where they fill the chip
+    if (dtype == EE_BF16 && (head_dim == 64 || head_dim == 128) && most_flat > 32 && all_flat >= KV4_WIDE * WIDE_ITEMS) return KV4_WIDE / 16;
     const int most = dtype == EE_BF16 ? std::min(4, 256 / head_dim) : std::min(2, 256 / head_dim);  // what a wave's registers hold
     int units = 1;
     while (units < most && 16 * units < most_flat) units *= 2;

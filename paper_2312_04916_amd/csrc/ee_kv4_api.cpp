@@ -85,7 +85,7 @@ StateLayout state_layout(const ee_kv4_config& c) {
     w.part_rows = 0;
     const int64_t most_flat = (int64_t)c.max_rows * (c.n_heads / c.n_kv_heads);
     for (int flat = 16; flat < 512; flat *= 2) {
-        const int units = kv4_tile_units(c.dtype, c.head_dim, (int)std::min<int64_t>(flat, most_flat));
+        const int units = kv4_tile_units(c.dtype, c.head_dim, (int)std::min<int64_t>(flat, most_flat), (int64_t)c.max_rows * c.n_heads);
         w.part_rows = std::max(w.part_rows, (2 * most_of_cut(units) + 64) * 16 * units);
     }
     w.part_ml = take((size_t)w.part_rows * 16);  // of parts, of joined ones
@@ -184,7 +184,7 @@ int ee_kv4_plan(ee_kv4* c, int n_seqs, const int32_t* dev_held, const int32_t* d
     p.n_parts = c->arrays.n_free + 1;
     p.arrived = (uint32_t*)c->arrays.n_free + 2;
     p.group = group, p.kv_heads = g.n_kv_heads;
-    const int units = kv4_tile_units(g.dtype, g.head_dim, (int)std::min<int64_t>((int64_t)most * group, 1 << 30));
+    const int units = kv4_tile_units(g.dtype, g.head_dim, (int)std::min<int64_t>((int64_t)most * group, 1 << 30), (int64_t)n_rows * g.n_heads);
     p.tile_rows = 16 * units;
     p.max_parts = (int)std::min(c->sl.max_parts, most_parts(g, n_seqs, n_rows, p.tile_rows));
     const Cut cut = cut_of(g, n_seqs, n_rows, units);

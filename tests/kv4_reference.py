@@ -86,17 +86,17 @@ def attend(q, k, v, positions, group, scale, window=0):
     out = torch.zeros(rows, heads, hd, dtype=torch.float64)
     weight = torch.zeros_like(out)
     lse = torch.full((rows, heads), -np.inf, dtype=torch.float64)
+    pos = torch.as_tensor(positions)
+    back = pos[:, None] - torch.arange(k.shape[0])[None, :]
+    seen = (back >= 0) & (back < (window or 1 << 30)) & (pos[:, None] >= 0)
+    some = seen.any(1)
     z_abs = 0.0
-    for r, p in enumerate(positions):
-        lo = max(0, p - window + 1) if window else 0
-        if p < 0:
-            continue
-        for h in range(heads):
-            kk, vv = k[lo:p + 1, h // group], v[lo:p + 1, h // group]
-            z = kk @ q[r, h] * scale
-            z_abs = max(z_abs, float((kk.abs() @ q[r, h].abs()).nan_to_num().max() * scale))
-            lse[r, h] = torch.logsumexp(z, 0)
-            w = torch.exp(z - lse[r, h])
-            out[r, h] = w @ vv
-            weight[r, h] = w @ vv.abs()
+    for h in range(heads):
+        kk, vv = k[:, h // group], v[:, h // group]
+        z = torch.where(seen, q[:, h] @ kk.T * scale, -torch.inf)
+        z_abs = max(z_abs, float(torch.where(seen, q[:, h].abs() @ kk.abs().T, 0.0).nan_to_num().max() * scale))
+        lse[:, h] = torch.logsumexp(z, 1)
+        w = torch.where(seen, torch.exp(z - torch.where(some, lse[:, h], 0.0)[:, None]), 0.0)
+        out[:, h] = w @ vv
+        weight[:, h] = w @ vv.abs()
     return out, lse, weight, z_abs

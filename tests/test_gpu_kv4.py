@@ -300,6 +300,30 @@ def test_prompts(heads, kvh, hd, block, dtype, window):
     s.c.close()
 
 
+@pytest.mark.parametrize("heads,kvh,hd,block", [(32, 4, 128, 64), (32, 32, 64, 16), (96, 1, 128, 32)])
+@pytest.mark.parametrize("window", [0, 1, 150])
+def test_many_rows(heads, kvh, hd, block, window):
+    """Enough rows that the tiles are wide (128 entries): prompts from their start, chunks, single tokens, a request that waits."""
+    s = Requests([300, 33, 700, 70, 150], [300, 33, 180, 0, 1], heads, kvh, hd, "bf16", block, seed=13)
+    assert sum(s.rows) * heads >= 16384
+    s.step()
+    out, lse = s.c.attend(0, s.q, window=window, lse=True)
+    s.check(out, lse, window=window)
+    assert torch.equal(out, s.c.attend(0, s.q, window=window))
+    s.c.close()
+
+
+def test_many_rows_over_a_long_context_are_cut_and_joined():
+    s = Requests([5001, 400], [260, 3], 64, 2, 64, "bf16", 32, seed=14)
+    s.step()
+    first = s.c.attend(0, s.q, lse=True)
+    s.check(*first)
+    for _ in range(3):
+        again = s.c.attend(0, s.q, lse=True)
+        assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
+    s.c.close()
+
+
 @pytest.mark.parametrize("dtype,heads,kvh,hd", [("bf16", 4, 1, 128), ("f32", 2, 2, 64), ("bf16", 2, 2, 32), ("bf16", 2, 1, 256)])
 @pytest.mark.parametrize("rows", [1, 3, 40])
 def test_long_contexts_are_cut_and_joined(dtype, heads, kvh, hd, rows):
@@ -348,17 +372,17 @@ def test_rows_that_see_nothing():
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("hd", [32, 64, 128, 256])
-@pytest.mark.parametrize("rows", [5, 60])
-def test_nan_reaches_the_rows_that_see_it_and_no_other(dtype, hd, rows):
+@pytest.mark.parametrize("rows,heads", [(5, 2), (60, 2), (130, 128)])
+def test_nan_reaches_the_rows_that_see_it_and_no_other(dtype, hd, rows, heads):
     """A NaN in K or V of a position shows in every row that sees it (and, in V, only in its group of 32 elements), not in
     earlier rows, nor in those whose window lies behind it."""
     n = 150
-    s = Requests([n], [rows], 2, 2, hd, dtype, 16, seed=8)
+    s = Requests([n], [rows], heads, 2, hd, dtype, 16, seed=8)
     s.step()
     clean = s.c.attend(0, s.q)
     window = 70
     clean_w = s.c.attend(0, s.q, window=window)
-    bad_k, bad_v, early = n - 3, n - 2, n - rows - window + 3  # early: the first rows' window still holds it
+    bad_k, bad_v, early = n - 3, n - 2, max(n - rows - window + 3, n - 128 if rows == 130 else -1)  # early: the first rows' window still holds it
     s.k[0][bad_k, 0, 1] = float("nan")
     s.v[0][bad_v, 1, hd - 1] = float("inf")
     if early >= 0:
@@ -370,12 +394,13 @@ def test_nan_reaches_the_rows_that_see_it_and_no_other(dtype, hd, rows):
     for window_, base in ((window, clean_w), (0, clean)):
         out = s.c.attend(0, s.q, window=window_)
         pos = torch.arange(n - rows, n, device="cuda:0")
-        want = torch.zeros(rows, 2, hd, dtype=torch.bool, device="cuda:0")
-        want[pos >= bad_k, 0, :] = True
-        want[pos >= bad_v, 1, hd - 32:] = True
+        want = torch.zeros(rows, heads, hd, dtype=torch.bool, device="cuda:0")
+        first, second = want[:, :heads // 2], want[:, heads // 2:]  # the query heads of the two kv heads
+        first[pos >= bad_k] = True
+        second[pos >= bad_v, :, hd - 32:] = True
         if early >= 0:
             sees = (pos >= early) & ((pos - window_ < early) if window_ else (pos >= 0))
-            want[sees, 1, :32] = True
+            second[sees, :, :32] = True
         assert torch.equal(torch.isnan(out), want), (window_, torch.isnan(out).sum(), want.sum())
         assert torch.equal(out[~want], base[~want])
     s.c.close()
