@@ -24,6 +24,9 @@ struct Kv4Tile {
     static constexpr int v_scales(int hd) { return 16 * hd + hd / 2; }
 };
 
+// multiplier for divisions by d > 1
+inline uint32_t magic_of(uint32_t d) { return 0xffffffffu / d + 1; }
+
 // One workgroup's share of the attention: part `part` of `n_parts` of the positions that one tile of rows of one kv head sees.
 // A request's rows and the query heads that share a kv head form one list, row-major (entry f = row f / group, head f % group);
 // a tile is the entries tile * M .. tile * M + M - 1.
@@ -46,7 +49,8 @@ struct Kv4Plan {
     int32_t* n_parts;
     uint32_t* arrived;  // workgroups that have read the lengths
     int max_parts;  // room in `parts`
-    int group, kv_heads, tile_rows;
+    int group, kv_heads, tile_rows, tile_shift;  // tile_rows = 1 << tile_shift
+    uint32_t kv_magic;                           // magic_of(kv_heads)
     int target_parts;  // a launch is cut so that it has about this many parts
     int min_chunks;    // of a part that is one of several
     int one_per_cu;    // a CU holds one workgroup of the launch
@@ -70,6 +74,7 @@ struct Kv4Attend {
     float* lse;
     float scale_log2;  // scale / ln 2
     int window, group, kv_heads;
+    uint32_t group_magic;  // magic_of(group)
     int min_chunks;  // of a part that is one of several
     int tiles_shift;  // log2(block_tokens / 16)
     int past_caches;  // K and V are read without keeping them in the caches

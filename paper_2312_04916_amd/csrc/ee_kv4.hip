@@ -19,6 +19,19 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// x / d, with magic = magic_of(d): the multiplier 2^32 / d, rounded up, gives it or one more.
+__device__ __forceinline__ uint32_t div_by(uint32_t x, uint32_t d, uint32_t magic) {
+    if (d == 1) return x;
+    const uint32_t q = __umulhi(x, magic);
+    return q * d > x ? q - 1 : q;
+}
+// x / d for 0 <= x < 2^20, d > 0: the reciprocal's and the product's errors leave the quotient, or one beside it.
+__device__ __forceinline__ int div_small(int x, int d) {
+    int q = (int)((float)x * __builtin_amdgcn_rcpf((float)d));
+    q -= q * d > x ? 1 : 0;
+    return q + ((q + 1) * d <= x ? 1 : 0);
+}
+
 constexpr uint32_t SCALE_NAN = 255;              // of a group that stands for NaN
 constexpr uint32_t SCALE_MIN = 16, SCALE_MAX = 252;  // 2^-111, 2^125: no held value is subnormal or infinite in bf16
 
@@ -53,6 +66,17 @@ __device__ __forceinline__ int lanes_scan(int v) {
     return v;
 }
 
+// largest of a wave's values, none of them negative
+__device__ __forceinline__ int lanes_max(int v) {
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
 // Sums over a workgroup of up to 16 waves: exclusive prefix of each thread's values, and the totals.  `waves` is used by one
 // call only.
 template <int N>
@@ -77,10 +101,13 @@ __device__ __forceinline__ void scan_sums(int (&v)[N], int (&total)[N], int (*wa
 // Last index i < n with first[i] <= x (first ascending, first[0] <= x): of several equal ones the last, which is the one that
 // is not empty.
 __device__ __forceinline__ int last_not_above(const int32_t* first, int n, int32_t x) {
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (first[mid] <= x) lo = mid; else hi = mid;
+    int lo = 0, len = n;  // (a step reads three places at once: LDS answers late, not slowly)
+    while (len > 1) {
+        const int q = (len + 3) >> 2, a = min(lo + q, lo + len - 1), b = min(lo + 2 * q, lo + len - 1), c = min(lo + 3 * q, lo + len - 1);
+        const bool ga = first[a] <= x, gb = first[b] <= x, gc = first[c] <= x;
+        const int end = gc ? lo + len : gb ? c : ga ? b : a;
+        lo = gc ? c : gb ? b : ga ? a : lo;
+        len = end - lo;
     }
     return lo;
 }
@@ -122,6 +149,8 @@ __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
         sum[3] = min(sum[3] + rows, cap);
     }
     scan_sums<4>(sum, all, s_sums);
+    uint32_t arrived = 0;  // (all of this workgroup's lengths have been read; the answer is needed at the end)
+    if (tid == 0 && gridDim.x > 1) arrived = __hip_atomic_fetch_add(p.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     const int left = max(0, p.n_blocks - all[0]);  // free before the call (the lengths may contradict the pool)
     const bool clipped = all[3] > p.n_rows;
     if (clipped) {
@@ -154,7 +183,7 @@ __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
             if (ok) {
                 if (asked) taken = take;
                 if (row1 > row0) {
-                    const int tiles = ((row1 - row0) * p.group + p.tile_rows - 1) / p.tile_rows;
+                    const int tiles = ((row1 - row0) * p.group + p.tile_rows - 1) >> p.tile_shift;
                     work += (float)tiles * (float)((s_start[i] + row1 - row0 + KV4_CHUNK - 1) / KV4_CHUNK);
                 }
             }
@@ -163,14 +192,14 @@ __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
         if (tid == 0) s_row[n] = rows_all, s_row[n + 1] = p.n_rows, s_give[n] = given;
     }
     work = wave_sum(work);
-    taken = max(taken, __shfl_xor(taken, 32)), taken = max(taken, __shfl_xor(taken, 16)), taken = max(taken, __shfl_xor(taken, 8));
-    taken = max(taken, __shfl_xor(taken, 4)), taken = max(taken, __shfl_xor(taken, 2)), taken = max(taken, __shfl_xor(taken, 1));
+    taken = lanes_max(taken);
     if (lane == 0) s_work[wave] = work, s_taken[wave] = taken;
     __syncthreads();
-    for (int v = 0; v < nt >> 6; ++v) work = v ? work + s_work[v] : s_work[0], taken = max(taken, s_taken[v]);
+    work = wave_sum(lane < nt >> 6 ? s_work[lane] : 0.f);
+    taken = lanes_max(lane < nt >> 6 ? s_taken[lane] : 0);
     // chunks of a part: an even share of the work.  Where a CU holds one workgroup, a request is cut into as many parts as it has
     // shares (more would run after the others have ended); else into one more, so that none is longer than a share.
-    const int per_part = max(p.min_chunks, (int)fminf(1e6f, ceilf(work * (float)p.kv_heads / (float)p.target_parts)));
+    const int per_part = max(p.min_chunks, (int)fminf(65536.f, ceilf(work * (float)p.kv_heads / (float)p.target_parts)));
     const int round_up = p.one_per_cu ? 0 : per_part - 1;
 
     // parts: items (tile of rows, kv head) in the requests' order, each cut alike; the rows behind the last request's are one
@@ -178,20 +207,21 @@ __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
     auto parts_of = [&](int i) {  // of an item
         const int rows = s_row[i + 1] - s_row[i];
         if (i == n || rows == 0 || !(s_had[i] & SERVED)) return 1;
-        return max(1, ((s_start[i] + rows + KV4_CHUNK - 1) / KV4_CHUNK + round_up) / per_part);
+        return max(1, div_small(min((s_start[i] + rows + KV4_CHUNK - 1) / KV4_CHUNK + round_up, (1 << 20) - 1), per_part));
     };
-    auto items_of = [&](int i) { return ((s_row[i + 1] - s_row[i]) * p.group + p.tile_rows - 1) / p.tile_rows * p.kv_heads; };
+    auto items_of = [&](int i) { return (((s_row[i + 1] - s_row[i]) * p.group + p.tile_rows - 1) >> p.tile_shift) * p.kv_heads; };
     int cnt[2] = {0, 0}, cnt_all[2];
     const int j0 = min(n + 1, tid * per), j1 = min(n + 1, j0 + per);
     for (int i = j0; i < j1; ++i) {
-        const int np = parts_of(i), items = items_of(i);
-        cnt[0] += items * np, cnt[1] += np > 1 ? items * np : 0;
+        const int np = parts_of(i), all_parts = items_of(i) * np;
+        s_part[i] = all_parts, s_slot[i] = np;  // (this thread's, for now)
+        cnt[0] += all_parts, cnt[1] += np > 1 ? all_parts : 0;
     }
     scan_sums<2>(cnt, cnt_all, s_sums3);
     for (int i = j0; i < j1; ++i) {
-        const int np = parts_of(i), items = items_of(i);
+        const int all_parts = s_part[i], np = s_slot[i];
         s_part[i] = cnt[0], s_slot[i] = cnt[1];
-        cnt[0] += items * np, cnt[1] += np > 1 ? items * np : 0;
+        cnt[0] += all_parts, cnt[1] += np > 1 ? all_parts : 0;
     }
     __syncthreads();
     const int n_parts = min(cnt_all[0], p.max_parts);
@@ -226,16 +256,17 @@ __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
         }
         t -= p.n_rows;
         if (t < n_parts) {
-            const int i = last_not_above(s_part, n + 1, (int)t), np = parts_of(i), local = (int)t - s_part[i], item = local / np;
-            const int rows = s_row[i + 1] - s_row[i], tiles = (rows * p.group + p.tile_rows - 1) / p.tile_rows;
+            const int i = last_not_above(s_part, n + 1, (int)t), np = parts_of(i), local = (int)t - s_part[i];
+            const int item = np == 1 ? local : local / np, tile = (int)div_by((uint32_t)item, (uint32_t)p.kv_heads, p.kv_magic);
+            const int rows = s_row[i + 1] - s_row[i], tiles = (rows * p.group + p.tile_rows - 1) >> p.tile_shift;
             Kv4Part w;
             w.seq = i < n && (s_had[i] & SERVED) ? i : -1;
             w.row0 = s_row[i];
             w.n_flat = rows * p.group;
             w.start = i < n ? s_start[i] : 0;
-            w.tile = tiles - 1 - item / p.kv_heads;  // (those that see most come first)
-            w.head = item % p.kv_heads;
-            w.part_of = local % np | np << 16;
+            w.tile = tiles - 1 - tile;  // (those that see most come first)
+            w.head = item - tile * p.kv_heads;
+            w.part_of = (local - item * np) | np << 16;
             w.slot = s_slot[i] + local;
             p.parts[t] = w;
             continue;
@@ -251,12 +282,8 @@ __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
     }
 
     if (tid == 0) {
-        s_last = 1;
-        if (gridDim.x > 1) {
-            const uint32_t before = __hip_atomic_fetch_add(p.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            s_last = before == gridDim.x - 1;
-            if (s_last) __hip_atomic_store(p.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
+        s_last = arrived == gridDim.x - 1;
+        if (s_last && gridDim.x > 1) __hip_atomic_store(p.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
     if (s_last)
@@ -568,12 +595,26 @@ __device__ __forceinline__ f32x2 handed2(const float* p) {
 }
 constexpr int FAN_IN = 32;  // parts that are joined at a time
 
+// row of an entry in its request; where the entry's results go
+__device__ __forceinline__ int row_of(const Kv4Attend& a, int f) { return (int)div_by((uint32_t)f, (uint32_t)a.group, a.group_magic); }
+__device__ __forceinline__ size_t out_row(const Kv4Attend& a, const Kv4Part& w, int f) {
+    const int row = row_of(a, f);
+    return (size_t)(w.row0 + row) * (a.group * a.kv_heads) + w.head * a.group + f - row * a.group;
+}
+
+// chunks first .. end of part `part` of `n_parts` that n_chunks from c_first on are cut into, as evenly as they can be
+__device__ __forceinline__ void part_of_chunks(int c_first, int n_chunks, int n_parts, int part, int& first, int& end) {
+    const int each = div_small(n_chunks, n_parts), more = n_chunks - each * n_parts;
+    first = c_first + part * each + min(part, more);
+    end = first + each + (part < more ? 1 : 0);
+}
+
 // rows that see nothing
 template <int HD, typename ST>
 __device__ __forceinline__ void sees_nothing(const Kv4Attend& a, const Kv4Part& w, int f0, int f_end, int threads, ST* out) {
     for (int i = threadIdx.x; i < (f_end - f0) * HD; i += threads) {
         const int f = f0 + i / HD;
-        const size_t o = (size_t)(w.row0 + f / a.group) * (a.group * a.kv_heads) + w.head * a.group + f % a.group;
+        const size_t o = out_row(a, w, f);
         out[o * HD + i % HD] = (ST)0.f;
         if (i % HD == 0 && a.lse) a.lse[o] = -INFINITY;
     }
@@ -585,7 +626,7 @@ __device__ __forceinline__ void sees_nothing(const Kv4Attend& a, const Kv4Part& 
 // by the workgroups that join alone made a ragged batch's 20 us 37.
 template <int HD, int THREADS, int M, typename ST>
 __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w, int n_parts, int f0, int f_end, uint32_t* s_last) {
-    const int part = w.part_of & 0xffff, slot0 = w.slot - part, n_heads = a.group * a.kv_heads;
+    const int part = w.part_of & 0xffff, slot0 = w.slot - part;
     const int groups = (n_parts + FAN_IN - 1) / FAN_IN, group0 = part / FAN_IN * FAN_IN;
     ST* out = (ST*)a.out;
     const bool two_levels = groups > 1;
@@ -637,7 +678,7 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
                 top = t;
             }
             if (whole) {
-                const size_t at = (size_t)(w.row0 + f / a.group) * n_heads + w.head * a.group + f % a.group;
+                const size_t at = out_row(a, w, f);
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
                 out[at * HD + d] = (ST)(acc[0] * inv);
                 out[at * HD + d + 1] = (ST)(acc[1] * inv);
@@ -670,7 +711,6 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const int f0 = w.tile * M, f_end = min(w.n_flat, f0 + M);  // entries
-    const int n_heads = a.group * a.kv_heads;
     ST* out = (ST*)a.out;
     if (w.seq < 0) {
         sees_nothing<HD>(a, w, f0, f_end, NW * 64, out);
@@ -683,7 +723,7 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
         const int f = min(f0 + 16 * u + col, f_end - 1);  // (columns behind the last entry repeat it; nobody reads them)
-        const int row = f / a.group, head = w.head * a.group + f % a.group;
+        const int row = row_of(a, f), head = w.head * a.group + f - row * a.group;
         hi[u] = w.start + row;
         lo[u] = a.window ? max(0, hi[u] - a.window + 1) : 0;
         const ST* src = (const ST*)a.q + (w.row0 + row) * a.q_row + head * a.q_head + quarter * 8;
@@ -711,14 +751,15 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
             }
         }
     }
-    const int pos_first = w.start + f0 / a.group, pos_last = w.start + (f_end - 1) / a.group;
+    const int pos_first = w.start + row_of(a, f0), pos_last = w.start + row_of(a, f_end - 1);
     const int lo_min = a.window ? max(0, pos_first - a.window + 1) : 0;
     const int lo_max = a.window ? max(0, pos_last - a.window + 1) : 0;
     const int c_first = lo_min / KV4_CHUNK, n_chunks = pos_last / KV4_CHUNK + 1 - c_first;
     // (a tile that sees less than the request's last row, because of its rows' positions or the window, needs fewer parts)
-    const int n_parts = min(w.part_of >> 16, max(1, (n_chunks + a.min_chunks - 1) / a.min_chunks)), part = w.part_of & 0xffff;
+    const int n_parts = min(w.part_of >> 16, max(1, div_small(n_chunks + a.min_chunks - 1, a.min_chunks))), part = w.part_of & 0xffff;
     if (part >= n_parts) return;
-    const int c_lo = c_first + (int)((int64_t)n_chunks * part / n_parts), c_hi = c_first + (int)((int64_t)n_chunks * (part + 1) / n_parts);
+    int c_lo, c_hi;
+    part_of_chunks(c_first, n_chunks, n_parts, part, c_lo, c_hi);
 
     const int32_t* table = a.table + (size_t)w.seq * a.table_stride;
     const int last_tile = pos_last >> 4;
@@ -962,7 +1003,7 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
                 for (int e = 0; e < EPT; ++e) acc[e] += wt * s_o[(v * 16 + my_row) * LDO + my_d + e];
             }
             if (n_parts == 1) {
-                const size_t r = (size_t)(w.row0 + f / a.group) * n_heads + w.head * a.group + f % a.group;
+                const size_t r = out_row(a, w, f);
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
                 for (int e = 0; e < EPT; ++e) out[r * HD + my_d + e] = (ST)(acc[e] * inv);
@@ -999,7 +1040,6 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     const int lane = threadIdx.x & 63, group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3;
     const int col = lane & 31, half = lane >> 5;
     const int f0 = w.tile * M, f_end = min(w.n_flat, f0 + M);
-    const int n_heads = a.group * a.kv_heads;
     __bf16* out = (__bf16*)a.out;
     if (w.seq < 0) {
         sees_nothing<HD>(a, w, f0, f_end, 512, out);
@@ -1008,7 +1048,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
 
     // entry of this lane's column; what the wave's and the workgroup's entries see
     const int f_wave = f0 + 32 * wave, f = min(f_wave + col, f_end - 1);
-    const int row = f / a.group, head = w.head * a.group + f % a.group;
+    const int row = row_of(a, f), head = w.head * a.group + f - row * a.group;
     const int hi = w.start + row, lo = a.window ? max(0, hi - a.window + 1) : 0;
     bf16x8 q[KS];  // elements 16 s + 8 half ..
     {
@@ -1024,14 +1064,15 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
         }
     }
     auto first_of = [&](int pos) { return a.window ? max(0, pos - a.window + 1) : 0; };
-    const int pos_first = w.start + f0 / a.group, pos_last = w.start + (f_end - 1) / a.group;
+    const int pos_first = w.start + row_of(a, f0), pos_last = w.start + row_of(a, f_end - 1);
     const bool idle = f_wave >= f_end;
-    const int wave_first = w.start + min(f_wave, f_end - 1) / a.group, wave_last = w.start + min(f_wave + 31, f_end - 1) / a.group;
+    const int wave_first = w.start + row_of(a, min(f_wave, f_end - 1)), wave_last = w.start + row_of(a, min(f_wave + 31, f_end - 1));
     const int c_first = first_of(pos_first) / KV4_CHUNK, n_chunks = pos_last / KV4_CHUNK + 1 - c_first;
     // (a tile that sees less than the request's last row, because of its rows' positions or the window, needs fewer parts)
-    const int n_parts = min(w.part_of >> 16, max(1, (n_chunks + a.min_chunks - 1) / a.min_chunks)), part = w.part_of & 0xffff;
+    const int n_parts = min(w.part_of >> 16, max(1, div_small(n_chunks + a.min_chunks - 1, a.min_chunks))), part = w.part_of & 0xffff;
     if (part >= n_parts) return;
-    const int c_lo = c_first + (int)((int64_t)n_chunks * part / n_parts), c_hi = c_first + (int)((int64_t)n_chunks * (part + 1) / n_parts);
+    int c_lo, c_hi;
+    part_of_chunks(c_first, n_chunks, n_parts, part, c_lo, c_hi);
 
     // this wave converts tile `tl` of a step's two, of K or of V
     const int tl = wave & 1, quarter = lane >> 4, t16 = lane & 15;
@@ -1244,7 +1285,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     halves_of(l, l0, l1);
     const float sum = l0 + l1;
     if (!group && f_wave + col < f_end) {
-        const size_t r = (size_t)(w.row0 + row) * n_heads + head, at = (size_t)w.slot * M + 32 * wave + col;
+        const size_t r = (size_t)(w.row0 + row) * (a.group * a.kv_heads) + head, at = (size_t)w.slot * M + 32 * wave + col;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {

@@ -185,14 +185,14 @@ int ee_kv4_plan(ee_kv4* c, int n_seqs, const int32_t* dev_held, const int32_t* d
     p.arrived = (uint32_t*)c->arrays.n_free + 2;
     p.group = group, p.kv_heads = g.n_kv_heads;
     const int units = kv4_tile_units(g.dtype, g.head_dim, (int)std::min<int64_t>((int64_t)most * group, 1 << 30), (int64_t)n_rows * g.n_heads);
-    p.tile_rows = 16 * units;
+    p.tile_rows = 16 * units, p.tile_shift = __builtin_ctz((unsigned)p.tile_rows), p.kv_magic = magic_of((uint32_t)g.n_kv_heads);
     p.max_parts = (int)std::min(c->sl.max_parts, most_parts(g, n_seqs, n_rows, p.tile_rows));
     const Cut cut = cut_of(g, n_seqs, n_rows, units);
     p.target_parts = cut.parts, p.min_chunks = cut.min_chunks, p.one_per_cu = cut.waves == 8;
-    // one thread per row and part, and for blocks that change hands, which only the GPU knows, a sixteenth of the pool; a small
+    // one thread per row and part, and for blocks that change hands, which only the GPU knows, an eighth of the pool; a small
     // step in one small workgroup
     const int threads = n_seqs < 256 && n_rows <= 1024 ? 256 : 1024;
-    const int64_t tasks = (int64_t)n_rows + p.max_parts + g.n_blocks / 16;
+    const int64_t tasks = (int64_t)n_rows + p.max_parts + g.n_blocks / 8;
     const int workgroups = n_rows + p.max_parts <= 2048 && g.n_blocks <= 4096 && threads == 256 ? 1 : (int)std::min<int64_t>(256, 1 + tasks / threads);
     const int rc = hip_status(launch_kv4_plan(p, workgroups, threads, (hipStream_t)stream));
     if (rc != EE_OK) return rc;
@@ -255,6 +255,7 @@ int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride,
     a.out = dev_out, a.lse = dev_lse;
     a.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt((float)g.head_dim)) * 1.4426950408889634f;
     a.window = window, a.group = g.n_heads / g.n_kv_heads, a.kv_heads = g.n_kv_heads, a.min_chunks = c->min_chunks;
+    a.group_magic = magic_of((uint32_t)a.group);
     a.tiles_shift = __builtin_ctz((unsigned)g.block_tokens) - 4;
     a.past_caches = layer_bytes(g) * g.n_layers > PAST_CACHES_BYTES;
     a.q_vec = ((uintptr_t)dev_q & 15) == 0 && (q_row_stride * (int64_t)es) % 16 == 0 && (q_head_stride * (int64_t)es) % 16 == 0;
