@@ -406,7 +406,8 @@ int ee_decode_step_static(ee_model* m, ee_kv_cache* c, int n_seqs, const int32_t
  * in every layer.  All the state that outlasts a call is the pool, the table and the stack of free blocks.
  *
  * Calls check what the host can see and return the codes above; lengths and slots are on the GPU, where a call that cannot
- * be served is marked (served, slot -1) and every access stays inside the buffers whatever the lengths are. */
+ * be served is marked (served, slot -1) and every access stays inside the buffers whatever the lengths are.  The calls of one
+ * cache share its state: calls on different streams have to be ordered by the caller. */
 
 typedef struct {
     int32_t n_layers, n_heads, n_kv_heads, head_dim; /* head_dim in {32, 64, 128, 256}; n_heads a multiple of n_kv_heads */

@@ -12,6 +12,7 @@ import torch
 
 EE_F32, EE_BF16 = 0, 1
 EE_MAX_ROWS, EE_MAX_SEQS, EE_MAX_EXITS = 256, 64, 8
+EE_KV4_MAX_SEQS = 4096
 EE_K_QKV, EE_K_ATTN, EE_K_OPROJ, EE_K_SWIGLU, EE_K_DOWN, EE_K_HEAD = range(6)
 EE_ROUTE_STAGED, EE_ROUTE_ROWS, EE_ROUTE_CUT, EE_ROUTE_PANELS = range(4)
 KERNEL_NAMES = ["qkv", "attention", "oproj", "swiglu", "down", "head"]

@@ -73,6 +73,7 @@ struct Kv4Attend {
     void* out;
     float* lse;
     float scale_log2;  // scale / ln 2
+    float slack;       // scores that differ by this have probabilities that differ by 2^8 (finite however small the scale is)
     int window, group, kv_heads;
     uint32_t group_magic;  // magic_of(group)
     int min_chunks;  // of a part that is one of several

@@ -785,8 +785,7 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
     };
 
     f32x4 o[UNITS][EPC];
-    float m[UNITS], l[UNITS];  // m: the scores' reference, at most `slack` below their maximum (so no probability passes 2^8)
-    const float slack = 8.f / a.scale_log2;
+    float m[UNITS], l[UNITS];  // m: the scores' reference, at most a.slack below their maximum (so no probability passes 2^8)
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
         m[u] = -INFINITY, l[u] = 0.f;
@@ -881,7 +880,7 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, s[u][t][i]);
             top = fmaxf(rows4_max(top), m[u]);
-            if (__any(top > m[u] + slack)) {
+            if (__any(top > m[u] + a.slack)) {
                 const float corr = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[u] - top) * a.scale_log2);
                 l[u] *= corr;
 #pragma unroll
@@ -1157,8 +1156,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     };
 
     f32x16 o[DB] = {};
-    float m = -INFINITY, l = 0.f;  // m: the scores' reference, at most `slack` below their maximum (so no probability passes 2^8)
-    const float slack = 8.f / a.scale_log2;
+    float m = -INFINITY, l = 0.f;  // m: the scores' reference, at most a.slack below their maximum (so no probability passes 2^8)
     // The second group's matrix products come when the first one's vector work does: its scores are formed an interval ahead, so K
     // is converted two steps ahead there.
     const int ahead = group && !of_v ? 2 : 1;
@@ -1207,7 +1205,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
             float t0, t1;
             halves_of(top, t0, t1);
             top = fmaxf(fmaxf(t0, t1), m);
-            if (__any(top > m + slack)) {
+            if (__any(top > m + a.slack)) {
                 const float corr = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * a.scale_log2);
                 l *= corr;
 #pragma unroll

@@ -254,6 +254,7 @@ int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride,
     a.q = dev_q, a.q_row = q_row_stride, a.q_head = q_head_stride;
     a.out = dev_out, a.lse = dev_lse;
     a.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt((float)g.head_dim)) * 1.4426950408889634f;
+    a.slack = std::min(8.f / a.scale_log2, 1e30f);
     a.window = window, a.group = g.n_heads / g.n_kv_heads, a.kv_heads = g.n_kv_heads, a.min_chunks = c->min_chunks;
     a.group_magic = magic_of((uint32_t)a.group);
     a.tiles_shift = __builtin_ctz((unsigned)g.block_tokens) - 4;

@@ -33,7 +33,9 @@ class Kv4Cache:
         pb, sb = C.c_size_t(), C.c_size_t()
         _chk(lib().ee_kv4_bytes(C.byref(cfg), C.byref(pb), C.byref(sb)), "ee_kv4_bytes")
         self.device, self.dtype = torch.device(device), _DTYPES[cfg.dtype]
-        self._index = self.device.index or 0
+        if self.device.index is None:
+            self.device = torch.device(self.device.type, torch.cuda.current_device())
+        self._index = self.device.index
         self.pool = torch.empty(pb.value, dtype=torch.uint8, device=self.device)
         self.state = torch.empty(sb.value, dtype=torch.uint8, device=self.device)
         _chk(lib().ee_kv4_create(C.byref(cfg), self.pool.data_ptr(), pb.value, self.state.data_ptr(), sb.value, _raw_stream(stream, self._index),
@@ -56,19 +58,20 @@ class Kv4Cache:
         self.n_free = view(a.n_free, 1, torch.int32)
         self.n_rows = 0
         # (calls of the loop over layers: looked up once)
+        self._heads, self._kv_heads, self._head_dim = n_heads, n_kv_heads, head_dim
         L = lib()
         self._plan, self._append, self._read, self._attend = L.ee_kv4_plan, L.ee_kv4_append, L.ee_kv4_read, L.ee_kv4_attend
 
     def _lengths(self, t: torch.Tensor, n: int, what: str) -> int:
-        if t.dtype != torch.int32 or t.device != self.device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        if t.dtype is not torch.int32 or t.get_device() != self._index or t.shape != (n,) or not t.is_contiguous():
             raise ValueError(f"{what}: int32[{n}] on {self.device}, contiguous")
         return t.data_ptr()
 
     def _vectors(self, t: torch.Tensor, heads: int, rows: Optional[int], what: str) -> Tuple[int, int, int]:
-        if t.dtype != self.dtype or t.device != self.device or t.dim() != 3:
+        if t.dtype is not self.dtype or t.get_device() != self._index or t.dim() != 3:
             raise ValueError(f"{what}: {self.dtype} [rows][heads][head_dim] on {self.device}")
         n, h, d = t.shape
-        if h != heads or d != self.cfg.head_dim or (rows is not None and n != rows):
+        if h != heads or d != self._head_dim or (rows is not None and n != rows):
             raise ValueError(f"{what}: shape {tuple(t.shape)}, expected [{'rows' if rows is None else rows}][{heads}][{self.cfg.head_dim}]")
         sr, sh, sd = t.stride()
         if sd != 1:
@@ -86,7 +89,7 @@ class Kv4Cache:
         self.n_rows = n_rows
 
     def _slot_ptr(self, slots: torch.Tensor, rows: int) -> int:
-        if slots.dtype != torch.int64 or slots.device != self.device or slots.shape != (rows,) or not slots.is_contiguous():
+        if slots.dtype is not torch.int64 or slots.get_device() != self._index or slots.shape != (rows,) or not slots.is_contiguous():
             raise ValueError(f"slots: int64[{rows}] on {self.device}, contiguous")
         return slots.data_ptr()
 
@@ -94,8 +97,8 @@ class Kv4Cache:
         """ee_kv4_append.  k, v: [rows][n_kv_heads][head_dim], any strides of rows and heads; slots: the latest plan's where not
         given."""
         rows = k.shape[0]
-        kp, kr, kh = self._vectors(k, self.cfg.n_kv_heads, None, "k")
-        vp, vr, vh = self._vectors(v, self.cfg.n_kv_heads, rows, "v")
+        kp, kr, kh = self._vectors(k, self._kv_heads, None, "k")
+        vp, vr, vh = self._vectors(v, self._kv_heads, rows, "v")
         code = self._append(self.h, layer, rows, kp, kr, kh, vp, vr, vh, None if slots is None else self._slot_ptr(slots, rows),
                             _raw_stream(stream, self._index))
         if code:
@@ -105,7 +108,8 @@ class Kv4Cache:
         """ee_kv4_read -> k, v [rows][n_kv_heads][head_dim]: the values that the slots hold."""
         rows = slots.shape[0]
         p = self._slot_ptr(slots, rows)
-        k, v = torch.empty(2, rows, self.cfg.n_kv_heads, self.cfg.head_dim, dtype=self.dtype, device=self.device).unbind()
+        k = torch.empty(rows, self._kv_heads, self._head_dim, dtype=self.dtype, device=self.device)
+        v = torch.empty_like(k)
         code = self._read(self.h, layer, rows, p, k.data_ptr(), v.data_ptr(), _raw_stream(stream, self._index))
         if code:
             _chk(code, "ee_kv4_read")
@@ -117,7 +121,7 @@ class Kv4Cache:
         plan, any strides of rows and heads; scale: 1 / sqrt(head_dim) where not given."""
         if scale is not None and not scale > 0:
             raise ValueError("scale: positive")
-        heads, hd = self.cfg.n_heads, self.cfg.head_dim
+        heads, hd = self._heads, self._head_dim
         qp, qr, qh = self._vectors(q, heads, self.n_rows, "q")
         if out is None:
             out = torch.empty(self.n_rows, heads, hd, dtype=self.dtype, device=self.device)

@@ -192,7 +192,7 @@ def test_large_plans_run_in_many_workgroups():
 
 
 def test_the_largest_number_of_requests():
-    n = ee.EE_KV4_MAX_SEQS if hasattr(ee, "EE_KV4_MAX_SEQS") else 4096
+    n = ee.EE_KV4_MAX_SEQS
     c = cache_of(2, 2, 32, "bf16", 16, n + 100, n, 64, 2 * n)
     blocks = ref.Blocks(n + 100, n, 64, 16)
     held = check_plan(c, blocks, [0] * n, [0] * n, [1] * n, n, 1)
@@ -450,6 +450,36 @@ def test_on_another_stream_and_in_a_graph():
         start.copy_(end)
         end.add_(1)
     c.close()
+
+
+@pytest.mark.parametrize("rows,heads", [(1, 8), (9, 8), (300, 64)])
+def test_offsets_beyond_32_bits(rows, heads):
+    """Two layers of 2.7 GB, and blocks from the pool's far end."""
+    n, hd, kvh, block = 333, 128, 8, 64
+    n_blocks = 40000
+    c = cache_of(heads, kvh, hd, "bf16", block, n_blocks, 1, 512, 512, layers=2)
+    assert c.pool.numel() > 5 << 30
+    c.free.copy_(torch.arange(n_blocks, device="cuda:0"))
+    c.plan(dev([0]), dev([0]), dev([n]), n)
+    assert c.table[0, :6].tolist() == [n_blocks - 1 - i for i in range(6)]
+    k, v, q = rand((n, kvh, hd), "bf16", 1), rand((n, kvh, hd), "bf16", 2), rand((rows, heads, hd), "bf16", 3)
+    c.append(1, k, v)
+    rk, rv = c.read(1, c.slots[:n].clone())
+    assert torch.equal(rk.cpu().double(), ref.held(k)) and torch.equal(rv.cpu().double(), ref.held(v))
+    c.plan(dev([n]), dev([n - rows]), dev([n]), rows)
+    out = c.attend(1, q)
+    want, _, weight, _ = ref.attend(q, ref.held(k), ref.held(v), list(range(n - rows, n)), heads // kvh, hd ** -0.5)
+    assert ((out.cpu().double() - want).abs() <= (weight + want.abs()) * 2.0 ** -8 + 1e-4 * weight).all()
+    c.close()
+
+
+def test_tiny_and_large_scales():
+    s = Requests([70, 200], [1, 3], 4, 2, 64, "bf16", 16, seed=21)
+    s.step()
+    for scale in (1e-38, 1e-20, 3.0):
+        out, lse = s.c.attend(0, s.q, scale=scale, lse=True)
+        s.check(out, lse, scale=scale)
+    s.c.close()
 
 
 def test_layers_do_not_touch_each_other():
