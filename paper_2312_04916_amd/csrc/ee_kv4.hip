@@ -593,7 +593,8 @@ __device__ __forceinline__ void hand_over2(float* p, f32x2 v) {
 __device__ __forceinline__ f32x2 handed2(const float* p) {
     return __builtin_bit_cast(f32x2, __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
-constexpr int FAN_IN = 32;  // parts that are joined at a time
+// parts that are joined at a time: all, or of many about their number's square root
+__device__ __forceinline__ int fan_shift_of(int n_parts) { return n_parts <= 16 ? 4 : n_parts <= 64 ? 3 : n_parts <= 256 ? 4 : 5; }
 
 // row of an entry in its request; where the entry's results go
 __device__ __forceinline__ int row_of(const Kv4Attend& a, int f) { return (int)div_by((uint32_t)f, (uint32_t)a.group, a.group_magic); }
@@ -627,10 +628,11 @@ __device__ __forceinline__ void sees_nothing(const Kv4Attend& a, const Kv4Part& 
 template <int HD, int THREADS, int M, typename ST>
 __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w, int n_parts, int f0, int f_end, uint32_t* s_last) {
     const int part = w.part_of & 0xffff, slot0 = w.slot - part;
-    const int groups = (n_parts + FAN_IN - 1) / FAN_IN, group0 = part / FAN_IN * FAN_IN;
+    const int fan_shift = fan_shift_of(n_parts), fan = 1 << fan_shift;
+    const int groups = (n_parts + fan - 1) >> fan_shift, group0 = part >> fan_shift << fan_shift;
     ST* out = (ST*)a.out;
     const bool two_levels = groups > 1;
-    int first = slot0 + group0, stride = 1, n = min(FAN_IN, n_parts - group0);
+    int first = slot0 + group0, stride = 1, n = min(fan, n_parts - group0);
     uint32_t* counter = a.arrived + first;
     const float* part_ml = a.part_ml;
     for (int level = 0;; ++level) {
@@ -644,54 +646,67 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
         __syncthreads();
         if ((int)*s_last != n - 1) return;
         const bool whole = level == 1 || !two_levels;
-        // one thread per two elements: it asks for eight parts at once, weights and elements, so that a join of few parts is one
-        // trip to memory (and for the whole of a prompt's tile four)
-        constexpr int AT_ONCE = 8;
-#pragma unroll(M > 64 ? 4 : 1)
-        for (int i = threadIdx.x; i < (f_end - f0) * (HD / 2); i += THREADS) {
-            const int r = i / (HD / 2), d = i % (HD / 2) * 2, f = f0 + r;
+        // a thread has PAIRS pairs of elements of a row, LANES apart, and asks for all of them of up to eight parts at once
+        constexpr int PAIRS = M * HD / 2 >= 4 * THREADS ? 4 : M * HD / 2 >= 2 * THREADS ? 2 : 1, LANES = HD / 2 / PAIRS;
+        const int d = threadIdx.x % LANES * 2;
+        for (int r = threadIdx.x / LANES; r < f_end - f0; r += THREADS / LANES) {
             const size_t row = (size_t)first * M + r, step = (size_t)stride * M;
             float top = -INFINITY, sum = 0.f;
-            f32x2 acc = {0.f, 0.f};
-            for (int v0 = 0; v0 < n; v0 += AT_ONCE) {
-                f32x2 ml[AT_ONCE], x[AT_ONCE];
+            f32x2 acc[PAIRS] = {};
+            auto add = [&](auto at_once, int v0) {
+                constexpr int N = decltype(at_once)::value;
+                f32x2 ml[N], x[N][PAIRS];
 #pragma unroll
-                for (int v = 0; v < AT_ONCE; ++v) {
-                    ml[v] = f32x2{-INFINITY, 0.f}, x[v] = f32x2{0.f, 0.f};
-                    if (v0 + v < n) {
-                        const size_t at = row + step * (v0 + v);
-                        ml[v] = handed2(part_ml + 2 * at);
-                        x[v] = handed2(a.part_o + at * HD + d);
-                    }
+                for (int v = 0; v < N; ++v) {
+                    const size_t at = row + step * min(v0 + v, n - 1);  // (no branch, so that no load waits for another one)
+                    ml[v] = handed2(part_ml + 2 * at);
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) x[v][i] = handed2(a.part_o + at * HD + d + 2 * LANES * i);
                 }
                 float t = top;
 #pragma unroll
-                for (int v = 0; v < AT_ONCE; ++v) t = fmaxf(t, ml[v][0]);
+                for (int v = 0; v < N; ++v) t = fmaxf(t, ml[v][0]);
                 const float ref = t == -INFINITY ? 0.f : t;
                 const float old = __builtin_amdgcn_exp2f(top - ref);
-                sum *= old, acc *= old;
+                sum *= old;
 #pragma unroll
-                for (int v = 0; v < AT_ONCE; ++v) {
+                for (int i = 0; i < PAIRS; ++i) acc[i] *= old;
+#pragma unroll
+                for (int v = 0; v < N; ++v) {
+                    if (v0 + v >= n) break;
                     const float wt = __builtin_amdgcn_exp2f(ml[v][0] - ref);
-                    sum += wt * ml[v][1], acc += wt * x[v];
+                    sum += wt * ml[v][1];
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) acc[i] += wt * x[v][i];
                 }
                 top = t;
+            };
+            for (int v0 = 0; v0 < n; v0 += 8) {
+                if (n - v0 <= 2)
+                    add(std::integral_constant<int, 2>(), v0);
+                else
+                    add(std::integral_constant<int, 8>(), v0);
             }
+            const int f = f0 + r;
             if (whole) {
                 const size_t at = out_row(a, w, f);
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                out[at * HD + d] = (ST)(acc[0] * inv);
-                out[at * HD + d + 1] = (ST)(acc[1] * inv);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) {
+                    out[at * HD + d + 2 * LANES * i] = (ST)(acc[i][0] * inv);
+                    out[at * HD + d + 2 * LANES * i + 1] = (ST)(acc[i][1] * inv);
+                }
                 if (a.lse && d == 0) a.lse[at] = ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.6931471805599453f;
             } else {  // elements into the first part's place, which no other thread reads; weights apart, as all of a row's threads read them
-                hand_over2(a.part_o + row * HD + d, acc);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) hand_over2(a.part_o + row * HD + d + 2 * LANES * i, acc[i]);
                 if (d == 0) hand_over2(a.joined_ml + 2 * row, f32x2{top, sum});
             }
         }
         if (whole) return;
         counter = a.arrived_groups + slot0;
         part_ml = a.joined_ml;
-        first = slot0, stride = FAN_IN, n = groups;
+        first = slot0, stride = fan, n = groups;
     }
 }
 
