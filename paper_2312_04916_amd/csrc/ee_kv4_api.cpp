@@ -25,17 +25,32 @@ int check_config(const ee_kv4_config& c) {
     return EE_OK;
 }
 
-// How a launch of the attention is cut: workgroups of `waves` waves, in about `parts` parts of at least `min_chunks` chunks.
+// How a launch of the attention is cut: workgroups of `waves` waves, in about `parts` parts of at least `min_chunks` chunks; whole:
+// an item is cut into as many parts as it has whole shares of the work (else into one more, so that none is longer than a share).
 constexpr int MOST_PARTS = 768;
 struct Cut {
     int waves, parts, min_chunks;
+    bool whole;
 };
 int most_of_cut(int units) { return units * 16 == KV4_WIDE ? 256 : MOST_PARTS; }
 Cut cut_of(const ee_kv4_config& c, int n_seqs, int n_rows, int units) {
-    const int items = std::min(n_seqs, n_rows) * c.n_kv_heads;
-    if (units * 16 == KV4_WIDE) return {8, most_of_cut(units), 32};
-    if (units == 1 && items < 128) return {8, 256, 8};
-    return {4, most_of_cut(units), 8};
+    if (units * 16 == KV4_WIDE) return {8, most_of_cut(units), 32, true};
+    if (units == 1) {
+        // few items: one workgroup of eight waves per CU (one request of 131 071 positions, 8 kv heads: 32 us, with three of four
+        // waves 43; 4 of 8000: 12.0, 15.7); many are balanced better by the smaller ones (64 of up to 16 384: 115, with eight
+        // waves 151; 16 of up to 2048, 32 heads: 20, 24)
+        const int items = std::min(n_seqs, n_rows) * c.n_kv_heads;
+        if (items < 128) return {8, 256, 8, true};
+        return {4, MOST_PARTS, 8, false};
+    }
+    // Larger tiles leave as many times more to be joined, and a CU holds two workgroups.  So few items are cut into no more parts
+    // than there are CUs (40 rows at 4000 positions, 32 heads on 8: 17.6 us, with 512 parts 24.8, with 768 31), some into two per
+    // CU (18 requests of up to 3245: 28.5, with 256 parts 32, with 768 37.5), and many, which fill the chip uncut, so that the
+    // longest do not end last (61 requests of up to 16 380: 268, with 512 parts 345).
+    const int64_t items = ((int64_t)n_rows * (c.n_heads / c.n_kv_heads) / (16 * units) + std::min(n_seqs, n_rows)) * c.n_kv_heads;
+    if (items <= 128) return {4, 256, 8, true};
+    if (items <= 512) return {4, 512, 8, true};
+    return {4, MOST_PARTS, 8, false};
 }
 
 // A pool of more than half of the last-level cache (256 MB) is not found there again by the next step, which has read weights in
@@ -188,7 +203,7 @@ int ee_kv4_plan(ee_kv4* c, int n_seqs, const int32_t* dev_held, const int32_t* d
     p.tile_rows = 16 * units, p.tile_shift = __builtin_ctz((unsigned)p.tile_rows), p.kv_magic = magic_of((uint32_t)g.n_kv_heads);
     p.max_parts = (int)std::min(c->sl.max_parts, most_parts(g, n_seqs, n_rows, p.tile_rows));
     const Cut cut = cut_of(g, n_seqs, n_rows, units);
-    p.target_parts = cut.parts, p.min_chunks = cut.min_chunks, p.one_per_cu = cut.waves == 8;
+    p.target_parts = cut.parts, p.min_chunks = cut.min_chunks, p.whole_shares = cut.whole;
     // one thread per row and part, and for blocks that change hands, which only the GPU knows, an eighth of the pool; a small
     // step in one small workgroup
     const int threads = n_seqs < 256 && n_rows <= 1024 ? 256 : 1024;
