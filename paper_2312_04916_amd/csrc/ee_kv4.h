@@ -53,7 +53,7 @@ struct Kv4Plan {
     uint32_t kv_magic;                           // magic_of(kv_heads)
     int target_parts;  // a launch is cut so that it has about this many parts
     int min_chunks;    // of a part that is one of several
-    int whole_shares;  // an item is cut into as many parts as it has whole shares of the work, else into one more
+    int whole_shares;  // an item is cut into as many parts as it has shares of the work, else into one more
 };
 
 struct Kv4Cache {

@@ -26,7 +26,7 @@ int check_config(const ee_kv4_config& c) {
 }
 
 // How a launch of the attention is cut: workgroups of `waves` waves, in about `parts` parts of at least `min_chunks` chunks; whole:
-// an item is cut into as many parts as it has whole shares of the work (else into one more, so that none is longer than a share).
+// an item is cut into as many parts as it has shares of the work (else into one more, so that none is longer than a share).
 constexpr int MOST_PARTS = 768;
 struct Cut {
     int waves, parts, min_chunks;
