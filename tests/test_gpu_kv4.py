@@ -339,6 +339,21 @@ def test_long_contexts_are_cut_and_joined(dtype, heads, kvh, hd, rows):
     s.c.close()
 
 
+@pytest.mark.parametrize("dtype,heads,hd,rows", [("bf16", 8, 32, 1), ("bf16", 20, 64, 2), ("f32", 24, 32, 1)])
+@pytest.mark.parametrize("longest", [4400, 17003, 70001])
+def test_one_long_request_among_many_short_ones(dtype, heads, hd, rows, longest):
+    """About 17, 67 and 274 parts of one request: joined at once, in groups of 16 or fewer, in groups of 32."""
+    lengths = [3] * 64 + [longest] + [40] * 65
+    s = Requests(lengths, [rows] * 130, heads, 1, hd, dtype, 64, seed=21)
+    s.step()
+    first = s.c.attend(0, s.q, lse=True)
+    s.check(*first)
+    for _ in range(3):
+        again = s.c.attend(0, s.q, lse=True)
+        assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
+    s.c.close()
+
+
 def test_scale_and_strided_queries():
     for dtype, off in (("bf16", 0), ("bf16", 1), ("f32", 0), ("f32", 3)):
         s = Requests([50, 90], [2, 3], 6, 3, 64, dtype, 16, seed=5)
