@@ -623,6 +623,39 @@ __device__ __forceinline__ void sees_nothing(const Kv4Attend& a, const Kv4Part& 
     }
 }
 
+__device__ __forceinline__ void store_pair(float* p, f32x2 x) { *(f32x2*)p = x; }
+__device__ __forceinline__ void store_pair(__bf16* p, f32x2 x) { *(bf16x2*)p = __builtin_convertvector(x, bf16x2); }
+
+// What a thread has in a pass over a part's M rows: pairs of elements of one row, and where a part holds them.  Each store or load
+// of a wave is of whole lines, as what goes past the caches is not put together there.
+template <int HD, int THREADS, int M>
+struct PartPlace {
+    // rows one after the other, a thread's pairs LANES apart
+    static constexpr int PAIRS = M * HD / 2 >= 4 * THREADS ? 4 : M * HD / 2 >= 2 * THREADS ? 2 : 1, LANES = HD / 2 / PAIRS;
+    static constexpr int ROWS = THREADS / LANES, PASSES = (M + ROWS - 1) / ROWS;
+    int row, at;
+    __device__ __forceinline__ explicit PartPlace(int pass) : row(pass * ROWS + threadIdx.x / LANES), at(threadIdx.x % LANES * 2) {}
+    __device__ __forceinline__ bool first() const { return at == 0; }
+    __device__ __forceinline__ int element(int i) const { return at + 2 * LANES * i; }
+    __device__ __forceinline__ int held(int i) const { return row * HD + element(i); }
+};
+template <int HD>
+struct PartPlace<HD, 512, KV4_WIDE> {
+    // as the registers of the prompts' kernel hold them: [32 rows each of a wave][column of V within its half][pair][lane]
+    static constexpr int PAIRS = HD / 32, PASSES = 4;
+    int row, column, at;
+    __device__ __forceinline__ PartPlace(int wave, int i) {  // i: 8 of a lane's columns
+        const int lane = threadIdx.x & 63;
+        row = 32 * wave + (lane & 31);
+        column = 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
+        at = ((wave * 8 + i) * PAIRS * 64 + lane) * 2;
+    }
+    __device__ __forceinline__ explicit PartPlace(int pass) : PartPlace((threadIdx.x >> 6) & 3, (threadIdx.x >> 8) * 4 + pass) {}
+    __device__ __forceinline__ bool first() const { return column == 0; }
+    __device__ __forceinline__ int element(int b) const { return column * (HD / 16) + 2 * b; }
+    __device__ __forceinline__ int held(int b) const { return at + b * 128; }
+};
+
 // Parts are joined by the workgroup that leaves the last one, in their order; many of them in two levels: first each FAN_IN
 // neighbours by the last of those, into the first one's place, then these.  The parts go past the caches of this XCD (agent-scope
 // stores and loads).  Fences instead act on the whole of its L2: a release cost a launch of 1024 parts 300 us, and an acquire
@@ -648,11 +681,15 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
         __syncthreads();
         if ((int)*s_last != n - 1) return;
         const bool whole = level == 1 || !two_levels;
-        // a thread has PAIRS pairs of elements of a row, LANES apart, and asks for all of them of up to eight parts at once
-        constexpr int PAIRS = M * HD / 2 >= 4 * THREADS ? 4 : M * HD / 2 >= 2 * THREADS ? 2 : 1, LANES = HD / 2 / PAIRS;
-        const int d = threadIdx.x % LANES * 2;
-        for (int r = threadIdx.x / LANES; r < f_end - f0; r += THREADS / LANES) {
+        // a thread has PAIRS pairs of elements of a row and asks for all of them of up to eight parts at once
+        using Place = PartPlace<HD, THREADS, M>;
+        constexpr int PAIRS = Place::PAIRS;
+        for (int pass = 0; pass < Place::PASSES; ++pass) {
+            const Place here(pass);
+            const int r = here.row;
+            if (r >= f_end - f0) continue;
             const size_t row = (size_t)first * M + r, step = (size_t)stride * M;
+            const float* o = a.part_o + (size_t)first * (M * HD);
             float top = -INFINITY, sum = 0.f;
             f32x2 acc[PAIRS] = {};
             auto add = [&](auto at_once, int v0) {
@@ -660,10 +697,10 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
                 f32x2 ml[N], x[N][PAIRS];
 #pragma unroll
                 for (int v = 0; v < N; ++v) {
-                    const size_t at = row + step * min(v0 + v, n - 1);  // (no branch, so that no load waits for another one)
-                    ml[v] = handed2(part_ml + 2 * at);
+                    const size_t at = step * min(v0 + v, n - 1);  // (no branch, so that no load waits for another one)
+                    ml[v] = handed2(part_ml + 2 * (row + at));
 #pragma unroll
-                    for (int i = 0; i < PAIRS; ++i) x[v][i] = handed2(a.part_o + at * HD + d + 2 * LANES * i);
+                    for (int i = 0; i < PAIRS; ++i) x[v][i] = handed2(o + at * HD + here.held(i));
                 }
                 float t = top;
 #pragma unroll
@@ -694,15 +731,12 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
                 const size_t at = out_row(a, w, f);
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) {
-                    out[at * HD + d + 2 * LANES * i] = (ST)(acc[i][0] * inv);
-                    out[at * HD + d + 2 * LANES * i + 1] = (ST)(acc[i][1] * inv);
-                }
-                if (a.lse && d == 0) a.lse[at] = ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.6931471805599453f;
+                for (int i = 0; i < PAIRS; ++i) store_pair(out + at * HD + here.element(i), acc[i] * inv);
+                if (a.lse && here.first()) a.lse[at] = ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.6931471805599453f;
             } else {  // elements into the first part's place, which no other thread reads; weights apart, as all of a row's threads read them
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) hand_over2(a.part_o + row * HD + d + 2 * LANES * i, acc[i]);
-                if (d == 0) hand_over2(a.joined_ml + 2 * row, f32x2{top, sum});
+                for (int i = 0; i < PAIRS; ++i) hand_over2((float*)o + here.held(i), acc[i]);
+                if (here.first()) hand_over2(a.joined_ml + 2 * row, f32x2{top, sum});
             }
         }
         if (whole) return;
@@ -987,7 +1021,8 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
 
     // join the waves' shares, 16 entries at a time
     constexpr int EPT = 16 * HD >= 2 * NW * 64 ? 16 * HD / (NW * 64) : 2;  // elements per thread
-    const int my_row = threadIdx.x * EPT / HD, my_d = threadIdx.x * EPT % HD;
+    constexpr int TPR = HD / EPT;  // threads of a row, whose pairs of elements lie next to each other
+    const int my_row = threadIdx.x / TPR, my_d = threadIdx.x % TPR * 2;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
         if (f0 + 16 * u >= f_end) break;
@@ -1016,18 +1051,18 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
                 sum += wt * s_l[v * 16 + my_row];
                 // (a wave that saw nothing has weight zero and zeros)
 #pragma unroll
-                for (int e = 0; e < EPT; ++e) acc[e] += wt * s_o[(v * 16 + my_row) * LDO + my_d + e];
+                for (int e = 0; e < EPT; ++e) acc[e] += wt * s_o[(v * 16 + my_row) * LDO + my_d + (e >> 1) * (2 * TPR) + (e & 1)];
             }
             if (n_parts == 1) {
                 const size_t r = out_row(a, w, f);
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-                for (int e = 0; e < EPT; ++e) out[r * HD + my_d + e] = (ST)(acc[e] * inv);
+                for (int e = 0; e < EPT; e += 2) store_pair(out + r * HD + my_d + e * TPR, f32x2{acc[e] * inv, acc[e + 1] * inv});
                 if (a.lse && my_d == 0) a.lse[r] = (ref + log2f(sum)) * 0.6931471805599453f;
             } else {
                 const size_t r = (size_t)w.slot * M + 16 * u + my_row;
 #pragma unroll
-                for (int e = 0; e < EPT; e += 2) hand_over2(a.part_o + r * HD + my_d + e, f32x2{acc[e], acc[e + 1]});
+                for (int e = 0; e < EPT; e += 2) hand_over2(a.part_o + r * HD + my_d + e * TPR, f32x2{acc[e], acc[e + 1]});
                 if (my_d == 0) hand_over2(a.part_ml + 2 * r, f32x2{top, sum});
             }
         }
@@ -1304,7 +1339,8 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int c = 8 * (i >> 2) + 4 * half + (i & 3);  // column of V: elements c * EPC ...
+            const PartPlace<HD, 512, M> place(wave, i);
+            const int c = place.column;  // of V: elements c * EPC ...
             if (n_parts == 1) {
                 uint32_t x[EPC / 2];
 #pragma unroll
@@ -1314,7 +1350,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
                 if constexpr (EPC == 4) *(u32x2*)(out + r * HD + c * EPC) = u32x2{x[0], x[1]};
             } else {
 #pragma unroll
-                for (int b = 0; b < DB; ++b) hand_over2(a.part_o + at * HD + c * EPC + 2 * b, f32x2{o[b][i], o[b][8 + i]});
+                for (int b = 0; b < DB; ++b) hand_over2(a.part_o + (size_t)w.slot * (M * HD) + place.held(b), f32x2{o[b][i], o[b][8 + i]});
             }
         }
         if (half == 0) {
