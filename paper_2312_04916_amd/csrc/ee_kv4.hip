@@ -112,12 +112,16 @@ __device__ __forceinline__ int last_not_above(const int32_t* first, int n, int32
     return lo;
 }
 
+// Blocks of a request: before ceil(held / B), after ceil(end / B); which ones go where follows from three running sums over the
+// requests (given back, asked for, rows) and from which of them are served, which again is a running sum's comparison.
 // Every workgroup forms the sums over all requests for itself (a few thousand lengths at most: cheaper than handing them on)
-// and takes its share of what has to be written, one thread per row, block and part.  What a workgroup reads, no other one
+// and takes its share of what has to be written, one thread per row, block and part, which finds its request by a search in LDS.  What a workgroup reads, no other one
 // writes: a block that one request gives back and another one takes is looked up in the table row of the first, behind what it
 // keeps, which nothing changes; and held_next, which may be where the lengths are read, is written by the workgroup that is
-// the last to have read them.  All sums fit 32 bits: a request has at most
-// 2^16 blocks, and a thread's rows are counted up to n_rows + 1, at most 2^20 + 1.
+// the last to have read them.  All sums fit 32 bits: a request has at most 2^16 blocks, and a thread's rows are counted up to
+// n_rows + 1, at most 2^20 + 1.
+// Bound by latency: lengths, sums, search, table, store, one after the other.  16 requests with 38 rows 4.8 us, of which an empty
+// launch is 3.5; 1000 requests with 6 800 rows 7.9 us; 200 that bring prompts of up to 2048 rows 8.2 us for 2.3 MB.
 constexpr int SERVED = 1 << 30, BLOCKS = SERVED - 1;  // in s_had
 __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
     __shared__ int32_t s_row[PLAN_SEQS + 1];    // first row
@@ -358,11 +362,11 @@ __device__ __forceinline__ uint32_t rows4_umax(uint32_t v) {
 }
 
 // One wave per 16 rows of one head of K or of V, its lanes as the attention reads a tile: lane (quarter h, row t) has elements
-// 8h .. 8h+7 of every group.  So a group's largest magnitude is two lane swaps away, K of 16 rows that fill a tile is written as one
+// 8h .. 8h+7 of every group.  Per group: e least with max|x| <= 7 * 2^e, then the nearest level of x / 2^e.  So a group's largest magnitude is two lane swaps away, K of 16 rows that fill a tile is written as one
 // run of 1 KB (head_dim 128) and its scales as one of 64 bytes; the conversion is the hardware's, which rounds to nearest even
 // and saturates.  Rows that follow each other usually lie in one tile, whose lines so come from one workgroup: with the heads
-// of a row together instead, eight XCDs wrote parts of each line (79 us where this takes 49: 40 768 rows of 8 heads of 128 in
-// bf16, 211 MB, which a copy moves in 41).
+// of a row together instead, eight XCDs wrote parts of each line (79 us where this takes 50: 40 768 rows of 8 heads of 128 in
+// bf16, 211 MB, which a copy moves in 41).  Bound by HBM there, by the launch in a decode step (3.8 us).
 template <int HD, typename ST>
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Cache c, int n_rows, const ST* __restrict__ k, int64_t k_row, int64_t k_head,
                                                          const ST* __restrict__ v, int64_t v_row, int64_t v_head, int vec,
@@ -427,7 +431,9 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Cache c, int n_rows,
     }
 }
 
-// What a thread of the read-back has: 8 elements of 16 rows of one head of K (of V), then of the next, for the same lines' sake.
+// Read-back: level times 2^e, exact in fp32 and in bf16.  A thread has 8 elements of a group, whose codes are a word of K or
+// lie in one to four columns of V, and writes them as one run; a workgroup has 16 rows of one head of K (of V), then of the next, so that each line of the cache
+// is asked for by one XCD.  Bound by HBM: 36.4 us for the 211 MB that a copy moves in 41, four fifths of them written.
 struct Kv4Work {
     int e8, which, head;
     int64_t row;
@@ -746,7 +752,21 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
     }
 }
 
-// NT: bf16 terms of an element of Q (1: Q is bf16; 3: fp32, exactly), PT: of a probability.  UNITS: 16 entries each of a tile.
+// Attention of one part: up to 16 * UNITS entries (row, query head) of a kv head over a run of chunks of 32 positions, by NW waves
+// that take every NW-th chunk.  With s = scale * q.k in units of ln 2, running maximum m and weights 2^(s - m):
+//   l <- l 2^(m - m') + sum 2^(s - m'),   o <- o 2^(m - m') + sum 2^(s - m') v,   m' = max(m, s),   out = o / l.
+// o and l are rescaled only when some maximum has grown by more than a factor 2^8 of the weights, which leaves them in fp32's
+// range; m, l and o are fp32.  Shares are joined in the same way: waves through LDS, parts through join_parts.
+// Products are 16x16x32 bf16 with positions as rows of the first (S^T = K Q^T): its result then lies in the lanes that the second one
+// (O^T = V^T P^T) wants its probabilities in, if V's tile has its positions in that order, and nothing moves between lanes.  K and
+// V are exact in bf16.  NT: bf16 terms of an element of Q (1: Q is bf16; 3: fp32, exactly), PT: of a probability: three for the
+// fp32 model, two for the tiles of 16, which wait for memory anyway (error against 64 bits 0.0017, all of it the result's own
+// rounding to bf16), one for larger ones (0.0021), where the products cost time.  UNITS: 16 entries each of a tile.
+// Bound by HBM where contexts are long: 64 requests of up to 16 384 positions, 32 heads on 8 of 128 elements, 589 MB: 114 us, 5.2 TB/s
+// (a copy's rate is 5.15), every byte read once.  So what counts is what is on its way: of the tiles DEPTH steps ahead each load
+// is asked for as soon as its registers have been read.  One request of 131 071 positions: 32 us for 143 MB, 4.5 TB/s; of which
+// 4 us are its parts' joins.  16 requests of up to 2048 positions, 32 heads: 19 us for 69 MB, launch and last parts included.
+// A single user's 513 positions (6.7 us) are bound by the launch and the chain part, table, K, V, join.
 template <int HD, int NT, int PT, int UNITS, int NW, int DEPTH, bool PAST, typename ST>
 __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 : NT == 1 ? 4 : 3) void kv4_attend_kernel(Kv4Attend a) {
     constexpr int G = HD / 32, EPC = HD / 16, M = 16 * UNITS;
@@ -1074,8 +1094,12 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
 // each, into bf16 in LDS in operand order, while they work on these; so an element is converted once for 128 entries, and
 // 32 x 32 products halve what is read from LDS per operation.  One barrier per 32 positions, two buffers.  Two such groups of
 // waves take every other 32 positions, so that a SIMD has two waves, and join their sums through LDS at the end.
-// Bound by the vector units (soft-max: an exponential, a multiply-add, a maximum, a sum and a conversion per score) about as much
-// as by the matrix units.
+// One bf16 term of a probability (its sum is that of the probabilities before they are rounded: error against 64 bits 0.0023, of
+// which the result's rounding is 0.0017; a second term would be half as many products again).
+// 1024 rows at the end of 8192 positions, 32 heads on 8 of 128 elements, 129 GFLOP: 148 us, 870 TFLOP/s, where a large matrix product
+// reaches 1215.  The vector units' work (per score an exponential, a multiply-add, a maximum, a sum, half a conversion) takes about
+// as long as the products, and two waves of a SIMD overlap them in part; LDS is active a third of the time.  Three groups of
+// waves with Q in LDS: 151 us.
 template <int HD>
 __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     constexpr int M = KV4_WIDE, G = HD / 32, EPC = HD / 16, KS = HD / 16, DB = HD / 32, LB = HD / 8;
@@ -1439,7 +1463,9 @@ hipError_t read_hd(const Kv4Cache& c, int n_rows, const int64_t* slots, void* k,
 constexpr int64_t WIDE_ITEMS = 128;
 
 int kv4_tile_units(int dtype, int head_dim, int most_flat, int64_t all_flat) {
-    // wide tiles where they fill the chip
+    // Wide tiles where at least half of the CUs have one (150 of them, three requests at 2013 positions: 46 us, in tiles of 32 entries
+    // 57), as an element is converted once for 128 entries; fewer leave CUs idle or much to be joined (107 of them, two requests at
+    // 427: 11.3 us, wide 15.5).
     if (dtype == EE_BF16 && (head_dim == 64 || head_dim == 128) && most_flat > 32 && all_flat >= KV4_WIDE * WIDE_ITEMS) return KV4_WIDE / 16;
     const int most = dtype == EE_BF16 ? std::min(4, 256 / head_dim) : std::min(2, 256 / head_dim);  // what a wave's registers hold
     int units = 1;
