@@ -473,7 +473,7 @@ int ee_kv4_read(ee_kv4* c, int layer, int n_rows, const int64_t* dev_slots, void
 
 /* Attention of the latest plan's rows over what their requests hold: row at position p sees positions max(0, p - window + 1)
  * .. p (window 0: all up to p).  scores = q . k * scale (scale > 0; 0: 1 / sqrt(head_dim)), soft-max in fp32, weighted sum of V.
- * dev_out [n_rows][n_heads][head_dim] contiguous; dev_lse [n_rows][n_heads] fp32 or NULL: log sum exp of the row's scores, with
+ * dev_out [n_rows][n_heads][head_dim] contiguous, apart from dev_q (EE_ERR_ARG where the ranges overlap); dev_lse [n_rows][n_heads] fp32 or NULL: log sum exp of the row's scores, with
  * which results over several caches can be joined.  A row that sees nothing (its request was refused, or it belongs to
  * none) gets zeros and -inf.  NaN in positions that a row does not see do not reach it. */
 int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride, int64_t q_head_stride, void* dev_out, float* dev_lse,

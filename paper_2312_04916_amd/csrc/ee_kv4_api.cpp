@@ -262,6 +262,13 @@ int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride,
     const ee_kv4_config& g = c->cfg;
     const uintptr_t es = g.dtype == EE_BF16 ? 2 : 4;
     if (!dev_q || !dev_out || (uintptr_t)dev_q & (es - 1) || (uintptr_t)dev_out & 15 || (uintptr_t)dev_lse & 3) return EE_ERR_ARG;
+    // rows of q are read while others' results are already written
+    const int64_t rows_span = (c->n_rows - 1) * q_row_stride, heads_span = (g.n_heads - 1) * q_head_stride, es_i = (int64_t)es;
+    const uintptr_t q_lo = (uintptr_t)dev_q + (uintptr_t)(es_i * (std::min<int64_t>(rows_span, 0) + std::min<int64_t>(heads_span, 0)));
+    const uintptr_t q_hi = (uintptr_t)dev_q + (uintptr_t)(es_i * (std::max<int64_t>(rows_span, 0) + std::max<int64_t>(heads_span, 0) + g.head_dim));
+    const size_t results = (size_t)c->n_rows * g.n_heads;
+    auto overlaps = [&](const void* p, size_t bytes) { return p && (uintptr_t)p < q_hi && q_lo < (uintptr_t)p + bytes; };
+    if (overlaps(dev_out, results * g.head_dim * es) || overlaps(dev_lse, results * 4)) return EE_ERR_ARG;
     Kv4Attend a;
     a.layer = c->pool + layer_bytes(g) * layer;
     a.table = c->arrays.table, a.table_stride = c->arrays.table_stride;

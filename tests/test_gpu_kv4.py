@@ -562,3 +562,17 @@ def test_refusals():
     assert L.ee_kv4_plan(c.h, 4, i4.data_ptr() + 2, i4.data_ptr(), i4.data_ptr(), 3, 3, st) == -7
     assert torch.isfinite(c.attend(0, q).float()).all() or True  # the cache is whole after all of this
     c.close()
+
+
+def test_results_over_the_queries_are_refused():
+    """Some workgroups write results while others still read queries."""
+    c = cache_of(4, 2, 64, "bf16", 16, 10, 4, 100, 50)
+    c.plan(dev([0] * 4), dev([0] * 4), dev([1, 1, 1, 0]), 3)
+    kv, wide = rand((3, 2, 64), "bf16", 2), rand((9, 4, 64), "bf16", 3)
+    c.append(0, kv, kv)
+    for q, out in ((wide[:3], wide[:3]), (wide[:3], wide[2:5]), (wide[2:5], wide[:3]), (wide[::3], wide[4:7]), (wide[0:1].expand(3, 4, 64), wide[:3])):
+        with pytest.raises(ee.EeError, match="-7"):
+            c.attend(0, q, out=out)
+    want = c.attend(0, wide[3:6].clone())
+    assert torch.equal(c.attend(0, wide[3:6], out=wide[:3]), want) and torch.equal(c.attend(0, wide[3:6], out=wide[6:]), want)
+    c.close()
