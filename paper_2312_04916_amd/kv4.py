@@ -11,9 +11,17 @@ from .binding import EE_BF16, EE_F32, _chk, ee_kv4_arrays, ee_kv4_config, lib
 _DTYPES = {EE_BF16: torch.bfloat16, EE_F32: torch.float32}
 _CODES = {torch.bfloat16: EE_BF16, torch.float32: EE_F32, "bf16": EE_BF16, "f32": EE_F32, EE_BF16: EE_BF16, EE_F32: EE_F32}
 
+_LEAST_SCALE = 2.0 ** -149  # of fp32: less would be passed as 0, which stands for the default
+
 
 def _raw_stream(stream, index: int) -> int:
     return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+
+
+def _used_on(stream, *tensors) -> None:
+    """Memory of the tensors is not given out again before what `stream` has been told to do with them is done."""
+    for t in tensors:
+        t.record_stream(stream)
 
 
 class Kv4Cache:
@@ -21,7 +29,10 @@ class Kv4Cache:
 
     Arrays of the latest plan, on the device, always at the same place: slots, positions, row_seq [max_rows], row_start
     [max_seqs + 1], served, held_next [max_seqs], n_free [1]; table [max_seqs][blocks] and free [n_blocks] are the state that
-    outlasts it."""
+    outlasts it.
+
+    Calls run on torch's current stream, or on `stream`; there the caller orders them after what wrote their inputs, and what reads
+    their results after them."""
 
     def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, block_tokens: int, n_blocks: int, max_seqs: int,
                  max_positions: int, max_rows: int, dtype="bf16", device="cuda:0", stream=None):
@@ -36,8 +47,8 @@ class Kv4Cache:
         if self.device.index is None:
             self.device = torch.device(self.device.type, torch.cuda.current_device())
         self._index = self.device.index
-        self.pool = torch.empty(pb.value, dtype=torch.uint8, device=self.device)
-        self.state = torch.empty(sb.value, dtype=torch.uint8, device=self.device)
+        self.pool = self._empty(stream, pb.value, dtype=torch.uint8)
+        self.state = self._empty(stream, sb.value, dtype=torch.uint8)
         _chk(lib().ee_kv4_create(C.byref(cfg), self.pool.data_ptr(), pb.value, self.state.data_ptr(), sb.value, _raw_stream(stream, self._index),
                                  C.byref(self.h)), "ee_kv4_create")
         a = ee_kv4_arrays()
@@ -61,6 +72,14 @@ class Kv4Cache:
         self._heads, self._kv_heads, self._head_dim = n_heads, n_kv_heads, head_dim
         L = lib()
         self._plan, self._append, self._read, self._attend = L.ee_kv4_plan, L.ee_kv4_append, L.ee_kv4_read, L.ee_kv4_attend
+
+    def _empty(self, stream, *shape, dtype) -> torch.Tensor:
+        if stream is None:
+            return torch.empty(*shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(stream):
+            t = torch.empty(*shape, dtype=dtype, device=self.device)
+        _used_on(torch.cuda.current_stream(self.device), t)  # where the caller will want it
+        return t
 
     def _lengths(self, t: torch.Tensor, n: int, what: str) -> int:
         if t.dtype is not torch.int32 or t.get_device() != self._index or t.shape != (n,) or not t.is_contiguous():
@@ -86,6 +105,8 @@ class Kv4Cache:
                           n_rows if max_rows_per_seq is None else max_rows_per_seq, _raw_stream(stream, self._index))
         if code:
             _chk(code, "ee_kv4_plan")
+        if stream is not None:
+            _used_on(stream, held, start, end)
         self.n_rows = n_rows
 
     def _slot_ptr(self, slots: torch.Tensor, rows: int) -> int:
@@ -103,35 +124,41 @@ class Kv4Cache:
                             _raw_stream(stream, self._index))
         if code:
             _chk(code, "ee_kv4_append")
+        if stream is not None:
+            _used_on(stream, k, v, *(() if slots is None else (slots,)))
 
     def read(self, layer: int, slots: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """ee_kv4_read -> k, v [rows][n_kv_heads][head_dim]: the values that the slots hold."""
         rows = slots.shape[0]
         p = self._slot_ptr(slots, rows)
-        k = torch.empty(rows, self._kv_heads, self._head_dim, dtype=self.dtype, device=self.device)
-        v = torch.empty_like(k)
+        k = self._empty(stream, rows, self._kv_heads, self._head_dim, dtype=self.dtype)
+        v = self._empty(stream, rows, self._kv_heads, self._head_dim, dtype=self.dtype)
         code = self._read(self.h, layer, rows, p, k.data_ptr(), v.data_ptr(), _raw_stream(stream, self._index))
         if code:
             _chk(code, "ee_kv4_read")
+        if stream is not None:
+            _used_on(stream, slots)
         return k, v
 
     def attend(self, layer: int, q: torch.Tensor, scale: Optional[float] = None, window: int = 0, lse: bool = False,
                out: Optional[torch.Tensor] = None, stream=None):
         """ee_kv4_attend -> [rows][n_heads][head_dim], with lse=True also log sum exp [rows][n_heads].  q: the rows of the latest
         plan, any strides of rows and heads; scale: 1 / sqrt(head_dim) where not given."""
-        if scale is not None and not scale > 0:
-            raise ValueError("scale: positive")
+        if scale is not None and not scale >= _LEAST_SCALE:
+            raise ValueError("scale: positive, in fp32")
         heads, hd = self._heads, self._head_dim
         qp, qr, qh = self._vectors(q, heads, self.n_rows, "q")
         if out is None:
-            out = torch.empty(self.n_rows, heads, hd, dtype=self.dtype, device=self.device)
+            out = self._empty(stream, self.n_rows, heads, hd, dtype=self.dtype)
         elif out.dtype != self.dtype or out.device != self.device or out.shape != (self.n_rows, heads, hd) or not out.is_contiguous():
             raise ValueError(f"out: {self.dtype} [{self.n_rows}][{heads}][{hd}] on {self.device}, contiguous")
-        s = torch.empty(self.n_rows, heads, dtype=torch.float32, device=self.device) if lse else None
+        s = self._empty(stream, self.n_rows, heads, dtype=torch.float32) if lse else None
         code = self._attend(self.h, layer, qp, qr, qh, out.data_ptr(), s.data_ptr() if lse else None, scale or 0.0, window,
                             _raw_stream(stream, self._index))
         if code:
             _chk(code, "ee_kv4_attend")
+        if stream is not None:
+            _used_on(stream, q, out)
         return (out, s) if lse else out
 
     def close(self) -> None:

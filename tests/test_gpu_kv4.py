@@ -576,3 +576,44 @@ def test_results_over_the_queries_are_refused():
     want = c.attend(0, wide[3:6].clone())
     assert torch.equal(c.attend(0, wide[3:6], out=wide[:3]), want) and torch.equal(c.attend(0, wide[3:6], out=wide[6:]), want)
     c.close()
+
+
+def test_scales_that_fp32_does_not_hold_are_refused():
+    s = Requests([40], [2], 4, 2, 64, "bf16", 16, seed=22)
+    s.step()
+    for bad in (1e-50, 2.0 ** -150):  # would be taken for 0, which stands for the default
+        with pytest.raises(ValueError, match="scale"):
+            s.c.attend(0, s.q, scale=bad)
+    with pytest.raises(ee.EeError, match="-7"):
+        s.c.attend(0, s.q, scale=1e39)
+    out, lse = s.c.attend(0, s.q, scale=2.0 ** -149, lse=True)
+    s.check(out, lse, scale=2.0 ** -149)
+    s.c.close()
+
+
+def test_memory_of_a_call_on_another_stream_is_not_given_out_early():
+    """Inputs that are dropped and results that are allocated while the other stream has still to run the call."""
+    s = Requests([300, 90], [2, 3], 8, 2, 128, "bf16", 16, seed=23)
+    s.step()
+    want, want_lse = s.c.attend(0, s.q, lse=True)
+    want_k, want_v = s.c.read(0, s.c.slots[:5])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(5):
+        q, slots = s.q.clone(), s.c.slots[:5].clone()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            busy = torch.zeros(1 << 26, device="cuda:0")
+            for _ in range(20):
+                busy.add_(1)
+        out, lse = s.c.attend(0, q, lse=True, stream=side)
+        k, v = s.c.read(0, slots, stream=side)
+        at = q.data_ptr(), slots.data_ptr()
+        del q, slots
+        for _ in range(8):  # would take the memory of what was dropped, were it free, and of results, had they come from this stream's
+            again = torch.full_like(s.q, float("nan"))
+            other = torch.full((5,), -1, dtype=torch.int64, device="cuda:0")
+            assert again.data_ptr() != at[0] and other.data_ptr() != at[1]
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse) and torch.equal(k, want_k) and torch.equal(v, want_v)
+    s.c.close()
