@@ -1391,10 +1391,12 @@ template <int HD, int UNITS, int NW>
 hipError_t attend_waves(const Kv4Attend& a, int dtype, int grid, hipStream_t s) {
     // (tiles of more than 16 entries: a request has several, which read the same K and V)
     const bool past = UNITS == 1 && a.past_caches;
-    constexpr int DEPTH = NW == 8 && HD <= 128 ? 2 : 1;
+    // Two steps ahead where registers allow it at the same number of waves: 8 waves alone on a CU, and bf16 tiles of 32 entries (17
+    // requests of up to 12 560 positions and 15 rows: 64 us, one step ahead 66; 3 rows at 84 869: 26.4, 28.3).
+    constexpr int DEPTH = NW == 8 && HD <= 128 ? 2 : 1, DEPTH_BF16 = UNITS == 2 && HD <= 128 ? 2 : DEPTH;
     if (dtype == EE_BF16)
-        EE_LAUNCH((past ? kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, DEPTH, UNITS == 1, __bf16>
-                        : kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, DEPTH, false, __bf16>),
+        EE_LAUNCH((past ? kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, DEPTH_BF16, UNITS == 1, __bf16>
+                        : kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, DEPTH_BF16, false, __bf16>),
                   dim3(grid), dim3(NW * 64), s, a);
     else if constexpr (UNITS <= 2)
         EE_LAUNCH((past ? kv4_attend_kernel<HD, 3, 3, UNITS, NW, DEPTH, UNITS == 1, float> : kv4_attend_kernel<HD, 3, 3, UNITS, NW, DEPTH, false, float>), dim3(grid),
