@@ -88,9 +88,10 @@ struct Kv4Attend {
 constexpr int KV4_WIDE = 128;  // entries of the tiles of prompts
 constexpr int KV4_CHUNK = 32;  // positions: what a wave works on at a time, and the grain of the parts
 
-// Entries of a tile in units of 16 (the columns of a matrix instruction), by the most that a request has for one kv head and by
-// all of the step's (rows x query heads).
-int kv4_tile_units(int dtype, int head_dim, int most_flat, int64_t all_flat);
+// Entries of a tile in units of 16 (the columns of a matrix instruction), by the most that a request has for one kv head, and by
+// what all requests may have for one.
+int kv4_tile_units(int dtype, int head_dim, int most_flat, int n_seqs, int64_t all_flat, int kv_heads);
+bool kv4_has_wide_tiles(int dtype, int head_dim);
 
 hipError_t launch_kv4_init(int32_t* table, int64_t n_table, int32_t* free_blocks, int n_blocks, uint32_t* arrived, int n_arrived,
                            uint32_t* counts, hipStream_t s);

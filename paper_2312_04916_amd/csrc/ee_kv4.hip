@@ -761,7 +761,7 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
 // (O^T = V^T P^T) wants its probabilities in, if V's tile has its positions in that order, and nothing moves between lanes.  K and
 // V are exact in bf16.  NT: bf16 terms of an element of Q (1: Q is bf16; 3: fp32, exactly), PT: of a probability: three for the
 // fp32 model, two for the tiles of 16, which wait for memory anyway (error against 64 bits 0.0017, all of it the result's own
-// rounding to bf16), one for larger ones (0.0021), where the products cost time.  UNITS: 16 entries each of a tile.
+// rounding to bf16), one for larger ones (0.0023), where the products cost time.  UNITS: 16 entries each of a tile.
 // Bound by HBM where contexts are long: 64 requests of up to 16 384 positions, 32 heads on 8 of 128 elements, 589 MB: 114 us, 5.2 TB/s
 // (a copy's rate is 5.15), every byte read once.  So what counts is what is on its way: of the tiles DEPTH steps ahead each load
 // is asked for as soon as its registers have been read.  One request of 131 071 positions: 32 us for 143 MB, 4.5 TB/s; of which
@@ -966,15 +966,12 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
                     f32x2 p;
                     p[0] = __builtin_amdgcn_exp2f(fmaf(s[u][t][i], a.scale_log2, -ref));
                     p[1] = __builtin_amdgcn_exp2f(fmaf(s[u][t][i + 1], a.scale_log2, -ref));
-                    // (with one term the sum is that of the rounded probabilities, so that the weights add up to one)
-                    if (PT > 1) l[u] += p[0] + p[1];
+                    l[u] += p[0] + p[1];  // (before they are rounded: the log-sum-exp keeps fp32's accuracy)
 #pragma unroll
                     for (int n = 0; n < PT; ++n) {
                         const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
                         pf[u][n][t * 2 + (i >> 1)] = h;
-                        const float h0 = __uint_as_float(h << 16), h1 = __uint_as_float(h & 0xffff0000u);
-                        if (PT == 1) l[u] += h0 + h1;
-                        if (n + 1 < PT) p[0] -= h0, p[1] -= h1;
+                        if (n + 1 < PT) p[0] -= __uint_as_float(h << 16), p[1] -= __uint_as_float(h & 0xffff0000u);
                     }
                 }
         }
@@ -1100,9 +1097,8 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
 // reaches 1215.  The vector units' work (per score an exponential, a multiply-add, a maximum, a sum, half a conversion) takes about
 // as long as the products, and two waves of a SIMD overlap them in part; LDS is active a third of the time.  Three groups of
 // waves with Q in LDS: 151 us.
-template <int HD>
 __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
-    constexpr int M = KV4_WIDE, G = HD / 32, EPC = HD / 16, KS = HD / 16, DB = HD / 32, LB = HD / 8;
+    constexpr int HD = 128, M = KV4_WIDE, G = HD / 32, EPC = HD / 16, KS = HD / 16, DB = HD / 32, LB = HD / 8;
     __shared__ u32x4 s_operands[2][2][(KS + 2 * DB) * 64];  // K, V of each group's two steps; at the end the second group's sums
     __shared__ float s_ml[2][256];
     __shared__ uint32_t s_scales_of[2][2][2][G * 4];  // of V, if some entry does not see all of the positions
@@ -1370,8 +1366,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
 #pragma unroll
                 for (int b = 0; b < DB; ++b)
                     x[b] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{o[b][i] * inv, o[b][8 + i] * inv}, bf16x2));
-                if constexpr (EPC == 8) *(u32x4*)(out + r * HD + c * EPC) = u32x4{x[0], x[1], x[2], x[3]};
-                if constexpr (EPC == 4) *(u32x2*)(out + r * HD + c * EPC) = u32x2{x[0], x[1]};
+                *(u32x4*)(out + r * HD + c * EPC) = u32x4{x[0], x[1], x[2], x[3]};
             } else {
 #pragma unroll
                 for (int b = 0; b < DB; ++b) hand_over2(a.part_o + (size_t)w.slot * (M * HD) + place.held(b), f32x2{o[b][i], o[b][8 + i]});
@@ -1418,9 +1413,9 @@ hipError_t attend_hd(const Kv4Attend& a, int dtype, int units, int waves, int gr
     if (units == 1) return attend_units<HD, 1>(a, dtype, waves, grid, s);
     if constexpr (HD <= 128)
         if (units == 2) return attend_units<HD, 2>(a, dtype, waves, grid, s);
-    if constexpr (HD == 64 || HD == 128) {
+    if constexpr (HD == 128) {
         if (units == KV4_WIDE / 16 && dtype == EE_BF16) {
-            EE_LAUNCH((kv4_attend_wide_kernel<HD>), dim3(grid), dim3(512), s, a);
+            EE_LAUNCH(kv4_attend_wide_kernel, dim3(grid), dim3(512), s, a);
             return hipGetLastError();
         }
     }
@@ -1462,13 +1457,21 @@ hipError_t read_hd(const Kv4Cache& c, int n_rows, const int64_t* slots, void* k,
 
 }  // namespace
 
-constexpr int64_t WIDE_ITEMS = 128;
+constexpr int64_t WIDE_ITEMS = 160;
 
-int kv4_tile_units(int dtype, int head_dim, int most_flat, int64_t all_flat) {
-    // Wide tiles where at least half of the CUs have one (150 of them, three requests at 2013 positions: 46 us, in tiles of 32 entries
-    // 57), as an element is converted once for 128 entries; fewer leave CUs idle or much to be joined (107 of them, two requests at
-    // 427: 11.3 us, wide 15.5).
-    if (dtype == EE_BF16 && (head_dim == 64 || head_dim == 128) && most_flat > 32 && all_flat >= KV4_WIDE * WIDE_ITEMS) return KV4_WIDE / 16;
+bool kv4_has_wide_tiles(int dtype, int head_dim) { return dtype == EE_BF16 && head_dim == 128; }
+
+int kv4_tile_units(int dtype, int head_dim, int most_flat, int n_seqs, int64_t all_flat, int kv_heads) {
+    // Wide tiles, in which an element is converted once for 128 entries, where they give more than half of the CUs work (130 of them,
+    // one request at 4000 positions: 85 us, in tiles of 32 entries 72; 225 of them: 77 and 88) and where not an eighth of them
+    // stays empty (24 requests of 88 entries: 99 and 76; of 132, which take two tiles: 167 and 127; of 128: 98 and 101).  Requests that
+    // do not all bring the most waste half a tile each on the average.  With 64 elements a wave holds 64 entries itself, and those
+    // tiles are as good or better (20 heads on 4, 4000 rows: 80 us, wide 91).
+    if (kv4_has_wide_tiles(dtype, head_dim) && all_flat * kv_heads >= KV4_WIDE * WIDE_ITEMS) {
+        const bool alike = (int64_t)n_seqs * most_flat <= all_flat;
+        const int64_t empty = (int64_t)n_seqs * (alike ? (KV4_WIDE - most_flat % KV4_WIDE) % KV4_WIDE : KV4_WIDE / 2);
+        if (empty * 8 <= all_flat) return KV4_WIDE / 16;
+    }
     const int most = dtype == EE_BF16 ? std::min(4, 256 / head_dim) : std::min(2, 256 / head_dim);  // what a wave's registers hold
     int units = 1;
     while (units < most && 16 * units < most_flat) units *= 2;

@@ -98,12 +98,10 @@ StateLayout state_layout(const ee_kv4_config& c) {
     w.parts = take((size_t)w.max_parts * sizeof(Kv4Part));
     w.max_slots = 2 * MOST_PARTS + 64;
     w.arrived = take((size_t)w.max_slots * 8);  // of groups of parts, of items
-    w.part_rows = 0;
-    const int64_t most_flat = (int64_t)c.max_rows * (c.n_heads / c.n_kv_heads);
-    for (int flat = 16; flat < 512; flat *= 2) {
-        const int units = kv4_tile_units(c.dtype, c.head_dim, (int)std::min<int64_t>(flat, most_flat), (int64_t)c.max_rows * c.n_heads);
-        w.part_rows = std::max(w.part_rows, (2 * most_of_cut(units) + 64) * 16 * units);
-    }
+    // (of the largest tiles of one wave, or of wide ones)
+    const int units = kv4_tile_units(c.dtype, c.head_dim, 64, 1, 0, c.n_kv_heads);
+    w.part_rows = (2 * most_of_cut(units) + 64) * 16 * units;
+    if (kv4_has_wide_tiles(c.dtype, c.head_dim)) w.part_rows = std::max(w.part_rows, (2 * most_of_cut(KV4_WIDE / 16) + 64) * KV4_WIDE);
     w.part_ml = take((size_t)w.part_rows * 16);  // of parts, of joined ones
     w.part_o = take((size_t)w.part_rows * c.head_dim * 4);
     w.total = off;
@@ -200,7 +198,8 @@ int ee_kv4_plan(ee_kv4* c, int n_seqs, const int32_t* dev_held, const int32_t* d
     p.n_parts = c->arrays.n_free + 1;
     p.arrived = (uint32_t*)c->arrays.n_free + 2;
     p.group = group, p.kv_heads = g.n_kv_heads;
-    const int units = kv4_tile_units(g.dtype, g.head_dim, (int)std::min<int64_t>((int64_t)most * group, 1 << 30), (int64_t)n_rows * g.n_heads);
+    const int units = kv4_tile_units(g.dtype, g.head_dim, (int)std::min<int64_t>((int64_t)most * group, 1 << 30), n_seqs, (int64_t)n_rows * group,
+                                     g.n_kv_heads);
     p.tile_rows = 16 * units, p.tile_shift = __builtin_ctz((unsigned)p.tile_rows), p.kv_magic = magic_of((uint32_t)g.n_kv_heads);
     p.max_parts = (int)std::min(c->sl.max_parts, most_parts(g, n_seqs, n_rows, p.tile_rows));
     const Cut cut = cut_of(g, n_seqs, n_rows, units);

@@ -617,3 +617,45 @@ def test_memory_of_a_call_on_another_stream_is_not_given_out_early():
         torch.cuda.current_stream().wait_stream(side)
         assert torch.equal(out, want) and torch.equal(lse, want_lse) and torch.equal(k, want_k) and torch.equal(v, want_v)
     s.c.close()
+
+
+# The tiles of 128 entries are chosen from 160 of them on, with 128 elements in bf16, if few of their entries stay empty.
+
+@pytest.mark.parametrize("window", [0, 300])
+def test_long_contexts_of_wide_tiles_are_cut_and_joined(window):
+    s = Requests([9001, 400, 400], [64, 300, 300], 64, 2, 128, "bf16", 32, seed=24)
+    s.step()
+    first = s.c.attend(0, s.q, window=window, lse=True)
+    s.check(*first, window=window)
+    for _ in range(3):
+        again = s.c.attend(0, s.q, window=window, lse=True)
+        assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
+    s.c.close()
+
+
+def test_wide_tiles_of_a_prompt_from_its_start():
+    s = Requests([650, 3], [650, 0], 32, 8, 128, "bf16", 64, seed=25)
+    s.step()
+    for window in (0, 1, 150):
+        s.check(*s.c.attend(0, s.q, window=window, lse=True), window=window)
+    s.c.close()
+
+
+def test_nan_in_wide_tiles():
+    test_nan_reaches_the_rows_that_see_it_and_no_other("bf16", 128, 130, 160)
+
+
+def test_wide_tiles_beyond_32_bits():
+    test_offsets_beyond_32_bits(320, 64)
+
+
+@pytest.mark.parametrize("heads,kvh,hd,rows", [(32, 8, 128, 20), (32, 8, 128, 33), (20, 4, 64, 40), (12, 12, 64, 150)])
+def test_batches_whose_wide_tiles_would_be_half_empty(heads, kvh, hd, rows):
+    s = Requests([200 + 37 * i for i in range(24)], [rows] * 24, heads, kvh, hd, "bf16", 32, seed=26)
+    s.step()
+    out, lse = s.c.attend(0, s.q, lse=True)
+    s.check(out, lse)
+    s.step(most=10 ** 6)  # the same where the caller does not say how many rows a request brings
+    out, lse = s.c.attend(0, s.q, lse=True)
+    s.check(out, lse)
+    s.c.close()
