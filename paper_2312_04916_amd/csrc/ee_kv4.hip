@@ -202,9 +202,9 @@ __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
     work = wave_sum(lane < nt >> 6 ? s_work[lane] : 0.f);
     taken = lanes_max(lane < nt >> 6 ? s_taken[lane] : 0);
     // chunks of a part: an even share of the work.  Where the parts all run at once, more of them would run after the others have
-    // ended: an item is cut into as many parts as it has shares, three quarters of one counting (39 requests of up to 15 570
-    // positions: 170 us, with whole shares only, and parts of nearly two, 202; halves counting too, 183, and even batches 20 %
-    // slower).  Else into one more, so that none is longer than a share.
+    // ended: an item is cut into as many parts as it has shares, three quarters of one counting (17 requests of up to 12 560
+    // positions and 15 rows: 61 us; with whole shares only, and parts of nearly two, 69; with halves counting too, 67, and 175 rows
+    // of one request 19.8 for 16.5).  Else into one more, so that none is longer than a share.
     const int per_part = max(p.min_chunks, (int)fminf(65536.f, ceilf(work * (float)p.kv_heads / (float)p.target_parts)));
     const int round_up = p.whole_shares ? per_part / 4 : per_part - 1;
 
@@ -1387,7 +1387,7 @@ hipError_t attend_waves(const Kv4Attend& a, int dtype, int grid, hipStream_t s) 
     // (tiles of more than 16 entries: a request has several, which read the same K and V)
     const bool past = UNITS == 1 && a.past_caches;
     // Two steps ahead where registers allow it at the same number of waves: 8 waves alone on a CU, and bf16 tiles of 32 entries (17
-    // requests of up to 12 560 positions and 15 rows: 64 us, one step ahead 66; 3 rows at 84 869: 26.4, 28.3).
+    // requests of up to 12 560 positions and 15 rows: 59 us, one step ahead 62; 64 of up to 16 384 and 5 rows: 128, 142).
     constexpr int DEPTH = NW == 8 && HD <= 128 ? 2 : 1, DEPTH_BF16 = UNITS == 2 && HD <= 128 ? 2 : DEPTH;
     if (dtype == EE_BF16)
         EE_LAUNCH((past ? kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, DEPTH_BF16, UNITS == 1, __bf16>
