@@ -81,7 +81,8 @@ struct Kv4Attend {
     int past_caches;  // K and V are read without keeping them in the caches
     int q_vec;        // rows of q can be read 16 bytes at a time
     float* part_o;    // [slot][tile rows][head_dim]
-    float *part_ml, *joined_ml;  // [slot][tile rows][2]: of parts; of groups of parts, at the first one's slot
+    float *part_ml, *joined_ml;  // [slot][tile rows][2]: reference and sum; of parts; of groups of parts, at the first one's slot
+    float *part_l, *joined_l;    // [slot][tile rows]: sums for the log-sum-exp, where they are apart
     uint32_t *arrived, *arrived_groups;  // [slot] of the first part of a group, of an item: parts, groups that have been left
 };
 

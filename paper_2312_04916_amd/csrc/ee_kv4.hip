@@ -601,6 +601,19 @@ __device__ __forceinline__ void hand_over2(float* p, f32x2 v) {
 __device__ __forceinline__ f32x2 handed2(const float* p) {
     return __builtin_bit_cast(f32x2, __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
+__device__ __forceinline__ void hand_over1(float* p, float v) {
+    __hip_atomic_store((uint32_t*)p, __float_as_uint(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float handed1(const float* p) {
+    return __uint_as_float(__hip_atomic_load((const uint32_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// l + both of a pair of bf16, in one instruction (fp32, within one unit in the last place of the sum)
+__device__ __forceinline__ float add_pair(uint32_t pair, float l) {
+    const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), one, l, false);
+}
+
 // parts that are joined at a time: all, or of many about their number's square root
 __device__ __forceinline__ int fan_shift_of(int n_parts) { return n_parts <= 16 ? 4 : n_parts <= 64 ? 3 : n_parts <= 256 ? 4 : 5; }
 
@@ -666,7 +679,8 @@ struct PartPlace<HD, 512, KV4_WIDE> {
 // neighbours by the last of those, into the first one's place, then these.  The parts go past the caches of this XCD (agent-scope
 // stores and loads).  Fences instead act on the whole of its L2: a release cost a launch of 1024 parts 300 us, and an acquire
 // by the workgroups that join alone made a ragged batch's 20 us 37.
-template <int HD, int THREADS, int M, typename ST>
+// APART: the log-sum-exp's sums come apart from the results' (see below).
+template <int HD, int THREADS, int M, bool APART, typename ST>
 __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w, int n_parts, int f0, int f_end, uint32_t* s_last) {
     const int part = w.part_of & 0xffff, slot0 = w.slot - part;
     const int fan_shift = fan_shift_of(n_parts), fan = 1 << fan_shift;
@@ -675,7 +689,7 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
     const bool two_levels = groups > 1;
     int first = slot0 + group0, stride = 1, n = min(fan, n_parts - group0);
     uint32_t* counter = a.arrived + first;
-    const float* part_ml = a.part_ml;
+    const float *part_ml = a.part_ml, *part_l = a.part_l;
     for (int level = 0;; ++level) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // each thread's stores have arrived before its workgroup is counted
         __syncthreads();
@@ -696,15 +710,17 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
             if (r >= f_end - f0) continue;
             const size_t row = (size_t)first * M + r, step = (size_t)stride * M;
             const float* o = a.part_o + (size_t)first * (M * HD);
-            float top = -INFINITY, sum = 0.f;
+            float top = -INFINITY, sum = 0.f, sum_lse = 0.f;
             f32x2 acc[PAIRS] = {};
             auto add = [&](auto at_once, int v0) {
                 constexpr int N = decltype(at_once)::value;
                 f32x2 ml[N], x[N][PAIRS];
+                float lse[APART ? N : 1];
 #pragma unroll
                 for (int v = 0; v < N; ++v) {
                     const size_t at = step * min(v0 + v, n - 1);  // (no branch, so that no load waits for another one)
                     ml[v] = handed2(part_ml + 2 * (row + at));
+                    if constexpr (APART) lse[v] = handed1(part_l + row + at);
 #pragma unroll
                     for (int i = 0; i < PAIRS; ++i) x[v][i] = handed2(o + at * HD + here.held(i));
                 }
@@ -714,6 +730,7 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
                 const float ref = t == -INFINITY ? 0.f : t;
                 const float old = __builtin_amdgcn_exp2f(top - ref);
                 sum *= old;
+                if constexpr (APART) sum_lse *= old;
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) acc[i] *= old;
 #pragma unroll
@@ -721,6 +738,7 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
                     if (v0 + v >= n) break;
                     const float wt = __builtin_amdgcn_exp2f(ml[v][0] - ref);
                     sum += wt * ml[v][1];
+                    if constexpr (APART) sum_lse += wt * lse[v];
 #pragma unroll
                     for (int i = 0; i < PAIRS; ++i) acc[i] += wt * x[v][i];
                 }
@@ -738,16 +756,19 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) store_pair(out + at * HD + here.element(i), acc[i] * inv);
-                if (a.lse && here.first()) a.lse[at] = ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.6931471805599453f;
+                if (a.lse && here.first()) a.lse[at] = ((top == -INFINITY ? 0.f : top) + log2f(APART ? sum_lse : sum)) * 0.6931471805599453f;
             } else {  // elements into the first part's place, which no other thread reads; weights apart, as all of a row's threads read them
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) hand_over2((float*)o + here.held(i), acc[i]);
-                if (here.first()) hand_over2(a.joined_ml + 2 * row, f32x2{top, sum});
+                if (here.first()) {
+                    hand_over2(a.joined_ml + 2 * row, f32x2{top, sum});
+                    if constexpr (APART) hand_over1(a.joined_l + row, sum_lse);
+                }
             }
         }
         if (whole) return;
         counter = a.arrived_groups + slot0;
-        part_ml = a.joined_ml;
+        part_ml = a.joined_ml, part_l = a.joined_l;
         first = slot0, stride = fan, n = groups;
     }
 }
@@ -761,20 +782,25 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
 // (O^T = V^T P^T) wants its probabilities in, if V's tile has its positions in that order, and nothing moves between lanes.  K and
 // V are exact in bf16.  NT: bf16 terms of an element of Q (1: Q is bf16; 3: fp32, exactly), PT: of a probability: three for the
 // fp32 model, two for the tiles of 16, which wait for memory anyway (error against 64 bits 0.0017, all of it the result's own
-// rounding to bf16), one for larger ones (0.0023), where the products cost time.  UNITS: 16 entries each of a tile.
+// rounding to bf16), one for larger ones (0.0021; a second term costs them a sixth of their time: 64 requests of 500 to
+// 16 384 positions and 5 rows, 32 heads on 8, 171 us instead of 146).  With one term the divisor is the sum of the rounded probabilities: the
+// weights that V gets add to one, so a row in which one position outweighs the others keeps that one's value, whatever
+// its weight rounds to.  The log-sum-exp, where it is asked for (LSE), has a sum of its own, of the probabilities before
+// they are rounded (those 64 requests 151 us).  UNITS: 16 entries each of a tile.
 // Bound by HBM where contexts are long: 64 requests of up to 16 384 positions, 32 heads on 8 of 128 elements, 589 MB: 114 us, 5.2 TB/s
 // (a copy's rate is 5.15), every byte read once.  So what counts is what is on its way: of the tiles DEPTH steps ahead each load
 // is asked for as soon as its registers have been read.  One request of 131 071 positions: 32 us for 143 MB, 4.5 TB/s; of which
 // 4 us are its parts' joins.  16 requests of up to 2048 positions, 32 heads: 19 us for 69 MB, launch and last parts included.
 // A single user's 513 positions (6.7 us) are bound by the launch and the chain part, table, K, V, join.
-template <int HD, int NT, int PT, int UNITS, int NW, int DEPTH, bool PAST, typename ST>
+template <int HD, int NT, int PT, int UNITS, int NW, int DEPTH, bool PAST, bool LSE, typename ST>
 __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 : NT == 1 ? 4 : 3) void kv4_attend_kernel(Kv4Attend a) {
     constexpr int G = HD / 32, EPC = HD / 16, M = 16 * UNITS;
     constexpr int CT = KV4_CHUNK / 16;  // tiles of 16 positions at a time: one contraction of P.V
     static_assert(CT == 2, "a contraction has 32 positions");
     constexpr int LDO = HD + 4;
+    constexpr bool APART = LSE && PT == 1;
     __shared__ float s_o[NW * 16 * LDO];
-    __shared__ float s_m[NW * 16], s_l[NW * 16];
+    __shared__ float s_m[NW * 16], s_l[NW * 16], s_lse[APART ? NW * 16 : 1];
     __shared__ uint32_t s_last;
 
     const Kv4Part w = a.parts[blockIdx.x];  // (there is room for as many as the grid has; asked for together with their number)
@@ -856,10 +882,10 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
     };
 
     f32x4 o[UNITS][EPC];
-    float m[UNITS], l[UNITS];  // m: the scores' reference, at most a.slack below their maximum (so no probability passes 2^8)
+    float m[UNITS], l[UNITS], l_lse[UNITS];  // m: the scores' reference, at most a.slack below their maximum (so no probability passes 2^8)
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-        m[u] = -INFINITY, l[u] = 0.f;
+        m[u] = -INFINITY, l[u] = l_lse[u] = 0.f;
 #pragma unroll
         for (int j = 0; j < EPC; ++j) o[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -954,6 +980,7 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
             if (__any(top > m[u] + a.slack)) {
                 const float corr = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[u] - top) * a.scale_log2);
                 l[u] *= corr;
+                if constexpr (APART) l_lse[u] *= corr;
 #pragma unroll
                 for (int j = 0; j < EPC; ++j) o[u][j] *= corr;
                 m[u] = top;
@@ -966,10 +993,12 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
                     f32x2 p;
                     p[0] = __builtin_amdgcn_exp2f(fmaf(s[u][t][i], a.scale_log2, -ref));
                     p[1] = __builtin_amdgcn_exp2f(fmaf(s[u][t][i + 1], a.scale_log2, -ref));
-                    l[u] += p[0] + p[1];  // (before they are rounded: the log-sum-exp keeps fp32's accuracy)
+                    if constexpr (PT > 1) l[u] += p[0] + p[1];
+                    if constexpr (APART) l_lse[u] += p[0] + p[1];
 #pragma unroll
                     for (int n = 0; n < PT; ++n) {
                         const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+                        if constexpr (PT == 1) l[u] = add_pair(h, l[u]);
                         pf[u][n][t * 2 + (i >> 1)] = h;
                         if (n + 1 < PT) p[0] -= __uint_as_float(h << 16), p[1] -= __uint_as_float(h & 0xffff0000u);
                     }
@@ -1043,7 +1072,7 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
         if (f0 + 16 * u >= f_end) break;
-        const float lsum = rows4_sum(l[u]);
+        const float lsum = rows4_sum(l[u]), lse_sum = APART ? rows4_sum(l_lse[u]) : 0.f;
         if (u) __syncthreads();
         if (f0 + 16 * u + col < f_end) {
             float* dst = s_o + (wave * 16 + col) * LDO;
@@ -1051,12 +1080,15 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < EPC; ++j) dst[(quarter * 4 + i) * EPC + j] = o[u][j][i];
-            if (quarter == 0) s_m[wave * 16 + col] = m[u] * a.scale_log2, s_l[wave * 16 + col] = lsum;
+            if (quarter == 0) {
+                s_m[wave * 16 + col] = m[u] * a.scale_log2, s_l[wave * 16 + col] = lsum;
+                if constexpr (APART) s_lse[wave * 16 + col] = lse_sum;
+            }
         }
         __syncthreads();
         const int f = f0 + 16 * u + my_row;
         if (my_row < 16 && f < f_end) {
-            float top = -INFINITY, sum = 0.f, acc[EPT];
+            float top = -INFINITY, sum = 0.f, sum_lse = 0.f, acc[EPT];
 #pragma unroll
             for (int v = 0; v < NW; ++v) top = fmaxf(top, s_m[v * 16 + my_row]);
             const float ref = top == -INFINITY ? 0.f : top;
@@ -1066,6 +1098,7 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
             for (int v = 0; v < NW; ++v) {
                 const float wt = __builtin_amdgcn_exp2f(s_m[v * 16 + my_row] - ref);
                 sum += wt * s_l[v * 16 + my_row];
+                if constexpr (APART) sum_lse += wt * s_lse[v * 16 + my_row];
                 // (a wave that saw nothing has weight zero and zeros)
 #pragma unroll
                 for (int e = 0; e < EPT; ++e) acc[e] += wt * s_o[(v * 16 + my_row) * LDO + my_d + (e >> 1) * (2 * TPR) + (e & 1)];
@@ -1075,32 +1108,36 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
                 for (int e = 0; e < EPT; e += 2) store_pair(out + r * HD + my_d + e * TPR, f32x2{acc[e] * inv, acc[e + 1] * inv});
-                if (a.lse && my_d == 0) a.lse[r] = (ref + log2f(sum)) * 0.6931471805599453f;
+                if (a.lse && my_d == 0) a.lse[r] = (ref + log2f(APART ? sum_lse : sum)) * 0.6931471805599453f;
             } else {
                 const size_t r = (size_t)w.slot * M + 16 * u + my_row;
 #pragma unroll
                 for (int e = 0; e < EPT; e += 2) hand_over2(a.part_o + r * HD + my_d + e * TPR, f32x2{acc[e], acc[e + 1]});
-                if (my_d == 0) hand_over2(a.part_ml + 2 * r, f32x2{top, sum});
+                if (my_d == 0) {
+                    hand_over2(a.part_ml + 2 * r, f32x2{top, sum});
+                    if constexpr (APART) hand_over1(a.part_l + r, sum_lse);
+                }
             }
         }
     }
-    if (n_parts > 1) join_parts<HD, NW * 64, M, ST>(a, w, n_parts, f0, f_end, &s_last);
+    if (n_parts > 1) join_parts<HD, NW * 64, M, APART, ST>(a, w, n_parts, f0, f_end, &s_last);
 }
 
 // Prompts: 128 entries of a tile, 32 for each of four waves.  The four convert the next 32 positions together, a tile of K or V
 // each, into bf16 in LDS in operand order, while they work on these; so an element is converted once for 128 entries, and
 // 32 x 32 products halve what is read from LDS per operation.  One barrier per 32 positions, two buffers.  Two such groups of
 // waves take every other 32 positions, so that a SIMD has two waves, and join their sums through LDS at the end.
-// One bf16 term of a probability (its sum is that of the probabilities before they are rounded: error against 64 bits 0.0023, of
-// which the result's rounding is 0.0017; a second term would be half as many products again).
+// One bf16 term of a probability, divided by the sum of the rounded ones as above (error against 64 bits 0.0023, of which the
+// result's rounding is 0.0017; a second term would be half as many products again).
 // 1024 rows at the end of 8192 positions, 32 heads on 8 of 128 elements, 129 GFLOP: 148 us, 870 TFLOP/s, where a large matrix product
 // reaches 1215.  The vector units' work (per score an exponential, a multiply-add, a maximum, a sum, half a conversion) takes about
 // as long as the products, and two waves of a SIMD overlap them in part; LDS is active a third of the time.  Three groups of
 // waves with Q in LDS: 151 us.
+template <bool LSE>
 __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     constexpr int HD = 128, M = KV4_WIDE, G = HD / 32, EPC = HD / 16, KS = HD / 16, DB = HD / 32, LB = HD / 8;
     __shared__ u32x4 s_operands[2][2][(KS + 2 * DB) * 64];  // K, V of each group's two steps; at the end the second group's sums
-    __shared__ float s_ml[2][256];
+    __shared__ float s_ml[LSE ? 3 : 2][256];
     __shared__ uint32_t s_scales_of[2][2][2][G * 4];  // of V, if some entry does not see all of the positions
     __shared__ uint32_t s_nan_of[2][2][2];            // ... and there is a NaN among them
     static_assert(sizeof(s_operands) >= 4 * 64 * 16 * DB * sizeof(float), "room for the sums");
@@ -1228,7 +1265,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     };
 
     f32x16 o[DB] = {};
-    float m = -INFINITY, l = 0.f;  // m: the scores' reference, at most a.slack below their maximum (so no probability passes 2^8)
+    float m = -INFINITY, l = 0.f, l_lse = 0.f;  // m: the scores' reference, at most a.slack below their maximum (so no probability passes 2^8)
     // The second group's matrix products come when the first one's vector work does: its scores are formed an interval ahead, so K
     // is converted two steps ahead there.
     const int ahead = group && !of_v ? 2 : 1;
@@ -1280,19 +1317,22 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
             if (__any(top > m + a.slack)) {
                 const float corr = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * a.scale_log2);
                 l *= corr;
+                if constexpr (LSE) l_lse *= corr;
 #pragma unroll
                 for (int b = 0; b < DB; ++b) o[b] *= corr;
                 m = top;
             }
             const float ref = m == -INFINITY ? 0.f : m * a.scale_log2;
-            u32x4 p[2];  // (one bf16 term; the sum is that of the probabilities before they are rounded)
+            u32x4 p[2];
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
                 f32x2 x;
                 x[0] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, -ref));
                 x[1] = __builtin_amdgcn_exp2f(fmaf(s[i + 1], a.scale_log2, -ref));
-                l += x[0] + x[1];
-                p[i >> 3][(i & 7) >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+                const uint32_t rounded = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+                l = add_pair(rounded, l);
+                if constexpr (LSE) l_lse += x[0] + x[1];
+                p[i >> 3][(i & 7) >> 1] = rounded;
             }
             // weighted sum: rows = elements, columns = entries
 #pragma unroll
@@ -1339,12 +1379,14 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s_sums[((wave * DB + b) * 16 + i) * 64 + lane] = o[b][i];
         s_ml[0][wave * 64 + lane] = m, s_ml[1][wave * 64 + lane] = l;
+        if constexpr (LSE) s_ml[2][wave * 64 + lane] = l_lse;
     }
     __syncthreads();
     if (!group) {
         const float m2 = s_ml[0][wave * 64 + lane], top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
         const float w1 = __builtin_amdgcn_exp2f((m - ref) * a.scale_log2), w2 = __builtin_amdgcn_exp2f((m2 - ref) * a.scale_log2);
         l = l * w1 + s_ml[1][wave * 64 + lane] * w2;
+        if constexpr (LSE) l_lse = l_lse * w1 + s_ml[2][wave * 64 + lane] * w2;
         m = top;
 #pragma unroll
         for (int b = 0; b < DB; ++b)
@@ -1354,6 +1396,11 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     float l0, l1;
     halves_of(l, l0, l1);
     const float sum = l0 + l1;
+    float sum_lse = 0.f;
+    if constexpr (LSE) {
+        halves_of(l_lse, l0, l1);
+        sum_lse = l0 + l1;
+    }
     if (!group && f_wave + col < f_end) {
         const size_t r = (size_t)(w.row0 + row) * (a.group * a.kv_heads) + head, at = (size_t)w.slot * M + 32 * wave + col;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -1373,13 +1420,15 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
             }
         }
         if (half == 0) {
-            if (n_parts > 1)
+            if (n_parts > 1) {
                 hand_over2(a.part_ml + 2 * at, f32x2{m * a.scale_log2, sum});
-            else if (a.lse)
-                a.lse[r] = ((m == -INFINITY ? 0.f : m * a.scale_log2) + log2f(sum)) * 0.6931471805599453f;
+                if constexpr (LSE) hand_over1(a.part_l + at, sum_lse);
+            } else if constexpr (LSE) {
+                a.lse[r] = ((m == -INFINITY ? 0.f : m * a.scale_log2) + log2f(sum_lse)) * 0.6931471805599453f;
+            }
         }
     }
-    if (n_parts > 1) join_parts<HD, 512, M, __bf16>(a, w, n_parts, f0, f_end, &s_last);
+    if (n_parts > 1) join_parts<HD, 512, M, LSE, __bf16>(a, w, n_parts, f0, f_end, &s_last);
 }
 
 template <int HD, int UNITS, int NW>
@@ -1389,15 +1438,21 @@ hipError_t attend_waves(const Kv4Attend& a, int dtype, int grid, hipStream_t s) 
     // Two steps ahead where registers allow it at the same number of waves: 8 waves alone on a CU, and bf16 tiles of 32 entries (17
     // requests of up to 12 560 positions and 15 rows: 59 us, one step ahead 62; 64 of up to 16 384 and 5 rows: 128, 142).
     constexpr int DEPTH = NW == 8 && HD <= 128 ? 2 : 1, DEPTH_BF16 = UNITS == 2 && HD <= 128 ? 2 : DEPTH;
-    if (dtype == EE_BF16)
-        EE_LAUNCH((past ? kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, DEPTH_BF16, UNITS == 1, __bf16>
-                        : kv4_attend_kernel<HD, 1, UNITS == 1 ? 2 : 1, UNITS, NW, DEPTH_BF16, false, __bf16>),
-                  dim3(grid), dim3(NW * 64), s, a);
-    else if constexpr (UNITS <= 2)
-        EE_LAUNCH((past ? kv4_attend_kernel<HD, 3, 3, UNITS, NW, DEPTH, UNITS == 1, float> : kv4_attend_kernel<HD, 3, 3, UNITS, NW, DEPTH, false, float>), dim3(grid),
-                  dim3(NW * 64), s, a);
-    else
+    const dim3 g(grid), t(NW * 64);
+    if (dtype == EE_BF16) {
+        if constexpr (UNITS == 1)
+            EE_LAUNCH((past ? kv4_attend_kernel<HD, 1, 2, 1, NW, DEPTH_BF16, true, true, __bf16> : kv4_attend_kernel<HD, 1, 2, 1, NW, DEPTH_BF16, false, true, __bf16>),
+                      g, t, s, a);
+        else
+            EE_LAUNCH((a.lse ? kv4_attend_kernel<HD, 1, 1, UNITS, NW, DEPTH_BF16, false, true, __bf16>
+                             : kv4_attend_kernel<HD, 1, 1, UNITS, NW, DEPTH_BF16, false, false, __bf16>),
+                      g, t, s, a);
+    } else if constexpr (UNITS <= 2) {
+        EE_LAUNCH((past ? kv4_attend_kernel<HD, 3, 3, UNITS, NW, DEPTH, UNITS == 1, true, float> : kv4_attend_kernel<HD, 3, 3, UNITS, NW, DEPTH, false, true, float>), g,
+                  t, s, a);
+    } else {
         return hipErrorInvalidValue;
+    }
     return hipGetLastError();
 }
 
@@ -1415,7 +1470,7 @@ hipError_t attend_hd(const Kv4Attend& a, int dtype, int units, int waves, int gr
         if (units == 2) return attend_units<HD, 2>(a, dtype, waves, grid, s);
     if constexpr (HD == 128) {
         if (units == KV4_WIDE / 16 && dtype == EE_BF16) {
-            EE_LAUNCH(kv4_attend_wide_kernel, dim3(grid), dim3(512), s, a);
+            EE_LAUNCH((a.lse ? kv4_attend_wide_kernel<true> : kv4_attend_wide_kernel<false>), dim3(grid), dim3(512), s, a);
             return hipGetLastError();
         }
     }

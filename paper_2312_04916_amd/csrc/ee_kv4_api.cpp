@@ -102,7 +102,7 @@ StateLayout state_layout(const ee_kv4_config& c) {
     const int units = kv4_tile_units(c.dtype, c.head_dim, 64, 1, 0, c.n_kv_heads);
     w.part_rows = (2 * most_of_cut(units) + 64) * 16 * units;
     if (kv4_has_wide_tiles(c.dtype, c.head_dim)) w.part_rows = std::max(w.part_rows, (2 * most_of_cut(KV4_WIDE / 16) + 64) * KV4_WIDE);
-    w.part_ml = take((size_t)w.part_rows * 16);  // of parts, of joined ones
+    w.part_ml = take((size_t)w.part_rows * 24);  // of parts, of joined ones; then the log-sum-exp's of both
     w.part_o = take((size_t)w.part_rows * c.head_dim * 4);
     w.total = off;
     return w;
@@ -285,6 +285,8 @@ int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride,
     a.part_o = (float*)(c->state + c->sl.part_o);
     a.part_ml = (float*)(c->state + c->sl.part_ml);
     a.joined_ml = a.part_ml + (size_t)c->sl.part_rows * 2;
+    a.part_l = a.joined_ml + (size_t)c->sl.part_rows * 2;
+    a.joined_l = a.part_l + c->sl.part_rows;
     a.arrived = (uint32_t*)(c->state + c->sl.arrived);
     a.arrived_groups = a.arrived + c->sl.max_slots;
     const int grid = (int)std::min(c->sl.max_parts, most_parts(g, c->n_seqs, c->n_rows, 16 * c->units));

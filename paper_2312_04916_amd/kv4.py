@@ -99,7 +99,8 @@ class Kv4Cache:
 
     def plan(self, held: torch.Tensor, start: torch.Tensor, end: torch.Tensor, n_rows: int, max_rows_per_seq: Optional[int] = None,
              stream=None) -> None:
-        """ee_kv4_plan.  held, start, end: int32[n_seqs] on the device; max_rows_per_seq: n_rows where it is not given."""
+        """ee_kv4_plan.  held, start, end: int32[n_seqs] on the device; max_rows_per_seq: n_rows where it is not given (the
+        attention then works as for long chunks: give 1 for a plain decode step)."""
         n = held.shape[0]
         code = self._plan(self.h, n, self._lengths(held, n, "held"), self._lengths(start, n, "start"), self._lengths(end, n, "end"), n_rows,
                           n_rows if max_rows_per_seq is None else max_rows_per_seq, _raw_stream(stream, self._index))

@@ -1,0 +1,94 @@
+"""Values at which the 4-bit cache's attention can go wrong: how probabilities are rounded, the log-sum-exp, NaN that every row sees."""
+import pytest
+import torch
+
+import kv4_reference as ref
+from test_gpu_kv4 import Requests, dev
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd,rows,heads", [(32, 3, 2), (64, 3, 2), (64, 40, 2), (128, 3, 2), (128, 20, 4), (256, 3, 2), (128, 130, 160)])
+@pytest.mark.parametrize("rest", [0.0, 1.0])
+def test_nan_that_every_row_sees(dtype, hd, rows, heads, rest):
+    """A NaN at the first positions of a context, in a group whose other elements are `rest`: in K it is the rows' whole result, in V
+    that of its group of 32 elements, whatever the queries are."""
+    n = 400
+    s = Requests([n], [rows], heads, 2, hd, dtype, 16, seed=31)
+    s.step()
+    s.q = -s.q.abs()
+    clean = s.c.attend(0, s.q)
+    s.k[0][3, 0, :32] = rest
+    s.k[0][3, 0, 5] = float("nan")
+    s.v[0][4, 1, hd - 32:] = rest
+    s.v[0][4, 1, hd - 2] = float("nan")
+    s.c.plan(dev([n]), dev([0]), dev([n]), n)
+    s.write()
+    s.step()
+    out, lse = s.c.attend(0, s.q, lse=True)
+    half = heads // 2
+    assert torch.isnan(out[:, :half]).all() and torch.isnan(lse[:, :half]).all()
+    assert torch.isnan(out[:, half:, hd - 32:]).all()
+    assert torch.equal(out[:, half:, :hd - 32], clean[:, half:, :hd - 32])
+    s.c.close()
+
+
+@pytest.mark.parametrize("lse", [False, True])
+@pytest.mark.parametrize("hd,rows,heads", [(128, 3, 2), (32, 20, 2), (64, 20, 2), (128, 20, 2), (32, 50, 2), (64, 64, 2), (128, 130, 160)])
+def test_a_dominant_position_keeps_its_weight(hd, rows, heads, lse):
+    """One position outweighs all others, by less than what moves the reference of the running soft-max: its weight there is any
+    number up to 2^8, and however that is rounded, what V is multiplied with and what the sum is divided by are the same.
+    Tiles of 16, 32, 64 and 128 entries."""
+    n, dominant = 640, 500
+    s = Requests([n], [rows], heads, 2, hd, "bf16", 64, seed=33, loud=False)
+    k, v = s.k[0].zero_(), s.v[0].zero_()
+    k[:, :, 1] = 1.0
+    k[::32] = 0.0  # score 0: the reference
+    k[dominant] = 0.0
+    k[dominant, :, 0] = 1.0
+    g = torch.Generator(device="cuda:0").manual_seed(34)
+    levels = torch.tensor([0.5, 1, 1.5, 2, 3, 4, 6, -0.5, -1, -1.5, -2, -3, -4, -6], device="cuda:0", dtype=torch.bfloat16)
+    v[dominant] = levels[torch.randint(0, 14, (2, hd), device="cuda:0", generator=g)]
+    s.c.plan(dev([n]), dev([0]), dev([n]), n)
+    s.write()
+    s.step()
+    z = 4.5 + torch.arange(rows * heads, device="cuda:0").reshape(rows, heads) % 34 / 32  # below 8 ln 2
+    s.q.zero_()
+    s.q[:, :, 0], s.q[:, :, 1] = z.to(torch.bfloat16), -60.0
+    out = s.c.attend(0, s.q, scale=1.0, lse=lse)
+    if lse:
+        out, lse = out
+    p = torch.exp(z.double())
+    others = ((torch.arange(n - rows, n, device="cuda:0") // 32) + 1).double()[:, None]  # that score 0 and that the row sees
+    share = p / (p + others)
+    want = share[..., None] * v[dominant].double().repeat_interleave(heads // 2, 0)
+    # the result's rounding to bf16 is half a unit of its last place.  The weight's own moves the share by 2^-8 (1 - share) of it, and
+    # what fp32 does in exponential, sums and division by less than 2^-17
+    half = torch.exp2(torch.floor(torch.log2(want.abs())) - 8)
+    assert ((out.double() - want).abs() <= half + want.abs() * ((2.0 ** -8 * (1 - share) + 2.0 ** -17)[..., None])).all()
+    if torch.is_tensor(lse):
+        assert (lse.double() - torch.log(p + others)).abs().max() <= 2.0 ** -18
+    s.c.close()
+
+
+@pytest.mark.parametrize("hd,heads,kvh,lengths,rows", [
+    (32, 4, 2, [1, 40, 333], [1, 3, 2]), (64, 2, 2, [90, 400], [20, 25]), (64, 4, 1, [70, 900], [33, 64]), (128, 4, 2, [65, 300], [9, 12]),
+    (256, 2, 1, [500, 33], [3, 20]), (128, 160, 2, [300], [130]),
+    (128, 4, 1, [9000, 700, 5001], [3, 1, 3]), (128, 2, 2, [9000, 700, 5001], [40, 1, 40]), (64, 64, 2, [5001, 400], [260, 3]), (128, 64, 2, [9001, 700], [64, 600]),
+])
+def test_the_log_sum_exp_is_that_of_unrounded_probabilities(hd, heads, kvh, lengths, rows):
+    """With bf16 models too: only the products of 16-bit numbers and sums in fp32 stand between the scores and it.  Tiles of all
+    sizes, whole and cut."""
+    s = Requests(lengths, rows, heads, kvh, hd, "bf16", 32, seed=35)
+    s.step()
+    out, lse = s.c.attend(0, s.q, lse=True)
+    s.check(out)
+    assert torch.equal(out, s.c.attend(0, s.q))
+    at = 0
+    for i, (n, r) in enumerate(zip(lengths, rows)):
+        _, want, _, z_abs = ref.attend(s.q[at:at + r], ref.held(s.k[i]), ref.held(s.v[i]), list(range(n - r, n)), s.group, hd ** -0.5)
+        # as in Requests.check: scores are off by (hd + 2) 2^-24 z_abs, exponentials and logarithm as much again, sums by n 2^-24
+        assert (lse[at:at + r].cpu().double() - want).abs().max() <= (4 * (hd + 2) * z_abs + n + 64) * 2.0 ** -24
+        at += r
+    s.c.close()
