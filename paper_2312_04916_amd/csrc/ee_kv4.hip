@@ -158,11 +158,12 @@ __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
     const int left = max(0, p.n_blocks - all[0]);  // free before the call (the lengths may contradict the pool)
     const bool clipped = all[3] > p.n_rows;
     if (clipped) {
-        // rows that do not fit: their requests are refused, and give and take nothing
+        // rows that do not fit: their requests are refused, and give and take nothing (no rows always fit: a request that ends gives
+        // its blocks back)
         int row = sum[3], again[4] = {0, 0, 0, 0};
         for (int i = i0; i < i1; ++i) {
             const int rows = s_row[i];
-            if (row + rows > p.n_rows) s_had[i] &= BLOCKS, s_take[i] = s_had[i];
+            if (rows > 0 && row + rows > p.n_rows) s_had[i] &= BLOCKS, s_take[i] = s_had[i];
             const int had = s_had[i] & BLOCKS, need = s_take[i];
             again[1] += max(had - need, 0), again[2] += max(need - had, 0);
             row = min(row + rows, cap);
