@@ -430,7 +430,7 @@ typedef struct {
     int32_t* positions;   /* [max_rows] position of each row in its request, -1: none */
     int32_t* row_seq;     /* [max_rows] request of each row, -1: a row behind the last request's */
     int32_t* row_start;   /* [max_seqs + 1] first row of each request; [n_seqs] = rows in all */
-    int32_t* served;      /* [max_seqs] 1: as asked, 0: refused (the pool is exhausted, or lengths out of range) */
+    int32_t* served;      /* [max_seqs] 1: as asked, 0: refused (the pool or the step's rows are exhausted, or lengths out of range) */
     int32_t* held_next;   /* [max_seqs] positions each request holds after the call: end, or held where it was refused */
     int32_t* n_free;      /* [1] free blocks after the call */
     int32_t table_stride; /* ceil(max_positions / block_tokens) */
@@ -448,7 +448,9 @@ int ee_kv4_get_arrays(const ee_kv4* c, ee_kv4_arrays* out);
 /* Blocks, slots and rows of a step.  Request i (all that hold blocks are in the call: 0 <= i < n_seqs) held dev_held[i]
  * positions, brings rows for positions dev_start[i] .. dev_end[i]-1 and holds dev_end[i] positions afterwards: a decode step
  * (start = held, end = held + 1), one that carries deferred tokens (start < held), a prompt (start = 0), a step taken back
- * (end < held), a request that ends (start = end = 0) or waits (start = end = held).  Rows are packed in the requests' order.
+ * (end < held), a request that ends (start = end = 0) or waits (start = end = held), one that takes blocks ahead (start = end >
+ * held: what lies between is then the caller's to write, by slots of its own).  Rows are packed in the requests' order.  A request whose rows begin behind what it held (held < start < end) is refused:
+ * they would see positions that no call has written, or that hold what another request has left.
  *   Blocks that are no longer needed go back on the stack of free blocks, the last request's first and of each request the
  *   last block first; blocks that are needed come off its top in the requests' order.  So a plan that is taken back leaves the
  *   stack as it was.  Where the free blocks do not suffice, the requests up to there are served, and behind it those that need

@@ -145,7 +145,8 @@ __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
     for (int i = i0; i < i1; ++i) {
         const int held = p.held[i], start = p.start[i], end = p.end[i];
         const bool range = start >= 0 && start <= end && end <= most;
-        const bool ok = range && held >= 0 && held <= most && end - start <= p.max_rows_per_seq;
+        const bool gap = start > held && start < end;  // (its rows would see positions that nobody has written)
+        const bool ok = range && held >= 0 && held <= most && !gap && end - start <= p.max_rows_per_seq;
         const int had = (min(max(held, 0), most) + bt - 1) >> bt_shift, need = ok ? (end + bt - 1) >> bt_shift : had;
         const int rows = range ? min(end - start, cap) : 0;
         s_start[i] = start, s_had[i] = had | (ok ? SERVED : 0), s_take[i] = need, s_row[i] = rows;  // (this thread's, for now)

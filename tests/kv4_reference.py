@@ -48,7 +48,7 @@ class Blocks:
         for h, s, e in zip(held_, start, end):
             in_range = 0 <= s <= e <= self.max_positions
             r = e - s if in_range else 0
-            ok.append(in_range and 0 <= h <= self.max_positions and r <= most and (r == 0 or at + r <= n_rows))
+            ok.append(in_range and (s <= h or s == e) and 0 <= h <= self.max_positions and r <= most and (r == 0 or at + r <= n_rows))
             rows.append(r)
             at += r
         need = [self.need(end[i]) if ok[i] else len(self.table[i]) for i in range(n)]

@@ -1,8 +1,9 @@
 """The 4-bit cache's plan where a step asks for more than there is room for, and where its lengths do not belong together."""
 import pytest
+import torch
 
 import kv4_reference as ref
-from test_gpu_kv4 import cache_of, check_plan, dev
+from test_gpu_kv4 import cache_of, check_plan, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -30,4 +31,27 @@ def test_requests_without_rows_are_served_behind_an_overflow(n_more):
     start = [0, 0, 0, 33, 20, 20, 7] + held_next[7:]
     held_next = check_plan(c, blocks, held_next, start, again, 102)
     assert c.served[:n].all() and held_next == again
+    c.close()
+
+
+@pytest.mark.parametrize("n_more", [0, 600])
+def test_rows_that_begin_behind_what_is_held_are_refused(n_more):
+    """Between what such a request held and its rows lie positions that nobody has written: in blocks of its own or in blocks that
+    another request has given back."""
+    n = 5 + n_more
+    c = cache_of(2, 2, 32, "bf16", 16, 30 + n_more, n, 200, 2000)
+    blocks = ref.Blocks(30 + n_more, n, 200, 16)
+    held = [20, 0, 20, 33, 20] + [3] * n_more
+    check_plan(c, blocks, [0] * n, [0] * n, held, sum(held))
+    free = c.n_free.item()
+    # one position on, from position 1 of an empty request, exactly at what is held, one past a block's end, blocks taken ahead
+    start, end = [21, 1, 20, 50, 60] + [3] * n_more, [22, 2, 22, 51, 60] + [4] * n_more
+    held_next = check_plan(c, blocks, held, start, end, 5 + n_more)
+    assert c.served[:5].tolist() == [0, 0, 1, 0, 1] and c.served[5:n].all()
+    assert held_next == [20, 0, 22, 33, 60] + [4] * n_more
+    assert c.slots[0].item() == c.slots[1].item() == c.slots[4].item() == -1 and (c.slots[2:4] >= 0).all()
+    assert c.n_free.item() == free - 2
+    q = rand((5 + n_more, 2, 32), "bf16", 3)
+    out, lse = c.attend(0, q, lse=True)
+    assert not out[[0, 1, 4]].any() and torch.isneginf(lse[[0, 1, 4]]).all()
     c.close()
