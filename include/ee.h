@@ -449,8 +449,9 @@ int ee_kv4_get_arrays(const ee_kv4* c, ee_kv4_arrays* out);
  * positions, brings rows for positions dev_start[i] .. dev_end[i]-1 and holds dev_end[i] positions afterwards: a decode step
  * (start = held, end = held + 1), one that carries deferred tokens (start < held), a prompt (start = 0), a step taken back
  * (end < held), a request that ends (start = end = 0) or waits (start = end = held), one that takes blocks ahead (start = end >
- * held: what lies between is then the caller's to write, by slots of its own).  Rows are packed in the requests' order.  A request whose rows begin behind what it held (held < start < end) is refused:
- * they would see positions that no call has written, or that hold what another request has left.
+ * held: what lies between is then the caller's to write, by slots of its own).  Rows are packed in the requests' order.  A
+ * request whose rows begin behind what it held (held < start < end) is refused: they would see positions that no call has
+ * written, or that hold what another request has left.
  *   Blocks that are no longer needed go back on the stack of free blocks, the last request's first and of each request the
  *   last block first; blocks that are needed come off its top in the requests' order.  So a plan that is taken back leaves the
  *   stack as it was.  Where the free blocks do not suffice, the requests up to there are served, and behind it those that need

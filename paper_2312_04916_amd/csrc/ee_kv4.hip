@@ -755,7 +755,7 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
             const int f = f0 + r;
             if (whole) {
                 const size_t at = out_row(a, w, f);
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                const float inv = 1.f / sum;
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) store_pair(out + at * HD + here.element(i), acc[i] * inv);
                 if (a.lse && here.first()) a.lse[at] = ((top == -INFINITY ? 0.f : top) + log2f(APART ? sum_lse : sum)) * 0.6931471805599453f;
@@ -779,7 +779,9 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
 // that take every NW-th chunk.  With s = scale * q.k in units of ln 2, running maximum m and weights 2^(s - m):
 //   l <- l 2^(m - m') + sum 2^(s - m'),   o <- o 2^(m - m') + sum 2^(s - m') v,   m' = max(m, s),   out = o / l.
 // o and l are rescaled only when some maximum has grown by more than a factor 2^8 of the weights, which leaves them in fp32's
-// range; m, l and o are fp32.  Shares are joined in the same way: waves through LDS, parts through join_parts.
+// range; m, l and o are fp32.  Shares are joined in the same way: waves through LDS, parts through join_parts.  A row that gets
+// there sees its own position at least, so l is at least 1, unless all of its scores are -inf: then 0 / 0 is the NaN that the
+// formula gives.
 // Products are 16x16x32 bf16 with positions as rows of the first (S^T = K Q^T): its result then lies in the lanes that the second one
 // (O^T = V^T P^T) wants its probabilities in, if V's tile has its positions in that order, and nothing moves between lanes.  K and
 // V are exact in bf16.  NT: bf16 terms of an element of Q (1: Q is bf16; 3: fp32, exactly), PT: of a probability: three for the
@@ -1107,7 +1109,7 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
             }
             if (n_parts == 1) {
                 const size_t r = out_row(a, w, f);
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                const float inv = 1.f / sum;
 #pragma unroll
                 for (int e = 0; e < EPT; e += 2) store_pair(out + r * HD + my_d + e * TPR, f32x2{acc[e] * inv, acc[e + 1] * inv});
                 if (a.lse && my_d == 0) a.lse[r] = (ref + log2f(APART ? sum_lse : sum)) * 0.6931471805599453f;
@@ -1405,7 +1407,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     }
     if (!group && f_wave + col < f_end) {
         const size_t r = (size_t)(w.row0 + row) * (a.group * a.kv_heads) + head, at = (size_t)w.slot * M + 32 * wave + col;
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const float inv = 1.f / sum;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const PartPlace<HD, 512, M> place(wave, i);

@@ -1,4 +1,5 @@
-"""Values at which the 4-bit cache's attention can go wrong: how probabilities are rounded, the log-sum-exp, NaN that every row sees."""
+"""Values at which the 4-bit cache's attention can go wrong: how probabilities are rounded, the log-sum-exp, NaN that every row sees,
+infinities in queries."""
 import pytest
 import torch
 
@@ -91,4 +92,25 @@ def test_the_log_sum_exp_is_that_of_unrounded_probabilities(hd, heads, kvh, leng
         # as in Requests.check: scores are off by (hd + 2) 2^-24 z_abs, exponentials and logarithm as much again, sums by n 2^-24
         assert (lse[at:at + r].cpu().double() - want).abs().max() <= (4 * (hd + 2) * z_abs + n + 64) * 2.0 ** -24
         at += r
+    s.c.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd,rows,heads", [(64, 2, 2), (128, 20, 4), (256, 3, 2), (128, 130, 160)])
+def test_a_query_with_an_infinity(dtype, hd, rows, heads):
+    """inf times an element of K is an infinity or NaN, so the row's soft-max is NaN, also where all its scores are -inf; a row that
+    sees nothing is the only one that is zero."""
+    n = 300
+    s = Requests([n], [rows], heads, 2, hd, dtype, 16, seed=32)
+    s.k[0].fill_(1.0)
+    s.c.plan(dev([n]), dev([0]), dev([n]), n)
+    s.write()
+    s.step()
+    clean = s.c.attend(0, s.q)
+    s.q[1, 0, 7] = float("-inf")
+    s.q[0, 1, 7] = float("inf")
+    out = s.c.attend(0, s.q)
+    assert torch.isnan(out[1, 0]).all() and torch.isnan(out[0, 1]).all()
+    out[1, 0], out[0, 1] = clean[1, 0], clean[0, 1]
+    assert torch.equal(out, clean)
     s.c.close()
