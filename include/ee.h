@@ -476,13 +476,15 @@ int ee_kv4_append(ee_kv4* c, int layer, int n_rows, const void* dev_k, int64_t k
 int ee_kv4_read(ee_kv4* c, int layer, int n_rows, const int64_t* dev_slots, void* dev_k, void* dev_v, void* stream);
 
 /* Attention of the latest plan's rows over what their requests hold: row at position p sees positions max(0, p - window + 1)
- * .. p (window 0: all up to p).  scores = q . k * scale (scale > 0; 0: 1 / sqrt(head_dim)), soft-max in fp32, weighted sum of V.
- * In that sum a bf16 model's weights are bf16: two terms of each where a request has at most 16 (row, query head) pairs per kv
- * head, by the plan's max_rows_per_seq, and where head_dim is 256, so that only the result's rounding is left; else one term (a
- * row's error is then that of two roundings to bf16).  An fp32 model's weights are fp32.
- * dev_out [n_rows][n_heads][head_dim] contiguous, apart from dev_q (EE_ERR_ARG where the ranges overlap); dev_lse
- * [n_rows][n_heads] fp32 or NULL: log sum exp of the row's scores, with which results over several caches can be joined.  A row that sees nothing (its request was refused, or it belongs to
- * none) gets zeros and -inf.  NaN in positions that a row does not see do not reach it. */
+ * .. p (window 0: all up to p).  scores = q . k * scale (scale > 0, scale / ln 2 in fp32's range; 0: 1 / sqrt(head_dim)),
+ * soft-max in fp32, weighted sum of V.
+ *   In that sum a bf16 model's weights are bf16: two terms of each where a request has at most 16 (row, query head) pairs per
+ * kv head, by the plan's max_rows_per_seq, and where head_dim is 256, so that only the result's rounding is left; else one term
+ * (a row's error is then that of two roundings to bf16).  An fp32 model's weights are fp32.
+ *   dev_out [n_rows][n_heads][head_dim] contiguous, apart from dev_q (EE_ERR_ARG where the ranges overlap); dev_lse
+ * [n_rows][n_heads] fp32 or NULL: log sum exp of the row's scores, with which results over several caches can be joined.  A
+ * row that sees nothing (its request was refused, or it belongs to none) gets zeros and -inf.  NaN in positions that a row does
+ * not see do not reach it. */
 int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride, int64_t q_head_stride, void* dev_out, float* dev_lse,
                   float scale, int window, void* stream);
 

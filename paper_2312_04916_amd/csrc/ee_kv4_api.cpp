@@ -256,7 +256,8 @@ int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride,
     const int rc = check_rows(c, layer, 0);
     if (rc != EE_OK) return rc;
     if (c->n_seqs == 0) return EE_ERR_STATE;
-    if (!(scale >= 0.f) || std::isinf(scale) || window < 0) return EE_ERR_ARG;
+    const float scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt((float)c->cfg.head_dim)) * 1.4426950408889634f;
+    if (!(scale >= 0.f) || std::isinf(scale_log2) || window < 0) return EE_ERR_ARG;
     if (c->n_rows == 0) return EE_OK;
     const ee_kv4_config& g = c->cfg;
     const uintptr_t es = g.dtype == EE_BF16 ? 2 : 4;
@@ -275,8 +276,8 @@ int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride,
     a.n_parts = c->arrays.n_free + 1;
     a.q = dev_q, a.q_row = q_row_stride, a.q_head = q_head_stride;
     a.out = dev_out, a.lse = dev_lse;
-    a.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt((float)g.head_dim)) * 1.4426950408889634f;
-    a.slack = std::min(8.f / a.scale_log2, 1e30f);
+    a.scale_log2 = scale_log2;
+    a.slack = std::min(8.f / scale_log2, 1e30f);
     a.window = window, a.group = g.n_heads / g.n_kv_heads, a.kv_heads = g.n_kv_heads, a.min_chunks = c->min_chunks;
     a.group_magic = magic_of((uint32_t)a.group);
     a.tiles_shift = __builtin_ctz((unsigned)g.block_tokens) - 4;

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import kv4_reference as ref
+import paper_2312_04916_amd as ee
 from test_gpu_kv4 import Requests, dev
 
 pytestmark = pytest.mark.gpu
@@ -113,4 +114,18 @@ def test_a_query_with_an_infinity(dtype, hd, rows, heads):
     assert torch.isnan(out[1, 0]).all() and torch.isnan(out[0, 1]).all()
     out[1, 0], out[0, 1] = clean[1, 0], clean[0, 1]
     assert torch.equal(out, clean)
+    s.c.close()
+
+
+def test_scales_at_the_end_of_fp32():
+    """The kernels work in units of ln 2: a scale that overflows there is refused (with it a score of 0 was NaN), one that does not
+    is taken."""
+    s = Requests([40], [2], 4, 2, 64, "bf16", 16, seed=36)
+    s.step()
+    s.q.zero_()
+    for scale in (2.4e38, 3.4e38):
+        with pytest.raises(ee.EeError, match="-7"):
+            s.c.attend(0, s.q, scale=scale)
+    out, lse = s.c.attend(0, s.q, scale=2.3e38, lse=True)
+    s.check(out, lse, scale=2.3e38)
     s.c.close()
