@@ -14,8 +14,15 @@ _CODES = {torch.bfloat16: EE_BF16, torch.float32: EE_F32, "bf16": EE_BF16, "f32"
 _LEAST_SCALE = 2.0 ** -149  # of fp32: less would be passed as 0, which stands for the default
 
 
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
 def _raw_stream(stream, index: int) -> int:
-    return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if stream is None:
+        return _current_stream(index)
+    if stream.device_index != index:
+        raise ValueError(f"stream of device {stream.device_index}, expected cuda:{index}")
+    return stream.cuda_stream
 
 
 def _used_on(stream, *tensors) -> None:
@@ -31,8 +38,8 @@ class Kv4Cache:
     [max_seqs + 1], served, held_next [max_seqs], n_free [1]; table [max_seqs][blocks] and free [n_blocks] are the state that
     outlasts it.
 
-    Calls run on torch's current stream, or on `stream`; there the caller orders them after what wrote their inputs, and what reads
-    their results after them."""
+    Calls run on the cache's device, whichever is current, on torch's current stream there or on `stream`; on the latter the
+    caller orders them after what wrote their inputs, and what reads their results after them."""
 
     def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, block_tokens: int, n_blocks: int, max_seqs: int,
                  max_positions: int, max_rows: int, dtype="bf16", device="cuda:0", stream=None):
@@ -49,8 +56,9 @@ class Kv4Cache:
         self._index = self.device.index
         self.pool = self._empty(stream, pb.value, dtype=torch.uint8)
         self.state = self._empty(stream, sb.value, dtype=torch.uint8)
-        _chk(lib().ee_kv4_create(C.byref(cfg), self.pool.data_ptr(), pb.value, self.state.data_ptr(), sb.value, _raw_stream(stream, self._index),
-                                 C.byref(self.h)), "ee_kv4_create")
+        with torch.cuda.device(self._index):
+            _chk(lib().ee_kv4_create(C.byref(cfg), self.pool.data_ptr(), pb.value, self.state.data_ptr(), sb.value,
+                                     _raw_stream(stream, self._index), C.byref(self.h)), "ee_kv4_create")
         a = ee_kv4_arrays()
         _chk(lib().ee_kv4_get_arrays(self.h, C.byref(a)), "ee_kv4_get_arrays")
 
@@ -101,6 +109,9 @@ class Kv4Cache:
              stream=None) -> None:
         """ee_kv4_plan.  held, start, end: int32[n_seqs] on the device; max_rows_per_seq: n_rows where it is not given (the
         attention then works as for long chunks: give 1 for a plain decode step)."""
+        if _current_device() != self._index:  # (the default stream's handle is 0 on every device: a launch goes to the current one)
+            with torch.cuda.device(self._index):
+                return self.plan(held, start, end, n_rows, max_rows_per_seq, stream)
         n = held.shape[0]
         code = self._plan(self.h, n, self._lengths(held, n, "held"), self._lengths(start, n, "start"), self._lengths(end, n, "end"), n_rows,
                           n_rows if max_rows_per_seq is None else max_rows_per_seq, _raw_stream(stream, self._index))
@@ -118,6 +129,9 @@ class Kv4Cache:
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, slots: Optional[torch.Tensor] = None, stream=None) -> None:
         """ee_kv4_append.  k, v: [rows][n_kv_heads][head_dim], any strides of rows and heads; slots: the latest plan's where not
         given."""
+        if _current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.append(layer, k, v, slots, stream)
         rows = k.shape[0]
         kp, kr, kh = self._vectors(k, self._kv_heads, None, "k")
         vp, vr, vh = self._vectors(v, self._kv_heads, rows, "v")
@@ -130,6 +144,9 @@ class Kv4Cache:
 
     def read(self, layer: int, slots: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """ee_kv4_read -> k, v [rows][n_kv_heads][head_dim]: the values that the slots hold."""
+        if _current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.read(layer, slots, stream)
         rows = slots.shape[0]
         p = self._slot_ptr(slots, rows)
         k = self._empty(stream, rows, self._kv_heads, self._head_dim, dtype=self.dtype)
@@ -145,6 +162,9 @@ class Kv4Cache:
                out: Optional[torch.Tensor] = None, stream=None):
         """ee_kv4_attend -> [rows][n_heads][head_dim], with lse=True also log sum exp [rows][n_heads].  q: the rows of the latest
         plan, any strides of rows and heads; scale: 1 / sqrt(head_dim) where not given."""
+        if _current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.attend(layer, q, scale, window, lse, out, stream)
         if scale is not None and not scale >= _LEAST_SCALE:
             raise ValueError("scale: positive, in fp32")
         heads, hd = self._heads, self._head_dim
@@ -164,7 +184,7 @@ class Kv4Cache:
 
     def close(self) -> None:
         if self.h:
-            torch.cuda.synchronize()
+            torch.cuda.synchronize(self.device)
             lib().ee_kv4_free(self.h)
             self.h = C.c_void_p()
 
