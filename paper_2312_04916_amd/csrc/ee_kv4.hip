@@ -1216,9 +1216,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
         if (of_v) {
             scales = *(const EE_GLOBAL uint32_t*)(at + Kv4Tile::v_scales(HD) + (uint32_t)(t16 * EPC / 32 * 16 + quarter * 4));
         } else {
-            const PoolPtr sc = at + Kv4Tile::k_scales(HD) + (uint32_t)(t16 * G);
-            if constexpr (G == 4) scales = *(const EE_GLOBAL uint32_t*)sc;
-            if constexpr (G == 2) scales = *(const EE_GLOBAL uint16_t*)sc;
+            scales = *(const EE_GLOBAL uint32_t*)(at + Kv4Tile::k_scales(HD) + (uint32_t)(t16 * G));
         }
     };
     auto convert = [&](int it, int buf) {
@@ -1443,20 +1441,20 @@ hipError_t attend_waves(const Kv4Attend& a, int dtype, int grid, hipStream_t s) 
     // requests of up to 12 560 positions and 15 rows: 59 us, one step ahead 62; 64 of up to 16 384 and 5 rows: 128, 142).
     constexpr int DEPTH = NW == 8 && HD <= 128 ? 2 : 1, DEPTH_BF16 = UNITS == 2 && HD <= 128 ? 2 : DEPTH;
     const dim3 g(grid), t(NW * 64);
-    if (dtype == EE_BF16) {
-        if constexpr (UNITS == 1)
-            EE_LAUNCH((past ? kv4_attend_kernel<HD, 1, 2, 1, NW, DEPTH_BF16, true, true, __bf16> : kv4_attend_kernel<HD, 1, 2, 1, NW, DEPTH_BF16, false, true, __bf16>),
+    if constexpr (UNITS <= 2)
+        if (dtype == EE_F32) {
+            EE_LAUNCH((past ? kv4_attend_kernel<HD, 3, 3, UNITS, NW, DEPTH, UNITS == 1, true, float>
+                            : kv4_attend_kernel<HD, 3, 3, UNITS, NW, DEPTH, false, true, float>),
                       g, t, s, a);
-        else
-            EE_LAUNCH((a.lse ? kv4_attend_kernel<HD, 1, 1, UNITS, NW, DEPTH_BF16, false, true, __bf16>
-                             : kv4_attend_kernel<HD, 1, 1, UNITS, NW, DEPTH_BF16, false, false, __bf16>),
-                      g, t, s, a);
-    } else if constexpr (UNITS <= 2) {
-        EE_LAUNCH((past ? kv4_attend_kernel<HD, 3, 3, UNITS, NW, DEPTH, UNITS == 1, true, float> : kv4_attend_kernel<HD, 3, 3, UNITS, NW, DEPTH, false, true, float>), g,
+            return hipGetLastError();
+        }
+    if constexpr (UNITS == 1)
+        EE_LAUNCH((past ? kv4_attend_kernel<HD, 1, 2, 1, NW, DEPTH_BF16, true, true, __bf16> : kv4_attend_kernel<HD, 1, 2, 1, NW, DEPTH_BF16, false, true, __bf16>), g,
                   t, s, a);
-    } else {
-        return hipErrorInvalidValue;
-    }
+    else
+        EE_LAUNCH((a.lse ? kv4_attend_kernel<HD, 1, 1, UNITS, NW, DEPTH_BF16, false, true, __bf16>
+                         : kv4_attend_kernel<HD, 1, 1, UNITS, NW, DEPTH_BF16, false, false, __bf16>),
+                  g, t, s, a);
     return hipGetLastError();
 }
 
@@ -1479,7 +1477,7 @@ hipError_t attend_hd(const Kv4Attend& a, int dtype, int units, int waves, int gr
         }
     }
     if constexpr (HD <= 64)
-        if (units == 4) return attend_units<HD, 4>(a, dtype, waves, grid, s);
+        if (units == 4 && dtype == EE_BF16) return attend_units<HD, 4>(a, dtype, waves, grid, s);
     return hipErrorInvalidValue;
 }
 
