@@ -129,3 +129,61 @@ def test_scales_at_the_end_of_fp32():
     out, lse = s.c.attend(0, s.q, scale=2.3e38, lse=True)
     s.check(out, lse, scale=2.3e38)
     s.c.close()
+
+
+@pytest.mark.parametrize("heads,kvh,hd,lengths,rows", [
+    (4, 4, 32, [1, 17, 600], [1, 3, 16]), (8, 1, 64, [2, 90, 9000], [1, 2, 1]), (32, 8, 128, [130, 5001], [4, 1]), (8, 1, 128, [300] * 20, [2] * 20),
+    (2, 1, 256, [33, 700], [1, 8]), (4, 2, 256, [200, 3000], [200, 40]),
+])
+@pytest.mark.parametrize("window", [0, 50])
+def test_tiles_of_16_entries_leave_the_result_s_rounding_only(heads, kvh, hd, lengths, rows, window):
+    """bf16 models, at most 16 entries of a request for a kv head, or 256 elements: the probabilities' second terms leave 2^-16."""
+    assert hd == 256 or max(rows) * heads // kvh <= 16
+    s = Requests(lengths, rows, heads, kvh, hd, "bf16", 32, seed=37)
+    s.step()
+    out = s.c.attend(0, s.q, window=window).cpu().double()
+    at = 0
+    for i, (n, r) in enumerate(zip(lengths, rows)):
+        want, _, weight, z_abs = ref.attend(s.q[at:at + r], ref.held(s.k[i]), ref.held(s.v[i]), list(range(n - r, n)), s.group, hd ** -0.5, window)
+        got = out[at:at + r]
+        half = torch.exp2(torch.floor(torch.log2(torch.maximum(want.abs(), got.abs()))) - 8)  # half a unit of the result's last place
+        assert ((got - want).abs() <= half + weight * ((4 * (hd + 2) * z_abs + n + 64) * 2.0 ** -24 + 2.0 ** -16)).all(), (i, n, r)
+        at += r
+    s.c.close()
+
+
+@pytest.mark.parametrize("heads,kvh,lengths,rows", [(32, 4, [300, 33, 900, 70, 150], [300, 33, 310, 0, 1]), (40, 40, [700, 400], [700, 400]), (96, 1, [260, 700], [100, 180])])
+@pytest.mark.parametrize("window", [0, 1, 150])
+def test_wide_tiles_of_several_requests(heads, kvh, lengths, rows, window):
+    """Tiles of 128 entries: prompts from their start, chunks, single tokens, a request that waits, with heads that share and that do
+    not."""
+    flat = sum(rows) * heads // kvh
+    assert flat * kvh >= 128 * 160 and len(rows) * 64 * 8 <= flat  # the rule: enough of them, and an eighth empty at most
+    s = Requests(lengths, rows, heads, kvh, 128, "bf16", 64, seed=38)
+    s.step()
+    out, lse = s.c.attend(0, s.q, window=window, lse=True)
+    s.check(out, lse, window=window)
+    assert torch.equal(out, s.c.attend(0, s.q, window=window))
+    s.c.close()
+
+
+def test_refused_calls_leave_the_cache_as_it_was():
+    s = Requests([40, 90], [2, 3], 4, 2, 64, "bf16", 16, seed=39)
+    s.step()
+    want = s.c.attend(0, s.q)
+    arrays = [getattr(s.c, a).clone() for a in ("slots", "positions", "row_seq", "row_start", "served", "held_next", "n_free", "table", "free", "pool")]
+    i2, kv = dev([40, 90]), s.k[1][:5]
+    for call in (lambda: s.c.plan(i2, i2, i2, 10 ** 7), lambda: s.c.plan(i2, i2, i2, 5, -1), lambda: s.c.append(3, kv, kv),
+                 lambda: s.c.append(0, s.k[1][:6], s.k[1][:6]), lambda: s.c.attend(7, s.q), lambda: s.c.attend(0, s.q, window=-5),
+                 lambda: s.c.attend(0, s.q, scale=float("inf")), lambda: s.c.attend(0, s.q, out=s.q)):
+        with pytest.raises(ee.EeError):
+            call()
+    for call in (lambda: s.c.plan(i2, i2, i2[:1], 5), lambda: s.c.append(0, kv.float(), kv), lambda: s.c.attend(0, s.q[:4]), lambda: s.c.read(0, i2)):
+        with pytest.raises(ValueError):
+            call()
+    for a, before in zip(("slots", "positions", "row_seq", "row_start", "served", "held_next", "n_free", "table", "free", "pool"), arrays):
+        assert torch.equal(getattr(s.c, a), before), a
+    out = s.c.attend(0, s.q)
+    assert torch.equal(out, want)
+    s.check(out)
+    s.c.close()
