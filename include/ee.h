@@ -394,7 +394,9 @@ int ee_decode_step_static(ee_model* m, ee_kv_cache* c, int n_seqs, const int32_t
  *     ee_kv4_plan    blocks and slots of the step's rows, from the requests' lengths       once
  *     ee_kv4_append  the rows' K and V into the cache                                      per layer
  *     ee_kv4_attend  the rows' attention over what their requests hold                     per layer
- * and nothing in it waits for the GPU, so that it can be captured into a graph.
+ * and nothing in it waits for the GPU, so that it can be captured into a graph.  A captured append or attention belongs to a plan
+ * of the n_rows and max_rows_per_seq that it was captured after: replayed after another one, an attention writes nothing, and
+ * an append only rows that the plan has.
  *
  * The 4 bits: 32 neighbouring elements of one head's vector share a power of two 2^e, e the least integer from -111 to
  * 125 with max|x| <= 7 * 2^e; each element is held as the nearest of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} * 2^e, a tie going to the

@@ -46,7 +46,8 @@ struct Kv4Plan {
     int block_shift, n_blocks, table_stride, max_positions;  // 1 << block_shift positions per block
     ee_kv4_arrays a;
     Kv4Part* parts;
-    int32_t* n_parts;
+    int32_t* counts;    // [2]: parts, shape
+    int32_t shape;      // plan_shape of its rows and tiles
     uint32_t* arrived;  // workgroups that have read the lengths
     int max_parts;  // room in `parts`
     int group, kv_heads, tile_rows, tile_shift;  // tile_rows = 1 << tile_shift
@@ -56,10 +57,15 @@ struct Kv4Plan {
     int whole_shares;  // an item is cut into as many parts as it has shares of the work, else into one more
 };
 
+// What calls of a plan's rows are launched for, and the plan leaves on the device: a captured call that is replayed after another
+// plan would have too few rows of its arrays, or another size of tiles.
+inline int32_t plan_shape(int n_rows, int tile_units) { return n_rows | tile_units << 24; }  // (n_rows <= 2^20, tile_units <= 8)
+
 struct Kv4Cache {
     char* layer;  // this layer's pool
     int kv_heads, head_dim, block_shift, dtype;  // 1 << block_shift positions per block
     int64_t n_slots;
+    const int32_t* counts;  // the plan's
 };
 
 struct Kv4Attend {
@@ -67,7 +73,8 @@ struct Kv4Attend {
     const int32_t* table;
     int table_stride;
     const Kv4Part* parts;
-    const int32_t* n_parts;
+    const int32_t* counts;  // the plan's
+    int32_t shape, grid;  // of the launch
     const void* q;
     int64_t q_row, q_head;
     void* out;
@@ -98,7 +105,7 @@ hipError_t launch_kv4_init(int32_t* table, int64_t n_table, int32_t* free_blocks
                            uint32_t* counts, hipStream_t s);
 hipError_t launch_kv4_plan(const Kv4Plan& p, int workgroups, int threads, hipStream_t s);
 hipError_t launch_kv4_append(const Kv4Cache& c, int n_rows, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row,
-                             int64_t v_head, const int64_t* slots, hipStream_t s);
+                             int64_t v_head, const int64_t* slots, bool of_plan, hipStream_t s);
 hipError_t launch_kv4_read(const Kv4Cache& c, int n_rows, const int64_t* slots, void* k, void* v, hipStream_t s);
 hipError_t launch_kv4_attend(const Kv4Attend& a, int dtype, int head_dim, int units, int waves, int grid, hipStream_t s);
 

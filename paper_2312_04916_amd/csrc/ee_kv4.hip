@@ -44,7 +44,7 @@ __global__ void kv4_init_kernel(int32_t* table, int64_t n_table, int32_t* free_b
     for (int64_t i = i0; i < n_table; i += step) table[i] = 0;
     for (int64_t i = i0; i < n_blocks; i += step) free_blocks[i] = n_blocks - 1 - (int)i;  // block 0 is on top
     for (int64_t i = i0; i < n_arrived; i += step) arrived[i] = 0;
-    if (i0 < 3) counts[i0] = i0 == 0 ? n_blocks : 0;
+    if (i0 < 4) counts[i0] = i0 == 0 ? n_blocks : 0;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
     }
     __syncthreads();
     const int n_parts = min(cnt_all[0], p.max_parts);
-    if (first_wg && tid == 0) *p.n_parts = n_parts, *p.a.n_free = have - taken, p.a.row_start[n] = rows_all;
+    if (first_wg && tid == 0) p.counts[0] = n_parts, p.counts[1] = p.shape, *p.a.n_free = have - taken, p.a.row_start[n] = rows_all;
 
     // entry `at` of the stack as it stands once everything given back lies on it
     auto stack = [&](int at) {
@@ -372,13 +372,14 @@ __device__ __forceinline__ uint32_t rows4_umax(uint32_t v) {
 template <int HD, typename ST>
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Cache c, int n_rows, const ST* __restrict__ k, int64_t k_row, int64_t k_head,
                                                          const ST* __restrict__ v, int64_t v_row, int64_t v_head, int vec,
-                                                         const int64_t* __restrict__ slots) {
+                                                         const int64_t* __restrict__ slots, int rows_given) {
     constexpr int G = HD / 32, LB = HD / 8;
     const int lane = threadIdx.x & 63, h = lane >> 4;
     const uint32_t vecs = blockIdx.x * 4u + (threadIdx.x >> 6);
     const int which = vecs & 1, head = (int)((vecs >> 1) % (uint32_t)c.kv_heads);
     const int64_t row = (int64_t)((vecs >> 1) / (uint32_t)c.kv_heads) * 16 + (lane & 15);
     const bool there = row < n_rows;
+    const int plan_rows = max(c.counts[1] & 0xffffff, rows_given);
     const int64_t slot = there ? slots[row] : -1;
     float x[G][8] = {};
     if (there) {
@@ -404,7 +405,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Cache c, int n_rows,
         code[g] = w;
         if (top >= 0x7f800000u) sc[g] = SCALE_NAN;
     }
-    if (slot < 0 || slot >= c.n_slots) return;
+    if (slot < 0 || slot >= c.n_slots || row >= plan_rows) return;  // (the plan's slots behind its rows are those of a plan before)
     int key;
     char* tile = tile_of<HD>(c, slot, head, key);
     if (which == 0) {
@@ -619,6 +620,13 @@ __device__ __forceinline__ float add_pair(uint32_t pair, float l) {
 // parts that are joined at a time: all, or of many about their number's square root
 __device__ __forceinline__ int fan_shift_of(int n_parts) { return n_parts <= 16 ? 4 : n_parts <= 64 ? 3 : n_parts <= 256 ? 4 : 5; }
 
+// The workgroup has a part, of a plan that the launch was made for: else nobody writes, so that no array is left and no counter of
+// parts stays behind.
+__device__ __forceinline__ bool of_this_plan(const Kv4Attend& a) {
+    const u32x2 counts = *(const u32x2*)a.counts;  // (in one load, beside that of the part)
+    return (blockIdx.x < counts[0]) & (counts[0] <= (uint32_t)a.grid) & (counts[1] == (uint32_t)a.shape);
+}
+
 // row of an entry in its request; where the entry's results go
 __device__ __forceinline__ int row_of(const Kv4Attend& a, int f) { return (int)div_by((uint32_t)f, (uint32_t)a.group, a.group_magic); }
 __device__ __forceinline__ size_t out_row(const Kv4Attend& a, const Kv4Part& w, int f) {
@@ -808,7 +816,7 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
     __shared__ uint32_t s_last;
 
     const Kv4Part w = a.parts[blockIdx.x];  // (there is room for as many as the grid has; asked for together with their number)
-    if ((int)blockIdx.x >= *a.n_parts) return;
+    if (!of_this_plan(a)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const int f0 = w.tile * M, f_end = min(w.n_flat, f0 + M);  // entries
@@ -1148,7 +1156,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     __shared__ uint32_t s_last;
 
     const Kv4Part w = a.parts[blockIdx.x];
-    if ((int)blockIdx.x >= *a.n_parts) return;
+    if (!of_this_plan(a)) return;
     const int lane = threadIdx.x & 63, group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3;
     const int col = lane & 31, half = lane >> 5;
     const int f0 = w.tile * M, f_end = min(w.n_flat, f0 + M);
@@ -1487,17 +1495,17 @@ inline bool aligned16(const void* p, int64_t row, int64_t head, int es) {
 
 template <int HD>
 hipError_t append_hd(const Kv4Cache& c, int n_rows, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row, int64_t v_head,
-                     const int64_t* slots, hipStream_t s) {
+                     const int64_t* slots, bool of_plan, hipStream_t s) {
     const int es = c.dtype == EE_BF16 ? 2 : 4;
     const int vec = (aligned16(k, k_row, k_head, es) ? 1 : 0) | (aligned16(v, v_row, v_head, es) ? 2 : 0);
     const int64_t waves = (int64_t)((n_rows + 15) / 16) * c.kv_heads * 2;
     const dim3 grid((unsigned)((waves + 3) / 4));
     if (c.dtype == EE_BF16)
         EE_LAUNCH((kv4_append_kernel<HD, __bf16>), grid, dim3(256), s, c, n_rows, (const __bf16*)k, k_row, k_head, (const __bf16*)v, v_row, v_head,
-                  vec, slots);
+                  vec, slots, of_plan ? 0 : n_rows);
     else
         EE_LAUNCH((kv4_append_kernel<HD, float>), grid, dim3(256), s, c, n_rows, (const float*)k, k_row, k_head, (const float*)v, v_row, v_head, vec,
-                  slots);
+                  slots, of_plan ? 0 : n_rows);
     return hipGetLastError();
 }
 
@@ -1547,12 +1555,12 @@ hipError_t launch_kv4_plan(const Kv4Plan& p, int workgroups, int threads, hipStr
 }
 
 hipError_t launch_kv4_append(const Kv4Cache& c, int n_rows, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row,
-                             int64_t v_head, const int64_t* slots, hipStream_t s) {
+                             int64_t v_head, const int64_t* slots, bool of_plan, hipStream_t s) {
     switch (c.head_dim) {
-        case 32: return append_hd<32>(c, n_rows, k, k_row, k_head, v, v_row, v_head, slots, s);
-        case 64: return append_hd<64>(c, n_rows, k, k_row, k_head, v, v_row, v_head, slots, s);
-        case 128: return append_hd<128>(c, n_rows, k, k_row, k_head, v, v_row, v_head, slots, s);
-        case 256: return append_hd<256>(c, n_rows, k, k_row, k_head, v, v_row, v_head, slots, s);
+        case 32: return append_hd<32>(c, n_rows, k, k_row, k_head, v, v_row, v_head, slots, of_plan, s);
+        case 64: return append_hd<64>(c, n_rows, k, k_row, k_head, v, v_row, v_head, slots, of_plan, s);
+        case 128: return append_hd<128>(c, n_rows, k, k_row, k_head, v, v_row, v_head, slots, of_plan, s);
+        case 256: return append_hd<256>(c, n_rows, k, k_row, k_head, v, v_row, v_head, slots, of_plan, s);
         default: return hipErrorInvalidValue;
     }
 }

@@ -93,7 +93,7 @@ StateLayout state_layout(const ee_kv4_config& c) {
     w.row_start = take(((size_t)c.max_seqs + 1) * 4);
     w.served = take((size_t)c.max_seqs * 4);
     w.held_next = take((size_t)c.max_seqs * 4);
-    w.counts = take(12);  // free blocks, parts, the plan's workgroups that have read the lengths
+    w.counts = take(16);  // free blocks, the plan's workgroups that have read the lengths, parts, the plan's shape
     w.max_parts = most_parts(c, c.max_seqs, c.max_rows, 16);
     w.parts = take((size_t)w.max_parts * sizeof(Kv4Part));
     w.max_slots = 2 * MOST_PARTS + 64;
@@ -195,11 +195,12 @@ int ee_kv4_plan(ee_kv4* c, int n_seqs, const int32_t* dev_held, const int32_t* d
     p.block_shift = __builtin_ctz((unsigned)g.block_tokens), p.n_blocks = g.n_blocks, p.table_stride = c->arrays.table_stride, p.max_positions = g.max_positions;
     p.a = c->arrays;
     p.parts = (Kv4Part*)(c->state + c->sl.parts);
-    p.n_parts = c->arrays.n_free + 1;
-    p.arrived = (uint32_t*)c->arrays.n_free + 2;
+    p.arrived = (uint32_t*)c->arrays.n_free + 1;
+    p.counts = c->arrays.n_free + 2;
     p.group = group, p.kv_heads = g.n_kv_heads;
     const int units = kv4_tile_units(g.dtype, g.head_dim, (int)std::min<int64_t>((int64_t)most * group, 1 << 30), n_seqs, (int64_t)n_rows * group,
                                      g.n_kv_heads);
+    p.shape = plan_shape(n_rows, units);
     p.tile_rows = 16 * units, p.tile_shift = __builtin_ctz((unsigned)p.tile_rows), p.kv_magic = magic_of((uint32_t)g.n_kv_heads);
     p.max_parts = (int)std::min(c->sl.max_parts, most_parts(g, n_seqs, n_rows, p.tile_rows));
     const Cut cut = cut_of(g, n_seqs, n_rows, units);
@@ -227,6 +228,7 @@ static Kv4Cache geometry(const ee_kv4* c, int layer) {
     k.layer = c->pool + layer_bytes(c->cfg) * layer;
     k.kv_heads = c->cfg.n_kv_heads, k.head_dim = c->cfg.head_dim, k.block_shift = __builtin_ctz((unsigned)c->cfg.block_tokens), k.dtype = c->cfg.dtype;
     k.n_slots = (int64_t)c->cfg.n_blocks * c->cfg.block_tokens;
+    k.counts = c->arrays.n_free + 2;
     return k;
 }
 
@@ -240,7 +242,7 @@ int ee_kv4_append(ee_kv4* c, int layer, int n_rows, const void* dev_k, int64_t k
     const uintptr_t es = c->cfg.dtype == EE_BF16 ? 2 : 4;
     if (!dev_k || !dev_v || ((uintptr_t)dev_k | (uintptr_t)dev_v) & (es - 1) || (uintptr_t)dev_slots & 7) return EE_ERR_ARG;
     return hip_status(launch_kv4_append(geometry(c, layer), n_rows, dev_k, k_row_stride, k_head_stride, dev_v, v_row_stride, v_head_stride,
-                                        dev_slots ? dev_slots : c->arrays.slots, (hipStream_t)stream));
+                                        dev_slots ? dev_slots : c->arrays.slots, !dev_slots, (hipStream_t)stream));
 }
 
 int ee_kv4_read(ee_kv4* c, int layer, int n_rows, const int64_t* dev_slots, void* dev_k, void* dev_v, void* stream) {
@@ -273,7 +275,8 @@ int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride,
     a.layer = c->pool + layer_bytes(g) * layer;
     a.table = c->arrays.table, a.table_stride = c->arrays.table_stride;
     a.parts = (const Kv4Part*)(c->state + c->sl.parts);
-    a.n_parts = c->arrays.n_free + 1;
+    a.counts = c->arrays.n_free + 2;
+    a.shape = plan_shape(c->n_rows, c->units);
     a.q = dev_q, a.q_row = q_row_stride, a.q_head = q_head_stride;
     a.out = dev_out, a.lse = dev_lse;
     a.scale_log2 = scale_log2;
@@ -290,8 +293,8 @@ int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride,
     a.joined_l = a.part_l + c->sl.part_rows;
     a.arrived = (uint32_t*)(c->state + c->sl.arrived);
     a.arrived_groups = a.arrived + c->sl.max_slots;
-    const int grid = (int)std::min(c->sl.max_parts, most_parts(g, c->n_seqs, c->n_rows, 16 * c->units));
-    return hip_status(launch_kv4_attend(a, g.dtype, g.head_dim, c->units, c->waves, grid, (hipStream_t)stream));
+    a.grid = (int)std::min(c->sl.max_parts, most_parts(g, c->n_seqs, c->n_rows, 16 * c->units));
+    return hip_status(launch_kv4_attend(a, g.dtype, g.head_dim, c->units, c->waves, a.grid, (hipStream_t)stream));
 }
 
 }  // extern "C"

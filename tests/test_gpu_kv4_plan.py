@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import kv4_reference as ref
-from test_gpu_kv4 import cache_of, check_plan, rand
+from test_gpu_kv4 import Requests, cache_of, check_plan, dev, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,58 @@ def test_rows_that_begin_behind_what_is_held_are_refused(n_more):
     out, lse = c.attend(0, q, lse=True)
     assert not out[[0, 1, 4]].any() and torch.isneginf(lse[[0, 1, 4]]).all()
     c.close()
+
+
+def captured(call):
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    return graph
+
+
+def test_captured_calls_after_another_plan():
+    """Graphs of an attention and of an append alone, replayed after plans of fewer and of more rows, of other tiles, and of their own
+    shape: arrays that are too short for the plan are not touched, nor rows of a plan before, and later calls are not disturbed."""
+    heads, kvh, hd, n = 160, 2, 128, 1500
+    s = Requests([n, 400], [2, 1], heads, kvh, hd, "bf16", 64, seed=41)
+
+    def step(rows):
+        s.rows = rows
+        s.q = rand((sum(rows), heads, hd), "bf16", 42 + sum(rows))
+        s.step()
+        return s.q, torch.full_like(s.q, 7.0)
+
+    shapes = ([2, 1], [2, 2], [40, 3], [140, 10])  # 3 and 4 rows of tiles of 32 entries (80 heads a kv head), wide tiles
+    graphs = []
+    for rows in shapes:
+        q, out = step(rows)
+        graphs.append((captured(lambda: s.c.attend(0, q, out=out)), q, out))
+    for planned in (3, 0, 1, 2, 3, 0):
+        q, _ = step(shapes[planned])
+        for i, (graph, gq, out) in enumerate(graphs):
+            out.fill_(7.0)
+            gq.copy_(q) if i == planned else None
+            graph.replay()
+            torch.cuda.synchronize()
+            if i == planned:
+                s.check(out)
+                assert torch.equal(out, s.c.attend(0, q))
+            else:
+                assert (out == 7.0).all(), (planned, i)
+    # an append of five rows after a plan of two: slots 2 .. 4 are still those of the plan before
+    kv = rand((5, kvh, hd), "bf16", 50)
+    lengths = dev([n, 400])
+    s.c.plan(lengths, dev([n - 5, 400]), lengths, 5)
+    graph = captured(lambda: s.c.append(0, kv, kv))
+    written = [t.clone() for t in s.c.read(0, s.c.slots[:5].clone())]
+    slots = s.c.slots[:5].clone()
+    s.c.plan(lengths, dev([n, 398]), lengths, 2)
+    kv.mul_(2)
+    graph.replay()
+    k, v = s.c.read(0, slots)
+    assert torch.equal(k, written[0]) and torch.equal(v, written[1])
+    k, _ = s.c.read(0, s.c.slots[:2].clone())
+    assert torch.equal(k.cpu().double(), ref.held(kv[:2]))
+    s.c.close()
