@@ -467,9 +467,9 @@ int ee_kv4_get_arrays(const ee_kv4* c, ee_kv4_arrays* out);
 int ee_kv4_plan(ee_kv4* c, int n_seqs, const int32_t* dev_held, const int32_t* dev_start, const int32_t* dev_end, int n_rows,
                 int max_rows_per_seq, void* stream);
 
-/* K and V of n_rows rows into the slots dev_slots[n_rows] (NULL: the latest plan's, n_rows at most its).  Element (row, head,
- * i) of K lies at dev_k[row * k_row_stride + head * k_head_stride + i]; strides in elements.  Rows whose slot is negative or
- * beyond the pool are skipped.  No slot may occur twice in a call. */
+/* K and V of n_rows rows (2^22 at most, here and in ee_kv4_read) into the slots dev_slots[n_rows] (NULL: the latest plan's,
+ * n_rows at most its).  Element (row, head, i) of K lies at dev_k[row * k_row_stride + head * k_head_stride + i]; strides in
+ * elements.  Rows whose slot is negative or beyond the pool are skipped.  No slot may occur twice in a call. */
 int ee_kv4_append(ee_kv4* c, int layer, int n_rows, const void* dev_k, int64_t k_row_stride, int64_t k_head_stride,
                   const void* dev_v, int64_t v_row_stride, int64_t v_head_stride, const int64_t* dev_slots, void* stream);
 

@@ -372,14 +372,14 @@ __device__ __forceinline__ uint32_t rows4_umax(uint32_t v) {
 template <int HD, typename ST>
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Cache c, int n_rows, const ST* __restrict__ k, int64_t k_row, int64_t k_head,
                                                          const ST* __restrict__ v, int64_t v_row, int64_t v_head, int vec,
-                                                         const int64_t* __restrict__ slots, int rows_given) {
+                                                         const int64_t* __restrict__ slots, int rows_given, int row0) {
     constexpr int G = HD / 32, LB = HD / 8;
     const int lane = threadIdx.x & 63, h = lane >> 4;
     const uint32_t vecs = blockIdx.x * 4u + (threadIdx.x >> 6);
     const int which = vecs & 1, head = (int)((vecs >> 1) % (uint32_t)c.kv_heads);
-    const int64_t row = (int64_t)((vecs >> 1) / (uint32_t)c.kv_heads) * 16 + (lane & 15);
+    const int64_t row = row0 + (int64_t)((vecs >> 1) / (uint32_t)c.kv_heads) * 16 + (lane & 15);
     const bool there = row < n_rows;
-    const int plan_rows = max(c.counts[1] & 0xffffff, rows_given);
+    const int plan_rows = max(c.counts[1] & 0xffffff, rows_given);  // (rows_given: 0 if the slots are the plan's)
     const int64_t slot = there ? slots[row] : -1;
     float x[G][8] = {};
     if (there) {
@@ -442,14 +442,14 @@ struct Kv4Work {
     int64_t row;
 };
 template <int TPV>
-__device__ __forceinline__ Kv4Work work_of(int kv_heads) {
+__device__ __forceinline__ Kv4Work work_of(int kv_heads, int row0) {
     const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
     const uint32_t in = (uint32_t)(idx % (16 * TPV)), vec = (uint32_t)(idx / (16 * TPV));
     Kv4Work w;
     w.e8 = in % TPV;
     w.which = vec & 1;
     w.head = (vec >> 1) % (uint32_t)kv_heads;
-    w.row = (int64_t)((vec >> 1) / (uint32_t)kv_heads) * 16 + in / TPV;
+    w.row = row0 + (int64_t)((vec >> 1) / (uint32_t)kv_heads) * 16 + in / TPV;
     return w;
 }
 
@@ -464,9 +464,9 @@ __device__ __forceinline__ void values8(uint32_t w, uint32_t sc, bf16x2 (&x)[4])
 
 template <int HD, typename ST>
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Cache c, int n_rows, const int64_t* __restrict__ slots, ST* __restrict__ k,
-                                                       ST* __restrict__ v) {
+                                                       ST* __restrict__ v, int row0) {
     constexpr int TPV = HD / 8, LB = HD / 8;
-    const Kv4Work w = work_of<TPV>(c.kv_heads);
+    const Kv4Work w = work_of<TPV>(c.kv_heads, row0);
     const int e8 = w.e8, which = w.which, head = w.head;
     const int64_t row = w.row;
     if (row >= n_rows) return;
@@ -1493,30 +1493,39 @@ inline bool aligned16(const void* p, int64_t row, int64_t head, int es) {
     return ((uintptr_t)p & 15) == 0 && (row * es) % 16 == 0 && (head * es) % 16 == 0;
 }
 
+// rows of a launch: a grid has less than 2^32 threads (half as many here)
+inline int rows_of_launch(int n_rows, int threads_per_row) { return std::min(n_rows, (int)((1ll << 31) / threads_per_row) & ~15); }
+
 template <int HD>
 hipError_t append_hd(const Kv4Cache& c, int n_rows, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row, int64_t v_head,
                      const int64_t* slots, bool of_plan, hipStream_t s) {
     const int es = c.dtype == EE_BF16 ? 2 : 4;
     const int vec = (aligned16(k, k_row, k_head, es) ? 1 : 0) | (aligned16(v, v_row, v_head, es) ? 2 : 0);
-    const int64_t waves = (int64_t)((n_rows + 15) / 16) * c.kv_heads * 2;
-    const dim3 grid((unsigned)((waves + 3) / 4));
-    if (c.dtype == EE_BF16)
-        EE_LAUNCH((kv4_append_kernel<HD, __bf16>), grid, dim3(256), s, c, n_rows, (const __bf16*)k, k_row, k_head, (const __bf16*)v, v_row, v_head,
-                  vec, slots, of_plan ? 0 : n_rows);
-    else
-        EE_LAUNCH((kv4_append_kernel<HD, float>), grid, dim3(256), s, c, n_rows, (const float*)k, k_row, k_head, (const float*)v, v_row, v_head, vec,
-                  slots, of_plan ? 0 : n_rows);
+    const int each = rows_of_launch(n_rows, c.kv_heads * 2 * 64 / 16);
+    for (int row0 = 0; row0 < n_rows; row0 += each) {
+        const int64_t waves = (int64_t)((std::min(each, n_rows - row0) + 15) / 16) * c.kv_heads * 2;
+        const dim3 grid((unsigned)((waves + 3) / 4));
+        if (c.dtype == EE_BF16)
+            EE_LAUNCH((kv4_append_kernel<HD, __bf16>), grid, dim3(256), s, c, n_rows, (const __bf16*)k, k_row, k_head, (const __bf16*)v, v_row, v_head,
+                      vec, slots, of_plan ? 0 : n_rows, row0);
+        else
+            EE_LAUNCH((kv4_append_kernel<HD, float>), grid, dim3(256), s, c, n_rows, (const float*)k, k_row, k_head, (const float*)v, v_row, v_head, vec,
+                      slots, of_plan ? 0 : n_rows, row0);
+    }
     return hipGetLastError();
 }
 
 template <int HD>
 hipError_t read_hd(const Kv4Cache& c, int n_rows, const int64_t* slots, void* k, void* v, hipStream_t s) {
-    const int64_t threads = (int64_t)((n_rows + 15) / 16 * 16) * c.kv_heads * 2 * (HD / 8);
-    const dim3 grid((unsigned)((threads + 255) / 256));
-    if (c.dtype == EE_BF16)
-        EE_LAUNCH((kv4_read_kernel<HD, __bf16>), grid, dim3(256), s, c, n_rows, slots, (__bf16*)k, (__bf16*)v);
-    else
-        EE_LAUNCH((kv4_read_kernel<HD, float>), grid, dim3(256), s, c, n_rows, slots, (float*)k, (float*)v);
+    const int per_row = c.kv_heads * 2 * (HD / 8), each = rows_of_launch(n_rows, per_row);
+    for (int row0 = 0; row0 < n_rows; row0 += each) {
+        const int64_t threads = (int64_t)((std::min(each, n_rows - row0) + 15) / 16 * 16) * per_row;
+        const dim3 grid((unsigned)((threads + 255) / 256));
+        if (c.dtype == EE_BF16)
+            EE_LAUNCH((kv4_read_kernel<HD, __bf16>), grid, dim3(256), s, c, n_rows, slots, (__bf16*)k, (__bf16*)v, row0);
+        else
+            EE_LAUNCH((kv4_read_kernel<HD, float>), grid, dim3(256), s, c, n_rows, slots, (float*)k, (float*)v, row0);
+    }
     return hipGetLastError();
 }
 

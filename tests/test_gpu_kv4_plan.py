@@ -87,7 +87,8 @@ def test_captured_calls_after_another_plan():
         q, _ = step(shapes[planned])
         for i, (graph, gq, out) in enumerate(graphs):
             out.fill_(7.0)
-            gq.copy_(q) if i == planned else None
+            if i == planned:
+                gq.copy_(q)
             graph.replay()
             torch.cuda.synchronize()
             if i == planned:

@@ -5,7 +5,7 @@ import torch
 
 import kv4_reference as ref
 import paper_2312_04916_amd as ee
-from test_gpu_kv4 import Requests, dev
+from test_gpu_kv4 import Requests, cache_of, dev, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -187,3 +187,23 @@ def test_refused_calls_leave_the_cache_as_it_was():
     assert torch.equal(out, want)
     s.check(out)
     s.c.close()
+
+
+def test_rows_beyond_the_threads_of_a_launch():
+    """2^22 rows of 128 heads: 2^32 threads and more.  K and V are one row for all; few rows have a slot."""
+    kvh, hd, n = 128, 32, 1 << 22
+    c = cache_of(kvh, kvh, hd, "bf16", 16, 4)
+    row = rand((2, 1, kvh, hd), "bf16", 40)
+    with_slot = torch.tensor([0, 17, n // 2 + 5, n - 1], device="cuda:0")
+    slots = torch.full((n,), -1, dtype=torch.int64, device="cuda:0")
+    slots[with_slot] = dev([5, 0, 63, 20], torch.int64)
+    c.append(0, row[0].expand(n, kvh, hd), row[1].expand(n, kvh, hd), slots)
+    for got, want in zip(c.read(0, slots[with_slot]), row):
+        assert torch.equal(got.cpu().double(), ref.held(want).expand(4, kvh, hd))
+    k = torch.full((n, kvh, hd), 7.0, dtype=torch.bfloat16, device="cuda:0")
+    stream = torch.cuda.current_stream().cuda_stream
+    assert ee.lib().ee_kv4_read(c.h, 0, n, slots.data_ptr(), k.data_ptr(), None, stream) == 0
+    assert torch.equal(k[with_slot].cpu().double(), ref.held(row[0]).expand(4, kvh, hd))
+    k[with_slot] = 0
+    assert not k.view(torch.int64).any()
+    c.close()
