@@ -78,10 +78,11 @@ def test_a_dominant_position_keeps_its_weight(hd, rows, heads, lse):
     (32, 4, 2, [1, 40, 333], [1, 3, 2]), (64, 2, 2, [90, 400], [20, 25]), (64, 4, 1, [70, 900], [33, 64]), (128, 4, 2, [65, 300], [9, 12]),
     (256, 2, 1, [500, 33], [3, 20]), (128, 160, 2, [300], [130]),
     (128, 4, 1, [9000, 700, 5001], [3, 1, 3]), (128, 2, 2, [9000, 700, 5001], [40, 1, 40]), (64, 64, 2, [5001, 400], [260, 3]), (128, 64, 2, [9001, 700], [64, 600]),
+    (128, 64, 2, [40001, 700], [8, 640]),  # about 26 parts of wide tiles: joined in groups, then these
 ])
 def test_the_log_sum_exp_is_that_of_unrounded_probabilities(hd, heads, kvh, lengths, rows):
     """With bf16 models too: only the products of 16-bit numbers and sums in fp32 stand between the scores and it.  Tiles of all
-    sizes, whole and cut."""
+    sizes, whole and cut; joined at once and in groups."""
     s = Requests(lengths, rows, heads, kvh, hd, "bf16", 32, seed=35)
     s.step()
     out, lse = s.c.attend(0, s.q, lse=True)
