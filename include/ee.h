@@ -460,9 +460,9 @@ int ee_kv4_get_arrays(const ee_kv4* c, ee_kv4_arrays* out);
  *   no block.
  *   The call is a function of the lengths, the table and the stack: called again with the same lengths it gives the same.
  * n_rows: rows that the caller has room for (0 <= n_rows <= max_rows of the config); rows beyond the requests' have slot -1, a
- * request whose rows do not fit is refused (one that brings none is not: it ends or waits).  max_rows_per_seq: most rows that a request brings (a request with more is
- * refused); the attention's tiles, and with them its speed and the bits of a bf16 model's weights, follow from it: give 1 for a plain
- * decode step.
+ * request whose rows do not fit is refused (one that brings none is not: it ends or waits).  max_rows_per_seq: most rows that a
+ * request brings (a request with more is refused); the attention's tiles, and with them its speed and the bits of a bf16
+ * model's weights, follow from it: give 1 for a plain decode step.
  * dev_held may be the held_next array of the plan before. */
 int ee_kv4_plan(ee_kv4* c, int n_seqs, const int32_t* dev_held, const int32_t* dev_start, const int32_t* dev_end, int n_rows,
                 int max_rows_per_seq, void* stream);

@@ -115,13 +115,13 @@ __device__ __forceinline__ int last_not_above(const int32_t* first, int n, int32
 // Blocks of a request: before ceil(held / B), after ceil(end / B); which ones go where follows from three running sums over the
 // requests (given back, asked for, rows) and from which of them are served, which again is a running sum's comparison.
 // Every workgroup forms the sums over all requests for itself (a few thousand lengths at most: cheaper than handing them on)
-// and takes its share of what has to be written, one thread per row, block and part, which finds its request by a search in LDS.  What a workgroup reads, no other one
-// writes: a block that one request gives back and another one takes is looked up in the table row of the first, behind what it
-// keeps, which nothing changes; and held_next, which may be where the lengths are read, is written by the workgroup that is
-// the last to have read them.  All sums fit 32 bits: a request has at most 2^16 blocks, and a thread's rows are counted up to
-// n_rows + 1, at most 2^20 + 1.
-// Bound by latency: lengths, sums, search, table, store, one after the other.  16 requests with 38 rows 4.8 us, of which an empty
-// launch is 3.5; 1000 requests with 6 800 rows 7.9 us; 200 that bring prompts of up to 2048 rows 8.2 us for 2.3 MB.
+// and takes its share of what has to be written, one thread per row, block and part, which finds its request by a search in
+// LDS.  What a workgroup reads, no other one writes: a block that one request gives back and another one takes is looked up in
+// the table row of the first, behind what it keeps, which nothing changes; and held_next, which may be where the lengths are
+// read, is written by the workgroup that is the last to have read them.  All sums fit 32 bits: a request has at most 2^16
+// blocks, and a thread's rows are counted up to n_rows + 1, at most 2^20 + 1.
+// Bound by latency: lengths, sums, search, table, store, one after the other.  16 requests with 38 rows 4.9 us, of which an empty
+// launch is 3.5; 1000 requests with 6 800 rows 8.0 us; 200 that bring prompts of up to 2048 rows 8.3 us for 2.3 MB.
 constexpr int SERVED = 1 << 30, BLOCKS = SERVED - 1;  // in s_had
 __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
     __shared__ int32_t s_row[PLAN_SEQS + 1];    // first row
@@ -159,8 +159,8 @@ __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
     const int left = max(0, p.n_blocks - all[0]);  // free before the call (the lengths may contradict the pool)
     const bool clipped = all[3] > p.n_rows;
     if (clipped) {
-        // rows that do not fit: their requests are refused, and give and take nothing (no rows always fit: a request that ends gives
-        // its blocks back)
+        // rows that do not fit: their requests are refused, and give and take nothing (no rows always fit: a request that ends
+        // gives its blocks back)
         int row = sum[3], again[4] = {0, 0, 0, 0};
         for (int i = i0; i < i1; ++i) {
             const int rows = s_row[i];
@@ -204,9 +204,9 @@ __global__ __launch_bounds__(1024) void kv4_plan_kernel(Kv4Plan p) {
     work = wave_sum(lane < nt >> 6 ? s_work[lane] : 0.f);
     taken = lanes_max(lane < nt >> 6 ? s_taken[lane] : 0);
     // chunks of a part: an even share of the work.  Where the parts all run at once, more of them would run after the others have
-    // ended: an item is cut into as many parts as it has shares, three quarters of one counting (17 requests of up to 12 560
-    // positions and 15 rows: 61 us; with whole shares only, and parts of nearly two, 69; with halves counting too, 67, and 175 rows
-    // of one request 19.8 for 16.5).  Else into one more, so that none is longer than a share.
+    // ended: an item is cut into as many parts as it has shares, three quarters of one counting (17 requests of 500 to 12 560
+    // positions, 32 heads on 8: 15 rows each 61 us, 1 to 15 rows 44; with whole shares only, and parts of nearly two, 68 and 44;
+    // with halves counting too, 66 and 52).  Else into one more, so that none is longer than a share.
     const int per_part = max(p.min_chunks, (int)fminf(65536.f, ceilf(work * (float)p.kv_heads / (float)p.target_parts)));
     const int round_up = p.whole_shares ? per_part / 4 : per_part - 1;
 
@@ -364,11 +364,12 @@ __device__ __forceinline__ uint32_t rows4_umax(uint32_t v) {
 }
 
 // One wave per 16 rows of one head of K or of V, its lanes as the attention reads a tile: lane (quarter h, row t) has elements
-// 8h .. 8h+7 of every group.  Per group: e least with max|x| <= 7 * 2^e, then the nearest level of x / 2^e.  So a group's largest magnitude is two lane swaps away, K of 16 rows that fill a tile is written as one
-// run of 1 KB (head_dim 128) and its scales as one of 64 bytes; the conversion is the hardware's, which rounds to nearest even
-// and saturates.  Rows that follow each other usually lie in one tile, whose lines so come from one workgroup: with the heads
-// of a row together instead, eight XCDs wrote parts of each line (79 us where this takes 50: 40 768 rows of 8 heads of 128 in
-// bf16, 211 MB, which a copy moves in 41).  Bound by HBM there, by the launch in a decode step (3.8 us).
+// 8h .. 8h+7 of every group.  Per group: e least with max|x| <= 7 * 2^e, then the nearest level of x / 2^e.  So a group's
+// largest magnitude is two lane swaps away, K of 16 rows that fill a tile is written as one run of 1 KB (head_dim 128) and its
+// scales as one of 64 bytes; the conversion is the hardware's, which rounds to nearest even and saturates.  Rows that follow
+// each other usually lie in one tile, whose lines so come from one workgroup: with the heads of a row together instead, eight
+// XCDs wrote parts of each line (79 us where this takes 50: 40 768 rows of 8 heads of 128 in bf16, 211 MB, which a copy moves
+// in 41).  Bound by HBM there, by the launch in a decode step (3.8 us).
 template <int HD, typename ST>
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Cache c, int n_rows, const ST* __restrict__ k, int64_t k_row, int64_t k_head,
                                                          const ST* __restrict__ v, int64_t v_row, int64_t v_head, int vec,
@@ -435,8 +436,9 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Cache c, int n_rows,
 }
 
 // Read-back: level times 2^e, exact in fp32 and in bf16.  A thread has 8 elements of a group, whose codes are a word of K or
-// lie in one to four columns of V, and writes them as one run; a workgroup has 16 rows of one head of K (of V), then of the next, so that each line of the cache
-// is asked for by one XCD.  Bound by HBM: 36.4 us for the 211 MB that a copy moves in 41, four fifths of them written.
+// lie in one to four columns of V, and writes them as one run; a workgroup has 16 rows of one head of K (of V), then of the
+// next, so that each line of the cache is asked for by one XCD.  Bound by HBM: 36.4 us for the 211 MB that a copy moves in 41,
+// four fifths of them written.
 struct Kv4Work {
     int e8, which, head;
     int64_t row;
@@ -767,7 +769,9 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) store_pair(out + at * HD + here.element(i), acc[i] * inv);
                 if (a.lse && here.first()) a.lse[at] = ((top == -INFINITY ? 0.f : top) + log2f(APART ? sum_lse : sum)) * 0.6931471805599453f;
-            } else {  // elements into the first part's place, which no other thread reads; weights apart, as all of a row's threads read them
+            } else {
+                // elements into the first part's place, which no other thread reads; weights apart, as all of a row's threads
+                // read them
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) hand_over2((float*)o + here.held(i), acc[i]);
                 if (here.first()) {
@@ -794,16 +798,16 @@ __device__ __forceinline__ void join_parts(const Kv4Attend& a, const Kv4Part& w,
 // (O^T = V^T P^T) wants its probabilities in, if V's tile has its positions in that order, and nothing moves between lanes.  K and
 // V are exact in bf16.  NT: bf16 terms of an element of Q (1: Q is bf16; 3: fp32, exactly), PT: of a probability: three for the
 // fp32 model, two for the tiles of 16, which wait for memory anyway (error against 64 bits 0.0017, all of it the result's own
-// rounding to bf16), one for larger ones (0.0021; a second term costs them a sixth of their time: 64 requests of 500 to
-// 16 384 positions and 5 rows, 32 heads on 8, 171 us instead of 146).  With one term the divisor is the sum of the rounded probabilities: the
-// weights that V gets add to one, so a row in which one position outweighs the others keeps that one's value, whatever
-// its weight rounds to.  The log-sum-exp, where it is asked for (LSE), has a sum of its own, of the probabilities before
+// rounding to bf16), one for larger ones (0.0021; a second term costs them a sixth of their time: 64 requests of 500
+// to 16 384 positions and 5 rows, 32 heads on 8, 171 us instead of 144).  With one term the divisor is the sum of the rounded
+// probabilities: the weights that V gets add to one, so a row in which one position outweighs the others keeps that one's value,
+// whatever its weight rounds to.  The log-sum-exp, where it is asked for (LSE), has a sum of its own, of the probabilities before
 // they are rounded (those 64 requests 151 us).  UNITS: 16 entries each of a tile.
-// Bound by HBM where contexts are long: 64 requests of up to 16 384 positions, 32 heads on 8 of 128 elements, 589 MB: 114 us, 5.2 TB/s
-// (a copy's rate is 5.15), every byte read once.  So what counts is what is on its way: of the tiles DEPTH steps ahead each load
-// is asked for as soon as its registers have been read.  One request of 131 071 positions: 32 us for 143 MB, 4.5 TB/s; of which
-// 4 us are its parts' joins.  16 requests of up to 2048 positions, 32 heads: 19 us for 69 MB, launch and last parts included.
-// A single user's 513 positions (6.7 us) are bound by the launch and the chain part, table, K, V, join.
+// Bound by HBM where contexts are long: 64 requests of up to 16 384 positions, 32 heads on 8 of 128 elements, 589 MB: 114 us,
+// 5.2 TB/s (a copy's rate is 5.15), every byte read once.  So what counts is what is on its way: of the tiles DEPTH steps ahead
+// each load is asked for as soon as its registers have been read.  One request of 131 071 positions: 32 us for 143 MB, 4.5
+// TB/s; of which 4 us are its parts' joins.  16 requests of up to 2048 positions, 32 heads: 19 us for 69 MB, launch and last
+// parts included.  A single user's 513 positions (6.7 us) are bound by the launch and the chain part, table, K, V, join.
 template <int HD, int NT, int PT, int UNITS, int NW, int DEPTH, bool PAST, bool LSE, typename ST>
 __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 : NT == 1 ? 4 : 3) void kv4_attend_kernel(Kv4Attend a) {
     constexpr int G = HD / 32, EPC = HD / 16, M = 16 * UNITS;
@@ -894,7 +898,8 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
     };
 
     f32x4 o[UNITS][EPC];
-    float m[UNITS], l[UNITS], l_lse[UNITS];  // m: the scores' reference, at most a.slack below their maximum (so no probability passes 2^8)
+    // m: the scores' reference, at most a.slack below their maximum (so no probability passes 2^8)
+    float m[UNITS], l[UNITS], l_lse[UNITS];
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
         m[u] = -INFINITY, l[u] = l_lse[u] = 0.f;
@@ -1141,10 +1146,10 @@ __global__ __launch_bounds__(NW * 64, HD > 128 ? 1 : UNITS > 1 || DEPTH > 1 ? 2 
 // waves take every other 32 positions, so that a SIMD has two waves, and join their sums through LDS at the end.
 // One bf16 term of a probability, divided by the sum of the rounded ones as above (error against 64 bits 0.0023, of which the
 // result's rounding is 0.0017; a second term would be half as many products again).
-// 1024 rows at the end of 8192 positions, 32 heads on 8 of 128 elements, 129 GFLOP: 148 us, 870 TFLOP/s, where a large matrix product
-// reaches 1215.  The vector units' work (per score an exponential, a multiply-add, a maximum, a sum, half a conversion) takes about
-// as long as the products, and two waves of a SIMD overlap them in part; LDS is active a third of the time.  Three groups of
-// waves with Q in LDS: 151 us.
+// 1024 rows at the end of 8192 positions, 32 heads on 8 of 128 elements, 129 GFLOP: 146 us, 885 TFLOP/s, where a large matrix
+// product reaches 1215.  The vector units' work (per score an exponential, a multiply-add, a maximum, half a sum and conversion)
+// takes about as long as the products, and two waves of a SIMD overlap them in part; LDS is active a third of the time.  Three
+// groups of waves with Q in LDS: 151 us.
 template <bool LSE>
 __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     constexpr int HD = 128, M = KV4_WIDE, G = HD / 32, EPC = HD / 16, KS = HD / 16, DB = HD / 32, LB = HD / 8;
@@ -1275,7 +1280,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
     };
 
     f32x16 o[DB] = {};
-    float m = -INFINITY, l = 0.f, l_lse = 0.f;  // m: the scores' reference, at most a.slack below their maximum (so no probability passes 2^8)
+    float m = -INFINITY, l = 0.f, l_lse = 0.f;  // m: as above
     // The second group's matrix products come when the first one's vector work does: its scores are formed an interval ahead, so K
     // is converted two steps ahead there.
     const int ahead = group && !of_v ? 2 : 1;
@@ -1443,10 +1448,13 @@ __global__ __launch_bounds__(512, 2) void kv4_attend_wide_kernel(Kv4Attend a) {
 
 template <int HD, int UNITS, int NW>
 hipError_t attend_waves(const Kv4Attend& a, int dtype, int grid, hipStream_t s) {
-    // (tiles of more than 16 entries: a request has several, which read the same K and V)
+    // (tiles of more than 16 entries: a request has several, which read the same K and V.  With 256 elements all tiles have 16,
+    // so a prompt's tiles there read them past the caches as well: 1024 rows at 8192 positions, 16 heads on 4, 237 us, its
+    // products 106)
     const bool past = UNITS == 1 && a.past_caches;
     // Two steps ahead where registers allow it at the same number of waves: 8 waves alone on a CU, and bf16 tiles of 32 entries (17
-    // requests of up to 12 560 positions and 15 rows: 59 us, one step ahead 62; 64 of up to 16 384 and 5 rows: 128, 142).
+    // requests of 500 to 12 560 positions and 15 rows, 32 heads on 8: 61 us, one step ahead 64; 64 of 500 to 16 384 and 5 rows: 144
+    // and 163).
     constexpr int DEPTH = NW == 8 && HD <= 128 ? 2 : 1, DEPTH_BF16 = UNITS == 2 && HD <= 128 ? 2 : DEPTH;
     const dim3 g(grid), t(NW * 64);
     if constexpr (UNITS <= 2)
@@ -1536,11 +1544,13 @@ constexpr int64_t WIDE_ITEMS = 160;
 bool kv4_has_wide_tiles(int dtype, int head_dim) { return dtype == EE_BF16 && head_dim == 128; }
 
 int kv4_tile_units(int dtype, int head_dim, int most_flat, int n_seqs, int64_t all_flat, int kv_heads) {
-    // Wide tiles, in which an element is converted once for 128 entries, where they give more than half of the CUs work (130 of them,
-    // one request at 4000 positions: 85 us, in tiles of 32 entries 72; 225 of them: 77 and 88) and where not an eighth of them
-    // stays empty (24 requests of 88 entries: 99 and 76; of 132, which take two tiles: 167 and 127; of 128: 98 and 101).  Requests that
-    // do not all bring the most waste half a tile each on the average.  With 64 elements a wave holds 64 entries itself, and those
-    // tiles are as good or better (20 heads on 4, 4000 rows: 80 us, wide 91).
+    // Wide tiles, in which an element is converted once for 128 entries, where they give more than half of the CUs work (32
+    // heads on 8, one request at 4000 positions: 520 rows, 130 tiles, 89 us, in tiles of 32 entries 72; 900 rows, 225 tiles, 81
+    // and 87) and where not an eighth of them stays empty (24 requests of 500 to 4000 positions and 33 rows, 132 entries and
+    // two tiles each: 98 and 75; 32 rows: 60 and 61).  Requests that do not all bring the most waste half a tile each on the
+    // average.  A tile has a CU to itself, so a second round for a few of them costs as much as for all: 1024 rows at 8192
+    // positions are 256 tiles and take 146 us, 1032 rows 262.  With 64 elements a wave holds 64 entries itself, and those tiles
+    // are as good or better (20 heads on 4, a prompt of 4000 rows: 76 us, wide 91).
     if (kv4_has_wide_tiles(dtype, head_dim) && all_flat * kv_heads >= KV4_WIDE * WIDE_ITEMS) {
         const bool alike = (int64_t)n_seqs * most_flat <= all_flat;
         const int64_t empty = (int64_t)n_seqs * (alike ? (KV4_WIDE - most_flat % KV4_WIDE) % KV4_WIDE : KV4_WIDE / 2);

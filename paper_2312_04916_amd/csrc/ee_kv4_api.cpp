@@ -45,7 +45,7 @@ Cut cut_of(const ee_kv4_config& c, int n_seqs, int n_rows, int units) {
     }
     // Larger tiles leave as many times more to be joined, and a CU holds two workgroups.  So few items are cut into no more parts
     // than there are CUs (40 rows at 4000 positions, 32 heads on 8: 16 us, with 512 parts 22.5, with 768 27), some into two per
-    // CU (17 requests of up to 12 560 and 15 rows: 61 us, with 256 parts 113, with 768 70), and many, which fill the chip uncut, so
+    // CU (17 requests of 500 to 12 560 and 15 rows: 61 us, with 256 parts 113, with 768 68), and many, which fill the chip uncut, so
     // that the longest do not end last (61 requests of up to 16 380 and 10 rows: 132, with 512 parts 169).
     const int64_t items = ((int64_t)n_rows * (c.n_heads / c.n_kv_heads) / (16 * units) + std::min(n_seqs, n_rows)) * c.n_kv_heads;
     if (items <= 128) return {4, 256, 8, true};
