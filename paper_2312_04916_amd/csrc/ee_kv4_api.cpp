@@ -38,15 +38,16 @@ Cut cut_of(const ee_kv4_config& c, int n_seqs, int n_rows, int units) {
     if (units == 1) {
         // few items: one workgroup of eight waves per CU (one request of 131 071 positions, 8 kv heads: 32 us, with three of four
         // waves 43; 4 of 8000: 12.0, 15.7); many are balanced better by the smaller ones (64 of up to 16 384: 115, with eight
-        // waves 151; 16 of up to 2048, 32 heads: 20, 24)
+        // waves 151; 16 of up to 2048, 32 heads: 20, 24).  A request counts as one tile, though with 256 elements, where all tiles
+        // are of 16 entries, one with many rows has more
         const int items = std::min(n_seqs, n_rows) * c.n_kv_heads;
         if (items < 128) return {8, 256, 8, true};
         return {4, MOST_PARTS, 8, false};
     }
     // Larger tiles leave as many times more to be joined, and a CU holds two workgroups.  So few items are cut into no more parts
     // than there are CUs (40 rows at 4000 positions, 32 heads on 8: 16 us, with 512 parts 22.5, with 768 27), some into two per
-    // CU (17 requests of 500 to 12 560 and 15 rows: 61 us, with 256 parts 113, with 768 68), and many, which fill the chip uncut, so
-    // that the longest do not end last (61 requests of up to 16 380 and 10 rows: 132, with 512 parts 169).
+    // CU (17 requests of 500 to 12 560 and 15 rows: 61 us, with 256 parts 113, with 768 68), and many, which fill the chip uncut,
+    // so that the longest do not end last (61 requests of up to 16 380 and 0 to 10 rows: 132, with 512 parts 169).
     const int64_t items = ((int64_t)n_rows * (c.n_heads / c.n_kv_heads) / (16 * units) + std::min(n_seqs, n_rows)) * c.n_kv_heads;
     if (items <= 128) return {4, 256, 8, true};
     if (items <= 512) return {4, 512, 8, true};
