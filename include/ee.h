@@ -490,6 +490,58 @@ int ee_kv4_read(ee_kv4* c, int layer, int n_rows, const int64_t* dev_slots, void
 int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride, int64_t q_head_stride, void* dev_out, float* dev_lse,
                   float scale, int window, void* stream);
 
+/* ---------------------------------------------------------------- products with weights held in 8 bits
+ *
+ * y = x W^T for a weight W [n][k] that is packed once into 8 bits an element, next to the decode step above for programs that run
+ * layers of their own (with ee_kv4_*): half the bytes of a bf16 weight in a decode step, twice the matrix cores' rate in a prompt.
+ *
+ * The 8 bits: a group of elements shares a power of two 2^e, e the least integer from -110 to 120 with max|x| <= 448 * 2^e; each
+ * element is held as the nearest value of e4m3 (4 bits of exponent, 3 of mantissa, up to 448) times 2^e, ties going to the even
+ * code.  A weight's groups are its blocks of 128 rows x 128 elements; the rows of x are brought into the same form within the call, in
+ * groups of 128 elements of a row (the last groups may be smaller).  A group that holds an infinity or a NaN stands for NaN.
+ * (An element of 248 * 2^120 or more is held as 2^128: infinite where it comes back in fp32 or bf16, and in fp32's sums.)
+ *
+ * A result in fp32 is what the held values give in fp32 arithmetic.  One in bf16 comes from the matrix cores' 8-bit products, which
+ * add eight products at a time in multiples of 2^-13 of the largest of them: on Gaussian rows that costs 1.5e-5 of the result
+ * next to the 1.7e-3 of its rounding, and never more than 7 * 2^-13 of sum |x w|.
+ *
+ * pair: two weights of n rows each, gate and up, packed side by side; y = silu(x Wgate^T) * (x Wup^T).
+ * Sizes: 1 <= n <= 2^22, 1 <= k <= 2^18, 0 <= m <= 2^20.  Strides are of rows, in elements; the elements of a row are contiguous. */
+int ee_f8_bytes(int n, int k, int pair, size_t* weight_bytes);
+/* dtype: EE_F32 | EE_BF16, of dev_w [n][k] and, with pair, dev_up [n][k] (else NULL). */
+int ee_f8_pack(int n, int k, int pair, int dtype, const void* dev_w, int64_t w_row_stride, const void* dev_up, int64_t up_row_stride,
+               void* dev_weight, size_t weight_bytes, void* stream);
+/* The values that a packed weight holds (a non-zero pair and up != 0: of the up weight), [n][k] contiguous; exact in either dtype. */
+int ee_f8_unpack(int n, int k, int pair, int up, const void* dev_weight, int dtype, void* dev_w, void* stream);
+/* Workspace of a product of m rows. */
+int ee_f8_matmul_bytes(int m, int n, int k, int pair, int y_dtype, size_t* workspace_bytes);
+/* x [m][k] in x_dtype, y [m][n] in y_dtype; dev_add: NULL, or rows [m][n] in y_dtype that are added before the rounding (y itself, or
+ * apart from it).  y must not overlap x (EE_ERR_ARG).  Calls that overlap in time need workspaces of their own; its contents need
+ * not be kept between calls.  The bits of a row of y depend on m, not on the other rows' values. */
+int ee_f8_matmul(int m, int n, int k, int pair, const void* dev_weight, int x_dtype, const void* dev_x, int64_t x_row_stride, int y_dtype,
+                 void* dev_y, int64_t y_row_stride, const void* dev_add, int64_t add_row_stride, void* dev_workspace,
+                 size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------- choosing tokens
+ *
+ * One token per row of logits [rows][vocab] (dtype EE_F32 | EE_BF16, 1 <= vocab <= 2^18, rows contiguous inside), from random numbers that
+ * the caller gives: dev_u [rows] fp32, each in [0, 1).  The settings come per row where the array is given, else from the number
+ * beside it: temperature >= 0, top_k >= 0 (0: off), top_p in [0, 1] (1: off), min_p in [0, 1] (0: off).
+ *   A row's tokens are ordered by logit z, the largest first, equal ones by index; a token's weight is
+ * exp((z - z_max) / temperature).  Kept are the first top_k; of these the shortest run from the start whose weights reach top_p of
+ * theirs, one token at least; of these the ones with z_max - z <= -ln(min_p) * temperature.  The token is the first one, by
+ * index, at which the running sum of the kept weights exceeds u times their total.  Temperature 0: the first of the order.
+ *   Weights are whole multiples of 2^-44 of the largest and their sums are exact, so that a row's token depends on nothing but
+ * the row and its settings: not on the other rows or their number.
+ *   dev_logprob [rows] (or NULL): the token's log-probability, z - log sum exp, under the logits as they are (temperature 1,
+ * nothing cut); dev_confidence [rows] (or NULL): the largest probability under them, which is what the exit rule of Section 5.2
+ * compares with its threshold.
+ *   A row without a distribution (nothing above -inf, a NaN, a +inf, or a setting or u out of range): token -1, log-probability
+ * -inf, confidence 0. */
+int ee_sample(int rows, int vocab, int dtype, const void* dev_logits, int64_t row_stride, const float* dev_u, const float* dev_temperature,
+              const int32_t* dev_top_k, const float* dev_top_p, const float* dev_min_p, float temperature, int32_t top_k, float top_p,
+              float min_p, int32_t* dev_token, float* dev_logprob, float* dev_confidence, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -6,3 +6,5 @@ fallback: importing :mod:`binding` fails loudly when the library has not been bu
 """
 from .binding import *  # noqa: F401,F403
 from .kv4 import Kv4Cache  # noqa: F401
+from .f8 import F8Weight  # noqa: F401
+from .sampling import sample  # noqa: F401

@@ -5,7 +5,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libee.so")
-SOURCES = ["ee_api.cpp", "ee_kernels.hip", "ee_prefill.hip", "ee_kv4_api.cpp", "ee_kv4.hip"]
+SOURCES = ["ee_api.cpp", "ee_kernels.hip", "ee_prefill.hip", "ee_kv4_api.cpp", "ee_kv4.hip", "ee_f8_api.cpp", "ee_f8.hip",
+           "ee_sample_api.cpp", "ee_sample.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 

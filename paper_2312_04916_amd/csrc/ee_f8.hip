@@ -1,0 +1,300 @@
+// Kernels of products with weights held in 8 bits (ee_f8_* of ee.h; layouts in ee_f8.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "ee_f8.h"
+#include "ee_lanes.h"
+#include "ee_launch.h"
+
+namespace ee {
+
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// ------------------------------------------------------------------------------------------------
+// the format
+// ------------------------------------------------------------------------------------------------
+
+// Exponent (e + 127) of a group whose largest magnitude has these bits: the least e with top <= 448 * 2^e, 448 = 1.75 * 2^8.  255: the
+// group holds an infinity or a NaN.
+__device__ __forceinline__ uint32_t exponent_of(uint32_t top) {
+    const int e = (int)(top >> 23) - 8 + ((top & 0x7fffff) > 0x600000 ? 1 : 0);
+    return top >= 0x7f800000u ? 255u : (uint32_t)min(max(e, 127 - 110), 127 + 120);
+}
+// 2^-e, to be multiplied by; exact where the product is at least 2^-126, and a product below that is far below the least step
+__device__ __forceinline__ float unit_inverse(uint32_t e) { return __uint_as_float((254 - e) << 23); }
+
+// Four elements, in units of 2^e, as four codes.  No value is above 448, so nothing saturates.
+__device__ __forceinline__ int codes4(float a, float b, float c, float d) {
+    return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+}
+constexpr int CODES_NAN = 0x7f7f7f7f;
+
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// 32 neighbouring elements of a row as floats, zeros behind the n that there are
+template <typename T>
+__device__ __forceinline__ void load32(const T* row, int n, bool vec, float (&v)[32]) {
+    constexpr int PER = 16 / sizeof(T);
+    if (vec && n >= 32) {
+#pragma unroll
+        for (int i = 0; i < 32 / PER; ++i) {
+            const i32x4 a = *(const i32x4*)(row + i * PER);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (sizeof(T) == 2) {
+                    v[i * 8 + j * 2] = __uint_as_float((uint32_t)a[j] << 16);
+                    v[i * 8 + j * 2 + 1] = __uint_as_float((uint32_t)a[j] & 0xffff0000u);
+                } else {
+                    v[i * 4 + j] = __int_as_float(a[j]);
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = i < n ? (float)row[i] : 0.f;
+    }
+}
+
+__device__ __forceinline__ uint32_t top_of(const float (&v)[32]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = max(top, magnitude(v[i]));
+    return top;
+}
+// largest over the four lanes that hold a row's group
+__device__ __forceinline__ uint32_t top_of_quarters(uint32_t t) {
+    const lanes_u32x2 a = __builtin_amdgcn_permlane16_swap(t, t, false, false);
+    t = max(a[0], a[1]);
+    const lanes_u32x2 b = __builtin_amdgcn_permlane32_swap(t, t, false, false);
+    return max(b[0], b[1]);
+}
+__device__ __forceinline__ void codes_of(const float (&v)[32], uint32_t e, i32x8& c) {
+    const float u = unit_inverse(min(e, 247u));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int q = codes4(v[4 * i] * u, v[4 * i + 1] * u, v[4 * i + 2] * u, v[4 * i + 3] * u);
+        c[i] = e == 255 ? CODES_NAN : q;
+    }
+}
+// the exponent that is stored for a group: of one that stands for NaN any will do
+__device__ __forceinline__ uint32_t stored(uint32_t e) { return e == 255 ? 127 : e; }
+
+__device__ __forceinline__ void store_fragment(char* f, int lane, const i32x8& c) {
+    *(i32x4*)(f + lane * 16) = __builtin_shufflevector(c, c, 0, 1, 2, 3);
+    *(i32x4*)(f + 1024 + lane * 16) = __builtin_shufflevector(c, c, 4, 5, 6, 7);
+}
+__device__ __forceinline__ i32x8 load_fragment(const char* f, int lane) {
+    const i32x4 a = *(const i32x4*)(f + lane * 16), b = *(const i32x4*)(f + 1024 + lane * 16);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// A workgroup packs one block of 128 rows x 128 elements, a wave the 16 rows of a fragment.
+template <typename T>
+__global__ __launch_bounds__(512) void f8_pack_kernel(F8Shape s, const T* w, int64_t w_row, const T* up, int64_t up_row, char* weight, int vec) {
+    __shared__ uint32_t s_top[8];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, step = blockIdx.x;
+    const int row = (blockIdx.y * 8 + wave) * 16 + (lane & 15), k0 = step * 128 + (lane >> 4) * 32;
+    const T* src = blockIdx.z ? up : w;
+    float v[32];
+    load32(src + (int64_t)min(row, s.n - 1) * (blockIdx.z ? up_row : w_row) + min(k0, s.k - 1), row < s.n ? s.k - k0 : 0, vec, v);
+    uint32_t top = top_of(v);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+    if (lane == 0) s_top[wave] = top;
+    __syncthreads();
+    for (int i = 0; i < 8; ++i) top = max(top, s_top[i]);
+    const uint32_t e = exponent_of(top);
+    const int tile = (blockIdx.y * 8 + wave) * (s.pair ? 2 : 1) + blockIdx.z;
+    if (tile >= s.tiles()) return;
+    i32x8 c;
+    codes_of(v, e, c);
+    const size_t f = (size_t)tile * s.steps() + step;
+    store_fragment(weight + f * F8_FRAGMENT, lane, c);
+    if (lane == 0) weight[s.exponents() + f] = (char)stored(e);
+}
+
+template <typename T>
+__global__ __launch_bounds__(64) void f8_unpack_kernel(F8Shape s, int up, const char* weight, T* w) {
+    const int lane = threadIdx.x, step = blockIdx.y, row = blockIdx.x * 16 + (lane & 15), k0 = step * 128 + (lane >> 4) * 32;
+    const size_t f = (size_t)(blockIdx.x * (s.pair ? 2 : 1) + up) * s.steps() + step;
+    const i32x8 c = load_fragment(weight + f * F8_FRAGMENT, lane);
+    const float unit = __uint_as_float((uint32_t)(uint8_t)weight[s.exponents() + f] << 23);
+    if (row >= s.n) return;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        const int word = c[i / 4] >> (i % 4 * 8);
+        if (k0 + i < s.k) w[(int64_t)row * s.k + k0 + i] = (T)(__builtin_amdgcn_cvt_f32_fp8(word, 0) * unit);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// rows into 8 bits
+// ------------------------------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void f8_rows_kernel(F8Rows r, const T* x, int64_t x_row, int k, int vec, char* out) {
+    const int lane = threadIdx.x & 63, step = blockIdx.y * 4 + (threadIdx.x >> 6), tile = blockIdx.x;
+    if (step >= r.steps) return;
+    const int row = tile * 16 + (lane & 15), k0 = step * 128 + (lane >> 4) * 32;
+    float v[32];
+    load32(x + (int64_t)min(row, r.m - 1) * x_row + min(k0, k - 1), row < r.m ? k - k0 : 0, vec, v);
+    const uint32_t e = exponent_of(top_of_quarters(top_of(v)));
+    i32x8 c;
+    codes_of(v, e, c);
+    const size_t f = (size_t)tile * r.steps + step;
+    store_fragment(out + f * F8_FRAGMENT, lane, c);
+    if (lane < 16) out[r.exponents() + f * 16 + lane] = (char)stored(e);
+}
+
+// ------------------------------------------------------------------------------------------------
+// products
+// ------------------------------------------------------------------------------------------------
+
+// The held values of a fragment in bf16, which all of them fit: operands of four instructions of 32 elements.
+__device__ __forceinline__ void values_of(const i32x8& c, float unit, bf16x8 (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * i], unit, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * i], unit, true);
+        const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * i + 1], unit, false);
+        const bf16x2 e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * i + 1], unit, true);
+        v[i] = bf16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
+    }
+}
+
+__device__ __forceinline__ float silu(float g) { return g / (1.f + __expf(-g)); }
+
+// Four neighbouring results of one row: activation, rows that are added, rounding.
+template <typename T>
+__device__ __forceinline__ void finish(const F8Product& p, int row, int col, f32x4 v) {
+    if (row >= p.m || col >= p.n) return;
+    T* y = (T*)p.y + row * p.y_row + col;
+    const T* add = p.add ? (const T*)p.add + row * p.add_row + col : nullptr;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    if (p.y_vec && col + 3 < p.n) {
+        if (add) {
+            const T4 a = *(const T4*)add;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += (float)a[i];
+        }
+        *(T4*)y = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (col + i < p.n) y[i] = (T)(add ? v[i] + (float)add[i] : v[i]);
+    }
+}
+
+// A wave computes 16 * MT rows of x by NT tiles of the weight, a workgroup's waves share the contraction and add up through LDS in
+// their order.  T: of the result; float: the held values go through the bf16 instructions, which keep every bit of a product.
+template <typename T, int MT, int NT, int W>
+__global__ __launch_bounds__(W * 64) void f8_matmul_kernel(F8Product p, F8Shape s, F8Rows r) {
+    __shared__ f32x4 s_part[W][MT * NT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile0 = blockIdx.x * NT, mt0 = blockIdx.y * MT, tiles = s.tiles(), steps = s.steps(), m_tiles = (p.m + 15) / 16;
+    f32x4 acc[MT][NT] = {};
+    for (int step = wave; step < steps; step += W) {
+        i32x8 w[NT], x[MT];
+        int we[NT], xe[MT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const size_t f = (size_t)min(tile0 + j, tiles - 1) * steps + step;
+            w[j] = load_fragment(p.weight + f * F8_FRAGMENT, lane);
+            we[j] = (uint8_t)p.weight[s.exponents() + f];
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const size_t f = (size_t)min(mt0 + i, m_tiles - 1) * steps + step;
+            x[i] = load_fragment(p.workspace + f * F8_FRAGMENT, lane);
+            xe[i] = (uint8_t)p.workspace[r.exponents() + f * 16 + (lane & 15)];
+        }
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j], x[i], acc[i][j], 0, 0, 0, we[j], 0, xe[i]);
+        } else {
+            bf16x8 wv[NT][4], xv[4];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) values_of(w[j], __uint_as_float((uint32_t)we[j] << 23), wv[j]);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                values_of(x[i], __uint_as_float((uint32_t)xe[i] << 23), xv);
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[j][h], xv[h], acc[i][j], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) s_part[wave][i * NT + j][lane] = acc[i][j];
+    __syncthreads();
+    auto sum = [&](int t) {
+        f32x4 v = s_part[0][t][lane];
+#pragma unroll
+        for (int i = 1; i < W; ++i) v += s_part[i][t][lane];
+        return v;
+    };
+    const int row = lane & 15, col = (lane >> 4) * 4;
+    if (p.pair) {
+        for (int t = wave; t < MT * NT / 2; t += W) {
+            const int i = t / (NT / 2), j = t % (NT / 2) * 2;
+            const f32x4 g = sum(i * NT + j), u = sum(i * NT + j + 1);
+            finish<T>(p, (mt0 + i) * 16 + row, (tile0 + j) / 2 * 16 + col, f32x4{silu(g[0]) * u[0], silu(g[1]) * u[1], silu(g[2]) * u[2], silu(g[3]) * u[3]});
+        }
+    } else {
+        for (int t = wave; t < MT * NT; t += W) finish<T>(p, (mt0 + t / NT) * 16 + row, (tile0 + t % NT) * 16 + col, sum(t));
+    }
+}
+
+}  // namespace
+
+size_t f8_workspace(int m, int n, int k, int pair, int y_dtype) { return F8Rows{m, (k + 127) / 128}.bytes(); }
+
+hipError_t launch_f8_pack(const F8Shape& s, int dtype, const void* w, int64_t w_row, const void* up, int64_t up_row, char* weight, hipStream_t st) {
+    const dim3 grid(s.steps(), (s.n + 127) / 128, s.pair ? 2 : 1);
+    const int64_t es = dtype == EE_BF16 ? 2 : 4;
+    const int vec = (((uintptr_t)w | (uintptr_t)up) & 15) == 0 && w_row * es % 16 == 0 && (!s.pair || up_row * es % 16 == 0);
+    if (dtype == EE_BF16)
+        EE_LAUNCH(f8_pack_kernel<__bf16>, grid, dim3(512), st, s, (const __bf16*)w, w_row, (const __bf16*)up, up_row, weight, vec);
+    else
+        EE_LAUNCH(f8_pack_kernel<float>, grid, dim3(512), st, s, (const float*)w, w_row, (const float*)up, up_row, weight, vec);
+    return hipGetLastError();
+}
+
+hipError_t launch_f8_unpack(const F8Shape& s, int up, const char* weight, int dtype, void* w, hipStream_t st) {
+    const dim3 grid((s.n + 15) / 16, s.steps());
+    if (dtype == EE_BF16)
+        EE_LAUNCH(f8_unpack_kernel<__bf16>, grid, dim3(64), st, s, up, weight, (__bf16*)w);
+    else
+        EE_LAUNCH(f8_unpack_kernel<float>, grid, dim3(64), st, s, up, weight, (float*)w);
+    return hipGetLastError();
+}
+
+hipError_t launch_f8_matmul(const F8Product& p, hipStream_t st) {
+    const F8Shape s{p.n, p.k, p.pair};
+    const F8Rows r{p.m, s.steps()};
+    const dim3 rows_grid((p.m + 15) / 16, (r.steps + 3) / 4);
+    if (p.x_dtype == EE_BF16)
+        EE_LAUNCH(f8_rows_kernel<__bf16>, rows_grid, dim3(256), st, r, (const __bf16*)p.x, p.x_row, p.k, p.x_vec, p.workspace);
+    else
+        EE_LAUNCH(f8_rows_kernel<float>, rows_grid, dim3(256), st, r, (const float*)p.x, p.x_row, p.k, p.x_vec, p.workspace);
+    constexpr int MT = 2, NT = 2, W = 4;
+    const dim3 grid((s.tiles() + NT - 1) / NT, ((p.m + 15) / 16 + MT - 1) / MT);
+    if (p.y_dtype == EE_BF16)
+        EE_LAUNCH((f8_matmul_kernel<__bf16, MT, NT, W>), grid, dim3(W * 64), st, p, s, r);
+    else
+        EE_LAUNCH((f8_matmul_kernel<float, MT, NT, W>), grid, dim3(W * 64), st, p, s, r);
+    return hipGetLastError();
+}
+
+}  // namespace ee
