@@ -531,16 +531,21 @@ int ee_f8_matmul(int m, int n, int k, int pair, const void* dev_weight, int x_dt
  * exp((z - z_max) / temperature).  Kept are the first top_k; of these the shortest run from the start whose weights reach top_p of
  * theirs, one token at least; of these the ones with z_max - z <= -ln(min_p) * temperature.  The token is the first one, by
  * index, at which the running sum of the kept weights exceeds u times their total.  Temperature 0: the first of the order.
- *   Weights are whole multiples of 2^-44 of the largest and their sums are exact, so that a row's token depends on nothing but
- * the row and its settings: not on the other rows or their number.
+ *   Weights are whole multiples of 2^-44 of the largest (where nothing is cut: of the largest of each run of 1024 tokens, whose sum is
+ * then rounded to such a multiple) and their sums are exact, so that a row's token depends on nothing but the row and its settings:
+ * not on the other rows or their number.
  *   dev_logprob [rows] (or NULL): the token's log-probability, z - log sum exp, under the logits as they are (temperature 1,
  * nothing cut); dev_confidence [rows] (or NULL): the largest probability under them, which is what the exit rule of Section 5.2
  * compares with its threshold.
  *   A row without a distribution (nothing above -inf, a NaN, a +inf, or a setting or u out of range): token -1, log-probability
  * -inf, confidence 0. */
+int ee_sample_bytes(int rows, int vocab, size_t* workspace_bytes);
+/* Calls that overlap in time need workspaces of their own; its contents need not be kept between calls.  Results, workspace and what is
+ * read must not overlap (EE_ERR_ARG). */
 int ee_sample(int rows, int vocab, int dtype, const void* dev_logits, int64_t row_stride, const float* dev_u, const float* dev_temperature,
               const int32_t* dev_top_k, const float* dev_top_p, const float* dev_min_p, float temperature, int32_t top_k, float top_p,
-              float min_p, int32_t* dev_token, float* dev_logprob, float* dev_confidence, void* stream);
+              float min_p, int32_t* dev_token, float* dev_logprob, float* dev_confidence, void* dev_workspace, size_t workspace_bytes,
+              void* stream);
 
 #ifdef __cplusplus
 }

@@ -73,6 +73,7 @@ class F8Weight:
         if _current_device() != self._index:  # (the default stream's handle is 0 on every device: a launch goes to the current one)
             with torch.cuda.device(self._index):
                 return self.matmul(x, add, dtype, out, stream)
+        raw = _raw_stream(stream, self._index)
         xp, xr = _rows(x, self._index, None, self.k, "x")
         m = x.shape[0]
         if out is None:
@@ -94,7 +95,7 @@ class F8Weight:
         size = self._workspace_bytes(m, code)
         work = self._empty(stream, size, dtype=torch.uint8) if size else None
         rc = self._matmul(m, self.n, self.k, self.pair, self._address, _CODES[x.dtype], xp, xr, code, op, orow, ap, ar,
-                          work.data_ptr() if size else None, size, _raw_stream(stream, self._index))
+                          work.data_ptr() if size else None, size, raw)
         if rc:
             _chk(rc, "ee_f8_matmul")
         if stream is not None:

@@ -1,6 +1,8 @@
 """ctypes binding of ee_sample (include/ee.h): argument marshalling only."""
 from __future__ import annotations
 
+import ctypes as C
+from numbers import Real
 from typing import Optional, Union
 
 import torch
@@ -9,18 +11,29 @@ from .binding import EE_BF16, EE_F32, _chk, lib
 from .kv4 import _current_device, _raw_stream, _used_on
 
 _CODES = {torch.bfloat16: EE_BF16, torch.float32: EE_F32}
-_fn = None
+_fn, _row_bytes = None, {}
+
+
+def _workspace_bytes(rows: int, vocab: int) -> int:
+    per_row = _row_bytes.get(vocab)
+    if per_row is None:
+        size = C.c_size_t()
+        _chk(lib().ee_sample_bytes(1, vocab, C.byref(size)), "ee_sample_bytes")
+        if len(_row_bytes) >= 4096:
+            _row_bytes.clear()
+        per_row = _row_bytes[vocab] = size.value
+    return rows * per_row
 
 
 def _setting(v, off, dtype, rows: int, index: int, what: str):
     """-> (address or None, number) of a setting: one per row, or one for all."""
     if v is None:
         return None, off
-    if isinstance(v, torch.Tensor):
-        if v.dtype is not dtype or v.get_device() != index or v.shape != (rows,) or not v.is_contiguous():
-            raise ValueError(f"{what}: {dtype}[{rows}] on cuda:{index}, contiguous, or a number")
-        return v.data_ptr(), off
-    return None, v
+    if isinstance(v, Real):
+        return None, v
+    if v.dtype is not dtype or v.get_device() != index or v.shape != (rows,) or not v.is_contiguous():
+        raise ValueError(f"{what}: {dtype}[{rows}] on cuda:{index}, contiguous, or a number")
+    return v.data_ptr(), off
 
 
 def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Union[None, float, torch.Tensor] = None, top_k: Union[None, int, torch.Tensor] = None,
@@ -42,18 +55,19 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Union[None, float
     rows, vocab = logits.shape
     if vocab > 1 and logits.stride(1) != 1:
         raise ValueError("logits: the elements of a row must be contiguous")
-    if not isinstance(u, torch.Tensor) or u.dtype is not torch.float32 or u.get_device() != index or u.shape != (rows,) or not u.is_contiguous():
+    if u.dtype is not torch.float32 or u.get_device() != index or u.shape != (rows,) or not u.is_contiguous():
         raise ValueError(f"u: float32[{rows}] on cuda:{index}, contiguous")
+    raw = _raw_stream(stream, index)
     tp, t = _setting(temperature, 1.0, torch.float32, rows, index, "temperature")
     kp, k = _setting(top_k, 0, torch.int32, rows, index, "top_k")
     pp, p = _setting(top_p, 1.0, torch.float32, rows, index, "top_p")
     mp, m = _setting(min_p, 0.0, torch.float32, rows, index, "min_p")
 
-    def empty(dtype):
+    def empty(dtype, n=rows):
         if stream is None:
-            return torch.empty(rows, dtype=dtype, device=logits.device)
+            return torch.empty(n, dtype=dtype, device=logits.device)
         with torch.cuda.stream(stream):
-            e = torch.empty(rows, dtype=dtype, device=logits.device)
+            e = torch.empty(n, dtype=dtype, device=logits.device)
         _used_on(torch.cuda.current_stream(logits.device), e)  # where the caller will want it
         return e
 
@@ -64,10 +78,13 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Union[None, float
     lp, cf = (empty(torch.float32), empty(torch.float32)) if scores else (None, None)
     if _fn is None:
         _fn = lib().ee_sample
+    size = _workspace_bytes(rows, vocab)
+    work = empty(torch.uint8, size)
     code = _fn(rows, vocab, _CODES[logits.dtype], logits.data_ptr(), logits.stride(0), u.data_ptr(), tp, kp, pp, mp, t, k, p, m, out.data_ptr(),
-               lp.data_ptr() if scores else None, cf.data_ptr() if scores else None, _raw_stream(stream, index))
+               lp.data_ptr() if scores else None, cf.data_ptr() if scores else None,
+               work.data_ptr(), size, raw)
     if code:
         _chk(code, "ee_sample")
     if stream is not None:
-        _used_on(stream, logits, u, out, *(a for a in (temperature, top_k, top_p, min_p) if isinstance(a, torch.Tensor)))
+        _used_on(stream, logits, u, out, *(a for a in (temperature, top_k, top_p, min_p) if a is not None and not isinstance(a, Real)))
     return (out, lp, cf) if scores else out

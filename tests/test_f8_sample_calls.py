@@ -65,11 +65,15 @@ def test_matmul_refusals():
 
 
 def test_sample_refusals():
-    L = ee.lib()
+    L, b = ee.lib(), C.c_size_t()
+    assert L.ee_sample_bytes(3, 1, C.byref(b)) == GOOD and b.value >= 3 * 76
+    assert L.ee_sample_bytes(0, 1 << 18, C.byref(b)) == GOOD and b.value == 0
+    assert L.ee_sample_bytes(1, 0, C.byref(b)) == CONFIG and L.ee_sample_bytes(1, (1 << 18) + 1, C.byref(b)) == CONFIG
+    assert L.ee_sample_bytes(-1, 5, C.byref(b)) == ARG and L.ee_sample_bytes(1, 5, None) == ARG
     M = 1 << 20
 
-    def sample(rows=4, vocab=100, dt=F32, z=M, zr=100, u=2 * M, tp=None, kp=None, pp=None, mp=None, t=1.0, k=0, p=1.0, m=0.0, token=3 * M, lp=None, cf=None):
-        return L.ee_sample(rows, vocab, dt, z, zr, u, tp, kp, pp, mp, t, k, p, m, token, lp, cf, None)
+    def sample(rows=4, vocab=100, dt=F32, z=M, zr=100, u=2 * M, tp=None, kp=None, pp=None, mp=None, t=1.0, k=0, p=1.0, m=0.0, token=3 * M, lp=None, cf=None, work=6 * M, size=1 << 30):
+        return L.ee_sample(rows, vocab, dt, z, zr, u, tp, kp, pp, mp, t, k, p, m, token, lp, cf, work, size, None)
 
     nan, inf = float("nan"), float("inf")
     for bad, code in ((dict(rows=-1), ARG), (dict(rows=(1 << 20) + 1), ARG), (dict(vocab=0), CONFIG), (dict(vocab=(1 << 18) + 1), CONFIG), (dict(dt=2), CONFIG),
@@ -78,7 +82,9 @@ def test_sample_refusals():
                       (dict(p=1.5), ARG), (dict(p=nan), ARG), (dict(m=-0.1), ARG), (dict(m=2.0), ARG), (dict(m=nan), ARG),
                       # results apart from what is read, and from one another
                       (dict(token=M + 1596), ARG), (dict(token=2 * M), ARG), (dict(lp=3 * M + 12), ARG), (dict(cf=3 * M), ARG), (dict(lp=4 * M, cf=4 * M), ARG),
-                      (dict(tp=4 * M, lp=4 * M), ARG)):
+                      (dict(tp=4 * M, lp=4 * M), ARG),
+                      (dict(work=None), ARG), (dict(work=6 * M + 16), ARG), (dict(size=100), NOMEM), (dict(work=M), ARG), (dict(work=3 * M), ARG),
+                      (dict(work=2 * M), ARG), (dict(cf=6 * M), ARG)):
         assert sample(**bad) == code, bad
     assert sample(rows=0) == GOOD and sample(rows=0, z=None, u=None, token=None) == GOOD
 
@@ -168,7 +174,6 @@ def test_samples_go_to_the_logits_device(machine, monkeypatch):
     empty = torch.empty
     monkeypatch.setattr(torch, "empty", lambda *a, device=None, **kw: empty(*a, **kw))
     z, u = Fake(torch.zeros(2, 16)), Fake(torch.zeros(2))
-    monkeypatch.setattr(sampling.torch, "Tensor", (torch.Tensor, Fake))
     for now in (0, 1, 2):
         current[0] = now
         sampling.sample(z, u)
@@ -178,7 +183,7 @@ def test_samples_go_to_the_logits_device(machine, monkeypatch):
         sampling.sample(z, u, out=Fake(torch.zeros(2, dtype=torch.int32)), stream=types.SimpleNamespace(device_index=0, cuda_stream=7))
     for bad in (dict(logits=Fake(torch.zeros(2, 16, dtype=torch.float16))), dict(logits=Fake(torch.zeros(16))), dict(logits=torch.zeros(2, 16)),
                 dict(logits=Fake(torch.zeros(16, 2).T)), dict(u=Fake(torch.zeros(3))), dict(u=Fake(torch.zeros(2), 0)), dict(u=Fake(torch.zeros(2, dtype=torch.float64))),
-                dict(u=0.5), dict(temperature=Fake(torch.zeros(3))), dict(top_k=Fake(torch.zeros(2))), dict(top_p=Fake(torch.zeros(4)[::2])),
+                dict(temperature=Fake(torch.zeros(3))), dict(top_k=Fake(torch.zeros(2))), dict(top_p=Fake(torch.zeros(4)[::2])),
                 dict(min_p=Fake(torch.zeros(2), 0)), dict(out=Fake(torch.zeros(2)))):
         with pytest.raises(ValueError):
             sampling.sample(**{"logits": z, "u": u, **bad})
