@@ -23,16 +23,30 @@ struct Sampling {
     int vec;  // rows can be read four elements at a time
 };
 
-// What the first kernel leaves of a row for the second, by index alone: the largest logit of each run of 64 tokens, and of each run of 1024
-// the sum of the weights, in 2^-44 of the run's largest, and the sum of exp(z - largest).
-constexpr int SAMPLE_RUN = 1024, SAMPLE_CHUNK = 64;
+// The workspace of a row.  The first kernel leaves, by index alone, the largest logit of each run of 64 tokens, and of each run of 1024 the
+// sum of the weights, in 2^-44 of the run's largest, and the sum of exp(z - largest).  The second one leaves a note for the third where
+// a row has too many tokens that may be kept.
+constexpr int SAMPLE_RUN = 1024, SAMPLE_CHUNK = 64, SAMPLE_BINS = 1024;
+struct SampleNote {
+    uint32_t wide;               // for the third kernel
+    uint32_t top_key, least;     // keys of the largest logit, of the floor
+    uint32_t arrived;            // workgroups of the row that have left their bins
+    unsigned long long total;    // of all weights, where it is asked for
+    double log_raw, raw;         // sum of exp(z - top)
+};
 struct SampleRow {
     int runs;
     constexpr explicit SampleRow(int vocab) : runs((vocab + SAMPLE_RUN - 1) / SAMPLE_RUN) {}
     constexpr size_t sums() const { return (size_t)runs * (SAMPLE_RUN / SAMPLE_CHUNK) * 4; }
     constexpr size_t raws() const { return sums() + (size_t)runs * 8; }
-    constexpr size_t bytes() const { return (raws() + (size_t)runs * 4 + 15) / 16 * 16; }
+    constexpr size_t note() const { return (raws() + (size_t)runs * 4 + 15) / 16 * 16; }
+    constexpr size_t bytes() const { return note() + (sizeof(SampleNote) + 15) / 16 * 16; }
 };
+// Workgroups that share a row in the third kernel, and what each hands over: for each bin a weight and where its elements begin, and the
+// part's elements.
+constexpr size_t sample_part_bytes(int part_length) { return (size_t)SAMPLE_BINS * 12 + 16 + (size_t)part_length * 2; }
+int sample_parts(int rows, int vocab);
+size_t sample_workspace(int rows, int vocab);
 
 hipError_t launch_sample(const Sampling& p, hipStream_t st);
 

@@ -14,14 +14,9 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int THREADS = 1024, WAVES = THREADS / 64;  // of the second kernel
-constexpr int BINS = 1024;
-constexpr int LIST = 512;       // elements of a bin that are ranked one by one
-constexpr int OWN = 8;          // candidates of a thread
-constexpr int CANDIDATES = THREADS * OWN;
-constexpr int SEGMENTS = 1024;  // of a row with more candidates: runs of 256 tokens
-constexpr int ONE = 44;         // weights are multiples of 2^-44 of the largest: 2^18 of them stay below 2^62
-constexpr int CHUNKS = SAMPLE_RUN / SAMPLE_CHUNK;
+constexpr int ONE = 44;  // weights are multiples of 2^-44 of the largest: 2^18 of them stay below 2^62
+constexpr int CHUNKS = SAMPLE_RUN / SAMPLE_CHUNK, RUNS = (1 << 18) / SAMPLE_RUN;
+constexpr int LIST = 256;  // elements of a bin that are ranked one by one
 
 // Order of the floats as unsigned numbers; -0 counts as 0, NaN as the largest.
 __device__ __forceinline__ uint32_t key_of(float z) {
@@ -31,11 +26,12 @@ __device__ __forceinline__ uint32_t key_of(float z) {
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 constexpr uint32_t KEY_INF = 0xff800000u, KEY_NINF = 0x007fffffu;
 
-// 2^y for y <= 0 as mantissa and exponent.  In 64 bits: the place of u * total among the sums has to be found in runs of 2^18
-// weights.  2^f on [-1/2, 1/2] is a polynomial through nine Chebyshev nodes, its constant term kept at 1 (error 2^-45).
-__device__ __forceinline__ double power_of(double y, int& exponent) {
-    y = fmax(y, -1000.0);
-    const double n = rint(y), f = y - n;
+// 2^y * 2^shift for y <= 0.  In 64 bits: the place of u * total among the sums has to be found in runs of 2^18 weights.  2^f on
+// [-1/2, 1/2] is a polynomial through nine Chebyshev nodes, its constant term kept at 1 (error 2^-45); adding 1.5 * 2^52 leaves the
+// nearest whole number in the low bits, and exponents are added as they are (rounding, conversion and scaling instructions for 64 bits
+// take four times as long as additions).
+__device__ __forceinline__ double power_of(double y, int shift) {
+    const double t = fmax(y, -900.0) + 0x1.8p52, f = fmax(y, -900.0) - (t - 0x1.8p52);
     double g = 0x1.b63880a30e9ffp-24;
     g = fma(g, f, 0x1.63d136366db24p-20);
     g = fma(g, f, 0x1.ffcb9515a8016p-17);
@@ -45,37 +41,65 @@ __device__ __forceinline__ double power_of(double y, int& exponent) {
     g = fma(g, f, 0x1.c6b08d7047e52p-5);
     g = fma(g, f, 0x1.ebfbdff823cedp-3);
     g = fma(g, f, 0x1.62e42fefa39efp-1);
-    exponent = (int)n;
-    return fma(g, f, 1.0);
+    const u64 m = (u64)__double_as_longlong(fma(g, f, 1.0));
+    const uint32_t n = (uint32_t)__double_as_longlong(t) + (uint32_t)shift;
+    return __longlong_as_double((long long)((u64)((uint32_t)(m >> 32) + (n << 20)) << 32 | (uint32_t)m));
 }
 // exp((z - top) / temperature) as a whole number of 2^-44, with per_t = log2(e) / temperature; adding 2^52 rounds to one and leaves it in the
 // low bits.
 __device__ __forceinline__ u64 weight_of(float z, float top, double per_t) {
-    int e;
-    const double m = power_of(((double)z - (double)top) * per_t, e);
-    return (u64)__double_as_longlong(ldexp(m, e + ONE) + 0x1p52) & ((1ull << 52) - 1);
+    return (u64)__double_as_longlong(power_of(((double)z - (double)top) * per_t, ONE) + 0x1p52) & ((1ull << 52) - 1);
 }
-// a sum of weights relative to `top` as one relative to another top, 2^y times as large
-__device__ __forceinline__ u64 rescaled(u64 sum, double y) {
-    int e;
-    const double m = power_of(y, e);
-    return y == 0 ? sum : (u64)rint(ldexp((double)sum * m, e));
+// The same with the bits of 2^52 on top: sums of n of them are the weights' sum and n times that, modulo 2^64.
+__device__ __forceinline__ u64 weight_bits(float z, float top, double per_t) {
+    return (u64)__double_as_longlong(power_of(((double)z - (double)top) * per_t, ONE) + 0x1p52);
 }
+constexpr u64 BITS = 0x4330000000000000ull;
+// a sum of weights relative to one top as one relative to another, 2^-y times as large
+__device__ __forceinline__ u64 rescaled(u64 sum, double y) { return y == 0 ? sum : (u64)rint((double)sum * power_of(y, 0)); }
 
-__device__ __forceinline__ u64 shfl_xor64(u64 v, int d) { return (u64)__shfl_xor((long long)v, d); }
-__device__ __forceinline__ u64 wave_total(u64 v) {
-    for (int d = 1; d < 64; d *= 2) v += shfl_xor64(v, d);
-    return v;
+// A value of the lane 1, 2, 4, 8 before in the row of 16 (0x110 + n), of the last lane of the row before (0x142, to rows 1 and 3), of the
+// first half (0x143, to rows 2 and 3); 0 where there is none.
+template <int FROM, int ROWS = 0xf>
+__device__ __forceinline__ uint32_t lanes_before(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, FROM, ROWS, 0xf, false);
 }
-// inclusive sums in the lanes' order
-template <typename T>
+template <int FROM, int ROWS = 0xf>
+__device__ __forceinline__ u64 lanes_before(u64 v) {
+    return (u64)lanes_before<FROM, ROWS>((uint32_t)(v >> 32)) << 32 | lanes_before<FROM, ROWS>((uint32_t)v);
+}
+// inclusive sums of the first N lanes, in their order
+template <int N = 64, typename T>
 __device__ __forceinline__ T wave_scan(T v) {
-    const int lane = threadIdx.x & 63;
-    for (int d = 1; d < 64; d *= 2) {
-        const T o = sizeof(T) == 8 ? (T)__shfl_up((long long)v, d) : (T)__shfl_up((int)v, d);
-        if (lane >= d) v += o;
+    v += lanes_before<0x111>(v);
+    v += lanes_before<0x112>(v);
+    v += lanes_before<0x114>(v);
+    if constexpr (N > 8) v += lanes_before<0x118>(v);
+    if constexpr (N > 16) {
+        v += lanes_before<0x142, 0xa>(v);
+        v += lanes_before<0x143, 0xc>(v);
     }
     return v;
+}
+__device__ __forceinline__ uint32_t last_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
+__device__ __forceinline__ u64 last_lane(u64 v) { return (u64)last_lane((uint32_t)(v >> 32)) << 32 | last_lane((uint32_t)v); }
+template <typename T>
+__device__ __forceinline__ T wave_total(T v) {
+    return last_lane(wave_scan(v));
+}
+__device__ __forceinline__ double wave_total(double v) {  // (in an order of its own: the same every time)
+    for (int d = 32; d; d /= 2) v += __shfl_xor(v, d);
+    return v;
+}
+// largest of a wave's numbers
+__device__ __forceinline__ uint32_t wave_most(uint32_t v) {
+    v = max(v, lanes_before<0x111>(v));
+    v = max(v, lanes_before<0x112>(v));
+    v = max(v, lanes_before<0x114>(v));
+    v = max(v, lanes_before<0x118>(v));
+    v = max(v, lanes_before<0x142, 0xa>(v));
+    v = max(v, lanes_before<0x143, 0xc>(v));
+    return last_lane(v);
 }
 
 // f * sum for 0 <= f < 1, rounded down (up): 24 bits of f times 62 of the sum, exactly.
@@ -127,22 +151,34 @@ __device__ __forceinline__ void load4(const T* z, int i, int n, bool vec, float 
 }
 
 // ------------------------------------------------------------------------------------------------
-// the pass over the logits: a wave per run of 1024 tokens
+// the pass over the logits: a wave takes `each` runs of 1024 tokens, one after the other
 // ------------------------------------------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(256) void sample_runs_kernel(Sampling p) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), waves = gridDim.x * 4;
+__global__ __launch_bounds__(256) void sample_runs_kernel(Sampling p, int each) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     const SampleRow at(p.vocab);
-    const uint32_t all = (uint32_t)p.rows * at.runs;
+    const uint32_t all = (uint32_t)p.rows * at.runs, i0 = (uint32_t)wave * each, i1 = min(all, i0 + each);
+    if (i0 >= i1) return;
     const bool scores = p.logprob || p.confidence;
-    for (uint32_t i = wave; i < all; i += waves) {
-        const int r = i / (uint32_t)at.runs, run = i - r * at.runs;
+    int r = i0 / (uint32_t)at.runs, run = i0 - r * at.runs;
+    Settings s(p, r);
+    float next[4][4];
+    auto load = [&](int r, int run) {
         const T* z = (const T*)p.logits + (int64_t)r * p.row_stride;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) load4(z, run * SAMPLE_RUN + j * 256 + lane * 4, p.vocab, p.vec, next[j]);
+    };
+    load(r, run);
+    for (uint32_t i = i0; i < i1; ++i) {
         float v[4][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) load4(z, run * SAMPLE_RUN + j * 256 + lane * 4, p.vocab, p.vec, v[j]);
-        char* out = p.workspace + (size_t)r * at.bytes();
-        const Settings s(p, r);
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[j][k] = next[j][k];
+        const int r_now = r, run_now = run;
+        if (++run == at.runs) run = 0, ++r;
+        if (i + 1 < i1) load(r, run);
+        char* out = p.workspace + (size_t)r_now * at.bytes();
         bool nan = false;
         float top[4];
 #pragma unroll
@@ -156,7 +192,7 @@ __global__ __launch_bounds__(256) void sample_runs_kernel(Sampling p) {
         if (__ballot(nan)) top[0] = top[1] = top[2] = top[3] = __uint_as_float(0x7fc00000u);
         if ((lane & 15) == 0) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) ((float*)out)[run * CHUNKS + j * 4 + (lane >> 4)] = top[j];
+            for (int j = 0; j < 4; ++j) ((float*)out)[run_now * CHUNKS + j * 4 + (lane >> 4)] = top[j];
         }
         const float ref = fmaxf(most, -3.4028235e38f);
         if (s.whole_sum()) {
@@ -164,9 +200,9 @@ __global__ __launch_bounds__(256) void sample_runs_kernel(Sampling p) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sum += weight_of(v[j][k], ref, s.per_t);
-            sum = wave_total(sum);
-            if (lane == 0) ((u64*)(out + at.sums()))[run] = sum;
+                for (int k = 0; k < 4; ++k) sum += weight_bits(v[j][k], ref, s.per_t);
+            sum = wave_scan(sum - 16 * BITS);
+            if (lane == 63) ((u64*)(out + at.sums()))[run_now] = sum;
         }
         if (scores) {
             float part[4];
@@ -174,8 +210,9 @@ __global__ __launch_bounds__(256) void sample_runs_kernel(Sampling p) {
             for (int j = 0; j < 4; ++j)
                 part[j] = (__expf(v[j][0] - ref) + __expf(v[j][1] - ref)) + (__expf(v[j][2] - ref) + __expf(v[j][3] - ref));
             const float raw = wave_sum((part[0] + part[1]) + (part[2] + part[3]));
-            if (lane == 0) ((float*)(out + at.raws()))[run] = raw;
+            if (lane == 0) ((float*)(out + at.raws()))[run_now] = raw;
         }
+        if (r != r_now && i + 1 < i1) s = Settings(p, r);
     }
 }
 
@@ -183,77 +220,200 @@ __global__ __launch_bounds__(256) void sample_runs_kernel(Sampling p) {
 // a row's token
 // ------------------------------------------------------------------------------------------------
 
-// What has been found out about a row: kept are the elements above `key` and the first `ties` ones (by index) that equal it.
+// What has been found out about a row: kept are the elements above `key` and the first `ties` of the ones that equal it, by index (all of
+// them, if not `some`).
 struct Cut {
     uint32_t key;
-    int ties;
+    int ties, some;
     u64 weight;  // of all that is kept
 };
+__device__ __forceinline__ Cut nothing_cut() { return Cut{0, 1 << 30, 0, 0}; }
 
-struct Shared {
-    u64 sums[WAVES];
-    double raw[WAVES];
-    uint32_t counts[WAVES], tops[WAVES];
-    u64 bin_weight[BINS];
-    uint32_t bin_count[BINS];
-    uint32_t list[LIST];
+template <int NT>
+struct CutShared {
+    u64 sums[NT / 64];
+    uint32_t counts[NT / 64];
+    u64 bin_weight[NT];
+    uint32_t bin_count[NT];
+    uint32_t list[LIST], list_index[LIST];  // the elements of the cut's bin, if they are few
     u64 list_weight[LIST];
-    int n_list;
-    uint32_t lo, hi;  // keys of the bin that is looked into
-    int bin;
+    uint32_t n_list, lo, hi;  // keys of the bin that is looked into
+    int bin, listed;
     u64 base_weight;
     uint32_t base_count, in_bin;
     Cut cut;
-    int place, ties_left;
-    u64 left;
-    float ref;
-    uint32_t chunks[(1 << 18) / SAMPLE_CHUNK];
-    union {
-        struct {
-            uint32_t key[CANDIDATES], index[CANDIDATES];
-        } candidates;
-        struct {
-            u64 weight[SEGMENTS];
-            uint32_t ties[SEGMENTS];
-        } segments;
-    };
 };
 
+__device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ u64 of_lane(u64 v, int lane) { return (u64)of_lane((uint32_t)(v >> 32), lane) << 32 | of_lane((uint32_t)v, lane); }
+
 // Sums over the workgroup: exclusive prefix of each thread's value, and the total.  `waves` is free again after the next barrier.
-template <typename T>
+template <int NT, typename T>
 __device__ __forceinline__ T before_me(T v, T& total, T* waves) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const T in = wave_scan(v);
     if (lane == 63) waves[wave] = in;
     __syncthreads();
-    T before = in - v;
-    total = 0;
-    for (int i = 0; i < WAVES; ++i) {
-        if (i < wave) before += waves[i];
-        total += waves[i];
-    }
-    return before;
+    const T sums = wave_scan<NT / 64>(lane < NT / 64 ? waves[lane] : (T)0);  // (of the waves, one in a lane)
+    total = of_lane(sums, NT / 64 - 1);
+    return in - v + (wave ? of_lane(sums, wave - 1) : (T)0);
 }
 
-// The elements that a cut is looked for among: f(key, weight()) for a thread's.  The whole row, those above a floor ...
-template <typename T>
-struct RowElements {
-    const T* z;
-    int n, vec;
-    float top, least;
-    double per_t;
-    template <typename F>
-    __device__ __forceinline__ void each(F f) const {
-        for (int i = threadIdx.x * 4; i < n; i += THREADS * 4) {
-            float v[4];
-            load4(z, i, n, vec, v);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (v[j] >= least && i + j < n) f(key_of(v[j]), [&] { return weight_of(v[j], top, per_t); });
+// Bins share the distance to the top, `per_bin` to one.
+__device__ __forceinline__ int bin_at(float z, float top, float per_bin, int bins) { return (int)fminf((top - z) * per_bin, (float)(bins - 1)); }
+
+// Counts and weights of the elements into the bins, which are empty.  E: each(f) calls f(key, index, weight()) for a thread's elements, and
+// each(lo, hi, f) for those whose logit is in [lo, hi] (and may for others); list() puts the elements of a bin by distance into s.list, if it can.
+template <int NT, typename E, typename B>
+__device__ __forceinline__ void fill_bins(const E& elements, CutShared<NT>& s, B bin_of) {
+    // (what lies furthest may be most of a row: it is counted apart, not at one place by all)
+    uint32_t last_count = 0;
+    u64 last_weight = 0;
+    elements.each([&](uint32_t key, int, auto weight) {
+        const int b = bin_of(key);
+        if (b < 0) return;
+        const u64 w = weight();
+        if (b == NT - 1) {
+            ++last_count, last_weight += w;
+        } else {
+            atomicAdd(&s.bin_count[b], 1u);
+            atomicAdd(&s.bin_weight[b], w);
         }
+    });
+    if (last_count) atomicAdd(&s.bin_count[NT - 1], last_count), atomicAdd(&s.bin_weight[NT - 1], last_weight);
+    __syncthreads();
+}
+
+// The last element that is kept where elements are kept, in their order, as long as fewer than `limit` came before (BY_COUNT) or
+// their weights' sum is below `limit`: the bin in which that happens, then its elements one by one, or finer bins if they are many,
+// which share the keys that are in the bin, until it holds one key only.  If all are kept, the cut is left as it was.
+// The bins by distance are filled; false: they no longer are.
+template <bool BY_COUNT, int NT, typename E>
+__device__ bool find_cut(const E& elements, CutShared<NT>& s, u64 limit, float top, float per_bin) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint32_t lo = 0, hi = 0;
+    int shift = -1;  // -1: bins by distance
+    u64 base_weight = 0;
+    uint32_t base_count = 0;
+    for (;;) {
+        auto bin_of = [&](uint32_t key) {
+            if (shift < 0) return bin_at(value_of(key), top, per_bin, NT);
+            return key >= lo && key <= hi ? (int)((hi - key) >> shift) : -1;
+        };
+        const uint32_t c = s.bin_count[tid];
+        const u64 w = s.bin_weight[tid];
+        const uint32_t c_in = wave_scan(c);
+        const u64 w_in = wave_scan(w);
+        if (lane == 63) s.counts[wave] = c_in, s.sums[wave] = w_in;
+        if (tid == 0) s.n_list = 0, s.lo = 0xffffffffu, s.hi = 0, s.bin = -1, s.listed = 0;
+        __syncthreads();
+        const uint32_t c_waves = wave_scan<NT / 64>(lane < NT / 64 ? s.counts[lane] : 0u);
+        const u64 w_waves = wave_scan<NT / 64>(lane < NT / 64 ? s.sums[lane] : 0ull);
+        const uint32_t c_before = base_count + c_in - c + (wave ? of_lane(c_waves, wave - 1) : 0u);
+        const u64 w_before = base_weight + w_in - w + (wave ? of_lane(w_waves, wave - 1) : 0ull);
+        // the bin in which the limit is reached
+        const bool here = c && (BY_COUNT ? c_before < limit && c_before + c >= limit : w_before < limit && w_before + w >= limit);
+        if (here) s.bin = tid, s.base_count = c_before, s.base_weight = w_before, s.in_bin = c;
+        __syncthreads();
+        const int bin = s.bin;
+        if (bin < 0) {  // all are kept
+            __syncthreads();
+            return shift < 0;
+        }
+        base_count = s.base_count, base_weight = s.base_weight;
+        const uint32_t in_bin = s.in_bin;
+        uint32_t key_lo = 0xffffffffu, key_hi = 0;
+        if (shift < 0 && in_bin <= LIST && elements.list(s, bin)) {
+        } else {
+        // (the bin's logits lie between these, and little else)
+        const float far = fabsf(top) * 1e-6f + (float)(bin + 1) / per_bin * 1e-5f;
+        const float z_lo = shift >= 0 ? value_of(lo) : bin == NT - 1 ? -INFINITY : top - (float)(bin + 1) / per_bin - far;
+        const float z_hi = shift >= 0 ? value_of(hi) : top - (float)bin / per_bin + far;
+        elements.each(z_lo, z_hi, [&](uint32_t key, int index, auto weight) {
+            if (bin_of(key) == bin) {
+                key_lo = min(key_lo, key), key_hi = max(key_hi, key);
+                if (in_bin <= LIST) {
+                    const uint32_t at = atomicAdd(&s.n_list, 1u);
+                    s.list[at] = key, s.list_index[at] = index, s.list_weight[at] = weight();
+                }
+            }
+        });
+        }
+        if (in_bin > LIST && key_lo <= key_hi) atomicMin(&s.lo, key_lo), atomicMax(&s.hi, key_hi);
+        __syncthreads();
+        if (in_bin <= LIST) {
+            const int n = (int)s.n_list;
+            if (tid == 0) s.listed = shift < 0;  // (whole)
+            // so many lanes for each that all threads have work, 16 at most
+            int lanes = NT / LIST;
+            while (lanes < 16 && 2 * lanes * n <= NT) lanes *= 2;
+            if (tid < n * lanes) {
+                const int e = tid / lanes;
+                const uint32_t key = s.list[e];
+                const u64 each = s.list_weight[e];
+                uint32_t above = 0, equal = 0;
+                u64 weight = 0;
+                for (int i = tid & (lanes - 1); i < n; i += lanes) {
+                    const uint32_t k = s.list[i];
+                    if (k > key) ++above, weight += s.list_weight[i];
+                    if (k == key) ++equal;
+                }
+                for (int d = 1; d < lanes; d *= 2) {
+                    above += __shfl_xor((int)above, d), equal += __shfl_xor((int)equal, d);
+                    weight += (u64)__shfl_xor((long long)weight, d);
+                }
+                above += base_count, weight += base_weight;
+                const bool mine = BY_COUNT ? above < limit && above + equal >= limit : weight < limit && weight + equal * each >= limit;
+                if (mine) {  // (all of one key write the same)
+                    const u64 ties = BY_COUNT ? limit - above : (limit - weight + each - 1) / each;
+                    s.cut = Cut{key, (int)ties, ties < equal, weight + ties * each};
+                }
+            }
+            __syncthreads();
+            return shift < 0;
+        }
+        lo = s.lo, hi = s.hi;
+        if (lo == hi) {  // one key: so many of them
+            if (tid == 0) {
+                const u64 each = s.bin_weight[bin] / in_bin;
+                const u64 ties = BY_COUNT ? limit - base_count : (limit - base_weight + each - 1) / each;
+                s.cut = Cut{lo, (int)ties, ties < in_bin, base_weight + ties * each};
+            }
+            __syncthreads();
+            return shift < 0;
+        }
+        shift = max(0, 32 - __builtin_clz(hi - lo) - (31 - __builtin_clz(NT)));
+        s.bin_weight[tid] = 0, s.bin_count[tid] = 0;
+        __syncthreads();
+        fill_bins<NT>(elements, s, bin_of);
     }
+}
+
+__device__ __forceinline__ void write_row(const Sampling& p, int r, int token, float z, float top, double raw, double log_raw) {
+    p.token[r] = token;
+    if (p.logprob) p.logprob[r] = (float)((double)z - (double)top - log_raw);
+    if (p.confidence) p.confidence[r] = (float)(1.0 / raw);
+}
+
+constexpr int ROW_THREADS = 512, ROW_WAVES = ROW_THREADS / 64;
+constexpr int OWN = 4, CANDIDATES = ROW_THREADS * OWN;  // that the threads hold
+constexpr int WAVE_CANDIDATES = 1024;                   // that a wave may find
+constexpr int AT_ONCE = 16;                             // runs of 64 tokens that a wave has on their way
+
+struct RowShared {
+    CutShared<ROW_THREADS> c;
+    uint32_t tops[ROW_WAVES];
+    double raw[ROW_WAVES];
+    double log_raw;
+    uint32_t place, found, candidates;
+    uint32_t floor_count[ROW_THREADS];
+    int floor_bin;
+    u64 left;
+    float ref;
+    uint16_t chunks[(1 << 18) / SAMPLE_CHUNK];
+    float2 found_at[ROW_WAVES][WAVE_CANDIDATES];  // logit, and the bits of the index
 };
-// ... or candidates that the threads hold.
+
 struct OwnElements {
     const uint32_t (&key)[OWN];
     const u64 (&weight)[OWN];
@@ -262,216 +422,54 @@ struct OwnElements {
     __device__ __forceinline__ void each(F f) const {
 #pragma unroll
         for (int j = 0; j < OWN; ++j)
-            if (j < n) f(key[j], [&] { return weight[j]; });
+            if (j < n) f(key[j], 0, [&] { return weight[j]; });
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(float, float, F f) const {
+        each(f);
+    }
+    template <int NT>
+    __device__ __forceinline__ bool list(CutShared<NT>&, int) const {
+        return false;
+    }
+    __device__ __forceinline__ u64 sum() const {
+        u64 all = 0;
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) all += weight[j];
+        return all;
     }
 };
-
-// The last element that is kept where elements are kept, in their order, as long as fewer than `limit` came before (BY_COUNT) or
-// their weights' sum is below `limit`: the bin in which that happens, then its elements one by one, or finer bins if they are many.
-// Bins share the distance to the top, `per_bin` to one, and then the keys that are in the bin, until it holds one key only.  If all
-// are kept, the cut is left as it was.
-template <bool BY_COUNT, typename E>
-__device__ void find_cut(const E& elements, Shared& s, u64 limit, float top, float per_bin) {
-    const int tid = threadIdx.x;
-    uint32_t lo = 0, hi = 0;
-    int shift = -1;  // -1: bins by distance
-    u64 base_weight = 0;
-    uint32_t base_count = 0;
-    for (;;) {
-        auto bin_of = [&](uint32_t key) {
-            if (shift < 0) return (int)fminf((top - value_of(key)) * per_bin, (float)(BINS - 1));
-            return key >= lo && key <= hi ? (int)((hi - key) >> shift) : -1;
-        };
-        __syncthreads();
-        s.bin_weight[tid] = 0, s.bin_count[tid] = 0;
-        __syncthreads();
-        // (what lies furthest may be most of a row: it is counted apart, not at one place by all)
-        uint32_t last_count = 0;
-        u64 last_weight = 0;
-        elements.each([&](uint32_t key, auto weight) {
-            const int b = bin_of(key);
-            if (b == BINS - 1) {
-                ++last_count;
-                if (!BY_COUNT) last_weight += weight();
-            } else if (b >= 0) {
-                atomicAdd(&s.bin_count[b], 1u);
-                if (!BY_COUNT) atomicAdd(&s.bin_weight[b], weight());
-            }
-        });
-        if (last_count) atomicAdd(&s.bin_count[BINS - 1], last_count);
-        if (last_weight) atomicAdd(&s.bin_weight[BINS - 1], last_weight);
-        __syncthreads();
-        // (BINS == THREADS)
-        const uint32_t c = s.bin_count[tid];
-        const u64 w = s.bin_weight[tid];
-        const uint32_t c_in = wave_scan(c);
-        const u64 w_in = BY_COUNT ? 0 : wave_scan(w);
-        if ((tid & 63) == 63) s.counts[tid >> 6] = c_in, s.sums[tid >> 6] = w_in;
-        if (tid == 0) s.n_list = 0, s.lo = 0xffffffffu, s.hi = 0, s.bin = -1;
-        __syncthreads();
-        uint32_t c_before = base_count + c_in - c;
-        u64 w_before = base_weight + w_in - w;
-        for (int i = 0; i < (tid >> 6); ++i) c_before += s.counts[i], w_before += s.sums[i];
-        // the bin in which the limit is reached
-        const bool here = c && (BY_COUNT ? c_before < limit && c_before + c >= limit : w_before < limit && w_before + w >= limit);
-        if (here) s.bin = tid, s.base_count = c_before, s.base_weight = w_before, s.in_bin = c;
-        __syncthreads();
-        const int bin = s.bin;
-        if (bin < 0) return;  // all are kept
-        base_count = s.base_count, base_weight = s.base_weight;
-        const uint32_t in_bin = s.in_bin;
-        uint32_t key_lo = 0xffffffffu, key_hi = 0;
-        elements.each([&](uint32_t key, auto weight) {
-            if (bin_of(key) == bin) {
-                key_lo = min(key_lo, key), key_hi = max(key_hi, key);
-                if (in_bin <= LIST) {
-                    const int at = atomicAdd(&s.n_list, 1);
-                    s.list[at] = key, s.list_weight[at] = BY_COUNT ? 0 : weight();
-                }
-            }
-        });
-        if (key_lo <= key_hi) atomicMin(&s.lo, key_lo), atomicMax(&s.hi, key_hi);
-        __syncthreads();
-        lo = s.lo, hi = s.hi;
-        if (in_bin <= LIST) {
-            const int n = s.n_list;
-            if (tid < n) {
-                const uint32_t key = s.list[tid];
-                const u64 each = s.list_weight[tid];
-                uint32_t above = base_count, equal = 0;
-                u64 weight = base_weight;
-                for (int i = 0; i < n; ++i) {
-                    const uint32_t k = s.list[i];
-                    if (k > key) ++above, weight += s.list_weight[i];
-                    if (k == key) ++equal;
-                }
-                const bool mine = BY_COUNT ? above < limit && above + equal >= limit : weight < limit && weight + equal * each >= limit;
-                if (mine)  // (all of one key write the same)
-                    s.cut = Cut{key, (int)(BY_COUNT ? limit - above : (limit - weight + each - 1) / each), 0};
-            }
-            __syncthreads();
-            return;
-        }
-        if (lo == hi) {  // one key: so many of them
-            if (tid == 0) {
-                const u64 each = s.bin_weight[bin] / in_bin;
-                s.cut = Cut{lo, (int)(BY_COUNT ? limit - base_count : (limit - base_weight + each - 1) / each), 0};
-            }
-            __syncthreads();
-            return;
-        }
-        shift = max(0, 32 - __builtin_clz(hi - lo) - 10);
-    }
-}
-
-// More candidates than the threads hold: the same over the whole row.  Sums by segments of 256 tokens, the segment in which u * total
-// lies, the token in it.
-template <typename T>
-__device__ int token_of_row(const RowElements<T>& row, const Settings& g, double reach, Shared& s, float per_bin) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    double far = INFINITY;
-    Cut cut;
-    auto kept_weight = [&](float z, uint32_t key) {
-        return key >= cut.key && (double)row.top - (double)z <= far ? weight_of(z, row.top, row.per_t) : 0;
-    };
-    auto sum_up = [&] {  // of what is kept, ties apart
-        for (int seg = wave; seg * 256 < row.n; seg += WAVES) {
-            float v[4];
-            load4(row.z, (seg * 64 + lane) * 4, row.n, row.vec, v);
-            u64 w = 0;
-            uint32_t ties = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t key = key_of(v[j]);
-                if (key == cut.key) ++ties;
-                else w += kept_weight(v[j], key);
-            }
-            if (__ballot(w != 0)) w = wave_total(w);
-            if (__ballot(ties != 0))
-                for (int d = 1; d < 64; d *= 2) ties += __shfl_xor(ties, d);
-            if (lane == 0) s.segments.weight[seg] = w, s.segments.ties[seg] = ties;
-        }
-        __syncthreads();
-    };
-    const int n_seg = (row.n + 255) / 256;  // (SEGMENTS == THREADS)
-    u64 tie, w, before, sum;
-    uint32_t ties, ties_before, all_ties;
-    int ties_left;
-    auto prefix = [&] {
-        cut = s.cut;
-        tie = cut.key ? kept_weight(value_of(cut.key), cut.key) : 0;
-        sum_up();
-        ties = tid < n_seg ? s.segments.ties[tid] : 0;
-        ties_before = before_me(ties, all_ties, s.counts);
-        ties_left = max(0, cut.ties - (int)ties_before);
-        w = (tid < n_seg ? s.segments.weight[tid] : 0) + tie * (u64)min((int)ties, ties_left);
-        before = before_me(w, sum, s.sums);
-        __syncthreads();
-    };
-    if (g.by_k) find_cut<true>(row, s, (u64)g.top_k, row.top, per_bin);
-    if (g.by_p) {
-        prefix();  // (of the first top_k, whatever min-p takes from them)
-        find_cut<false>(row, s, max(share_of(g.top_p, sum, true), 1ull), row.top, per_bin);
-    }
-    far = reach;
-    prefix();
-    const u64 target = share_of(g.u, sum, false);
-    if (before <= target && before + w > target) s.place = tid, s.left = target - before, s.ties_left = ties_left;
-    __syncthreads();
-    int token = 0;
-    if (wave == 0) {
-        const int i0 = (s.place * 64 + lane) * 4;
-        float v[4];
-        load4(row.z, i0, row.n, row.vec, v);
-        uint32_t n_ties = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) n_ties += key_of(v[j]) == cut.key;
-        int left = s.ties_left - (int)(wave_scan(n_ties) - n_ties);
-        u64 own[4], mine = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t key = key_of(v[j]);
-            own[j] = key == cut.key ? (left-- > 0 ? tie : 0) : kept_weight(v[j], key);
-            mine += own[j];
-        }
-        u64 upto = wave_scan(mine) - mine;
-        int at = 1 << 30;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            upto += own[j];
-            if (upto > s.left) at = min(at, i0 + j);
-        }
-        for (int d = 1; d < 64; d *= 2) at = min(at, __shfl_xor(at, d));
-        token = at;
-    }
-    return token;  // (of the first wave)
-}
 
 // Candidates are what may be kept: the tokens that are not below a floor which follows from the runs' numbers alone.
 //   top-k  the floor is the k-th largest of the largest logits of runs of 64, or a little less: k tokens at least are not below it
 //   top-p  tokens of a weight below (1 - p) * sum / vocab have less than (1 - p) * sum together, so that the others have p of it
 //   min-p  its own
-// They are few in most rows: read from the runs that have any, in the order of their indices, and held by the threads, eight each.
+// They are few in most rows: read from the runs that have any, in the order of their indices, and held by the threads, four each.
 template <typename T>
-__global__ __launch_bounds__(THREADS) void sample_kernel(Sampling p) {
-    __shared__ Shared s;
+__global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, int wide_follows) {
+    __shared__ RowShared s;
+    constexpr int NT = ROW_THREADS;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x;
     const T* z = (const T*)p.logits + (int64_t)r * p.row_stride;
     const SampleRow at(p.vocab);
-    const char* work = p.workspace + (size_t)r * at.bytes();
+    char* work = p.workspace + (size_t)r * at.bytes();
     const float* tops = (const float*)work;
-    const int n_chunks = at.runs * CHUNKS, per = (n_chunks + THREADS - 1) / THREADS;  // (4 at most)
+    SampleNote* note = (SampleNote*)(work + at.note());
+    const int n_chunks = at.runs * CHUNKS, per = (n_chunks + 4 * NT - 1) / (4 * NT);  // fours of chunks of a thread: 2 at most
     const Settings g(p, r);
     const bool scores = p.logprob || p.confidence;
 
     // the top, and the sums relative to it
-    float chunk[4];
-    uint32_t top_key = 0;
+    float chunk[8];
+    float most = -INFINITY;
+    bool nan = false;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int c = tid * per + j;
-        chunk[j] = j < per && c < n_chunks ? tops[c] : -INFINITY;
-        top_key = max(top_key, key_of(chunk[j]));
+    for (int j = 0; j < 2; ++j) {
+        const int c = (tid * per + j) * 4;
+        const float4 f = j < per && c < n_chunks ? *(const float4*)(tops + c) : float4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        chunk[4 * j] = f.x, chunk[4 * j + 1] = f.y, chunk[4 * j + 2] = f.z, chunk[4 * j + 3] = f.w;
+        most = fmaxf(most, fmaxf(fmaxf(f.x, f.y), fmaxf(f.z, f.w)));
+        nan |= f.x != f.x;  // (a run of 1024 with a NaN has sixteen)
     }
     u64 sum = 0;
     float raw_run = 0, run_top = -INFINITY;
@@ -482,12 +480,14 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(Sampling p) {
 #pragma unroll
         for (int j = 0; j < CHUNKS / 4; ++j) run_top = fmaxf(run_top, fmaxf(fmaxf(f[j].x, f[j].y), fmaxf(f[j].z, f[j].w)));
     }
-    for (int d = 1; d < 64; d *= 2) top_key = max(top_key, (uint32_t)__shfl_xor((int)top_key, d));
-    if (lane == 0) s.tops[wave] = top_key;
-    s.bin_count[tid] = 0;
-    if (tid == 0) s.cut = Cut{0, 1 << 30, 0}, s.place = 1 << 30, s.left = 0, s.hi = 0xffffffffu;
+    const uint32_t wave_top = wave_most(nan ? 0xffffffffu : key_of(most));
+    if (lane == 0) s.tops[wave] = wave_top;
+    s.c.bin_count[tid] = 0, s.c.bin_weight[tid] = 0;
+    s.floor_count[tid] = 0;
+    if (tid == 0) s.c.cut = nothing_cut(), s.place = 0xffffffffu, s.found = 0xffffffffu, s.candidates = 0, s.floor_bin = NT, note->wide = 0;
     __syncthreads();
-    for (int i = 0; i < WAVES; ++i) top_key = max(top_key, s.tops[i]);
+    uint32_t top_key = s.tops[0];
+    for (int i = 1; i < ROW_WAVES; ++i) top_key = max(top_key, s.tops[i]);
     if (g.bad || top_key >= KEY_INF || top_key <= KEY_NINF) {
         if (tid == 0) {
             p.token[r] = -1;
@@ -502,44 +502,43 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(Sampling p) {
     if (wave < (at.runs + 63) / 64) {
         if (g.whole_sum()) sum = rescaled(sum, ((double)run_ref - (double)top) * g.per_t);
         if (scores) {
-            int e;
-            const double m = power_of(((double)run_ref - (double)top) * 1.4426950408889634, e);
-            raw = ldexp((double)raw_run * m, e);
-            for (int d = 1; d < 64; d *= 2) raw += __shfl_xor(raw, d);
+            raw = wave_total((double)raw_run * power_of(((double)run_ref - (double)top) * 1.4426950408889634, 0));
         }
     }
     if (lane == 0) s.raw[wave] = raw;
     u64 total;
-    const u64 sum_before = before_me(sum, total, s.sums);
+    const u64 sum_before = before_me<NT>(sum, total, s.c.sums);
     raw = 0;
-    for (int i = 0; i < WAVES; ++i) raw += s.raw[i];
+    for (int i = 0; i < (RUNS + 63) / 64; ++i) raw += s.raw[i];
+    if (scores && wave == ROW_WAVES - 1) {
+        const double l = log(raw);
+        if (lane == 0) s.log_raw = l;
+    }
 
-    int token = 0;  // (of the first wave, or of all)
     if (g.greedy) {
         // the first chunk that has it, the first in the chunk
 #pragma unroll
-        for (int j = 3; j >= 0; --j)
-            if (j < per && chunk[j] == top) atomicMin(&s.place, tid * per + j);
+        for (int j = 7; j >= 0; --j)
+            if (j < 4 * per && chunk[j] == top) atomicMin(&s.place, tid * per * 4 + j);
         __syncthreads();
-        const int i = s.place * SAMPLE_CHUNK + lane;
-        const u64 equal = __ballot(i < p.vocab && (float)z[min(i, p.vocab - 1)] == top);
-        token = s.place * SAMPLE_CHUNK + __builtin_ctzll(equal);
+        if (wave == 0) {
+            const int i = s.place * SAMPLE_CHUNK + lane;
+            const u64 equal = __ballot(i < p.vocab && (float)z[min(i, p.vocab - 1)] == top);
+            if (lane == 0) s.found = s.place * SAMPLE_CHUNK + __builtin_ctzll(equal);
+        }
     } else if (!g.by_k && !g.by_p && !g.by_m) {
         // the run in which u * total lies, then the token in it, by the run's own weights
         const u64 target = share_of(g.u, total, false);
         if (sum_before <= target && sum_before + sum > target) s.place = tid, s.left = target - sum_before, s.ref = run_ref;
         __syncthreads();
-        const int i = s.place * SAMPLE_RUN + tid;
+        const int i = s.place * SAMPLE_RUN + tid * 2;
         const u64 left = s.left;
         const float ref = s.ref;
-        const u64 w = i < p.vocab ? weight_of((float)z[i], ref, g.per_t) : 0;
+        const u64 w0 = i < p.vocab ? weight_of((float)z[i], ref, g.per_t) : 0, w1 = i + 1 < p.vocab ? weight_of((float)z[i + 1], ref, g.per_t) : 0;
         u64 all;
-        const u64 before = before_me(w, all, s.sums);
-        if (tid == 0) s.hi = 0xffffffffu;
-        __syncthreads();
-        if (w && rescaled(before + w, ((double)ref - (double)top) * g.per_t) > left) atomicMin(&s.hi, (uint32_t)i);
-        __syncthreads();
-        token = (int)s.hi;
+        const u64 before = before_me<NT>(w0 + w1, all, s.c.sums);
+        const double y = ((double)ref - (double)top) * g.per_t;
+        if (rescaled(before, y) <= left && rescaled(before + w0 + w1, y) > left) s.found = rescaled(before + w0, y) > left ? i : i + 1;
     } else {
         const double reach = g.by_m ? -log((double)g.min_p) * (double)g.t : INFINITY;
         uint32_t least = KEY_NINF;  // the floor's key
@@ -547,33 +546,35 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(Sampling p) {
             // bins between the largest and the least of the runs' largest
             uint32_t low = KEY_INF;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 8; ++j)
                 if (chunk[j] > -INFINITY) low = min(low, key_of(chunk[j]));
-            for (int d = 1; d < 64; d *= 2) low = min(low, (uint32_t)__shfl_xor((int)low, d));
-            if (lane == 0) s.counts[wave] = low;
+            low = ~wave_most(~low);
+            if (lane == 0) s.c.counts[wave] = low;
             __syncthreads();
-            for (int i = 0; i < WAVES; ++i) low = min(low, s.counts[i]);
-            const float per_bin = fminf((BINS - 1) / (top - value_of(low)), 3e38f);
-            int bin[4];
+            for (int i = 0; i < ROW_WAVES; ++i) low = min(low, s.c.counts[i]);
+            const float per_bin = fminf((NT - 1) / (top - value_of(low)), 3e38f);
+            int bin[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                bin[j] = chunk[j] > -INFINITY ? (int)fminf((top - chunk[j]) * per_bin, (float)(BINS - 1)) : BINS;
-                if (bin[j] < BINS) atomicAdd(&s.bin_count[bin[j]], 1u);
+            for (int j = 0; j < 8; ++j) {
+                bin[j] = chunk[j] > -INFINITY ? bin_at(chunk[j], top, per_bin, NT) : NT;
+                if (bin[j] < NT) atomicAdd(&s.floor_count[bin[j]], 1u);
             }
             __syncthreads();
-            const uint32_t c = s.bin_count[tid];
+            const uint32_t c = s.floor_count[tid];
             uint32_t all;
-            const uint32_t c_before = before_me(c, all, s.counts);
-            if (tid == 0) s.bin = BINS, s.lo = KEY_INF;
+            const uint32_t c_before = before_me<NT>(c, all, s.c.counts);
+            if (c_before < (uint32_t)g.top_k && c_before + c >= (uint32_t)g.top_k) s.floor_bin = tid;
             __syncthreads();
-            if (c_before < (uint32_t)g.top_k && c_before + c >= (uint32_t)g.top_k) s.bin = tid;
-            __syncthreads();
-            if (s.bin < BINS) {  // (else fewer than k runs have any: no floor)
+            if (s.floor_bin < NT) {  // (else fewer than k runs have any: no floor)
+                uint32_t floor = KEY_INF;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (bin[j] <= s.bin) atomicMin(&s.lo, key_of(chunk[j]));
+                for (int j = 0; j < 8; ++j)
+                    if (bin[j] <= s.floor_bin) floor = min(floor, key_of(chunk[j]));
+                floor = ~wave_most(~floor);
+                if (lane == 0) s.tops[wave] = floor;
                 __syncthreads();
-                least = s.lo;
+                for (int i = 0; i < ROW_WAVES; ++i) floor = min(floor, s.tops[i]);
+                least = floor;
             }
         } else if (g.by_p && !g.by_k) {
             // (weights are off by less than one: what is below the floor's in full may be one above it as a whole number)
@@ -588,132 +589,476 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(Sampling p) {
         // the runs that have candidates, in order
         uint32_t flags = 0, n_some;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) flags |= (uint32_t)(chunk[j] >= least_z && chunk[j] > -INFINITY) << j;
+        for (int j = 0; j < 8; ++j) flags |= (uint32_t)(chunk[j] >= least_z && chunk[j] > -INFINITY) << j;
         __syncthreads();
-        uint32_t place = before_me((uint32_t)__popc(flags), n_some, s.counts);
+        uint32_t place = before_me<NT>((uint32_t)__popc(flags), n_some, s.c.counts);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (flags >> j & 1) s.chunks[place++] = tid * per + j;
+        for (int j = 0; j < 8; ++j)
+            if (flags >> j & 1) s.chunks[place++] = (uint16_t)(tid * per * 4 + j);
         __syncthreads();
-        // a wave takes neighbouring ones, eight loads at a time: how many candidates, then where they go
-        const int each = ((int)n_some + WAVES - 1) / WAVES, c0 = min((int)n_some, wave * each), c1 = min((int)n_some, c0 + each);
-        constexpr int AT_ONCE = 8;
-        float v[AT_ONCE];
-        int first[AT_ONCE];
-        auto load = [&](int c) {
+        // a wave takes neighbouring ones and keeps what it finds in its own place
+        const int each = ((int)n_some + ROW_WAVES - 1) / ROW_WAVES, c0 = min((int)n_some, wave * each), c1 = min((int)n_some, c0 + each);
+        uint32_t found = 0;
+        const float from_z = fmaxf(least_z, -3.4028235e38f);  // (nothing that is -inf)
+        float next[AT_ONCE / 4][4];
+        int next_at[AT_ONCE / 4];
+        auto load = [&](int c) {  // sixteen lanes a chunk, so that the lanes' order is that of the indices
 #pragma unroll
-            for (int j = 0; j < AT_ONCE; ++j) {
-                first[j] = (int)s.chunks[max(0, min(c + j, c1 - 1))] * SAMPLE_CHUNK;
-                const int i = first[j] + lane;
-                v[j] = c + j < c1 && i < p.vocab ? (float)z[i] : -INFINITY;
+            for (int j = 0; j < AT_ONCE / 4; ++j) {
+                const int mine = c + 4 * j + (lane >> 4);
+                next_at[j] = s.chunks[min(mine, c1 - 1)] * SAMPLE_CHUNK + (lane & 15) * 4;
+                load4(z, mine < c1 ? next_at[j] : p.vocab, p.vocab, p.vec, next[j]);
             }
         };
-        auto wanted = [&](float x) { return x >= least_z && x > -INFINITY; };
-        uint32_t found = 0;
+        if (c0 < c1) load(c0);
         for (int c = c0; c < c1; c += AT_ONCE) {
-            load(c);
+            float v[AT_ONCE / 4][4];
+            int at_index[AT_ONCE / 4];
 #pragma unroll
-            for (int j = 0; j < AT_ONCE; ++j) found += __popcll(__ballot(wanted(v[j])));
+            for (int j = 0; j < AT_ONCE / 4; ++j) {
+                at_index[j] = next_at[j];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[j][k] = next[j][k];
+            }
+            if (c + AT_ONCE < c1) load(c + AT_ONCE);
+            const uint32_t found_before = found;
+#pragma unroll
+            for (int j = 0; j < AT_ONCE / 4; j += 2) {  // (two counts of 256 at most in a number)
+                uint32_t n = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) n += (v[j][k] >= from_z ? 1u : 0u) + (v[j + 1][k] >= from_z ? 0x10000u : 0u);
+                const uint32_t upto = wave_scan(n), total_n = last_lane(upto), before = upto - n;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t slot = found + (h ? before >> 16 : before & 0xffff);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (v[j + h][k] >= from_z) {
+                            if (slot < WAVE_CANDIDATES) s.found_at[wave][slot] = float2{v[j + h][k], __int_as_float(at_index[j + h] + k)};
+                            ++slot;
+                        }
+                    found += h ? total_n >> 16 : total_n & 0xffff;
+                }
+            }
+            if (c + AT_ONCE < c1) {  // (too many already: the rest need not be read)
+                uint32_t all = 0;
+                if (lane == 0) all = atomicAdd(&s.candidates, found - found_before) + found - found_before;
+                if ((uint32_t)__builtin_amdgcn_readfirstlane((int)all) > CANDIDATES) {
+                    found = WAVE_CANDIDATES + 1;
+                    break;
+                }
+            }
         }
         if (lane == 0) s.tops[wave] = found;
         __syncthreads();
-        uint32_t n = 0, base = 0;
-        for (int i = 0; i < WAVES; ++i) {
-            if (i < wave) base += s.tops[i];
-            n += s.tops[i];
-        }
-        if (n > CANDIDATES) {
-            const RowElements<T> row{z, p.vocab, p.vec, top, least_z, g.per_t};
-            const float spread = least > KEY_NINF ? top - least_z : 32.f * g.t;
-            token = token_of_row(row, g, reach, s, fminf((BINS - 1) / spread, 3e38f));
-        } else {
-            uint32_t index[OWN], key[OWN], to = base;
-            u64 weight[OWN];
-            for (int c = c0; c < c1; c += AT_ONCE) {
-                if (each > AT_ONCE) load(c);  // (else they are here still)
+        uint32_t n = 0;
+        bool wide = false;
+        uint32_t from[ROW_WAVES];
 #pragma unroll
-                for (int j = 0; j < AT_ONCE; ++j) {
-                    const u64 some = __ballot(wanted(v[j]));
-                    if (wanted(v[j])) {
-                        const uint32_t slot = to + __popcll(some & ((1ull << lane) - 1));
-                        s.candidates.key[slot] = key_of(v[j]), s.candidates.index[slot] = first[j] + lane;
-                    }
-                    to += __popcll(some);
+        for (int i = 0; i < ROW_WAVES; ++i) from[i] = n, n += s.tops[i], wide |= s.tops[i] > WAVE_CANDIDATES;
+        if (wide || n > CANDIDATES) {
+            if (tid == 0) {
+                note->top_key = top_key, note->least = least, note->arrived = 0, note->total = total, note->raw = raw;
+                note->log_raw = scores ? s.log_raw : 0.0;
+                note->wide = wide_follows;
+            }
+            return;
+        }
+        const int mine = ((int)n + NT - 1) / NT, at0 = tid * mine;
+        uint32_t index[OWN], key[OWN];
+        u64 weight[OWN];
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) {
+            const bool ok = j < mine && at0 + j < (int)n;
+            int w = 0, i = at0 + j;
+#pragma unroll
+            for (int k = 1; k < ROW_WAVES; ++k)
+                if (at0 + j >= (int)from[k]) w = k, i = at0 + j - (int)from[k];
+            const float2 f = ok ? s.found_at[w][i] : float2{-INFINITY, __uint_as_float(0xffffffffu)};
+            key[j] = ok ? key_of(f.x) : 0;
+            index[j] = __float_as_uint(f.y);
+            weight[j] = ok ? weight_of(f.x, top, g.per_t) : 0;
+        }
+        const OwnElements own{key, weight, max(0, min(mine, (int)n - at0))};
+        const float per_bin = fminf((NT - 1) / (top - least_z), 3e38f);
+        if (g.by_k || g.by_p) {
+            fill_bins<NT>(own, s.c, [&](uint32_t key) { return bin_at(value_of(key), top, per_bin, NT); });
+            u64 whole = total;
+            if (g.by_k) {
+                const bool intact = find_cut<true, NT>(own, s.c, (u64)g.top_k, top, per_bin);
+                whole = s.c.cut.weight;
+                if (!g.by_p) whole = 1;
+                else if (!whole) before_me<NT>(own.sum(), whole, s.c.sums);  // (all are kept)
+                if (g.by_p && !intact) {
+                    __syncthreads();
+                    s.c.bin_weight[tid] = 0, s.c.bin_count[tid] = 0;
+                    __syncthreads();
+                    fill_bins<NT>(own, s.c, [&](uint32_t key) { return bin_at(value_of(key), top, per_bin, NT); });
                 }
             }
-            __syncthreads();
-            const int mine = ((int)n + THREADS - 1) / THREADS, at0 = tid * mine;
+            if (g.by_p) find_cut<false, NT>(own, s.c, max(share_of(g.top_p, whole, true), 1ull), top, per_bin);
+        }
+        // kept weights by index
+        const Cut cut = s.c.cut;
+        int left = 1 << 30;
+        if (cut.some) {
+            uint32_t ties = 0, all;
+#pragma unroll
+            for (int j = 0; j < OWN; ++j) ties += j < own.n && key[j] == cut.key;
+            left = cut.ties - (int)before_me<NT>(ties, all, s.c.counts);
+        }
+        u64 w[OWN], all, part = 0;
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) {
+            const bool in = j < own.n && (double)top - (double)value_of(key[j]) <= reach && (key[j] == cut.key ? left-- > 0 : key[j] > cut.key);
+            w[j] = in ? weight[j] : 0;
+            part += w[j];
+        }
+        u64 upto = before_me<NT>(part, all, s.c.sums);
+        const u64 target = share_of(g.u, all, false);
+        if (upto <= target && upto + part > target) {
+            uint32_t token = 0xffffffffu;
 #pragma unroll
             for (int j = 0; j < OWN; ++j) {
-                const bool ok = j < mine && at0 + j < (int)n;
-                key[j] = ok ? s.candidates.key[at0 + j] : 0;
-                index[j] = ok ? s.candidates.index[at0 + j] : 0xffffffffu;
-                weight[j] = ok ? weight_of(value_of(key[j]), top, g.per_t) : 0;
+                upto += w[j];
+                if (w[j] && upto > target) token = min(token, index[j]);
             }
-            const OwnElements own{key, weight, max(0, min(mine, (int)n - at0))};
-            const float per_bin = fminf((BINS - 1) / (top - least_z), 3e38f);
-            // kept weights by index
-            auto kept = [&](const Cut& cut, double far, u64 (&w)[OWN]) {
-                uint32_t ties = 0, all;
-#pragma unroll
-                for (int j = 0; j < OWN; ++j) ties += j < own.n && key[j] == cut.key;
-                int left = cut.ties - (int)before_me(ties, all, s.counts);
-                u64 part = 0;
-#pragma unroll
-                for (int j = 0; j < OWN; ++j) {
-                    const bool in = j < own.n && (double)top - (double)value_of(key[j]) <= far && (key[j] == cut.key ? left-- > 0 : key[j] > cut.key);
-                    w[j] = in ? weight[j] : 0;
-                    part += w[j];
-                }
-                return part;
-            };
-            u64 w[OWN], upto;
-            if (g.by_k) find_cut<true>(own, s, (u64)g.top_k, top, per_bin);
-            if (g.by_p) {
-                u64 limit_of = total;
-                if (g.by_k) {
-                    const u64 part = kept(s.cut, INFINITY, w);
-                    before_me(part, limit_of, s.sums);
-                }
-                find_cut<false>(own, s, max(share_of(g.top_p, limit_of, true), 1ull), top, per_bin);
-            }
-            const u64 part = kept(s.cut, reach, w);
-            u64 all;
-            upto = before_me(part, all, s.sums);
-            const u64 target = share_of(g.u, all, false);
-            if (tid == 0) s.hi = 0xffffffffu;
-            __syncthreads();
-            if (upto <= target && upto + part > target) {
-#pragma unroll
-                for (int j = 0; j < OWN; ++j) {
-                    upto += w[j];
-                    if (upto > target) atomicMin(&s.hi, index[j]);
-                }
-            }
-            __syncthreads();
-            token = (int)s.hi;
+            s.found = token;
         }
     }
+    __syncthreads();
     if (tid == 0) {
-        token = max(0, min(token, p.vocab - 1));
-        p.token[r] = token;
-        if (p.logprob) p.logprob[r] = (float)((double)(float)z[token] - (double)top - log(raw));
-        if (p.confidence) p.confidence[r] = (float)(1.0 / raw);
+        const int token = (int)min(s.found, (uint32_t)p.vocab - 1);
+        write_row(p, r, token, scores ? (float)z[token] : 0.f, top, raw, scores ? s.log_raw : 0.0);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// rows with many candidates
+// ------------------------------------------------------------------------------------------------
+constexpr int WIDE_THREADS = SAMPLE_BINS, WIDE_WAVES = WIDE_THREADS / 64;
+constexpr int MOST_PARTS = 8;
+
+// What a workgroup of the row leaves for the last one: for each bin its weight, and the first of its elements in a list of the part's
+// elements by bins, as indices in the part.  It goes past the caches of the XCD, by agent-scope stores and loads of single values.
+struct Part {
+    u64* weight;
+    uint32_t* first;  // [SAMPLE_BINS + 1]
+    uint16_t* element;
+    __device__ __forceinline__ Part(char* bins, int part_length, int i) {
+        char* base = bins + (size_t)i * sample_part_bytes(part_length);
+        weight = (u64*)base, first = (uint32_t*)(weight + SAMPLE_BINS), element = (uint16_t*)(first + SAMPLE_BINS + 4);
+    }
+};
+template <typename T>
+__device__ __forceinline__ void leave(T* p, T v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename T>
+__device__ __forceinline__ T take(const T* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The row's elements that are not below the floor, of [i0, i1), i0 a multiple of 4.
+template <typename T>
+struct RowElements {
+    static constexpr int AT_ONCE = 4;
+    const T* z;
+    int i0, i1, vec;
+    float top, least;
+    double per_t;
+    char* bins;  // of the parts, if they are there
+    int parts, part_length;
+    const uint32_t (*firsts)[SAMPLE_BINS + 1];  // where the parts' elements of each bin begin (LDS)
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        each(least, INFINITY, f);
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(float lo, float hi, F f) const {
+        lo = fmaxf(lo, least);
+        constexpr int STEP = WIDE_THREADS * 4;
+        float next[AT_ONCE][4];
+        auto load = [&](int i) {
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) load4(z, i + k * STEP, i1, vec, next[k]);
+        };
+        int i = i0 + threadIdx.x * 4;
+        if (i < i1) load(i);
+        for (; i < i1; i += STEP * AT_ONCE) {
+            float v[AT_ONCE][4];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[k][j] = next[k][j];
+            if (i + STEP * AT_ONCE < i1) load(i + STEP * AT_ONCE);
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (v[k][j] >= lo && v[k][j] <= hi && i + k * STEP + j < i1)
+                        f(key_of(v[k][j]), i + k * STEP + j, [&] { return weight_of(v[k][j], top, per_t); });
+        }
+    }
+    template <int NT>
+    __device__ __forceinline__ bool list(CutShared<NT>& s, int bin) const {
+        if (parts == 1) return false;
+        const int tid = threadIdx.x, lane = tid & 63;
+        // (every wave looks the parts' shares up, one in a lane)
+        uint32_t first = 0, n = 0;
+        if (lane < parts) first = firsts[lane][bin], n = firsts[lane][bin + 1] - first;
+        const uint32_t upto = wave_scan<16>(n);
+        const int all = (int)of_lane(upto, 15);
+        int at_part = 0;
+        for (int i = 1; i < parts; ++i) at_part = tid >= (int)of_lane(upto, i - 1) ? i : at_part;
+        const uint32_t start = (uint32_t)__shfl((int)first, at_part), before = (uint32_t)__shfl((int)(upto - n), at_part);
+        if (tid < all) {  // (LIST at most)
+            const int i = at_part * part_length + take(Part(bins, part_length, at_part).element + start + (tid - before));
+            const float v = (float)z[i];
+            s.list[tid] = key_of(v), s.list_index[tid] = i, s.list_weight[tid] = weight_of(v, top, per_t);
+        }
+        if (tid == 0) s.n_list = all;
+        return true;
+    }
+};
+
+struct WideShared {
+    CutShared<WIDE_THREADS> c;
+    uint32_t firsts[MOST_PARTS][SAMPLE_BINS + 1];
+    uint32_t last, found;
+    int place, ties_left, first_run, n_runs;
+    u64 left;
+    u64 part_weight[MOST_PARTS];
+    uint32_t part_ties[MOST_PARTS];
+    u64 run_weight[RUNS];
+    uint32_t run_ties[RUNS];
+};
+
+// The bins of a row are filled by `parts` workgroups, and whoever is the last goes on: the cuts; the part of the row in which u * total
+// lies, by the bins of each part and the elements of the bin in which the cut is; the run of 1024 tokens, by the sums of what is kept
+// in the part's runs; the token in it.  All sums are of whole numbers, so that their order does not matter.  One CU reads a row of
+// 50 304 in 10 us, so that nothing but the part's runs is read twice.
+template <typename T>
+__global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, int parts, char* shared_bins) {
+    __shared__ WideShared s;
+    constexpr int NT = WIDE_THREADS;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x / parts, part = blockIdx.x % parts;
+    const SampleRow at(p.vocab);
+    SampleNote* note = (SampleNote*)(p.workspace + (size_t)r * at.bytes() + at.note());
+    if (!note->wide) return;
+    const T* z = (const T*)p.logits + (int64_t)r * p.row_stride;
+    const Settings g(p, r);
+    const float top = value_of(note->top_key), least_z = value_of(note->least);
+    const float spread = note->least > KEY_NINF ? top - least_z : 32.f * g.t, per_bin = fminf((NT - 1) / spread, 3e38f);
+    auto bin_of = [&](uint32_t key) { return bin_at(value_of(key), top, per_bin, NT); };
+
+    s.c.bin_weight[tid] = 0, s.c.bin_count[tid] = 0;
+    if (tid == 0) s.c.cut = nothing_cut(), s.found = 0xffffffffu;
+    if (tid < MOST_PARTS) s.part_weight[tid] = 0, s.part_ties[tid] = 0;
+    __syncthreads();
+    const int runs_each = (at.runs + parts - 1) / parts, part_length = runs_each * SAMPLE_RUN;
+    char* bins = shared_bins + (size_t)r * parts * sample_part_bytes(part_length);
+    const RowElements<T> own{z, part * part_length, min(p.vocab, (part + 1) * part_length), p.vec, top, least_z, g.per_t, bins, parts, part_length, s.firsts};
+    fill_bins<NT>(own, s.c, bin_of);
+    u64 others[MOST_PARTS] = {};
+    if (parts > 1) {
+        const Part here(bins, part_length, part);
+        uint32_t n;
+        const uint32_t first = before_me<NT>(s.c.bin_count[tid], n, s.c.counts);
+        s.firsts[0][tid] = first;
+        leave(here.weight + tid, s.c.bin_weight[tid]);
+        leave(here.first + tid, first);
+        if (tid == 0) leave(here.first + NT, n);
+        __syncthreads();
+        own.each([&](uint32_t key, int i, auto) { leave(here.element + atomicAdd(&s.firsts[0][bin_of(key)], 1u), (uint16_t)(i - part * part_length)); });
+        // each thread's stores have arrived before its workgroup is counted
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (tid == 0) s.last = __hip_atomic_fetch_add(&note->arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)parts - 1;
+        __syncthreads();
+        if (!s.last) return;
+        uint32_t c = 0, firsts[MOST_PARTS];
+        u64 w = 0;
+        if (tid < MOST_PARTS) s.firsts[tid][NT] = take(Part(bins, part_length, min(tid, parts - 1)).first + NT);
+#pragma unroll
+        for (int i = 0; i < MOST_PARTS; ++i) {
+            const Part other(bins, part_length, min(i, parts - 1));
+            others[i] = take(other.weight + tid), firsts[i] = take(other.first + tid);
+        }
+#pragma unroll
+        for (int i = 0; i < MOST_PARTS; ++i) s.firsts[i][tid] = firsts[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < MOST_PARTS; ++i) {
+            others[i] = i < parts ? others[i] : 0;
+            w += others[i], c += i < parts ? s.firsts[i][tid + 1] - firsts[i] : 0;
+        }
+        s.c.bin_weight[tid] = w, s.c.bin_count[tid] = c;
+        __syncthreads();
+    }
+    const RowElements<T> row{z, 0, p.vocab, p.vec, top, least_z, g.per_t, bins, parts, part_length, s.firsts};
+    const double reach = g.by_m ? -log((double)g.min_p) * (double)g.t : INFINITY;
+    u64 whole = note->total;
+    if (g.by_k) {
+        const bool intact = find_cut<true, NT>(row, s.c, (u64)g.top_k, top, per_bin);
+        whole = s.c.cut.weight;
+        if (g.by_p) {
+            if (!whole) {  // all are kept
+                u64 w = 0;
+                row.each([&](uint32_t, int, auto weight) { w += weight(); });
+                before_me<NT>(w, whole, s.c.sums);
+            }
+            if (!intact) {
+                __syncthreads();
+                s.c.bin_weight[tid] = 0, s.c.bin_count[tid] = 0;
+                __syncthreads();
+                fill_bins<NT>(row, s.c, bin_of);
+            }
+        }
+    }
+    if (g.by_p) find_cut<false, NT>(row, s.c, max(share_of(g.top_p, whole, true), 1ull), top, per_bin);
+    __syncthreads();
+    const Cut cut = s.c.cut;
+    auto kept_weight = [&](float v, uint32_t key) { return key >= cut.key && (double)top - (double)v <= reach ? weight_of(v, top, g.per_t) : 0; };
+    const u64 tie = cut.key ? kept_weight(value_of(cut.key), cut.key) : 0;
+    // The part: what is kept in the bins before the cut's is all of them, in the cut's bin those of the list that are.  Where there is no
+    // list, or min-p takes some of them (or nothing is cut), all of the row is one part.
+    int first_run = 0, n_runs = at.runs, ties_before = 0;
+    u64 target;
+    const bool by_parts = parts > 1 && tie && s.c.listed;
+    if (by_parts) {
+        const int bin = bin_of(cut.key);
+#pragma unroll
+        for (int i = 0; i < MOST_PARTS; ++i) {
+            const u64 w = wave_total(tid < bin ? others[i] : 0ull);
+            if (lane == 0 && w) atomicAdd(&s.part_weight[i], w);
+        }
+        if (tid < (int)s.c.n_list) {
+            const int at_part = (int)s.c.list_index[tid] / part_length;
+            if (s.c.list[tid] == cut.key) atomicAdd(&s.part_ties[at_part], 1u);
+            else if (s.c.list[tid] > cut.key) atomicAdd(&s.part_weight[at_part], s.c.list_weight[tid]);
+        }
+        __syncthreads();
+        // (every wave for itself, a part in a lane)
+        const uint32_t ties = lane < MOST_PARTS ? s.part_ties[lane] : 0;
+        const int ties_left = max(0, cut.ties - (int)(wave_scan<16>(ties) - ties));
+        const u64 w = (lane < MOST_PARTS ? s.part_weight[lane] : 0) + tie * (u64)min((int)ties, ties_left);
+        const u64 upto = wave_scan<16>(w);
+        target = share_of(g.u, of_lane(upto, 15), false);
+        const int at_part = __builtin_ctzll(__ballot(lane < MOST_PARTS && upto > target));
+        target -= of_lane(upto - w, at_part);
+        ties_before = cut.ties - __builtin_amdgcn_readlane(ties_left, at_part);
+        first_run = at_part * runs_each, n_runs = min(runs_each, at.runs - first_run);
+    }
+    float v[4][4];
+    auto load = [&](int run) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) load4(z, run * SAMPLE_RUN + k * 256 + lane * 4, p.vocab, p.vec, v[k]);
+    };
+    for (int run = wave; run < n_runs; run += WIDE_WAVES) {
+        u64 w = 0;
+        uint32_t ties = 0;
+        load(first_run + run);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t key = key_of(v[k][j]);
+                if (key == cut.key) ++ties;
+                else w += kept_weight(v[k][j], key);
+            }
+        w = wave_scan(w), ties = wave_scan(ties);
+        if (lane == 63) s.run_weight[run] = w, s.run_ties[run] = ties;
+    }
+    __syncthreads();
+    {
+        const uint32_t ties = tid < n_runs ? s.run_ties[tid] : 0;
+        uint32_t all_ties;
+        u64 all;
+        const int ties_left = max(0, cut.ties - ties_before - (int)before_me<NT>(ties, all_ties, s.c.counts));
+        const u64 w = (tid < n_runs ? s.run_weight[tid] : 0) + tie * (u64)min((int)ties, ties_left);
+        const u64 before = before_me<NT>(w, all, s.c.sums);
+        if (!by_parts) target = share_of(g.u, all, false);
+        if (before <= target && before + w > target) s.place = tid, s.left = target - before, s.ties_left = ties_left;
+        __syncthreads();
+    }
+    if (s.place % WIDE_WAVES == wave) {
+        // (where a wave has one run only, its logits are still here)
+        if (n_runs > WIDE_WAVES) load(first_run + s.place);
+        u64 left = s.left;
+        int ties_left = s.ties_left;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t ties = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ties += key_of(v[k][j]) == cut.key;
+            const uint32_t ties_upto = wave_scan(ties);
+            int mine_left = ties_left - (int)(ties_upto - ties);
+            u64 w[4], mine = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t key = key_of(v[k][j]);
+                w[j] = key == cut.key ? (mine_left-- > 0 ? tie : 0) : kept_weight(v[k][j], key);
+                mine += w[j];
+            }
+            const u64 upto = wave_scan(mine), all = last_lane(upto);
+            u64 sum = upto - mine;
+            if (left < all && sum <= left && upto > left) {
+                int j_at = -1;
+#pragma unroll
+                for (int j = 3; j >= 0; --j) {
+                    u64 to = sum;
+#pragma unroll
+                    for (int i = 0; i <= j; ++i) to += w[i];
+                    if (to > left) j_at = j;
+                }
+                s.found = (first_run + s.place) * SAMPLE_RUN + k * 256 + lane * 4 + j_at;
+            }
+            if (left < all) break;
+            left -= all, ties_left -= (int)last_lane(ties_upto);
+        }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        const int token = (int)min(s.found, (uint32_t)p.vocab - 1);
+        write_row(p, r, token, (float)z[token], top, note->raw, note->log_raw);
     }
 }
 
 }  // namespace
 
+// Rows with many candidates take eight workgroups each as long as rows are few.  (An element is noted in 16 bits in its part.)
+int sample_parts(int rows, int vocab) {
+    if (vocab < 16384 || rows > 256) return 1;
+    return std::max(rows > 128 ? 2 : rows > 64 ? 4 : MOST_PARTS, (SampleRow(vocab).runs + 63) / 64);
+}
+
+size_t sample_workspace(int rows, int vocab) {
+    const int parts = sample_parts(rows, vocab), runs = SampleRow(vocab).runs;
+    const size_t shared = parts > 1 ? sample_part_bytes((runs + parts - 1) / parts * SAMPLE_RUN) * parts * rows : 0;
+    return (SampleRow(vocab).bytes() * rows + 255) / 256 * 256 + shared;
+}
+
+template <typename T>
+static void launch_typed(const Sampling& p, hipStream_t st) {
+    const SampleRow at(p.vocab);
+    // as many waves as the chip holds at once, or so many fewer that all have the same number of runs
+    const int64_t runs = (int64_t)p.rows * at.runs, each = (runs + 8191) / 8192, waves = (runs + each - 1) / each;
+    EE_LAUNCH(sample_runs_kernel<T>, dim3((int)((waves + 3) / 4)), dim3(256), st, p, (int)each);
+    // what the host knows of the settings and sizes may rule out rows with many candidates
+    const bool cuts = p.top_k || p.top_p || p.min_p || (p.one_top_k > 0 && p.one_top_k < p.vocab) || p.one_top_p < 1.f || p.one_min_p > 0.f;
+    const bool wide = cuts && p.vocab > WAVE_CANDIDATES;
+    EE_LAUNCH(sample_row_kernel<T>, dim3(p.rows), dim3(ROW_THREADS), st, p, wide);
+    if (!wide) return;
+    const int parts = sample_parts(p.rows, p.vocab);
+    EE_LAUNCH(sample_wide_kernel<T>, dim3(p.rows * parts), dim3(WIDE_THREADS), st, p, parts, p.workspace + (at.bytes() * p.rows + 255) / 256 * 256);
+}
+
 hipError_t launch_sample(const Sampling& p, hipStream_t st) {
-    const int64_t waves = (int64_t)p.rows * SampleRow(p.vocab).runs;
-    const int grid = (int)std::min<int64_t>((waves + 3) / 4, 256 * 8);
-    if (p.dtype == EE_BF16) {
-        EE_LAUNCH(sample_runs_kernel<__bf16>, dim3(grid), dim3(256), st, p);
-        EE_LAUNCH(sample_kernel<__bf16>, dim3(p.rows), dim3(THREADS), st, p);
-    } else {
-        EE_LAUNCH(sample_runs_kernel<float>, dim3(grid), dim3(256), st, p);
-        EE_LAUNCH(sample_kernel<float>, dim3(p.rows), dim3(THREADS), st, p);
-    }
+    if (p.dtype == EE_BF16)
+        launch_typed<__bf16>(p, st);
+    else
+        launch_typed<float>(p, st);
     return hipGetLastError();
 }
 

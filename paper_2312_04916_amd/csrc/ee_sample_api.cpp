@@ -9,7 +9,7 @@ extern "C" {
 int ee_sample_bytes(int rows, int vocab, size_t* workspace_bytes) {
     if (!workspace_bytes || rows < 0 || rows > (1 << 20)) return EE_ERR_ARG;
     if (vocab < 1 || vocab > (1 << 18)) return EE_ERR_CONFIG;
-    *workspace_bytes = SampleRow(vocab).bytes() * rows;
+    *workspace_bytes = sample_workspace(rows, vocab);
     return EE_OK;
 }
 
@@ -28,7 +28,7 @@ int ee_sample(int rows, int vocab, int dtype, const void* dev_logits, int64_t ro
          (uintptr_t)dev_logprob | (uintptr_t)dev_confidence) & 3)
         return EE_ERR_ARG;
     if (!dev_workspace || (uintptr_t)dev_workspace & 255) return EE_ERR_ARG;
-    const size_t need = SampleRow(vocab).bytes() * rows;
+    const size_t need = sample_workspace(rows, vocab);
     if (workspace_bytes < need) return EE_ERR_NOMEM;
     // rows are read while others' results are already written
     const int64_t span = (int64_t)(rows - 1) * row_stride * es;

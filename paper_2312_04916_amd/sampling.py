@@ -11,18 +11,18 @@ from .binding import EE_BF16, EE_F32, _chk, lib
 from .kv4 import _current_device, _raw_stream, _used_on
 
 _CODES = {torch.bfloat16: EE_BF16, torch.float32: EE_F32}
-_fn, _row_bytes = None, {}
+_fn, _sizes = None, {}
 
 
 def _workspace_bytes(rows: int, vocab: int) -> int:
-    per_row = _row_bytes.get(vocab)
-    if per_row is None:
-        size = C.c_size_t()
-        _chk(lib().ee_sample_bytes(1, vocab, C.byref(size)), "ee_sample_bytes")
-        if len(_row_bytes) >= 4096:
-            _row_bytes.clear()
-        per_row = _row_bytes[vocab] = size.value
-    return rows * per_row
+    size = _sizes.get((rows, vocab))
+    if size is None:
+        s = C.c_size_t()
+        _chk(lib().ee_sample_bytes(rows, vocab, C.byref(s)), "ee_sample_bytes")
+        if len(_sizes) >= 4096:
+            _sizes.clear()
+        size = _sizes[(rows, vocab)] = s.value
+    return size
 
 
 def _setting(v, off, dtype, rows: int, index: int, what: str):
