@@ -11,7 +11,7 @@ namespace ee {
 // 16 rows (of a weight, or of x) by 128 elements of the contraction are one fragment of 2048 bytes, in the order in which a wave's
 // lanes hold an operand of the 8-bit matrix instructions: two halves of 16 bytes per lane, so that every load is one contiguous
 // kilobyte.  Lane = 16 * quarter + row holds elements 32 * quarter .. + 31, the first 16 in half 0.  A weight is
-// [n tiles][k steps] fragments and as many bytes of exponents (e + 127); of a pair, tile 2i is the gate's tile i and tile 2i + 1 the
+// [n tiles][k steps] fragments and, behind them, [k steps][n tiles, rounded up to 4] bytes of exponents (e + 127); of a pair, tile 2i is the gate's tile i and tile 2i + 1 the
 // up weight's, so that a wave that has both multiplies them where they are.  Quantised rows are [m tiles][k steps] fragments and
 // [m tiles][k steps][16] exponents.  What lies behind n, m and k is zero.
 constexpr int F8_FRAGMENT = 2048;
@@ -21,7 +21,8 @@ struct F8Shape {
     constexpr int tiles() const { return (n + 15) / 16 * (pair ? 2 : 1); }
     constexpr int steps() const { return (k + 127) / 128; }
     constexpr size_t exponents() const { return (size_t)tiles() * steps() * F8_FRAGMENT; }  // where they begin
-    constexpr size_t bytes() const { return exponents() + (size_t)tiles() * steps(); }
+    constexpr int exponent_row() const { return (tiles() + 3) / 4 * 4; }
+    constexpr size_t bytes() const { return exponents() + (size_t)exponent_row() * steps(); }
 };
 
 struct F8Rows {
@@ -42,7 +43,7 @@ struct F8Product {
     const void* add;
     int64_t add_row;
     char* workspace;
-    int x_vec, y_vec;  // rows of x, of y and add, can be moved 16 bytes, four elements at a time
+    int x_vec, y_vec;  // rows of x can be moved 16 bytes at a time, rows of y and add so many elements (8, 4 or 1)
 };
 
 size_t f8_workspace(int m, int n, int k, int pair, int y_dtype);

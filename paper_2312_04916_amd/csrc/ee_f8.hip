@@ -15,6 +15,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
@@ -118,15 +119,19 @@ __global__ __launch_bounds__(512) void f8_pack_kernel(F8Shape s, const T* w, int
     codes_of(v, e, c);
     const size_t f = (size_t)tile * s.steps() + step;
     store_fragment(weight + f * F8_FRAGMENT, lane, c);
-    if (lane == 0) weight[s.exponents() + f] = (char)stored(e);
+    // (the row's rounding up is written too: by the last tile)
+    if (lane == 0) {
+        for (int i = tile; i < (tile == s.tiles() - 1 ? s.exponent_row() : tile + 1); ++i)
+            weight[s.exponents() + (size_t)step * s.exponent_row() + i] = (char)stored(e);
+    }
 }
 
 template <typename T>
 __global__ __launch_bounds__(64) void f8_unpack_kernel(F8Shape s, int up, const char* weight, T* w) {
     const int lane = threadIdx.x, step = blockIdx.y, row = blockIdx.x * 16 + (lane & 15), k0 = step * 128 + (lane >> 4) * 32;
-    const size_t f = (size_t)(blockIdx.x * (s.pair ? 2 : 1) + up) * s.steps() + step;
-    const i32x8 c = load_fragment(weight + f * F8_FRAGMENT, lane);
-    const float unit = __uint_as_float((uint32_t)(uint8_t)weight[s.exponents() + f] << 23);
+    const int tile = blockIdx.x * (s.pair ? 2 : 1) + up;
+    const i32x8 c = load_fragment(weight + ((size_t)tile * s.steps() + step) * F8_FRAGMENT, lane);
+    const float unit = __uint_as_float((uint32_t)(uint8_t)weight[s.exponents() + (size_t)step * s.exponent_row() + tile] << 23);
     if (row >= s.n) return;
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
@@ -177,7 +182,7 @@ __device__ __forceinline__ void finish(const F8Product& p, int row, int col, f32
     T* y = (T*)p.y + row * p.y_row + col;
     const T* add = p.add ? (const T*)p.add + row * p.add_row + col : nullptr;
     typedef T T4 __attribute__((ext_vector_type(4)));
-    if (p.y_vec && col + 3 < p.n) {
+    if (p.y_vec >= 4 && col + 3 < p.n) {
         if (add) {
             const T4 a = *(const T4*)add;
 #pragma unroll
@@ -189,6 +194,24 @@ __device__ __forceinline__ void finish(const F8Product& p, int row, int col, f32
         for (int i = 0; i < 4; ++i)
             if (col + i < p.n) y[i] = (T)(add ? v[i] + (float)add[i] : v[i]);
     }
+}
+
+// Eight of them.
+template <typename T>
+__device__ __forceinline__ void finish8(const F8Product& p, int row, int col, f32x4 a, f32x4 b) {
+    if (row >= p.m || col >= p.n) return;
+    if (p.y_vec < 8 || col + 7 >= p.n) {
+        finish<T>(p, row, col, a);
+        finish<T>(p, row, col + 4, b);
+        return;
+    }
+    typedef T T8 __attribute__((ext_vector_type(8)));
+    if (p.add) {
+        const T8 v = *(const T8*)((const T*)p.add + row * p.add_row + col);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] += (float)v[i], b[i] += (float)v[i + 4];
+    }
+    *(T8*)((T*)p.y + row * p.y_row + col) = T8{(T)a[0], (T)a[1], (T)a[2], (T)a[3], (T)b[0], (T)b[1], (T)b[2], (T)b[3]};
 }
 
 // A wave computes 16 * MT rows of x by NT tiles of the weight, a workgroup's waves share the contraction and add up through LDS in
@@ -204,9 +227,9 @@ __global__ __launch_bounds__(W * 64) void f8_matmul_kernel(F8Product p, F8Shape 
         int we[NT], xe[MT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const size_t f = (size_t)min(tile0 + j, tiles - 1) * steps + step;
-            w[j] = load_fragment(p.weight + f * F8_FRAGMENT, lane);
-            we[j] = (uint8_t)p.weight[s.exponents() + f];
+            const int tile = min(tile0 + j, tiles - 1);
+            w[j] = load_fragment(p.weight + ((size_t)tile * steps + step) * F8_FRAGMENT, lane);
+            we[j] = (uint8_t)p.weight[s.exponents() + (size_t)step * s.exponent_row() + tile];
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
@@ -256,6 +279,175 @@ __global__ __launch_bounds__(W * 64) void f8_matmul_kernel(F8Product p, F8Shape 
     }
 }
 
+typedef const char __attribute__((address_space(1))) global_char;
+typedef const void __attribute__((address_space(1))) global_void;
+#define F8_LDS(p) ((__attribute__((address_space(3))) void*)(p))
+// (as in the prompt phase: the compiler would let every read wait for all copies into LDS that are on their way)
+#define F8_READ(dst, at, off) asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(dst) : "v"(at), "n"(off))
+#define F8_READ_BYTE(dst, at, off) asm volatile("ds_read_u8 %0, %1 offset:%2" : "=v"(dst) : "v"(at), "n"(off))
+
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// Many rows: a workgroup of 2 x 2 waves computes 64 * MI rows of x by 4 * NI tiles of the weight, a wave 32 * MI by 2 * NI tiles in
+// instructions of 32 x 32 x 64.  Both operands come through LDS, copied past the registers in their own order, 64 elements of
+// the contraction at a time, four such stages in turn; the next stage's operands are read while the products of this one run.
+template <typename T, int MI, int NI>
+__global__ __launch_bounds__(256, 1) void f8_tile_kernel(F8Product p, F8Shape s, F8Rows r, int m_groups, int n_groups) {
+    constexpr int WT = 4 * NI, XT = 4 * MI, FRAGS = WT + XT, STAGES = 4;
+    constexpr int EXPONENTS = FRAGS * 1024, STAGE = EXPONENTS + 1024;  // 256 bytes of x's, of the weight's, two unused copies of them
+    constexpr int COPIES = FRAGS / 4 + 1;                             // of a wave
+    __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wn = wave & 1, wm = wave >> 1;
+    // an XCD takes whole panels of the weight, all rows of one after the other: a panel comes from memory once
+    const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, n_group = turn / m_groups * 8 + xcd, m_group = turn % m_groups;
+    if (n_group >= n_groups) return;
+    const int steps = s.steps(), tile0 = n_group * WT, mt0 = m_group * XT, m_tiles = (p.m + 15) / 16, halves = 2 * steps;
+    // what this wave copies: fragments, 512 bytes of either half of each, and a kind of exponents
+    global_char* from[FRAGS / 4];
+#pragma unroll
+    for (int i = 0; i < FRAGS / 4; ++i) {
+        const int f = wave * (FRAGS / 4) + i;
+        from[i] = (global_char*)(f < WT ? p.weight + (size_t)min(tile0 + f, s.tiles() - 1) * steps * F8_FRAGMENT
+                                        : p.workspace + (size_t)min(mt0 + f - WT, m_tiles - 1) * steps * F8_FRAGMENT);
+    }
+    const bool of_x = (wave & 1) == 0;
+    global_char* from_e = (global_char*)(of_x ? p.workspace + r.exponents() + (size_t)mt0 * steps * 16 : p.weight + s.exponents());
+    const uint32_t e_step = of_x ? 16 : s.exponent_row(), at_lane = (lane >> 5) * 1024 + (lane & 31) * 16;
+    const uint32_t e_lane = of_x ? (uint32_t)min(lane >> 2, m_tiles - 1 - mt0) * steps * 16 + (lane & 3) * 4 : (uint32_t)min(tile0 + lane * 4, s.exponent_row() - 4);
+    auto copy_one = [&](int buffer, size_t on, uint32_t on_e, int i) {
+        if (i < FRAGS / 4)
+            __builtin_amdgcn_global_load_lds((global_void*)(from[min(i, FRAGS / 4 - 1)] + on + at_lane), F8_LDS(lds + buffer * STAGE + (wave * (FRAGS / 4) + i) * 1024), 16, 0, 0);
+        else
+            __builtin_amdgcn_global_load_lds((global_void*)(from_e + on_e + e_lane), F8_LDS(lds + buffer * STAGE + EXPONENTS + wave * 256), 4, 0, 0);
+    };
+    auto offset_of = [&](int half) { return (size_t)(half >> 1) * F8_FRAGMENT + (half & 1) * 512; };
+    struct Operands {
+        i32x4 w[NI][2], x[MI][2];
+        int we[NI], xe[MI];
+    };
+    const unsigned lds0 = (unsigned)(size_t)F8_LDS(lds), row32 = lane & 31;
+    const unsigned at = (row32 >> 4) * 1024 + (lane >> 5) * 256 + (row32 & 15) * 16;
+    const unsigned at_w = lds0 + wn * (2 * NI) * 1024 + at, at_x = lds0 + (WT + wm * (2 * MI)) * 1024 + at;
+    const unsigned at_we = lds0 + EXPONENTS + 256 + wn * (2 * NI) + (row32 >> 4), at_xe = lds0 + EXPONENTS + wm * (32 * MI) + row32;
+    f32x16 acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
+    auto read_w = [&](Operands& o, unsigned stage, int j) {
+        switch (j) {
+            case 0: F8_READ(o.w[0][0], at_w + stage, 0); F8_READ(o.w[0][1], at_w + stage, 512); F8_READ_BYTE(o.we[0], at_we + stage, 0); break;
+            case 1: F8_READ(o.w[1][0], at_w + stage, 2048); F8_READ(o.w[1][1], at_w + stage, 2560); F8_READ_BYTE(o.we[1], at_we + stage, 2); break;
+            case 2: if constexpr (NI > 2) { F8_READ(o.w[2][0], at_w + stage, 4096); F8_READ(o.w[2][1], at_w + stage, 4608); F8_READ_BYTE(o.we[2], at_we + stage, 4); } break;
+            case 3: if constexpr (NI > 3) { F8_READ(o.w[3][0], at_w + stage, 6144); F8_READ(o.w[3][1], at_w + stage, 6656); F8_READ_BYTE(o.we[3], at_we + stage, 6); } break;
+        }
+    };
+    auto read_x = [&](Operands& o, unsigned stage, int i) {
+        switch (i) {
+            case 0: F8_READ(o.x[0][0], at_x + stage, 0); F8_READ(o.x[0][1], at_x + stage, 512); F8_READ_BYTE(o.xe[0], at_xe + stage, 0); break;
+            case 1: F8_READ(o.x[1][0], at_x + stage, 2048); F8_READ(o.x[1][1], at_x + stage, 2560); F8_READ_BYTE(o.xe[1], at_xe + stage, 32); break;
+            case 2: if constexpr (MI > 2) { F8_READ(o.x[2][0], at_x + stage, 4096); F8_READ(o.x[2][1], at_x + stage, 4608); F8_READ_BYTE(o.xe[2], at_xe + stage, 64); } break;
+            case 3: if constexpr (MI > 3) { F8_READ(o.x[3][0], at_x + stage, 6144); F8_READ(o.x[3][1], at_x + stage, 6656); F8_READ_BYTE(o.xe[3], at_xe + stage, 96); } break;
+        }
+    };
+    auto landed = [&](Operands& o) {  // (products that use them do not move above this)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int j = 0; j < NI; ++j) asm volatile("" : "+v"(o.w[j][0]), "+v"(o.w[j][1]), "+v"(o.we[j]));
+#pragma unroll
+        for (int i = 0; i < MI; ++i) asm volatile("" : "+v"(o.x[i][0]), "+v"(o.x[i][1]), "+v"(o.xe[i]));
+    };
+    // One stage's products; the next one's operands are read and a copy is begun in between.
+    auto stage = [&](const Operands& now, Operands& next, int half) {
+        // (behind the last stage an old one is read and copied again, for nothing)
+        const unsigned next_stage = ((half + 1) & (STAGES - 1)) * STAGE;
+        const int ahead = min(half + STAGES, halves - 1), buffer = half & (STAGES - 1);
+        const size_t on = offset_of(ahead);
+        const uint32_t on_e = (uint32_t)(ahead >> 1) * e_step;
+        constexpr int SLOTS = MI * NI - 1;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const i32x8 x = __builtin_shufflevector(now.x[i][0], now.x[i][1], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                const i32x8 w = __builtin_shufflevector(now.w[j][0], now.w[j][1], 0, 1, 2, 3, 4, 5, 6, 7);
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, acc[i][j], 0, 0, 0, now.we[j], 0, now.xe[i]);
+                __builtin_amdgcn_sched_barrier(0);
+                const int t = i * NI + j;
+                if (t == 0) {
+                    // the next stage is there once no more than the two behind it are on their way; then this one's buffer,
+                    // which all waves have read, is filled again
+                    wait_copies<2 * COPIES>();
+                    __builtin_amdgcn_s_barrier();
+                } else {
+#pragma unroll
+                    for (int k = 0; k < NI + MI; ++k) {
+                        if (k * SLOTS / (NI + MI) != t - 1) continue;
+                        if (k < NI) read_w(next, next_stage, k);
+                        else read_x(next, next_stage, k - NI);
+                    }
+#pragma unroll
+                    for (int k = 0; k < COPIES; ++k)
+                        if (k * SLOTS / COPIES == t - 1) copy_one(buffer, on, on_e, k);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        landed(next);
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) {
+        const int half = min(i, halves - 1);
+#pragma unroll
+        for (int k = 0; k < COPIES; ++k) copy_one(i, offset_of(half), (uint32_t)(half >> 1) * e_step, k);
+    }
+    wait_copies<(STAGES - 1) * COPIES>();
+    __builtin_amdgcn_s_barrier();
+    Operands a, b;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) read_w(a, 0, j);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) read_x(a, 0, i);
+    landed(a);
+    for (int half = 0; half < halves; half += 2) {  // (an even number)
+        stage(a, b, half);
+        stage(b, a, half + 1);
+    }
+    wait_copies<0>();
+    __builtin_amdgcn_s_barrier();  // (the stages' buffers are read no more)
+    // Results go through LDS, 32 rows at a time, so that they are written in whole lines.
+    constexpr int COLS = 32 * NI, PITCH = COLS + 4;  // floats
+    float* mine = (float*)(lds + wave * (32 * PITCH * 4));
+    const int col0 = (lane >> 5) * 4, cols = p.pair ? COLS / 2 : COLS, per_row = cols / 8, out0 = (tile0 + wn * 2 * NI) / (p.pair ? 2 : 1) * 16;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                f32x4 v = {acc[i][j][4 * k], acc[i][j][4 * k + 1], acc[i][j][4 * k + 2], acc[i][j][4 * k + 3]};
+                if (p.pair) {
+                    if (k >= 2) continue;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) v[h] = silu(v[h]) * acc[i][j][4 * (k + 2) + h];
+                }
+                *(f32x4*)(mine + row32 * PITCH + j * (p.pair ? 16 : 32) + k * 8 + col0) = v;
+            }
+        }
+        const int row0 = (mt0 + (wm * MI + i) * 2) * 16;
+        for (int e = lane; e < 32 * per_row; e += 64) {
+            const int row = e / per_row, col = e % per_row * 8;
+            const float* from_row = mine + row * PITCH + col;
+            finish8<T>(p, row0 + row, out0 + col, *(const f32x4*)from_row, *(const f32x4*)(from_row + 4));
+        }
+    }
+}
+
 }  // namespace
 
 size_t f8_workspace(int m, int n, int k, int pair, int y_dtype) { return F8Rows{m, (k + 127) / 128}.bytes(); }
@@ -288,6 +480,13 @@ hipError_t launch_f8_matmul(const F8Product& p, hipStream_t st) {
         EE_LAUNCH(f8_rows_kernel<__bf16>, rows_grid, dim3(256), st, r, (const __bf16*)p.x, p.x_row, p.k, p.x_vec, p.workspace);
     else
         EE_LAUNCH(f8_rows_kernel<float>, rows_grid, dim3(256), st, r, (const float*)p.x, p.x_row, p.k, p.x_vec, p.workspace);
+    if (p.m > 256 && p.y_dtype == EE_BF16) {
+        constexpr int MI = 4, NI = 4;
+        const int m_groups = (p.m + 64 * MI - 1) / (64 * MI), n_groups = (s.tiles() + 4 * NI - 1) / (4 * NI);
+        const dim3 grid((n_groups + 7) / 8 * 8 * m_groups);
+        EE_LAUNCH((f8_tile_kernel<__bf16, MI, NI>), grid, dim3(256), st, p, s, r, m_groups, n_groups);
+        return hipGetLastError();
+    }
     constexpr int MT = 2, NT = 2, W = 4;
     const dim3 grid((s.tiles() + NT - 1) / NT, ((p.m + 15) / 16 + MT - 1) / MT);
     if (p.y_dtype == EE_BF16)
