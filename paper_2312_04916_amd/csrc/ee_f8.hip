@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "ee_f8.h"
 #include "ee_lanes.h"
@@ -214,48 +215,119 @@ __device__ __forceinline__ void finish8(const F8Product& p, int row, int col, f3
     *(T8*)((T*)p.y + row * p.y_row + col) = T8{(T)a[0], (T)a[1], (T)a[2], (T)a[3], (T)b[0], (T)b[1], (T)b[2], (T)b[3]};
 }
 
-// A wave computes 16 * MT rows of x by NT tiles of the weight, a workgroup's waves share the contraction and add up through LDS in
-// their order.  T: of the result; float: the held values go through the bf16 instructions, which keep every bit of a product.
-template <typename T, int MT, int NT, int W>
-__global__ __launch_bounds__(W * 64) void f8_matmul_kernel(F8Product p, F8Shape s, F8Rows r) {
+// Rows of x as a kernel takes them that quantises them itself: [16 rows][k] in their own type, k a multiple of 128 and rows aligned.
+template <typename X>
+struct RawRows {
+    i32x4 v[sizeof(X) * 2];
+    __device__ __forceinline__ void load(const X* row) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(X) * 2; ++i) v[i] = ((const i32x4*)row)[i];
+    }
+    __device__ __forceinline__ void codes(i32x8& c, int& e) const {
+        float f[32];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(X) * 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (sizeof(X) == 2) {
+                    f[i * 8 + j * 2] = __uint_as_float((uint32_t)v[i][j] << 16);
+                    f[i * 8 + j * 2 + 1] = __uint_as_float((uint32_t)v[i][j] & 0xffff0000u);
+                } else {
+                    f[i * 4 + j] = __int_as_float(v[i][j]);
+                }
+            }
+        const uint32_t ex = exponent_of(top_of_quarters(top_of(f)));
+        codes_of(f, ex, c);
+        e = (int)stored(ex);
+    }
+};
+struct HeldRows {};  // they are in the workspace
+
+// Few rows: the weight comes straight from memory into the registers of the wave that multiplies it.  A wave computes 16 * MT rows of x by NT
+// tiles of the weight in every W-th step of 128 elements, D steps ahead of which its loads are; the waves' sums are added up in
+// LDS in their order.  T: of the result; float: the held values go through the bf16 instructions, which keep every bit of a
+// product.  X: HeldRows, or the type in which the rows come, which every wave then quantises for itself (MT = 1).
+template <typename T, typename X, int MT, int NT, int W, int D>
+__global__ __launch_bounds__(W * 64) void f8_stream_kernel(F8Product p, F8Shape s, F8Rows r, int m_groups, int n_groups) {
+    constexpr bool RAW = !__is_same(X, HeldRows);
+    static_assert(!RAW || MT == 1, "rows that are quantised here");
     __shared__ f32x4 s_part[W][MT * NT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tile0 = blockIdx.x * NT, mt0 = blockIdx.y * MT, tiles = s.tiles(), steps = s.steps(), m_tiles = (p.m + 15) / 16;
+    // the groups of rows that take the same tiles of the weight follow one another on one XCD
+    const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, n_group = turn / m_groups * 8 + xcd, m_group = turn % m_groups;
+    if (n_group >= n_groups) return;
+    const int tile0 = n_group * NT, mt0 = m_group * MT, tiles = s.tiles(), steps = s.steps(), m_tiles = (p.m + 15) / 16;
+    const int exponent_row = s.exponent_row(), mine = (steps - wave + W - 1) / W;
     f32x4 acc[MT][NT] = {};
-    for (int step = wave; step < steps; step += W) {
-        i32x8 w[NT], x[MT];
-        int we[NT], xe[MT];
+    struct Step {
+        i32x8 w[NT], x[RAW ? 1 : MT];
+        int we[NT], xe[RAW ? 1 : MT];
+        RawRows<typename std::conditional<RAW, X, float>::type> raw;
+    };
+    const char *w_at[NT], *x_at[MT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) w_at[j] = p.weight + (size_t)min(tile0 + j, tiles - 1) * steps * F8_FRAGMENT;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) x_at[i] = p.workspace + (size_t)min(mt0 + i, m_tiles - 1) * steps * F8_FRAGMENT;
+    const char* x_exponents = p.workspace + r.exponents();
+    auto load = [&](Step& b, int i) {
+        const int step = wave + i * W;
+        if constexpr (RAW) {
+            b.raw.load((const X*)p.x + (int64_t)min(mt0 * 16 + (lane & 15), p.m - 1) * p.x_row + step * 128 + (lane >> 4) * 32);
+        } else {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                b.x[i] = load_fragment(x_at[i] + (size_t)step * F8_FRAGMENT, lane);
+                b.xe[i] = (uint8_t)x_exponents[((size_t)min(mt0 + i, m_tiles - 1) * steps + step) * 16 + (lane & 15)];
+            }
+        }
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const int tile = min(tile0 + j, tiles - 1);
-            w[j] = load_fragment(p.weight + ((size_t)tile * steps + step) * F8_FRAGMENT, lane);
-            we[j] = (uint8_t)p.weight[s.exponents() + (size_t)step * s.exponent_row() + tile];
+            b.w[j] = load_fragment(w_at[j] + (size_t)step * F8_FRAGMENT, lane);
+            b.we[j] = (uint8_t)p.weight[s.exponents() + (size_t)step * exponent_row + min(tile0 + j, tiles - 1)];
         }
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const size_t f = (size_t)min(mt0 + i, m_tiles - 1) * steps + step;
-            x[i] = load_fragment(p.workspace + f * F8_FRAGMENT, lane);
-            xe[i] = (uint8_t)p.workspace[r.exponents() + f * 16 + (lane & 15)];
-        }
+    };
+    auto multiply = [&](Step& b) {
+        if constexpr (RAW) b.raw.codes(b.x[0], b.xe[0]);
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j], x[i], acc[i][j], 0, 0, 0, we[j], 0, xe[i]);
+                for (int j = 0; j < NT; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.w[j], b.x[i], acc[i][j], 0, 0, 0, b.we[j], 0, b.xe[i]);
         } else {
             bf16x8 wv[NT][4], xv[4];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) values_of(w[j], __uint_as_float((uint32_t)we[j] << 23), wv[j]);
+            for (int j = 0; j < NT; ++j) values_of(b.w[j], __uint_as_float((uint32_t)b.we[j] << 23), wv[j]);
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                values_of(x[i], __uint_as_float((uint32_t)xe[i] << 23), xv);
+                values_of(b.x[i], __uint_as_float((uint32_t)b.xe[i] << 23), xv);
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
 #pragma unroll
                     for (int h = 0; h < 4; ++h) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[j][h], xv[h], acc[i][j], 0, 0, 0);
             }
         }
+    };
+    Step ring[D];
+#pragma unroll
+    for (int d = 0; d < D; ++d) load(ring[d], min(d, max(mine - 1, 0)));  // (a wave without a step reads one of another's)
+    int i = 0;
+    for (; i + 2 * D <= mine; i += D) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) multiply(ring[d]), load(ring[d], i + D + d);
     }
+    if (i + D <= mine) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            multiply(ring[d]);
+            if (i + D + d < mine) load(ring[d], i + D + d);
+        }
+        i += D;
+    }
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+        if (i + d < mine) multiply(ring[d]);
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -269,10 +341,12 @@ __global__ __launch_bounds__(W * 64) void f8_matmul_kernel(F8Product p, F8Shape 
     };
     const int row = lane & 15, col = (lane >> 4) * 4;
     if (p.pair) {
-        for (int t = wave; t < MT * NT / 2; t += W) {
-            const int i = t / (NT / 2), j = t % (NT / 2) * 2;
-            const f32x4 g = sum(i * NT + j), u = sum(i * NT + j + 1);
-            finish<T>(p, (mt0 + i) * 16 + row, (tile0 + j) / 2 * 16 + col, f32x4{silu(g[0]) * u[0], silu(g[1]) * u[1], silu(g[2]) * u[2], silu(g[3]) * u[3]});
+        if constexpr (NT > 1) {
+            for (int t = wave; t < MT * NT / 2; t += W) {
+                const int i = t / (NT / 2), j = t % (NT / 2) * 2;
+                const f32x4 g = sum(i * NT + j), u = sum(i * NT + j + 1);
+                finish<T>(p, (mt0 + i) * 16 + row, (tile0 + j) / 2 * 16 + col, f32x4{silu(g[0]) * u[0], silu(g[1]) * u[1], silu(g[2]) * u[2], silu(g[3]) * u[3]});
+            }
         }
     } else {
         for (int t = wave; t < MT * NT; t += W) finish<T>(p, (mt0 + t / NT) * 16 + row, (tile0 + t % NT) * 16 + col, sum(t));
@@ -387,7 +461,8 @@ __global__ __launch_bounds__(256, 1) void f8_tile_kernel(F8Product p, F8Shape s,
                 } else {
 #pragma unroll
                     for (int k = 0; k < NI + MI; ++k) {
-                        if (k * SLOTS / (NI + MI) != t - 1) continue;
+                        // (early, so that they have arrived when the last product is through)
+                        if ((SLOTS >= NI + MI ? k : k * SLOTS / (NI + MI)) != t - 1) continue;
                         if (k < NI) read_w(next, next_stage, k);
                         else read_x(next, next_stage, k - NI);
                     }
@@ -450,6 +525,9 @@ __global__ __launch_bounds__(256, 1) void f8_tile_kernel(F8Product p, F8Shape s,
 
 }  // namespace
 
+// Sixteen rows at most are quantised by the kernel that multiplies them, where they lie so that it can.
+static bool quantised_first(const F8Product& p) { return p.m > 16 || !p.x_vec || p.k % 128; }
+
 size_t f8_workspace(int m, int n, int k, int pair, int y_dtype) { return F8Rows{m, (k + 127) / 128}.bytes(); }
 
 hipError_t launch_f8_pack(const F8Shape& s, int dtype, const void* w, int64_t w_row, const void* up, int64_t up_row, char* weight, hipStream_t st) {
@@ -472,27 +550,63 @@ hipError_t launch_f8_unpack(const F8Shape& s, int up, const char* weight, int dt
     return hipGetLastError();
 }
 
+template <typename T, typename X, int MT, int NT, int W, int D>
+static void launch_stream(const F8Product& p, const F8Shape& s, const F8Rows& r, hipStream_t st) {
+    const int m_groups = ((p.m + 15) / 16 + MT - 1) / MT, n_groups = (s.tiles() + NT - 1) / NT;
+    EE_LAUNCH((f8_stream_kernel<T, X, MT, NT, W, D>), dim3((n_groups + 7) / 8 * 8 * m_groups), dim3(W * 64), st, p, s, r, m_groups, n_groups);
+}
+
+template <typename T, int MI, int NI>
+static void launch_tile(const F8Product& p, const F8Shape& s, const F8Rows& r, hipStream_t st) {
+    const int m_groups = (p.m + 64 * MI - 1) / (64 * MI), n_groups = (s.tiles() + 4 * NI - 1) / (4 * NI);
+    EE_LAUNCH((f8_tile_kernel<T, MI, NI>), dim3((n_groups + 7) / 8 * 8 * m_groups), dim3(256), st, p, s, r, m_groups, n_groups);
+}
+
+template <typename T, typename X>
+static void launch_few(const F8Product& p, const F8Shape& s, const F8Rows& r, hipStream_t st) {
+    if (s.tiles() >= 1024)
+        launch_stream<T, X, 1, 4, 4, 2>(p, s, r, st);
+    else if (s.tiles() >= 512 || p.pair)
+        launch_stream<T, X, 1, 2, 4, 4>(p, s, r, st);
+    else
+        launch_stream<T, X, 1, 1, 4, 4>(p, s, r, st);
+}
+
+template <typename T>
+static void launch_product(const F8Product& p, const F8Shape& s, const F8Rows& r, hipStream_t st) {
+    const int m_tiles = (p.m + 15) / 16;
+    if (!quantised_first(p)) {
+        if (p.x_dtype == EE_BF16) return launch_few<T, __bf16>(p, s, r, st);
+        return launch_few<T, float>(p, s, r, st);
+    }
+    if (m_tiles == 1) return launch_few<T, HeldRows>(p, s, r, st);
+    const bool narrow = s.tiles() < 512;
+    if (m_tiles == 2) {
+        if (narrow && !p.pair) return launch_stream<T, HeldRows, 2, 1, 8, 2>(p, s, r, st);
+        return launch_stream<T, HeldRows, 2, 2, 4, 2>(p, s, r, st);
+    }
+    if (m_tiles <= 4) {
+        if (narrow && !p.pair) return launch_stream<T, HeldRows, 4, 1, 8, 2>(p, s, r, st);
+        return launch_stream<T, HeldRows, 4, 2, 4, 2>(p, s, r, st);
+    }
+    if (sizeof(T) == 2 && p.m > 256) return launch_tile<__bf16, 4, 4>(p, s, r, st);
+    launch_stream<T, HeldRows, 4, 4, 4, 1>(p, s, r, st);
+}
+
 hipError_t launch_f8_matmul(const F8Product& p, hipStream_t st) {
     const F8Shape s{p.n, p.k, p.pair};
     const F8Rows r{p.m, s.steps()};
-    const dim3 rows_grid((p.m + 15) / 16, (r.steps + 3) / 4);
-    if (p.x_dtype == EE_BF16)
-        EE_LAUNCH(f8_rows_kernel<__bf16>, rows_grid, dim3(256), st, r, (const __bf16*)p.x, p.x_row, p.k, p.x_vec, p.workspace);
-    else
-        EE_LAUNCH(f8_rows_kernel<float>, rows_grid, dim3(256), st, r, (const float*)p.x, p.x_row, p.k, p.x_vec, p.workspace);
-    if (p.m > 256 && p.y_dtype == EE_BF16) {
-        constexpr int MI = 4, NI = 4;
-        const int m_groups = (p.m + 64 * MI - 1) / (64 * MI), n_groups = (s.tiles() + 4 * NI - 1) / (4 * NI);
-        const dim3 grid((n_groups + 7) / 8 * 8 * m_groups);
-        EE_LAUNCH((f8_tile_kernel<__bf16, MI, NI>), grid, dim3(256), st, p, s, r, m_groups, n_groups);
-        return hipGetLastError();
+    if (quantised_first(p)) {
+        const dim3 rows_grid((p.m + 15) / 16, (r.steps + 3) / 4);
+        if (p.x_dtype == EE_BF16)
+            EE_LAUNCH(f8_rows_kernel<__bf16>, rows_grid, dim3(256), st, r, (const __bf16*)p.x, p.x_row, p.k, p.x_vec, p.workspace);
+        else
+            EE_LAUNCH(f8_rows_kernel<float>, rows_grid, dim3(256), st, r, (const float*)p.x, p.x_row, p.k, p.x_vec, p.workspace);
     }
-    constexpr int MT = 2, NT = 2, W = 4;
-    const dim3 grid((s.tiles() + NT - 1) / NT, ((p.m + 15) / 16 + MT - 1) / MT);
     if (p.y_dtype == EE_BF16)
-        EE_LAUNCH((f8_matmul_kernel<__bf16, MT, NT, W>), grid, dim3(W * 64), st, p, s, r);
+        launch_product<__bf16>(p, s, r, st);
     else
-        EE_LAUNCH((f8_matmul_kernel<float, MT, NT, W>), grid, dim3(W * 64), st, p, s, r);
+        launch_product<float>(p, s, r, st);
     return hipGetLastError();
 }
 
