@@ -368,17 +368,20 @@ __device__ __forceinline__ void wait_copies() {
 // Many rows: a workgroup of 2 x 2 waves computes 64 * MI rows of x by 4 * NI tiles of the weight, a wave 32 * MI by 2 * NI tiles in
 // instructions of 32 x 32 x 64.  Both operands come through LDS, copied past the registers in their own order, 64 elements of
 // the contraction at a time, four such stages in turn; the next stage's operands are read while the products of this one run.
+constexpr int XCDS = 8, XCD_CUS = 32, CUS = XCDS * XCD_CUS;
+constexpr int tile_stages(int mi, int ni) { return mi * ni > 8 || mi * ni == 4 ? 4 : 3; }  // (two workgroups share a CU up to 8)
+constexpr int tile_stage_bytes(int mi, int ni) { return 4 * (mi + ni) * 1024 + 1024; }
+constexpr int tile_lds(int mi, int ni) {
+    const int stages = tile_stages(mi, ni) * tile_stage_bytes(mi, ni), results = 4 * 32 * (32 * ni + 4) * 4;
+    return stages > results ? stages : results;
+}
 template <typename T, int MI, int NI>
-__global__ __launch_bounds__(256, 1) void f8_tile_kernel(F8Product p, F8Shape s, F8Rows r, int m_groups, int n_groups) {
-    constexpr int WT = 4 * NI, XT = 4 * MI, FRAGS = WT + XT, STAGES = 4;
-    constexpr int EXPONENTS = FRAGS * 1024, STAGE = EXPONENTS + 1024;  // 256 bytes of x's, of the weight's, two unused copies of them
+__device__ __forceinline__ void f8_tile(const F8Product& p, const F8Shape& s, const F8Rows& r, int tile0, int mt0, char* lds) {
+    constexpr int WT = 4 * NI, XT = 4 * MI, FRAGS = WT + XT, STAGES = tile_stages(MI, NI);
+    constexpr int EXPONENTS = FRAGS * 1024, STAGE = tile_stage_bytes(MI, NI);  // 256 bytes of x's, of the weight's, two unused copies of them
     constexpr int COPIES = FRAGS / 4 + 1;                             // of a wave
-    __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wn = wave & 1, wm = wave >> 1;
-    // an XCD takes whole panels of the weight, all rows of one after the other: a panel comes from memory once
-    const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, n_group = turn / m_groups * 8 + xcd, m_group = turn % m_groups;
-    if (n_group >= n_groups) return;
-    const int steps = s.steps(), tile0 = n_group * WT, mt0 = m_group * XT, m_tiles = (p.m + 15) / 16, halves = 2 * steps;
+    const int steps = s.steps(), m_tiles = (p.m + 15) / 16, halves = 2 * steps;
     // what this wave copies: fragments, 512 bytes of either half of each, and a kind of exponents
     global_char* from[FRAGS / 4];
 #pragma unroll
@@ -437,43 +440,58 @@ __global__ __launch_bounds__(256, 1) void f8_tile_kernel(F8Product p, F8Shape s,
         for (int i = 0; i < MI; ++i) asm volatile("" : "+v"(o.x[i][0]), "+v"(o.x[i][1]), "+v"(o.xe[i]));
     };
     // One stage's products; the next one's operands are read and a copy is begun in between.
+    int buffer = 0;  // of the stage that is multiplied
     auto stage = [&](const Operands& now, Operands& next, int half) {
         // (behind the last stage an old one is read and copied again, for nothing)
-        const unsigned next_stage = ((half + 1) & (STAGES - 1)) * STAGE;
-        const int ahead = min(half + STAGES, halves - 1), buffer = half & (STAGES - 1);
+        const int next_buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
+        const unsigned next_stage = next_buffer * STAGE;
+        const int ahead = min(half + STAGES, halves - 1);
         const size_t on = offset_of(ahead);
         const uint32_t on_e = (uint32_t)(ahead >> 1) * e_step;
         constexpr int SLOTS = MI * NI - 1;
+        bf16x8 wv[NI][4], xv[4];
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+                values_of(__builtin_shufflevector(now.w[j][0], now.w[j][1], 0, 1, 2, 3, 4, 5, 6, 7), __uint_as_float((uint32_t)now.we[j] << 23), wv[j]);
+        }
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const i32x8 x = __builtin_shufflevector(now.x[i][0], now.x[i][1], 0, 1, 2, 3, 4, 5, 6, 7);
+            if constexpr (sizeof(T) == 4) values_of(x, __uint_as_float((uint32_t)now.xe[i] << 23), xv);
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
                 const i32x8 w = __builtin_shufflevector(now.w[j][0], now.w[j][1], 0, 1, 2, 3, 4, 5, 6, 7);
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, acc[i][j], 0, 0, 0, now.we[j], 0, now.xe[i]);
+                if constexpr (sizeof(T) == 2) {
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, acc[i][j], 0, 0, 0, now.we[j], 0, now.xe[i]);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv[j][h], xv[h], acc[i][j], 0, 0, 0);
+                }
                 __builtin_amdgcn_sched_barrier(0);
                 const int t = i * NI + j;
                 if (t == 0) {
-                    // the next stage is there once no more than the two behind it are on their way; then this one's buffer,
+                    // the next stage is there once no more than the ones behind it are on their way; then this one's buffer,
                     // which all waves have read, is filled again
-                    wait_copies<2 * COPIES>();
+                    wait_copies<(STAGES - 2) * COPIES>();
                     __builtin_amdgcn_s_barrier();
                 } else {
+                    // (early, so that they have arrived when the last product is through)
+                    constexpr int READS = (NI + MI + SLOTS - 1) / SLOTS;
 #pragma unroll
-                    for (int k = 0; k < NI + MI; ++k) {
-                        // (early, so that they have arrived when the last product is through)
-                        if ((SLOTS >= NI + MI ? k : k * SLOTS / (NI + MI)) != t - 1) continue;
+                    for (int k = (t - 1) * READS; k < t * READS && k < NI + MI; ++k) {
                         if (k < NI) read_w(next, next_stage, k);
                         else read_x(next, next_stage, k - NI);
                     }
 #pragma unroll
                     for (int k = 0; k < COPIES; ++k)
-                        if (k * SLOTS / COPIES == t - 1) copy_one(buffer, on, on_e, k);
+                        if ((SLOTS >= COPIES + NI ? k + NI : k * SLOTS / COPIES) == t - 1) copy_one(buffer, on, on_e, k);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
         landed(next);
+        buffer = next_buffer;
     };
 #pragma unroll
     for (int i = 0; i < STAGES; ++i) {
@@ -523,6 +541,26 @@ __global__ __launch_bounds__(256, 1) void f8_tile_kernel(F8Product p, F8Shape s,
     }
 }
 
+// An XCD takes whole panels of the weight, all rows of one after the other, so that a panel comes from memory once.  What its CUs have
+// left over after whole rounds goes in tiles of half as many rows, if these are one round then (4096 rows by 22 016, 5.5 rounds for 6:
+// 345 -> 320 us).
+template <typename T, int MI, int NI>
+__global__ __launch_bounds__(256, MI * NI <= 8 ? 2 : 1) void f8_tile_kernel(F8Product p, F8Shape s, F8Rows r, int m_groups, int n_groups) {
+    constexpr bool HALVES = MI == 4 && NI > 2;
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(MI, NI)];
+    const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, all = (n_groups - xcd + 7) / 8 * m_groups;
+    const int left = HALVES ? all % XCD_CUS : 0, whole = left <= XCD_CUS / 2 ? all - left : all;
+    if (turn < whole) {
+        f8_tile<T, MI, NI>(p, s, r, (turn / m_groups * 8 + xcd) * (4 * NI), turn % m_groups * (4 * MI), lds);
+    } else if constexpr (HALVES) {
+        const int t = whole + (turn - whole) / 2;
+        if (t < all) {
+            const int mt0 = t % m_groups * (4 * MI) + (turn - whole) % 2 * (2 * MI);
+            if (mt0 * 16 < p.m) f8_tile<T, MI / 2, NI>(p, s, r, (t / m_groups * 8 + xcd) * (4 * NI), mt0, lds);
+        }
+    }
+}
+
 }  // namespace
 
 // Sixteen rows at most are quantised by the kernel that multiplies them, where they lie so that it can.
@@ -559,7 +597,33 @@ static void launch_stream(const F8Product& p, const F8Shape& s, const F8Rows& r,
 template <typename T, int MI, int NI>
 static void launch_tile(const F8Product& p, const F8Shape& s, const F8Rows& r, hipStream_t st) {
     const int m_groups = (p.m + 64 * MI - 1) / (64 * MI), n_groups = (s.tiles() + 4 * NI - 1) / (4 * NI);
-    EE_LAUNCH((f8_tile_kernel<T, MI, NI>), dim3((n_groups + 7) / 8 * 8 * m_groups), dim3(256), st, p, s, r, m_groups, n_groups);
+    const int most = (n_groups + 7) / 8 * m_groups;  // of an XCD; what is left over may be twice as many
+    EE_LAUNCH((f8_tile_kernel<T, MI, NI>), dim3(8 * (most + (MI == 4 && NI > 2 ? XCD_CUS / 2 : 0))), dim3(256), st, p, s, r, m_groups, n_groups);
+}
+
+// Which tiles take a product of many rows: the ones with the least time by the rounds that they take on 256 CUs.  Of a step of 64
+// elements, in ns, measured: a workgroup that has its CU to itself, and two that share one.
+struct TileKind {
+    int mi, ni, alone, two;
+};
+static const TileKind TILE_KINDS[] = {{4, 4, 860, 0}, {4, 3, 770, 0}, {3, 3, 600, 0}, {4, 2, 570, 990}, {2, 3, 520, 900}, {2, 2, 360, 630}};
+static int tile_kind(int m, int tiles) {
+    int best = 0;
+    int64_t least = INT64_MAX;
+    for (int i = 0; i < (int)(sizeof(TILE_KINDS) / sizeof(TILE_KINDS[0])); ++i) {
+        const TileKind& k = TILE_KINDS[i];
+        const int64_t n = (int64_t)((m + 64 * k.mi - 1) / (64 * k.mi)) * ((tiles + 4 * k.ni - 1) / (4 * k.ni));
+        int64_t t;
+        if (k.two) {
+            const int64_t left = n % (2 * CUS);
+            t = n / (2 * CUS) * k.two + (left > CUS ? k.two : left ? k.alone : 0);
+        } else {
+            const int64_t left = n % CUS;
+            t = n / CUS * k.alone + (left > CUS / 2 || (left && k.mi != 4) ? k.alone : left ? k.alone * 6 / 10 : 0);
+        }
+        if (t < least) least = t, best = i;
+    }
+    return best;
 }
 
 template <typename T, typename X>
@@ -589,8 +653,15 @@ static void launch_product(const F8Product& p, const F8Shape& s, const F8Rows& r
         if (narrow && !p.pair) return launch_stream<T, HeldRows, 4, 1, 8, 2>(p, s, r, st);
         return launch_stream<T, HeldRows, 4, 2, 4, 2>(p, s, r, st);
     }
-    if (sizeof(T) == 2 && p.m > 256) return launch_tile<__bf16, 4, 4>(p, s, r, st);
-    launch_stream<T, HeldRows, 4, 4, 4, 1>(p, s, r, st);
+    if (p.m <= 256) return launch_stream<T, HeldRows, 8, 4, 4, 2>(p, s, r, st);
+    switch (tile_kind(p.m, s.tiles())) {
+        case 0: return launch_tile<T, 4, 4>(p, s, r, st);
+        case 1: return launch_tile<T, 4, 3>(p, s, r, st);
+        case 2: return launch_tile<T, 3, 3>(p, s, r, st);
+        case 3: return launch_tile<T, 4, 2>(p, s, r, st);
+        case 4: return launch_tile<T, 2, 3>(p, s, r, st);
+        default: return launch_tile<T, 2, 2>(p, s, r, st);
+    }
 }
 
 hipError_t launch_f8_matmul(const F8Product& p, hipStream_t st) {
