@@ -215,43 +215,43 @@ __device__ __forceinline__ void finish8(const F8Product& p, int row, int col, f3
     *(T8*)((T*)p.y + row * p.y_row + col) = T8{(T)a[0], (T)a[1], (T)a[2], (T)a[3], (T)b[0], (T)b[1], (T)b[2], (T)b[3]};
 }
 
-// Rows of x as a kernel takes them that quantises them itself: [16 rows][k] in their own type, k a multiple of 128 and rows aligned.
-template <typename X>
-struct RawRows {
-    i32x4 v[sizeof(X) * 2];
-    __device__ __forceinline__ void load(const X* row) {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(X) * 2; ++i) v[i] = ((const i32x4*)row)[i];
-    }
-    __device__ __forceinline__ void codes(i32x8& c, int& e) const {
-        float f[32];
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(X) * 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (sizeof(X) == 2) {
-                    f[i * 8 + j * 2] = __uint_as_float((uint32_t)v[i][j] << 16);
-                    f[i * 8 + j * 2 + 1] = __uint_as_float((uint32_t)v[i][j] & 0xffff0000u);
-                } else {
-                    f[i * 4 + j] = __int_as_float(v[i][j]);
-                }
-            }
-        const uint32_t ex = exponent_of(top_of_quarters(top_of(f)));
-        codes_of(f, ex, c);
-        e = (int)stored(ex);
-    }
-};
 struct HeldRows {};  // they are in the workspace
+
+// What a workgroup needs in LDS that quantises m rows itself: codes as [step][half][quarter][row] of 16 bytes, exponents as [step][row].
+__host__ __device__ constexpr size_t own_rows_bytes(int m, int steps) { return (size_t)m * steps * 129; }
+
+template <typename X, int THREADS>
+__device__ __forceinline__ void quantise_rows(const F8Product& p, int steps, char* codes) {
+    uint8_t* exponents = (uint8_t*)codes + (size_t)p.m * steps * 128;
+    const int quarter = threadIdx.x & 3;
+    for (int i = threadIdx.x / 4; i < p.m * steps; i += THREADS / 4) {
+        const int row = i / steps, step = i - row * steps, k0 = step * 128 + quarter * 32;
+        float v[32];
+        load32((const X*)p.x + row * p.x_row + min(k0, p.k - 1), p.k - k0, p.x_vec, v);
+        uint32_t top = top_of(v);
+        top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xb1, 0xf, 0xf, false));  // of the four lanes: 1 0 3 2
+        top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4e, 0xf, 0xf, false));  // 2 3 0 1
+        const uint32_t e = exponent_of(top);
+        i32x8 c;
+        codes_of(v, e, c);
+        char* at = codes + ((size_t)(step * 8 + quarter) * p.m + row) * 16;
+        *(i32x4*)at = __builtin_shufflevector(c, c, 0, 1, 2, 3);
+        *(i32x4*)(at + (size_t)p.m * 64) = __builtin_shufflevector(c, c, 4, 5, 6, 7);
+        if (quarter == 0) exponents[step * p.m + row] = (uint8_t)stored(e);
+    }
+}
 
 // Few rows: the weight comes straight from memory into the registers of the wave that multiplies it.  A wave computes 16 * MT rows of x by NT
 // tiles of the weight in every W-th step of 128 elements, D steps ahead of which its loads are; the waves' sums are added up in
 // LDS in their order.  T: of the result; float: the held values go through the bf16 instructions, which keep every bit of a
-// product.  X: HeldRows, or the type in which the rows come, which every wave then quantises for itself (MT = 1).
+// product.  X: HeldRows, or the type in which sixteen rows at most come, which every workgroup then
+// quantises for itself, into LDS, while its first loads of the weight are on their way.
 template <typename T, typename X, int MT, int NT, int W, int D>
 __global__ __launch_bounds__(W * 64) void f8_stream_kernel(F8Product p, F8Shape s, F8Rows r, int m_groups, int n_groups) {
     constexpr bool RAW = !__is_same(X, HeldRows);
     static_assert(!RAW || MT == 1, "rows that are quantised here");
-    __shared__ f32x4 s_part[W][MT * NT][64];
+    extern __shared__ __attribute__((aligned(16))) char dynamic[];  // own rows, then the waves' sums
+    f32x4(*s_part)[MT * NT][64] = (f32x4(*)[MT * NT][64])dynamic;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // the groups of rows that take the same tiles of the weight follow one another on one XCD
     const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, n_group = turn / m_groups * 8 + xcd, m_group = turn % m_groups;
@@ -260,9 +260,8 @@ __global__ __launch_bounds__(W * 64) void f8_stream_kernel(F8Product p, F8Shape 
     const int exponent_row = s.exponent_row(), mine = (steps - wave + W - 1) / W;
     f32x4 acc[MT][NT] = {};
     struct Step {
-        i32x8 w[NT], x[RAW ? 1 : MT];
-        int we[NT], xe[RAW ? 1 : MT];
-        RawRows<typename std::conditional<RAW, X, float>::type> raw;
+        i32x8 w[NT], x[MT];
+        int we[NT], xe[MT];
     };
     const char *w_at[NT], *x_at[MT];
 #pragma unroll
@@ -272,9 +271,7 @@ __global__ __launch_bounds__(W * 64) void f8_stream_kernel(F8Product p, F8Shape 
     const char* x_exponents = p.workspace + r.exponents();
     auto load = [&](Step& b, int i) {
         const int step = wave + i * W;
-        if constexpr (RAW) {
-            b.raw.load((const X*)p.x + (int64_t)min(mt0 * 16 + (lane & 15), p.m - 1) * p.x_row + step * 128 + (lane >> 4) * 32);
-        } else {
+        if constexpr (!RAW) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 b.x[i] = load_fragment(x_at[i] + (size_t)step * F8_FRAGMENT, lane);
@@ -287,8 +284,15 @@ __global__ __launch_bounds__(W * 64) void f8_stream_kernel(F8Product p, F8Shape 
             b.we[j] = (uint8_t)p.weight[s.exponents() + (size_t)step * exponent_row + min(tile0 + j, tiles - 1)];
         }
     };
-    auto multiply = [&](Step& b) {
-        if constexpr (RAW) b.raw.codes(b.x[0], b.xe[0]);
+    const int own_row = min(lane & 15, p.m - 1);
+    auto multiply = [&](Step& b, int i) {
+        if constexpr (RAW) {
+            const int step = wave + i * W;
+            const char* at = dynamic + ((size_t)(step * 8 + (lane >> 4)) * p.m + own_row) * 16;
+            const i32x4 lo = *(const i32x4*)at, hi = *(const i32x4*)(at + (size_t)p.m * 64);
+            b.x[0] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            b.xe[0] = ((const uint8_t*)dynamic)[(size_t)p.m * steps * 128 + step * p.m + own_row];
+        }
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
             for (int i = 0; i < MT; ++i)
@@ -312,22 +316,27 @@ __global__ __launch_bounds__(W * 64) void f8_stream_kernel(F8Product p, F8Shape 
     Step ring[D];
 #pragma unroll
     for (int d = 0; d < D; ++d) load(ring[d], min(d, max(mine - 1, 0)));  // (a wave without a step reads one of another's)
+    if constexpr (RAW) {
+        quantise_rows<X, W * 64>(p, steps, dynamic);
+        __syncthreads();
+    }
     int i = 0;
     for (; i + 2 * D <= mine; i += D) {
 #pragma unroll
-        for (int d = 0; d < D; ++d) multiply(ring[d]), load(ring[d], i + D + d);
+        for (int d = 0; d < D; ++d) multiply(ring[d], i + d), load(ring[d], i + D + d);
     }
     if (i + D <= mine) {
 #pragma unroll
         for (int d = 0; d < D; ++d) {
-            multiply(ring[d]);
+            multiply(ring[d], i + d);
             if (i + D + d < mine) load(ring[d], i + D + d);
         }
         i += D;
     }
 #pragma unroll
     for (int d = 0; d < D; ++d)
-        if (i + d < mine) multiply(ring[d]);
+        if (i + d < mine) multiply(ring[d], i + d);
+    if constexpr (RAW) __syncthreads();  // (the rows are read no more)
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -563,10 +572,14 @@ __global__ __launch_bounds__(256, MI * NI <= 8 ? 2 : 1) void f8_tile_kernel(F8Pr
 
 }  // namespace
 
-// Sixteen rows at most are quantised by the kernel that multiplies them, where they lie so that it can.
-static bool quantised_first(const F8Product& p) { return p.m > 16 || !p.x_vec || p.k % 128; }
+// Up to 32 768 elements of sixteen rows at most are quantised by the workgroups that multiply them, which saves a launch of 3 us and the
+// gap behind it, but is done by all of them (1 row by 4096 x 4096 6.4 us, apart 6.0 + 3.5; 16 rows by 12 288 x 4096 16.5, apart 11.3 + 2.9).
+static bool quantised_first(int m, int steps) { return m > 16 || m * steps > 256; }
 
-size_t f8_workspace(int m, int n, int k, int pair, int y_dtype) { return F8Rows{m, (k + 127) / 128}.bytes(); }
+size_t f8_workspace(int m, int n, int k, int pair, int y_dtype) {
+    const int steps = (k + 127) / 128;
+    return quantised_first(m, steps) ? F8Rows{m, steps}.bytes() : 0;
+}
 
 hipError_t launch_f8_pack(const F8Shape& s, int dtype, const void* w, int64_t w_row, const void* up, int64_t up_row, char* weight, hipStream_t st) {
     const dim3 grid(s.steps(), (s.n + 127) / 128, s.pair ? 2 : 1);
@@ -591,7 +604,8 @@ hipError_t launch_f8_unpack(const F8Shape& s, int up, const char* weight, int dt
 template <typename T, typename X, int MT, int NT, int W, int D>
 static void launch_stream(const F8Product& p, const F8Shape& s, const F8Rows& r, hipStream_t st) {
     const int m_groups = ((p.m + 15) / 16 + MT - 1) / MT, n_groups = (s.tiles() + NT - 1) / NT;
-    EE_LAUNCH((f8_stream_kernel<T, X, MT, NT, W, D>), dim3((n_groups + 7) / 8 * 8 * m_groups), dim3(W * 64), st, p, s, r, m_groups, n_groups);
+    const size_t sums = (size_t)W * MT * NT * 1024, lds = __is_same(X, HeldRows) ? sums : std::max(sums, own_rows_bytes(p.m, s.steps()));
+    EE_LAUNCH_SM((f8_stream_kernel<T, X, MT, NT, W, D>), dim3((n_groups + 7) / 8 * 8 * m_groups), dim3(W * 64), lds, st, p, s, r, m_groups, n_groups);
 }
 
 template <typename T, int MI, int NI>
@@ -601,73 +615,71 @@ static void launch_tile(const F8Product& p, const F8Shape& s, const F8Rows& r, h
     EE_LAUNCH((f8_tile_kernel<T, MI, NI>), dim3(8 * (most + (MI == 4 && NI > 2 ? XCD_CUS / 2 : 0))), dim3(256), st, p, s, r, m_groups, n_groups);
 }
 
-// Which tiles take a product of many rows: the ones with the least time by the rounds that they take on 256 CUs.  Of a step of 64
-// elements, in ns, measured: a workgroup that has its CU to itself, and two that share one.
-struct TileKind {
-    int mi, ni, alone, two;
+// What takes a product of more than 64 rows: the kind with the least time for a step of 128 elements, by the workgroups that it takes on
+// 256 CUs; in ns, measured with weights that come from memory.  Tiles run in rounds (alone: a workgroup that has its CU to
+// itself, two: a pair that shares one), the others a few on a CU.  203 rows by 6656 x 6656: 8 x 4 tiles of 16 x 16 straight into registers 24 us,
+// tiles of 128 x 128 through LDS 31; 256 rows by 12 288 x 4096: 32 and 25; 70 rows by 4096 x 4096: 4 x 2 9 us, 8 x 4 16.
+struct Kind {
+    int m, n;  // rows, rows of the weight, of a workgroup
+    int alone, two;
 };
-static const TileKind TILE_KINDS[] = {{4, 4, 860, 0}, {4, 3, 770, 0}, {3, 3, 600, 0}, {4, 2, 570, 990}, {2, 3, 520, 900}, {2, 2, 360, 630}};
-static int tile_kind(int m, int tiles) {
+static const Kind TILES[] = {{256, 256, 1720, 0}, {256, 192, 1540, 0}, {192, 192, 1200, 0}, {256, 128, 1140, 1980}, {128, 192, 1040, 1800}, {128, 128, 720, 1260}};
+static const Kind STREAMS[] = {{128, 64, 500, 0}, {64, 64, 300, 0}, {64, 32, 250, 0}, {64, 16, 160, 0}};
+constexpr int N_TILES = sizeof(TILES) / sizeof(Kind), N_STREAMS = sizeof(STREAMS) / sizeof(Kind);
+
+static int kind_of(int m, int tiles, bool pair) {
     int best = 0;
     int64_t least = INT64_MAX;
-    for (int i = 0; i < (int)(sizeof(TILE_KINDS) / sizeof(TILE_KINDS[0])); ++i) {
-        const TileKind& k = TILE_KINDS[i];
-        const int64_t n = (int64_t)((m + 64 * k.mi - 1) / (64 * k.mi)) * ((tiles + 4 * k.ni - 1) / (4 * k.ni));
-        int64_t t;
-        if (k.two) {
-            const int64_t left = n % (2 * CUS);
-            t = n / (2 * CUS) * k.two + (left > CUS ? k.two : left ? k.alone : 0);
-        } else {
-            const int64_t left = n % CUS;
-            t = n / CUS * k.alone + (left > CUS / 2 || (left && k.mi != 4) ? k.alone : left ? k.alone * 6 / 10 : 0);
-        }
-        if (t < least) least = t, best = i;
+    auto workgroups = [&](const Kind& k) { return (int64_t)((m + k.m - 1) / k.m) * ((tiles * 16 + k.n - 1) / k.n); };
+    auto take = [&](int kind, int64_t t) {
+        if (t < least) least = t, best = kind;
+    };
+    for (int i = 0; i < N_TILES; ++i) {
+        const Kind& k = TILES[i];
+        const int64_t n = workgroups(k), at_once = k.two ? 2 * CUS : CUS, left = n % at_once;
+        const bool halves = k.m == 256 && !k.two;
+        take(i, n / at_once * (k.two ? k.two : k.alone) + (left == 0 ? 0 : k.two && left > CUS ? k.two : halves && left <= CUS / 2 && n > CUS ? k.alone * 6 / 10 : k.alone));
+    }
+    for (int i = 0; i < N_STREAMS - (pair ? 1 : 0); ++i) {
+        const Kind& k = STREAMS[i];
+        const int64_t n = workgroups(k);
+        take(N_TILES + i, i == 0 ? (n + CUS - 1) / CUS * k.alone : std::max<int64_t>(k.alone, n * (k.n * 30 / 8 + 70) / CUS));
     }
     return best;
 }
 
-template <typename T, typename X>
-static void launch_few(const F8Product& p, const F8Shape& s, const F8Rows& r, hipStream_t st) {
-    if (s.tiles() >= 1024)
-        launch_stream<T, X, 1, 4, 4, 2>(p, s, r, st);
-    else if (s.tiles() >= 512 || p.pair)
-        launch_stream<T, X, 1, 2, 4, 4>(p, s, r, st);
-    else
-        launch_stream<T, X, 1, 1, 4, 4>(p, s, r, st);
-}
-
 template <typename T>
 static void launch_product(const F8Product& p, const F8Shape& s, const F8Rows& r, hipStream_t st) {
-    const int m_tiles = (p.m + 15) / 16;
-    if (!quantised_first(p)) {
-        if (p.x_dtype == EE_BF16) return launch_few<T, __bf16>(p, s, r, st);
-        return launch_few<T, float>(p, s, r, st);
+    const int m_tiles = (p.m + 15) / 16, tiles = s.tiles();
+    const bool pair = p.pair;
+    typedef HeldRows H;
+    if (!quantised_first(p.m, s.steps())) {
+        // (all widths of the framework's workloads, 1 row: within 0.4 us of the best of eight kinds)
+        if (p.x_dtype == EE_BF16) return tiles >= 1024 || pair ? launch_stream<T, __bf16, 1, 2, 8, 2>(p, s, r, st) : launch_stream<T, __bf16, 1, 1, 8, 2>(p, s, r, st);
+        return tiles >= 1024 || pair ? launch_stream<T, float, 1, 2, 8, 2>(p, s, r, st) : launch_stream<T, float, 1, 1, 8, 2>(p, s, r, st);
     }
-    if (m_tiles == 1) return launch_few<T, HeldRows>(p, s, r, st);
-    const bool narrow = s.tiles() < 512;
-    if (m_tiles == 2) {
-        if (narrow && !p.pair) return launch_stream<T, HeldRows, 2, 1, 8, 2>(p, s, r, st);
-        return launch_stream<T, HeldRows, 2, 2, 4, 2>(p, s, r, st);
-    }
-    if (m_tiles <= 4) {
-        if (narrow && !p.pair) return launch_stream<T, HeldRows, 4, 1, 8, 2>(p, s, r, st);
-        return launch_stream<T, HeldRows, 4, 2, 4, 2>(p, s, r, st);
-    }
-    if (p.m <= 256) return launch_stream<T, HeldRows, 8, 4, 4, 2>(p, s, r, st);
-    switch (tile_kind(p.m, s.tiles())) {
+    // Few tiles: one to a workgroup, so that there are as many as CUs (16 rows by 4096 x 11 008: 11.3 us, two 15); many: two, four.
+    if (m_tiles == 1) return pair ? launch_stream<T, H, 1, 2, 4, 4>(p, s, r, st) : tiles >= 1024 ? launch_stream<T, H, 1, 2, 8, 2>(p, s, r, st) : launch_stream<T, H, 1, 1, 4, 4>(p, s, r, st);
+    if (m_tiles == 2) return tiles <= 256 && !pair ? launch_stream<T, H, 2, 1, 8, 2>(p, s, r, st) : launch_stream<T, H, 2, 2, 4, 4>(p, s, r, st);
+    if (m_tiles <= 4) return tiles < 512 && !pair ? launch_stream<T, H, 4, 1, 4, 4>(p, s, r, st) : tiles < 512 ? launch_stream<T, H, 4, 2, 4, 2>(p, s, r, st) : launch_stream<T, H, 4, 4, 4, 2>(p, s, r, st);
+    switch (kind_of(p.m, tiles, pair)) {
         case 0: return launch_tile<T, 4, 4>(p, s, r, st);
         case 1: return launch_tile<T, 4, 3>(p, s, r, st);
         case 2: return launch_tile<T, 3, 3>(p, s, r, st);
         case 3: return launch_tile<T, 4, 2>(p, s, r, st);
         case 4: return launch_tile<T, 2, 3>(p, s, r, st);
-        default: return launch_tile<T, 2, 2>(p, s, r, st);
+        case 5: return launch_tile<T, 2, 2>(p, s, r, st);
+        case 6: return launch_stream<T, H, 8, 4, 4, 2>(p, s, r, st);
+        case 7: return launch_stream<T, H, 4, 4, 4, 2>(p, s, r, st);
+        case 8: return launch_stream<T, H, 4, 2, 4, 2>(p, s, r, st);
+        default: return launch_stream<T, H, 4, 1, 4, 4>(p, s, r, st);
     }
 }
 
 hipError_t launch_f8_matmul(const F8Product& p, hipStream_t st) {
     const F8Shape s{p.n, p.k, p.pair};
     const F8Rows r{p.m, s.steps()};
-    if (quantised_first(p)) {
+    if (quantised_first(p.m, s.steps())) {
         const dim3 rows_grid((p.m + 15) / 16, (r.steps + 3) / 4);
         if (p.x_dtype == EE_BF16)
             EE_LAUNCH(f8_rows_kernel<__bf16>, rows_grid, dim3(256), st, r, (const __bf16*)p.x, p.x_row, p.k, p.x_vec, p.workspace);
