@@ -42,8 +42,9 @@ struct SampleRow {
     constexpr size_t note() const { return (raws() + (size_t)runs * 4 + 15) / 16 * 16; }
     constexpr size_t bytes() const { return note() + (sizeof(SampleNote) + 15) / 16 * 16; }
 };
-// Workgroups that share a row in the third kernel, and what each hands over: for each bin a weight and where its elements begin, and the
-// part's elements.
+// For the third kernel, for each row: a weight and a count for each bin, to which its workgroups add; and what each of these leaves, for
+// each bin a weight and where its elements begin, and the part's elements.
+constexpr size_t SAMPLE_ROW_BINS = (size_t)SAMPLE_BINS * 12;
 constexpr size_t sample_part_bytes(int part_length) { return (size_t)SAMPLE_BINS * 12 + 16 + (size_t)part_length * 2; }
 int sample_parts(int rows, int vocab);
 size_t sample_workspace(int rows, int vocab);

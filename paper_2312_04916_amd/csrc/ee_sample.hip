@@ -17,6 +17,7 @@ typedef unsigned long long u64;
 constexpr int ONE = 44;  // weights are multiples of 2^-44 of the largest: 2^18 of them stay below 2^62
 constexpr int CHUNKS = SAMPLE_RUN / SAMPLE_CHUNK, RUNS = (1 << 18) / SAMPLE_RUN;
 constexpr int LIST = 256;  // elements of a bin that are ranked one by one
+constexpr float MOST_FLOAT = 3.4028235e38f;
 
 // Order of the floats as unsigned numbers; -0 counts as 0, NaN as the largest.
 __device__ __forceinline__ uint32_t key_of(float z) {
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(256) void sample_runs_kernel(Sampling p, int each) 
 #pragma unroll
             for (int j = 0; j < 4; ++j) ((float*)out)[run_now * CHUNKS + j * 4 + (lane >> 4)] = top[j];
         }
-        const float ref = fmaxf(most, -3.4028235e38f);
+        const float ref = fmaxf(most, -MOST_FLOAT);
         if (s.whole_sum()) {
             u64 sum = 0;
 #pragma unroll
@@ -229,12 +230,21 @@ struct Cut {
 };
 __device__ __forceinline__ Cut nothing_cut() { return Cut{0, 1 << 30, 0, 0}; }
 
+// The threads that look for a row's cut: a whole workgroup, or one wave of it, which needs no barriers.
 template <int NT>
+__device__ __forceinline__ void meet() {
+    if constexpr (NT == 64)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (LDS serves a wave in its order)
+    else
+        __syncthreads();
+}
+
+template <int NT, int N_BINS>
 struct CutShared {
     u64 sums[NT / 64];
     uint32_t counts[NT / 64];
-    u64 bin_weight[NT];
-    uint32_t bin_count[NT];
+    u64 bin_weight[N_BINS];
+    uint32_t bin_count[N_BINS];
     uint32_t list[LIST], list_index[LIST];  // the elements of the cut's bin, if they are few
     u64 list_weight[LIST];
     uint32_t n_list, lo, hi;  // keys of the bin that is looked into
@@ -247,25 +257,31 @@ struct CutShared {
 __device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
 __device__ __forceinline__ u64 of_lane(u64 v, int lane) { return (u64)of_lane((uint32_t)(v >> 32), lane) << 32 | of_lane((uint32_t)v, lane); }
 
-// Sums over the workgroup: exclusive prefix of each thread's value, and the total.  `waves` is free again after the next barrier.
+// Sums over the threads: exclusive prefix of each one's value, and the total.  `waves` is free again after the next meeting.
 template <int NT, typename T>
 __device__ __forceinline__ T before_me(T v, T& total, T* waves) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const T in = wave_scan(v);
-    if (lane == 63) waves[wave] = in;
-    __syncthreads();
-    const T sums = wave_scan<NT / 64>(lane < NT / 64 ? waves[lane] : (T)0);  // (of the waves, one in a lane)
-    total = of_lane(sums, NT / 64 - 1);
-    return in - v + (wave ? of_lane(sums, wave - 1) : (T)0);
+    if constexpr (NT == 64) {
+        total = last_lane(in);
+        return in - v;
+    } else {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (lane == 63) waves[wave] = in;
+        __syncthreads();
+        const T sums = wave_scan<NT / 64>(lane < NT / 64 ? waves[lane] : (T)0);  // (of the waves, one in a lane)
+        total = of_lane(sums, NT / 64 - 1);
+        return in - v + (wave ? of_lane(sums, wave - 1) : (T)0);
+    }
 }
 
 // Bins share the distance to the top, `per_bin` to one.
 __device__ __forceinline__ int bin_at(float z, float top, float per_bin, int bins) { return (int)fminf((top - z) * per_bin, (float)(bins - 1)); }
 
 // Counts and weights of the elements into the bins, which are empty.  E: each(f) calls f(key, index, weight()) for a thread's elements, and
-// each(lo, hi, f) for those whose logit is in [lo, hi] (and may for others); list() puts the elements of a bin by distance into s.list, if it can.
-template <int NT, typename E, typename B>
-__device__ __forceinline__ void fill_bins(const E& elements, CutShared<NT>& s, B bin_of) {
+// each(lo, hi, f) for those whose logit is in [lo, hi] (and may for others); list() puts the elements of a bin by distance into s.list,
+// if it can.
+template <int NT, int N_BINS, typename E, typename B>
+__device__ __forceinline__ void fill_bins(const E& elements, CutShared<NT, N_BINS>& s, B bin_of) {
     // (what lies furthest may be most of a row: it is counted apart, not at one place by all)
     uint32_t last_count = 0;
     u64 last_weight = 0;
@@ -273,84 +289,101 @@ __device__ __forceinline__ void fill_bins(const E& elements, CutShared<NT>& s, B
         const int b = bin_of(key);
         if (b < 0) return;
         const u64 w = weight();
-        if (b == NT - 1) {
+        if (b == N_BINS - 1) {
             ++last_count, last_weight += w;
         } else {
             atomicAdd(&s.bin_count[b], 1u);
             atomicAdd(&s.bin_weight[b], w);
         }
     });
-    if (last_count) atomicAdd(&s.bin_count[NT - 1], last_count), atomicAdd(&s.bin_weight[NT - 1], last_weight);
-    __syncthreads();
+    if (last_count) atomicAdd(&s.bin_count[N_BINS - 1], last_count), atomicAdd(&s.bin_weight[N_BINS - 1], last_weight);
+    meet<NT>();
+}
+template <int NT, int N_BINS>
+__device__ __forceinline__ void empty_bins(CutShared<NT, N_BINS>& s, int tid) {
+#pragma unroll
+    for (int i = 0; i < N_BINS / NT; ++i) s.bin_weight[tid + i * NT] = 0, s.bin_count[tid + i * NT] = 0;
 }
 
 // The last element that is kept where elements are kept, in their order, as long as fewer than `limit` came before (BY_COUNT) or
 // their weights' sum is below `limit`: the bin in which that happens, then its elements one by one, or finer bins if they are many,
 // which share the keys that are in the bin, until it holds one key only.  If all are kept, the cut is left as it was.
 // The bins by distance are filled; false: they no longer are.
-template <bool BY_COUNT, int NT, typename E>
-__device__ bool find_cut(const E& elements, CutShared<NT>& s, u64 limit, float top, float per_bin) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+template <bool BY_COUNT, int NT, int N_BINS, typename E>
+__device__ bool find_cut(const E& elements, CutShared<NT, N_BINS>& s, u64 limit, float top, float per_bin) {
+    constexpr int PER = N_BINS / NT;
+    const int tid = threadIdx.x & (NT - 1), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     uint32_t lo = 0, hi = 0;
     int shift = -1;  // -1: bins by distance
     u64 base_weight = 0;
     uint32_t base_count = 0;
     for (;;) {
         auto bin_of = [&](uint32_t key) {
-            if (shift < 0) return bin_at(value_of(key), top, per_bin, NT);
+            if (shift < 0) return bin_at(value_of(key), top, per_bin, N_BINS);
             return key >= lo && key <= hi ? (int)((hi - key) >> shift) : -1;
         };
-        const uint32_t c = s.bin_count[tid];
-        const u64 w = s.bin_weight[tid];
-        const uint32_t c_in = wave_scan(c);
-        const u64 w_in = wave_scan(w);
+        // (a thread's bins lie next to one another)
+        uint32_t c[PER], c_all = 0;
+        u64 w[PER], w_all = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] = s.bin_count[tid * PER + i], w[i] = s.bin_weight[tid * PER + i], c_all += c[i], w_all += w[i];
+        const uint32_t c_in = wave_scan(c_all);
+        const u64 w_in = wave_scan(w_all);
         if (lane == 63) s.counts[wave] = c_in, s.sums[wave] = w_in;
         if (tid == 0) s.n_list = 0, s.lo = 0xffffffffu, s.hi = 0, s.bin = -1, s.listed = 0;
-        __syncthreads();
-        const uint32_t c_waves = wave_scan<NT / 64>(lane < NT / 64 ? s.counts[lane] : 0u);
-        const u64 w_waves = wave_scan<NT / 64>(lane < NT / 64 ? s.sums[lane] : 0ull);
-        const uint32_t c_before = base_count + c_in - c + (wave ? of_lane(c_waves, wave - 1) : 0u);
-        const u64 w_before = base_weight + w_in - w + (wave ? of_lane(w_waves, wave - 1) : 0ull);
+        meet<NT>();
+        uint32_t c_before = base_count + c_in - c_all;
+        u64 w_before = base_weight + w_in - w_all;
+        if constexpr (NT > 64) {
+            const uint32_t c_waves = wave_scan<NT / 64>(lane < NT / 64 ? s.counts[lane] : 0u);
+            const u64 w_waves = wave_scan<NT / 64>(lane < NT / 64 ? s.sums[lane] : 0ull);
+            if (wave) c_before += of_lane(c_waves, wave - 1), w_before += of_lane(w_waves, wave - 1);
+        }
         // the bin in which the limit is reached
-        const bool here = c && (BY_COUNT ? c_before < limit && c_before + c >= limit : w_before < limit && w_before + w >= limit);
-        if (here) s.bin = tid, s.base_count = c_before, s.base_weight = w_before, s.in_bin = c;
-        __syncthreads();
+        if (BY_COUNT ? c_before < limit && c_before + c_all >= limit : w_before < limit && w_before + w_all >= limit) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                if (c[i] && (BY_COUNT ? c_before < limit && c_before + c[i] >= limit : w_before < limit && w_before + w[i] >= limit))
+                    s.bin = tid * PER + i, s.base_count = c_before, s.base_weight = w_before, s.in_bin = c[i];
+                c_before += c[i], w_before += w[i];
+            }
+        }
+        meet<NT>();
         const int bin = s.bin;
         if (bin < 0) {  // all are kept
-            __syncthreads();
+            meet<NT>();
             return shift < 0;
         }
         base_count = s.base_count, base_weight = s.base_weight;
         const uint32_t in_bin = s.in_bin;
         uint32_t key_lo = 0xffffffffu, key_hi = 0;
-        if (shift < 0 && in_bin <= LIST && elements.list(s, bin)) {
-        } else {
-        // (the bin's logits lie between these, and little else)
-        const float far = fabsf(top) * 1e-6f + (float)(bin + 1) / per_bin * 1e-5f;
-        const float z_lo = shift >= 0 ? value_of(lo) : bin == NT - 1 ? -INFINITY : top - (float)(bin + 1) / per_bin - far;
-        const float z_hi = shift >= 0 ? value_of(hi) : top - (float)bin / per_bin + far;
-        elements.each(z_lo, z_hi, [&](uint32_t key, int index, auto weight) {
-            if (bin_of(key) == bin) {
-                key_lo = min(key_lo, key), key_hi = max(key_hi, key);
-                if (in_bin <= LIST) {
-                    const uint32_t at = atomicAdd(&s.n_list, 1u);
-                    s.list[at] = key, s.list_index[at] = index, s.list_weight[at] = weight();
+        if (!(shift < 0 && in_bin <= LIST && elements.list(s, bin))) {
+            // (the bin's logits lie between these, and little else)
+            const float far = fabsf(top) * 1e-6f + (float)(bin + 1) / per_bin * 1e-5f;
+            const float z_lo = shift >= 0 ? value_of(lo) : bin == N_BINS - 1 ? -INFINITY : top - (float)(bin + 1) / per_bin - far;
+            const float z_hi = shift >= 0 ? value_of(hi) : top - (float)bin / per_bin + far;
+            elements.each(z_lo, z_hi, [&](uint32_t key, int index, auto weight) {
+                if (bin_of(key) == bin) {
+                    key_lo = min(key_lo, key), key_hi = max(key_hi, key);
+                    if (in_bin <= LIST) {
+                        const uint32_t at = atomicAdd(&s.n_list, 1u);
+                        s.list[at] = key, s.list_index[at] = index, s.list_weight[at] = weight();
+                    }
                 }
-            }
-        });
+            });
         }
         if (in_bin > LIST && key_lo <= key_hi) atomicMin(&s.lo, key_lo), atomicMax(&s.hi, key_hi);
-        __syncthreads();
+        meet<NT>();
         if (in_bin <= LIST) {
             const int n = (int)s.n_list;
             if (tid == 0) s.listed = shift < 0;  // (whole)
             // so many lanes for each that all threads have work, 16 at most
-            int lanes = NT / LIST;
+            int lanes = 1;
             while (lanes < 16 && 2 * lanes * n <= NT) lanes *= 2;
-            if (tid < n * lanes) {
-                const int e = tid / lanes;
-                const uint32_t key = s.list[e];
-                const u64 each = s.list_weight[e];
+            for (int e0 = 0; e0 < n; e0 += NT / lanes) {
+                const int e = e0 + tid / lanes;
+                const uint32_t key = e < n ? s.list[e] : 0;
+                const u64 each = e < n ? s.list_weight[e] : 0;
                 uint32_t above = 0, equal = 0;
                 u64 weight = 0;
                 for (int i = tid & (lanes - 1); i < n; i += lanes) {
@@ -363,13 +396,13 @@ __device__ bool find_cut(const E& elements, CutShared<NT>& s, u64 limit, float t
                     weight += (u64)__shfl_xor((long long)weight, d);
                 }
                 above += base_count, weight += base_weight;
-                const bool mine = BY_COUNT ? above < limit && above + equal >= limit : weight < limit && weight + equal * each >= limit;
+                const bool mine = e < n && (BY_COUNT ? above < limit && above + equal >= limit : weight < limit && weight + equal * each >= limit);
                 if (mine) {  // (all of one key write the same)
                     const u64 ties = BY_COUNT ? limit - above : (limit - weight + each - 1) / each;
                     s.cut = Cut{key, (int)ties, ties < equal, weight + ties * each};
                 }
             }
-            __syncthreads();
+            meet<NT>();
             return shift < 0;
         }
         lo = s.lo, hi = s.hi;
@@ -379,13 +412,13 @@ __device__ bool find_cut(const E& elements, CutShared<NT>& s, u64 limit, float t
                 const u64 ties = BY_COUNT ? limit - base_count : (limit - base_weight + each - 1) / each;
                 s.cut = Cut{lo, (int)ties, ties < in_bin, base_weight + ties * each};
             }
-            __syncthreads();
+            meet<NT>();
             return shift < 0;
         }
-        shift = max(0, 32 - __builtin_clz(hi - lo) - (31 - __builtin_clz(NT)));
-        s.bin_weight[tid] = 0, s.bin_count[tid] = 0;
-        __syncthreads();
-        fill_bins<NT>(elements, s, bin_of);
+        shift = max(0, 32 - __builtin_clz(hi - lo) - (31 - __builtin_clz(N_BINS)));
+        empty_bins(s, tid);
+        meet<NT>();
+        fill_bins(elements, s, bin_of);
     }
 }
 
@@ -396,13 +429,18 @@ __device__ __forceinline__ void write_row(const Sampling& p, int r, int token, f
 }
 
 constexpr int ROW_THREADS = 512, ROW_WAVES = ROW_THREADS / 64;
-constexpr int OWN = 4, CANDIDATES = ROW_THREADS * OWN;  // that the threads hold
-constexpr int WAVE_CANDIDATES = 1024;                   // that a wave may find
-constexpr int AT_ONCE = 16;                             // runs of 64 tokens that a wave has on their way
+constexpr int CANDIDATES = 2048;        // that the threads hold
+constexpr int WAVE_CANDIDATES = 1024;   // that a wave may find
+constexpr int ONE_WAVE = 512;           // candidates that one wave takes
+constexpr int AT_ONCE = 16;             // runs of 64 tokens that a wave has on their way
 
 struct RowShared {
-    CutShared<ROW_THREADS> c;
-    uint32_t tops[ROW_WAVES];
+    union {
+        CutShared<ROW_THREADS, ROW_THREADS> all;
+        CutShared<64, ROW_THREADS> one;
+    };
+    u64 sums[ROW_WAVES];
+    uint32_t tops[ROW_WAVES], lows[ROW_WAVES], founds[ROW_WAVES], places[ROW_WAVES], floors[ROW_WAVES];
     double raw[ROW_WAVES];
     double log_raw;
     uint32_t place, found, candidates;
@@ -414,9 +452,11 @@ struct RowShared {
     float2 found_at[ROW_WAVES][WAVE_CANDIDATES];  // logit, and the bits of the index
 };
 
+// Candidates that threads hold.
+template <int OWN>
 struct OwnElements {
-    const uint32_t (&key)[OWN];
-    const u64 (&weight)[OWN];
+    uint32_t key[OWN], index[OWN];
+    u64 weight[OWN];
     int n;
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
@@ -428,25 +468,94 @@ struct OwnElements {
     __device__ __forceinline__ void each(float, float, F f) const {
         each(f);
     }
-    template <int NT>
-    __device__ __forceinline__ bool list(CutShared<NT>&, int) const {
+    template <typename S>
+    __device__ __forceinline__ bool list(S&, int) const {
         return false;
     }
-    __device__ __forceinline__ u64 sum() const {
-        u64 all = 0;
-#pragma unroll
-        for (int j = 0; j < OWN; ++j) all += weight[j];
-        return all;
-    }
 };
+
+// The token among n candidates, which lie in s.found_at in the order of their indices, from[] of them before each wave's; held by NT
+// threads, OWN each, neighbouring ones by a thread.
+template <int NT, int OWN, typename S>
+__device__ void token_of(const Settings& g, RowShared& s, S& c, const uint32_t (&from)[ROW_WAVES], int n, float top, float least_z, double reach, u64 total) {
+    const int tid = threadIdx.x & (NT - 1);
+    const int mine = (n + NT - 1) / NT, at0 = tid * mine;
+    OwnElements<OWN> own;
+    own.n = max(0, min(mine, n - at0));
+    u64 part = 0;
+#pragma unroll
+    for (int j = 0; j < OWN; ++j) {
+        int w = 0, i = at0 + j;
+#pragma unroll
+        for (int k = 1; k < ROW_WAVES; ++k)
+            if (at0 + j >= (int)from[k]) w = k, i = at0 + j - (int)from[k];
+        own.key[j] = 0, own.index[j] = 0, own.weight[j] = 0;
+        if (j < own.n) {
+            const float2 f = s.found_at[w][i];
+            own.key[j] = key_of(f.x), own.index[j] = __float_as_uint(f.y), own.weight[j] = weight_of(f.x, top, g.per_t);
+        }
+        part += own.weight[j];
+    }
+    if (g.by_k || g.by_p) {
+        const float per_bin = fminf((ROW_THREADS - 1) / (top - least_z), 3e38f);
+        auto bin_of = [&](uint32_t key) { return bin_at(value_of(key), top, per_bin, ROW_THREADS); };
+        empty_bins(c, tid);
+        if (tid == 0) c.cut = nothing_cut();
+        meet<NT>();
+        fill_bins(own, c, bin_of);
+        u64 whole = total;
+        if (g.by_k) {
+            const bool intact = find_cut<true>(own, c, (u64)g.top_k, top, per_bin);
+            whole = c.cut.weight;
+            if (g.by_p && !whole) before_me<NT>(part, whole, c.sums);  // (all are kept)
+            if (g.by_p && !intact) {
+                meet<NT>();
+                empty_bins(c, tid);
+                meet<NT>();
+                fill_bins(own, c, bin_of);
+            }
+        }
+        if (g.by_p) find_cut<false>(own, c, max(share_of(g.top_p, whole, true), 1ull), top, per_bin);
+    }
+    // kept weights by index
+    const Cut cut = g.by_k || g.by_p ? c.cut : nothing_cut();
+    int left = 1 << 30;
+    if (cut.some) {
+        uint32_t ties = 0, all;
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) ties += j < own.n && own.key[j] == cut.key;
+        left = cut.ties - (int)before_me<NT>(ties, all, c.counts);
+    }
+    u64 w[OWN], all;
+    part = 0;
+#pragma unroll
+    for (int j = 0; j < OWN; ++j) {
+        const bool in = j < own.n && (double)top - (double)value_of(own.key[j]) <= reach && (own.key[j] == cut.key ? left-- > 0 : own.key[j] > cut.key);
+        w[j] = in ? own.weight[j] : 0;
+        part += w[j];
+    }
+    meet<NT>();
+    u64 upto = before_me<NT>(part, all, c.sums);
+    const u64 target = share_of(g.u, all, false);
+    if (upto <= target && upto + part > target) {
+        uint32_t token = 0xffffffffu;
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) {
+            upto += w[j];
+            if (w[j] && upto > target) token = min(token, own.index[j]);
+        }
+        s.found = token;
+    }
+}
 
 // Candidates are what may be kept: the tokens that are not below a floor which follows from the runs' numbers alone.
 //   top-k  the floor is the k-th largest of the largest logits of runs of 64, or a little less: k tokens at least are not below it
 //   top-p  tokens of a weight below (1 - p) * sum / vocab have less than (1 - p) * sum together, so that the others have p of it
 //   min-p  its own
-// They are few in most rows: read from the runs that have any, in the order of their indices, and held by the threads, four each.
+// They are few in most rows: read from the runs that have any, in the order of their indices, and held by one wave, or by all if they are
+// more than 512: a wave alone needs no barriers (up to 512 of them: 2 us behind the loads, all eight waves 5).
 template <typename T>
-__global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, int wide_follows) {
+__global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, char* shared_bins) {
     __shared__ RowShared s;
     constexpr int NT = ROW_THREADS;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x;
@@ -461,7 +570,7 @@ __global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, int
 
     // the top, and the sums relative to it
     float chunk[8];
-    float most = -INFINITY;
+    float most = -INFINITY, low = INFINITY;
     bool nan = false;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -471,6 +580,8 @@ __global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, int
         most = fmaxf(most, fmaxf(fmaxf(f.x, f.y), fmaxf(f.z, f.w)));
         nan |= f.x != f.x;  // (a run of 1024 with a NaN has sixteen)
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) low = chunk[j] > -INFINITY ? fminf(low, chunk[j]) : low;
     u64 sum = 0;
     float raw_run = 0, run_top = -INFINITY;
     if (tid < at.runs) {
@@ -480,14 +591,13 @@ __global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, int
 #pragma unroll
         for (int j = 0; j < CHUNKS / 4; ++j) run_top = fmaxf(run_top, fmaxf(fmaxf(f[j].x, f[j].y), fmaxf(f[j].z, f[j].w)));
     }
-    const uint32_t wave_top = wave_most(nan ? 0xffffffffu : key_of(most));
-    if (lane == 0) s.tops[wave] = wave_top;
-    s.c.bin_count[tid] = 0, s.c.bin_weight[tid] = 0;
+    const uint32_t wave_top = wave_most(nan ? 0xffffffffu : key_of(most)), wave_low = ~wave_most(~key_of(low));
+    if (lane == 0) s.tops[wave] = wave_top, s.lows[wave] = wave_low;
     s.floor_count[tid] = 0;
-    if (tid == 0) s.c.cut = nothing_cut(), s.place = 0xffffffffu, s.found = 0xffffffffu, s.candidates = 0, s.floor_bin = NT, note->wide = 0;
+    if (tid == 0) s.place = 0xffffffffu, s.found = 0xffffffffu, s.candidates = 0, s.floor_bin = NT, note->wide = 0;
     __syncthreads();
-    uint32_t top_key = s.tops[0];
-    for (int i = 1; i < ROW_WAVES; ++i) top_key = max(top_key, s.tops[i]);
+    uint32_t top_key = s.tops[0], low_key = s.lows[0];
+    for (int i = 1; i < ROW_WAVES; ++i) top_key = max(top_key, s.tops[i]), low_key = min(low_key, s.lows[i]);
     if (g.bad || top_key >= KEY_INF || top_key <= KEY_NINF) {
         if (tid == 0) {
             p.token[r] = -1;
@@ -497,7 +607,7 @@ __global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, int
         return;
     }
     const float top = value_of(top_key);
-    const float run_ref = fmaxf(run_top, -3.4028235e38f);
+    const float run_ref = fmaxf(run_top, -MOST_FLOAT);
     double raw = 0;
     if (wave < (at.runs + 63) / 64) {
         if (g.whole_sum()) sum = rescaled(sum, ((double)run_ref - (double)top) * g.per_t);
@@ -506,8 +616,16 @@ __global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, int
         }
     }
     if (lane == 0) s.raw[wave] = raw;
+    // bins for top-k's floor, between the largest and the least of the runs' largest
+    const bool by_floor = g.by_k && g.top_k <= n_chunks;
+    const float floor_per_bin = fminf((NT - 1) / (top - value_of(low_key)), 3e38f);
+    if (by_floor) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (chunk[j] > -INFINITY) atomicAdd(&s.floor_count[bin_at(chunk[j], top, floor_per_bin, NT)], 1u);
+    }
     u64 total;
-    const u64 sum_before = before_me<NT>(sum, total, s.c.sums);
+    const u64 sum_before = before_me<NT>(sum, total, s.sums);
     raw = 0;
     for (int i = 0; i < (RUNS + 63) / 64; ++i) raw += s.raw[i];
     if (scores && wave == ROW_WAVES - 1) {
@@ -536,46 +654,21 @@ __global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, int
         const float ref = s.ref;
         const u64 w0 = i < p.vocab ? weight_of((float)z[i], ref, g.per_t) : 0, w1 = i + 1 < p.vocab ? weight_of((float)z[i + 1], ref, g.per_t) : 0;
         u64 all;
-        const u64 before = before_me<NT>(w0 + w1, all, s.c.sums);
+        const u64 before = before_me<NT>(w0 + w1, all, s.sums);
         const double y = ((double)ref - (double)top) * g.per_t;
         if (rescaled(before, y) <= left && rescaled(before + w0 + w1, y) > left) s.found = rescaled(before + w0, y) > left ? i : i + 1;
     } else {
         const double reach = g.by_m ? -log((double)g.min_p) * (double)g.t : INFINITY;
         uint32_t least = KEY_NINF;  // the floor's key
-        if (g.by_k && g.top_k <= n_chunks) {
-            // bins between the largest and the least of the runs' largest
-            uint32_t low = KEY_INF;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (chunk[j] > -INFINITY) low = min(low, key_of(chunk[j]));
-            low = ~wave_most(~low);
-            if (lane == 0) s.c.counts[wave] = low;
-            __syncthreads();
-            for (int i = 0; i < ROW_WAVES; ++i) low = min(low, s.c.counts[i]);
-            const float per_bin = fminf((NT - 1) / (top - value_of(low)), 3e38f);
-            int bin[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                bin[j] = chunk[j] > -INFINITY ? bin_at(chunk[j], top, per_bin, NT) : NT;
-                if (bin[j] < NT) atomicAdd(&s.floor_count[bin[j]], 1u);
-            }
-            __syncthreads();
+        if (by_floor) {
             const uint32_t c = s.floor_count[tid];
             uint32_t all;
-            const uint32_t c_before = before_me<NT>(c, all, s.c.counts);
+            const uint32_t c_before = before_me<NT>(c, all, s.floors);
             if (c_before < (uint32_t)g.top_k && c_before + c >= (uint32_t)g.top_k) s.floor_bin = tid;
             __syncthreads();
-            if (s.floor_bin < NT) {  // (else fewer than k runs have any: no floor)
-                uint32_t floor = KEY_INF;
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (bin[j] <= s.floor_bin) floor = min(floor, key_of(chunk[j]));
-                floor = ~wave_most(~floor);
-                if (lane == 0) s.tops[wave] = floor;
-                __syncthreads();
-                for (int i = 0; i < ROW_WAVES; ++i) floor = min(floor, s.tops[i]);
-                least = floor;
-            }
+            // (what is in these bins is above this, whatever the roundings; fewer than k runs with any: no floor)
+            const int b = s.floor_bin;
+            if (b < NT - 1) least = key_of(top - (float)(b + 1) / floor_per_bin * 1.00001f - fabsf(top) * 1e-6f);
         } else if (g.by_p && !g.by_k) {
             // (weights are off by less than one: what is below the floor's in full may be one above it as a whole number)
             const double floor_weight = (1.0 - (double)g.top_p) * (double)total / p.vocab * 0.99 - 1.0;
@@ -590,140 +683,93 @@ __global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, int
         uint32_t flags = 0, n_some;
 #pragma unroll
         for (int j = 0; j < 8; ++j) flags |= (uint32_t)(chunk[j] >= least_z && chunk[j] > -INFINITY) << j;
-        __syncthreads();
-        uint32_t place = before_me<NT>((uint32_t)__popc(flags), n_some, s.c.counts);
+        uint32_t place = before_me<NT>((uint32_t)__popc(flags), n_some, s.places);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (flags >> j & 1) s.chunks[place++] = (uint16_t)(tid * per * 4 + j);
         __syncthreads();
-        // a wave takes neighbouring ones and keeps what it finds in its own place
-        const int each = ((int)n_some + ROW_WAVES - 1) / ROW_WAVES, c0 = min((int)n_some, wave * each), c1 = min((int)n_some, c0 + each);
-        uint32_t found = 0;
-        const float from_z = fmaxf(least_z, -3.4028235e38f);  // (nothing that is -inf)
-        float next[AT_ONCE / 4][4];
-        int next_at[AT_ONCE / 4];
-        auto load = [&](int c) {  // sixteen lanes a chunk, so that the lanes' order is that of the indices
-#pragma unroll
-            for (int j = 0; j < AT_ONCE / 4; ++j) {
-                const int mine = c + 4 * j + (lane >> 4);
-                next_at[j] = s.chunks[min(mine, c1 - 1)] * SAMPLE_CHUNK + (lane & 15) * 4;
-                load4(z, mine < c1 ? next_at[j] : p.vocab, p.vocab, p.vec, next[j]);
-            }
-        };
-        if (c0 < c1) load(c0);
-        for (int c = c0; c < c1; c += AT_ONCE) {
-            float v[AT_ONCE / 4][4];
-            int at_index[AT_ONCE / 4];
-#pragma unroll
-            for (int j = 0; j < AT_ONCE / 4; ++j) {
-                at_index[j] = next_at[j];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[j][k] = next[j][k];
-            }
-            if (c + AT_ONCE < c1) load(c + AT_ONCE);
-            const uint32_t found_before = found;
-#pragma unroll
-            for (int j = 0; j < AT_ONCE / 4; j += 2) {  // (two counts of 256 at most in a number)
-                uint32_t n = 0;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) n += (v[j][k] >= from_z ? 1u : 0u) + (v[j + 1][k] >= from_z ? 0x10000u : 0u);
-                const uint32_t upto = wave_scan(n), total_n = last_lane(upto), before = upto - n;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t slot = found + (h ? before >> 16 : before & 0xffff);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (v[j + h][k] >= from_z) {
-                            if (slot < WAVE_CANDIDATES) s.found_at[wave][slot] = float2{v[j + h][k], __int_as_float(at_index[j + h] + k)};
-                            ++slot;
-                        }
-                    found += h ? total_n >> 16 : total_n & 0xffff;
-                }
-            }
-            if (c + AT_ONCE < c1) {  // (too many already: the rest need not be read)
-                uint32_t all = 0;
-                if (lane == 0) all = atomicAdd(&s.candidates, found - found_before) + found - found_before;
-                if ((uint32_t)__builtin_amdgcn_readfirstlane((int)all) > CANDIDATES) {
-                    found = WAVE_CANDIDATES + 1;
-                    break;
-                }
-            }
-        }
-        if (lane == 0) s.tops[wave] = found;
-        __syncthreads();
+        // Tokens that lie anywhere leave exp(-n / chunks) of the runs without one: where this says that they are many more than can be
+        // held, they are not looked for.
+        bool wide = shared_bins && (float)n_some > (float)n_chunks * (1.f - __expf(-1.25f * CANDIDATES / (float)n_chunks));
         uint32_t n = 0;
-        bool wide = false;
         uint32_t from[ROW_WAVES];
+        if (!wide) {
+            // a wave takes neighbouring ones and keeps what it finds in its own place
+            const int each = ((int)n_some + ROW_WAVES - 1) / ROW_WAVES, c0 = min((int)n_some, wave * each), c1 = min((int)n_some, c0 + each);
+            uint32_t found = 0;
+            const float from_z = fmaxf(least_z, -MOST_FLOAT);  // (nothing that is -inf)
+            float next[AT_ONCE / 4][4];
+            int next_at[AT_ONCE / 4];
+            auto load = [&](int c) {  // sixteen lanes a chunk, so that the lanes' order is that of the indices
 #pragma unroll
-        for (int i = 0; i < ROW_WAVES; ++i) from[i] = n, n += s.tops[i], wide |= s.tops[i] > WAVE_CANDIDATES;
-        if (wide || n > CANDIDATES) {
+                for (int j = 0; j < AT_ONCE / 4; ++j) {
+                    const int mine = c + 4 * j + (lane >> 4);
+                    next_at[j] = s.chunks[min(mine, c1 - 1)] * SAMPLE_CHUNK + (lane & 15) * 4;
+                    load4(z, mine < c1 ? next_at[j] : p.vocab, p.vocab, p.vec, next[j]);
+                }
+            };
+            if (c0 < c1) load(c0);
+            for (int c = c0; c < c1; c += AT_ONCE) {
+                float v[AT_ONCE / 4][4];
+                int at_index[AT_ONCE / 4];
+#pragma unroll
+                for (int j = 0; j < AT_ONCE / 4; ++j) {
+                    at_index[j] = next_at[j];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[j][k] = next[j][k];
+                }
+                if (c + AT_ONCE < c1) load(c + AT_ONCE);
+                const uint32_t found_before = found;
+#pragma unroll
+                for (int j = 0; j < AT_ONCE / 4; j += 2) {  // (two counts of 256 at most in a number)
+                    uint32_t n = 0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) n += (v[j][k] >= from_z ? 1u : 0u) + (v[j + 1][k] >= from_z ? 0x10000u : 0u);
+                    const uint32_t upto = wave_scan(n), total_n = last_lane(upto), before = upto - n;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t slot = found + (h ? before >> 16 : before & 0xffff);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (v[j + h][k] >= from_z) {
+                                if (slot < WAVE_CANDIDATES) s.found_at[wave][slot] = float2{v[j + h][k], __int_as_float(at_index[j + h] + k)};
+                                ++slot;
+                            }
+                        found += h ? total_n >> 16 : total_n & 0xffff;
+                    }
+                }
+                if (c + AT_ONCE < c1) {  // (too many already: the rest need not be read)
+                    uint32_t all = 0;
+                    if (lane == 0) all = atomicAdd(&s.candidates, found - found_before) + found - found_before;
+                    if ((uint32_t)__builtin_amdgcn_readfirstlane((int)all) > CANDIDATES) {
+                        found = WAVE_CANDIDATES + 1;
+                        break;
+                    }
+                }
+            }
+            if (lane == 0) s.founds[wave] = found;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < ROW_WAVES; ++i) from[i] = n, n += s.founds[i], wide |= s.founds[i] > WAVE_CANDIDATES;
+            wide |= n > CANDIDATES;
+        }
+        if (wide) {
+            // (not without a third kernel: the host launches one wherever a row can have as many)
+            if (!shared_bins) return;
+            u64* weights = (u64*)(shared_bins + (size_t)r * SAMPLE_ROW_BINS);
+            uint32_t* counts = (uint32_t*)(weights + SAMPLE_BINS);
+            for (int i = tid; i < SAMPLE_BINS; i += NT) weights[i] = 0, counts[i] = 0;
             if (tid == 0) {
                 note->top_key = top_key, note->least = least, note->arrived = 0, note->total = total, note->raw = raw;
-                note->log_raw = scores ? s.log_raw : 0.0;
-                note->wide = wide_follows;
+                note->log_raw = scores ? log(raw) : 0.0;
+                note->wide = 1;
             }
             return;
         }
-        const int mine = ((int)n + NT - 1) / NT, at0 = tid * mine;
-        uint32_t index[OWN], key[OWN];
-        u64 weight[OWN];
-#pragma unroll
-        for (int j = 0; j < OWN; ++j) {
-            const bool ok = j < mine && at0 + j < (int)n;
-            int w = 0, i = at0 + j;
-#pragma unroll
-            for (int k = 1; k < ROW_WAVES; ++k)
-                if (at0 + j >= (int)from[k]) w = k, i = at0 + j - (int)from[k];
-            const float2 f = ok ? s.found_at[w][i] : float2{-INFINITY, __uint_as_float(0xffffffffu)};
-            key[j] = ok ? key_of(f.x) : 0;
-            index[j] = __float_as_uint(f.y);
-            weight[j] = ok ? weight_of(f.x, top, g.per_t) : 0;
-        }
-        const OwnElements own{key, weight, max(0, min(mine, (int)n - at0))};
-        const float per_bin = fminf((NT - 1) / (top - least_z), 3e38f);
-        if (g.by_k || g.by_p) {
-            fill_bins<NT>(own, s.c, [&](uint32_t key) { return bin_at(value_of(key), top, per_bin, NT); });
-            u64 whole = total;
-            if (g.by_k) {
-                const bool intact = find_cut<true, NT>(own, s.c, (u64)g.top_k, top, per_bin);
-                whole = s.c.cut.weight;
-                if (!g.by_p) whole = 1;
-                else if (!whole) before_me<NT>(own.sum(), whole, s.c.sums);  // (all are kept)
-                if (g.by_p && !intact) {
-                    __syncthreads();
-                    s.c.bin_weight[tid] = 0, s.c.bin_count[tid] = 0;
-                    __syncthreads();
-                    fill_bins<NT>(own, s.c, [&](uint32_t key) { return bin_at(value_of(key), top, per_bin, NT); });
-                }
-            }
-            if (g.by_p) find_cut<false, NT>(own, s.c, max(share_of(g.top_p, whole, true), 1ull), top, per_bin);
-        }
-        // kept weights by index
-        const Cut cut = s.c.cut;
-        int left = 1 << 30;
-        if (cut.some) {
-            uint32_t ties = 0, all;
-#pragma unroll
-            for (int j = 0; j < OWN; ++j) ties += j < own.n && key[j] == cut.key;
-            left = cut.ties - (int)before_me<NT>(ties, all, s.c.counts);
-        }
-        u64 w[OWN], all, part = 0;
-#pragma unroll
-        for (int j = 0; j < OWN; ++j) {
-            const bool in = j < own.n && (double)top - (double)value_of(key[j]) <= reach && (key[j] == cut.key ? left-- > 0 : key[j] > cut.key);
-            w[j] = in ? weight[j] : 0;
-            part += w[j];
-        }
-        u64 upto = before_me<NT>(part, all, s.c.sums);
-        const u64 target = share_of(g.u, all, false);
-        if (upto <= target && upto + part > target) {
-            uint32_t token = 0xffffffffu;
-#pragma unroll
-            for (int j = 0; j < OWN; ++j) {
-                upto += w[j];
-                if (w[j] && upto > target) token = min(token, index[j]);
-            }
-            s.found = token;
+        if (n <= ONE_WAVE) {
+            if (wave == 0) token_of<64, ONE_WAVE / 64>(g, s, s.one, from, (int)n, top, least_z, reach, total);
+        } else {
+            token_of<NT, CANDIDATES / NT>(g, s, s.all, from, (int)n, top, least_z, reach, total);
         }
     }
     __syncthreads();
@@ -736,17 +782,18 @@ __global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, int
 // ------------------------------------------------------------------------------------------------
 // rows with many candidates
 // ------------------------------------------------------------------------------------------------
-constexpr int WIDE_THREADS = SAMPLE_BINS, WIDE_WAVES = WIDE_THREADS / 64;
+constexpr int WIDE_THREADS = 256, WIDE_WAVES = WIDE_THREADS / 64;
 constexpr int MOST_PARTS = 8;
 
-// What a workgroup of the row leaves for the last one: for each bin its weight, and the first of its elements in a list of the part's
-// elements by bins, as indices in the part.  It goes past the caches of the XCD, by agent-scope stores and loads of single values.
+// What a workgroup of the row leaves for the last one: for each bin the weight of the part's elements before it, and how many these
+// are in a list of them by bins, as indices in the part.  It goes past the caches of the XCD, by agent-scope stores and loads of
+// single values.
 struct Part {
     u64* weight;
     uint32_t* first;  // [SAMPLE_BINS + 1]
     uint16_t* element;
-    __device__ __forceinline__ Part(char* bins, int part_length, int i) {
-        char* base = bins + (size_t)i * sample_part_bytes(part_length);
+    __device__ __forceinline__ Part(char* parts, int part_length, int i) {
+        char* base = parts + (size_t)i * sample_part_bytes(part_length);
         weight = (u64*)base, first = (uint32_t*)(weight + SAMPLE_BINS), element = (uint16_t*)(first + SAMPLE_BINS + 4);
     }
 };
@@ -767,9 +814,8 @@ struct RowElements {
     int i0, i1, vec;
     float top, least;
     double per_t;
-    char* bins;  // of the parts, if they are there
+    char* left;  // by the parts, if there are several
     int parts, part_length;
-    const uint32_t (*firsts)[SAMPLE_BINS + 1];  // where the parts' elements of each bin begin (LDS)
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
         each(least, INFINITY, f);
@@ -800,20 +846,23 @@ struct RowElements {
                         f(key_of(v[k][j]), i + k * STEP + j, [&] { return weight_of(v[k][j], top, per_t); });
         }
     }
-    template <int NT>
-    __device__ __forceinline__ bool list(CutShared<NT>& s, int bin) const {
+    template <typename S>
+    __device__ __forceinline__ bool list(S& s, int bin) const {
         if (parts == 1) return false;
         const int tid = threadIdx.x, lane = tid & 63;
         // (every wave looks the parts' shares up, one in a lane)
         uint32_t first = 0, n = 0;
-        if (lane < parts) first = firsts[lane][bin], n = firsts[lane][bin + 1] - first;
+        if (lane < parts) {
+            const Part part(left, part_length, lane);
+            first = take(part.first + bin), n = take(part.first + bin + 1) - first;
+        }
         const uint32_t upto = wave_scan<16>(n);
         const int all = (int)of_lane(upto, 15);
         int at_part = 0;
         for (int i = 1; i < parts; ++i) at_part = tid >= (int)of_lane(upto, i - 1) ? i : at_part;
         const uint32_t start = (uint32_t)__shfl((int)first, at_part), before = (uint32_t)__shfl((int)(upto - n), at_part);
         if (tid < all) {  // (LIST at most)
-            const int i = at_part * part_length + take(Part(bins, part_length, at_part).element + start + (tid - before));
+            const int i = at_part * part_length + take(Part(left, part_length, at_part).element + start + (tid - before));
             const float v = (float)z[i];
             s.list[tid] = key_of(v), s.list_index[tid] = i, s.list_weight[tid] = weight_of(v, top, per_t);
         }
@@ -821,12 +870,12 @@ struct RowElements {
         return true;
     }
 };
+static_assert(LIST <= WIDE_THREADS, "a thread takes one element of a list");
 
 struct WideShared {
-    CutShared<WIDE_THREADS> c;
-    uint32_t firsts[MOST_PARTS][SAMPLE_BINS + 1];
+    CutShared<WIDE_THREADS, SAMPLE_BINS> c;
     uint32_t last, found;
-    int place, ties_left, first_run, n_runs;
+    int place, ties_left;
     u64 left;
     u64 part_weight[MOST_PARTS];
     uint32_t part_ties[MOST_PARTS];
@@ -835,13 +884,13 @@ struct WideShared {
 };
 
 // The bins of a row are filled by `parts` workgroups, and whoever is the last goes on: the cuts; the part of the row in which u * total
-// lies, by the bins of each part and the elements of the bin in which the cut is; the run of 1024 tokens, by the sums of what is kept
-// in the part's runs; the token in it.  All sums are of whole numbers, so that their order does not matter.  One CU reads a row of
-// 50 304 in 10 us, so that nothing but the part's runs is read twice.
+// lies, by the weights before the cut's bin in each part and the elements of that bin; the run of 1024 tokens, by the sums of what is
+// kept in the part's runs; the token in it.  All sums are of whole numbers, so that their order does not matter.  One CU reads a
+// row of 50 304 in 10 us, so that nothing but the part's runs is read twice.
 template <typename T>
-__global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, int parts, char* shared_bins) {
+__global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, int parts, char* shared_bins, char* shared_parts) {
     __shared__ WideShared s;
-    constexpr int NT = WIDE_THREADS;
+    constexpr int NT = WIDE_THREADS, PER = SAMPLE_BINS / NT;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x / parts, part = blockIdx.x % parts;
     const SampleRow at(p.vocab);
     SampleNote* note = (SampleNote*)(p.workspace + (size_t)r * at.bytes() + at.note());
@@ -849,58 +898,59 @@ __global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, i
     const T* z = (const T*)p.logits + (int64_t)r * p.row_stride;
     const Settings g(p, r);
     const float top = value_of(note->top_key), least_z = value_of(note->least);
-    const float spread = note->least > KEY_NINF ? top - least_z : 32.f * g.t, per_bin = fminf((NT - 1) / spread, 3e38f);
-    auto bin_of = [&](uint32_t key) { return bin_at(value_of(key), top, per_bin, NT); };
+    const float spread = note->least > KEY_NINF ? top - least_z : 32.f * g.t, per_bin = fminf((SAMPLE_BINS - 1) / spread, 3e38f);
+    auto bin_of = [&](uint32_t key) { return bin_at(value_of(key), top, per_bin, SAMPLE_BINS); };
 
-    s.c.bin_weight[tid] = 0, s.c.bin_count[tid] = 0;
+    empty_bins(s.c, tid);
     if (tid == 0) s.c.cut = nothing_cut(), s.found = 0xffffffffu;
     if (tid < MOST_PARTS) s.part_weight[tid] = 0, s.part_ties[tid] = 0;
     __syncthreads();
     const int runs_each = (at.runs + parts - 1) / parts, part_length = runs_each * SAMPLE_RUN;
-    char* bins = shared_bins + (size_t)r * parts * sample_part_bytes(part_length);
-    const RowElements<T> own{z, part * part_length, min(p.vocab, (part + 1) * part_length), p.vec, top, least_z, g.per_t, bins, parts, part_length, s.firsts};
-    fill_bins<NT>(own, s.c, bin_of);
-    u64 others[MOST_PARTS] = {};
+    char* left = shared_parts + (size_t)r * parts * sample_part_bytes(part_length);
+    const RowElements<T> own{z, part * part_length, min(p.vocab, (part + 1) * part_length), p.vec, top, least_z, g.per_t, left, parts, part_length};
+    fill_bins(own, s.c, bin_of);
     if (parts > 1) {
-        const Part here(bins, part_length, part);
-        uint32_t n;
-        const uint32_t first = before_me<NT>(s.c.bin_count[tid], n, s.c.counts);
-        s.firsts[0][tid] = first;
-        leave(here.weight + tid, s.c.bin_weight[tid]);
-        leave(here.first + tid, first);
-        if (tid == 0) leave(here.first + NT, n);
+        const Part here(left, part_length, part);
+        u64* weights = (u64*)(shared_bins + (size_t)r * SAMPLE_ROW_BINS);
+        uint32_t* counts = (uint32_t*)(weights + SAMPLE_BINS);
+        uint32_t c[PER], c_all = 0, n;
+        u64 w[PER], w_all = 0, all;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] = s.c.bin_count[tid * PER + i], w[i] = s.c.bin_weight[tid * PER + i], c_all += c[i], w_all += w[i];
+        uint32_t first = before_me<NT>(c_all, n, s.c.counts);
+        u64 weight = before_me<NT>(w_all, all, s.c.sums);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int b = tid * PER + i;
+            if (c[i]) {
+                __hip_atomic_fetch_add(weights + b, w[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __hip_atomic_fetch_add(counts + b, c[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            leave(here.weight + b, weight);
+            leave(here.first + b, first);
+            s.c.bin_count[b] = first;  // (where the next of the bin's elements goes)
+            first += c[i], weight += w[i];
+        }
+        if (tid == 0) leave(here.first + SAMPLE_BINS, n);
         __syncthreads();
-        own.each([&](uint32_t key, int i, auto) { leave(here.element + atomicAdd(&s.firsts[0][bin_of(key)], 1u), (uint16_t)(i - part * part_length)); });
-        // each thread's stores have arrived before its workgroup is counted
+        own.each([&](uint32_t key, int i, auto) { leave(here.element + atomicAdd(&s.c.bin_count[bin_of(key)], 1u), (uint16_t)(i - part * part_length)); });
+        // what each thread has sent has arrived before its workgroup is counted
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (tid == 0) s.last = __hip_atomic_fetch_add(&note->arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)parts - 1;
         __syncthreads();
         if (!s.last) return;
-        uint32_t c = 0, firsts[MOST_PARTS];
-        u64 w = 0;
-        if (tid < MOST_PARTS) s.firsts[tid][NT] = take(Part(bins, part_length, min(tid, parts - 1)).first + NT);
 #pragma unroll
-        for (int i = 0; i < MOST_PARTS; ++i) {
-            const Part other(bins, part_length, min(i, parts - 1));
-            others[i] = take(other.weight + tid), firsts[i] = take(other.first + tid);
-        }
+        for (int i = 0; i < PER; ++i) w[i] = take(weights + tid * PER + i), c[i] = take(counts + tid * PER + i);
 #pragma unroll
-        for (int i = 0; i < MOST_PARTS; ++i) s.firsts[i][tid] = firsts[i];
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < MOST_PARTS; ++i) {
-            others[i] = i < parts ? others[i] : 0;
-            w += others[i], c += i < parts ? s.firsts[i][tid + 1] - firsts[i] : 0;
-        }
-        s.c.bin_weight[tid] = w, s.c.bin_count[tid] = c;
+        for (int i = 0; i < PER; ++i) s.c.bin_weight[tid * PER + i] = w[i], s.c.bin_count[tid * PER + i] = c[i];
         __syncthreads();
     }
-    const RowElements<T> row{z, 0, p.vocab, p.vec, top, least_z, g.per_t, bins, parts, part_length, s.firsts};
+    const RowElements<T> row{z, 0, p.vocab, p.vec, top, least_z, g.per_t, left, parts, part_length};
     const double reach = g.by_m ? -log((double)g.min_p) * (double)g.t : INFINITY;
     u64 whole = note->total;
     if (g.by_k) {
-        const bool intact = find_cut<true, NT>(row, s.c, (u64)g.top_k, top, per_bin);
+        const bool intact = find_cut<true>(row, s.c, (u64)g.top_k, top, per_bin);
         whole = s.c.cut.weight;
         if (g.by_p) {
             if (!whole) {  // all are kept
@@ -910,13 +960,13 @@ __global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, i
             }
             if (!intact) {
                 __syncthreads();
-                s.c.bin_weight[tid] = 0, s.c.bin_count[tid] = 0;
+                empty_bins(s.c, tid);
                 __syncthreads();
-                fill_bins<NT>(row, s.c, bin_of);
+                fill_bins(row, s.c, bin_of);
             }
         }
     }
-    if (g.by_p) find_cut<false, NT>(row, s.c, max(share_of(g.top_p, whole, true), 1ull), top, per_bin);
+    if (g.by_p) find_cut<false>(row, s.c, max(share_of(g.top_p, whole, true), 1ull), top, per_bin);
     __syncthreads();
     const Cut cut = s.c.cut;
     auto kept_weight = [&](float v, uint32_t key) { return key >= cut.key && (double)top - (double)v <= reach ? weight_of(v, top, g.per_t) : 0; };
@@ -927,22 +977,17 @@ __global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, i
     u64 target;
     const bool by_parts = parts > 1 && tie && s.c.listed;
     if (by_parts) {
-        const int bin = bin_of(cut.key);
-#pragma unroll
-        for (int i = 0; i < MOST_PARTS; ++i) {
-            const u64 w = wave_total(tid < bin ? others[i] : 0ull);
-            if (lane == 0 && w) atomicAdd(&s.part_weight[i], w);
-        }
         if (tid < (int)s.c.n_list) {
             const int at_part = (int)s.c.list_index[tid] / part_length;
             if (s.c.list[tid] == cut.key) atomicAdd(&s.part_ties[at_part], 1u);
             else if (s.c.list[tid] > cut.key) atomicAdd(&s.part_weight[at_part], s.c.list_weight[tid]);
         }
+        const u64 before_bin = lane < parts ? take(Part(left, part_length, lane).weight + bin_of(cut.key)) : 0;
         __syncthreads();
         // (every wave for itself, a part in a lane)
         const uint32_t ties = lane < MOST_PARTS ? s.part_ties[lane] : 0;
         const int ties_left = max(0, cut.ties - (int)(wave_scan<16>(ties) - ties));
-        const u64 w = (lane < MOST_PARTS ? s.part_weight[lane] : 0) + tie * (u64)min((int)ties, ties_left);
+        const u64 w = before_bin + (lane < MOST_PARTS ? s.part_weight[lane] : 0) + tie * (u64)min((int)ties, ties_left);
         const u64 upto = wave_scan<16>(w);
         target = share_of(g.u, of_lane(upto, 15), false);
         const int at_part = __builtin_ctzll(__ballot(lane < MOST_PARTS && upto > target));
@@ -972,7 +1017,7 @@ __global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, i
     }
     __syncthreads();
     {
-        const uint32_t ties = tid < n_runs ? s.run_ties[tid] : 0;
+        const uint32_t ties = tid < n_runs ? s.run_ties[tid] : 0;  // (RUNS <= WIDE_THREADS)
         uint32_t all_ties;
         u64 all;
         const int ties_left = max(0, cut.ties - ties_before - (int)before_me<NT>(ties, all_ties, s.c.counts));
@@ -983,8 +1028,7 @@ __global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, i
         __syncthreads();
     }
     if (s.place % WIDE_WAVES == wave) {
-        // (where a wave has one run only, its logits are still here)
-        if (n_runs > WIDE_WAVES) load(first_run + s.place);
+        load(first_run + s.place);
         u64 left = s.left;
         int ties_left = s.ties_left;
 #pragma unroll
@@ -1032,11 +1076,12 @@ int sample_parts(int rows, int vocab) {
     if (vocab < 16384 || rows > 256) return 1;
     return std::max(rows > 128 ? 2 : rows > 64 ? 4 : MOST_PARTS, (SampleRow(vocab).runs + 63) / 64);
 }
+static size_t bins_at(int rows, int vocab) { return (SampleRow(vocab).bytes() * rows + 255) / 256 * 256; }
 
 size_t sample_workspace(int rows, int vocab) {
     const int parts = sample_parts(rows, vocab), runs = SampleRow(vocab).runs;
     const size_t shared = parts > 1 ? sample_part_bytes((runs + parts - 1) / parts * SAMPLE_RUN) * parts * rows : 0;
-    return (SampleRow(vocab).bytes() * rows + 255) / 256 * 256 + shared;
+    return bins_at(rows, vocab) + SAMPLE_ROW_BINS * rows + shared;
 }
 
 template <typename T>
@@ -1048,10 +1093,11 @@ static void launch_typed(const Sampling& p, hipStream_t st) {
     // what the host knows of the settings and sizes may rule out rows with many candidates
     const bool cuts = p.top_k || p.top_p || p.min_p || (p.one_top_k > 0 && p.one_top_k < p.vocab) || p.one_top_p < 1.f || p.one_min_p > 0.f;
     const bool wide = cuts && p.vocab > WAVE_CANDIDATES;
-    EE_LAUNCH(sample_row_kernel<T>, dim3(p.rows), dim3(ROW_THREADS), st, p, wide);
+    char* bins = p.workspace + bins_at(p.rows, p.vocab);
+    EE_LAUNCH(sample_row_kernel<T>, dim3(p.rows), dim3(ROW_THREADS), st, p, wide ? bins : nullptr);
     if (!wide) return;
     const int parts = sample_parts(p.rows, p.vocab);
-    EE_LAUNCH(sample_wide_kernel<T>, dim3(p.rows * parts), dim3(WIDE_THREADS), st, p, parts, p.workspace + (at.bytes() * p.rows + 255) / 256 * 256);
+    EE_LAUNCH(sample_wide_kernel<T>, dim3(p.rows * parts), dim3(WIDE_THREADS), st, p, parts, bins, bins + SAMPLE_ROW_BINS * p.rows);
 }
 
 hipError_t launch_sample(const Sampling& p, hipStream_t st) {
