@@ -360,8 +360,9 @@ __device__ bool find_cut(const E& elements, CutShared<NT, N_BINS>& s, u64 limit,
         if (!(shift < 0 && in_bin <= LIST && elements.list(s, bin))) {
             // (the bin's logits lie between these, and little else)
             const float far = fabsf(top) * 1e-6f + (float)(bin + 1) / per_bin * 1e-5f;
-            const float z_lo = shift >= 0 ? value_of(lo) : bin == N_BINS - 1 ? -INFINITY : top - (float)(bin + 1) / per_bin - far;
-            const float z_hi = shift >= 0 ? value_of(hi) : top - (float)bin / per_bin + far;
+            // (per_bin is 0 where the spread is infinite: fmaxf and fminf drop what is then no number)
+            const float z_lo = shift >= 0 ? value_of(lo) : bin == N_BINS - 1 ? -INFINITY : fmaxf(top - (float)(bin + 1) / per_bin - far, -INFINITY);
+            const float z_hi = shift >= 0 ? value_of(hi) : fminf(top - (float)bin / per_bin + far, INFINITY);
             elements.each(z_lo, z_hi, [&](uint32_t key, int index, auto weight) {
                 if (bin_of(key) == bin) {
                     key_lo = min(key_lo, key), key_hi = max(key_hi, key);
@@ -902,7 +903,7 @@ __global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, i
     auto bin_of = [&](uint32_t key) { return bin_at(value_of(key), top, per_bin, SAMPLE_BINS); };
 
     empty_bins(s.c, tid);
-    if (tid == 0) s.c.cut = nothing_cut(), s.found = 0xffffffffu;
+    if (tid == 0) s.c.cut = nothing_cut(), s.found = 0xffffffffu, s.place = 0, s.left = 0, s.ties_left = 0;
     if (tid < MOST_PARTS) s.part_weight[tid] = 0, s.part_ties[tid] = 0;
     __syncthreads();
     const int runs_each = (at.runs + parts - 1) / parts, part_length = runs_each * SAMPLE_RUN;

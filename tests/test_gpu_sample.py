@@ -131,6 +131,26 @@ def test_extreme_temperatures(t):
         check(z, torch.tensor([0.0, 0.2, 0.5, 0.7, 0.9, MOST_U], device="cuda:0"), t, k, p, m)
 
 
+def t32(x):
+    return float(torch.tensor(x, dtype=torch.float32))
+
+
+@pytest.mark.parametrize("t", [1.0, 2e37, 3e38])
+@pytest.mark.parametrize("vocab", [1500, 5003, 70000])
+def test_spreads_that_overflow(vocab, t):
+    """Many candidates whose distance to the top, or 32 temperatures, has no fp32 value."""
+    z = logits(4, vocab, "f32", 8)
+    z[1] = torch.where(z[1] > 0, 3e38, -3e38)
+    z[2] = z[2].sign() * 3.4e38 * torch.rand(vocab, device="cuda:0", generator=gen(3))
+    z[3, ::3] = -3.4e38
+    z = z.contiguous()
+    zc, u = z.double().cpu().numpy(), torch.tensor([0.0, 0.2, 0.5, MOST_U], device="cuda:0")
+    for k, p, m in ((0, 0.7, 0.0), (vocab - 300, 0.9, 0.0), (vocab // 2, 1.0, 0.0), (0, 0.7, 0.01), (0, 1.0, 0.001)):
+        token = ee.sample(z, u, temperature=t, top_k=k, top_p=p, min_p=m)
+        for i in range(4):
+            assert int(token[i]) == ref.choose(zc[i], float(u[i]), t32(t), k, t32(p), t32(m))[0], (i, k, p, m)
+
+
 def test_masks_and_rows_without_a_distribution():
     z = logits(9, 3000, "f32", 9)
     z[0] = -torch.inf
