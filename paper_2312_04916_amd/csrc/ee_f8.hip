@@ -269,8 +269,7 @@ __global__ __launch_bounds__(W * 64) void f8_stream_kernel(F8Product p, F8Shape 
 #pragma unroll
     for (int i = 0; i < MT; ++i) x_at[i] = p.workspace + (size_t)min(mt0 + i, m_tiles - 1) * steps * F8_FRAGMENT;
     const char* x_exponents = p.workspace + r.exponents();
-    auto load = [&](Step& b, int i) {
-        const int step = wave + i * W;
+    auto load = [&](Step& b, int step) {
         if constexpr (!RAW) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
@@ -315,7 +314,7 @@ __global__ __launch_bounds__(W * 64) void f8_stream_kernel(F8Product p, F8Shape 
     };
     Step ring[D];
 #pragma unroll
-    for (int d = 0; d < D; ++d) load(ring[d], min(d, max(mine - 1, 0)));  // (a wave without a step reads one of another's)
+    for (int d = 0; d < D; ++d) load(ring[d], min(wave + d * W, steps - 1));  // (what a wave has no step for is never multiplied)
     if constexpr (RAW) {
         quantise_rows<X, W * 64>(p, steps, dynamic);
         __syncthreads();
@@ -323,13 +322,13 @@ __global__ __launch_bounds__(W * 64) void f8_stream_kernel(F8Product p, F8Shape 
     int i = 0;
     for (; i + 2 * D <= mine; i += D) {
 #pragma unroll
-        for (int d = 0; d < D; ++d) multiply(ring[d], i + d), load(ring[d], i + D + d);
+        for (int d = 0; d < D; ++d) multiply(ring[d], i + d), load(ring[d], wave + (i + D + d) * W);
     }
     if (i + D <= mine) {
 #pragma unroll
         for (int d = 0; d < D; ++d) {
             multiply(ring[d], i + d);
-            if (i + D + d < mine) load(ring[d], i + D + d);
+            if (i + D + d < mine) load(ring[d], wave + (i + D + d) * W);
         }
         i += D;
     }

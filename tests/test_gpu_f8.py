@@ -1,9 +1,12 @@
 """Products with weights held in 8 bits on the GPU against plain forms in 64 bits (f8_reference.py): the format, and the products at
 the sizes, types and layouts where they can go wrong."""
+import ctypes as C
+
 import pytest
 import torch
 
 import paper_2312_04916_amd as ee
+from paper_2312_04916_amd import binding
 
 import f8_reference as ref
 
@@ -266,3 +269,23 @@ def test_two_streams_at_once():
     got = [(p.matmul(a, stream=s), q.matmul(b, stream=t)) for _ in range(20)]
     torch.cuda.synchronize()
     assert all(torch.equal(x, want[0]) and torch.equal(y, want[1]) for x, y in got)
+
+
+@pytest.mark.parametrize("m", [1, 6, 16, 24, 40, 64, 70, 200])
+@pytest.mark.parametrize("n,k,pair", [(48, 1, False), (64, 128, True), (272, 256, False), (1000, 256, True), (640, 513, False)])
+def test_buffers_that_end_where_their_memory_does(m, n, k, pair):
+    """Few steps along k, fewer than a workgroup has waves, with the packed weight, the workspace, x and y at the end of their allocations:
+    a read behind them would leave what is mapped."""
+    size, need = C.c_size_t(), C.c_size_t()
+    L = binding.lib()
+    assert L.ee_f8_bytes(n, k, pair, C.byref(size)) == 0 and L.ee_f8_matmul_bytes(m, n, k, pair, binding.EE_BF16, C.byref(need)) == 0
+    a, w, up = rand((m, k), "bf16", m), rand((n, k), "bf16", n), rand((n, k), "bf16", k)
+    memory = [torch.zeros(32 << 20, dtype=torch.uint8, device="cuda:0") for _ in range(4)]
+    at = [t.data_ptr() + (t.numel() - length) // 256 * 256 for t, length in zip(memory, (size.value, need.value, 2 * m * k, 2 * m * n))]
+    memory[2][at[2] - memory[2].data_ptr():][:2 * m * k].copy_(a.view(-1).view(torch.uint8))
+    stream = torch.cuda.current_stream().cuda_stream
+    assert L.ee_f8_pack(n, k, pair, binding.EE_BF16, w.data_ptr(), k, up.data_ptr() if pair else None, k, at[0], size.value, stream) == 0
+    assert L.ee_f8_matmul(m, n, k, pair, at[0], binding.EE_BF16, at[2], k, binding.EE_BF16, at[3], n, None, 0, at[1] if need.value else None, need.value, stream) == 0
+    torch.cuda.synchronize()
+    y = memory[3][at[3] - memory[3].data_ptr():][:2 * m * n].view(torch.bfloat16).view(m, n)
+    check(y, a, w, up=up if pair else None)
