@@ -43,7 +43,7 @@ struct F8Product {
     const void* add;
     int64_t add_row;
     char* workspace;
-    int x_vec, y_vec;  // rows of x can be moved 16 bytes at a time, rows of y and add so many elements (8, 4 or 1)
+    int y_vec;  // so many elements of y and add can be moved at a time (8, 4 or 1)
 };
 
 size_t f8_workspace(int m, int n, int k, int pair, int y_dtype);
