@@ -43,7 +43,6 @@ struct F8Product {
     const void* add;
     int64_t add_row;
     char* workspace;
-    int y_vec;  // so many elements of y and add can be moved at a time (8, 4 or 1)
 };
 
 size_t f8_workspace(int m, int n, int k, int pair, int y_dtype);

@@ -181,20 +181,22 @@ __device__ __forceinline__ void values_of(const i32x8& c, float unit, bf16x8 (&v
 
 __device__ __forceinline__ float silu(float g) { return g / (1.f + __expf(-g)); }
 
-// Four neighbouring results of one row: activation, rows that are added, rounding.
+// Four neighbouring results of one row: rows that are added, rounding to the nearest.  Moved at once wherever the row begins (one by one where rows
+// were not aligned, 1321 rows by 2603 x 1267 took 19.2 us for 14.0, with fp32 results 31.4 for 22.6).
 template <typename T>
 __device__ __forceinline__ void finish(const F8Product& p, int row, int col, f32x4 v) {
     if (row >= p.m || col >= p.n) return;
     T* y = (T*)p.y + row * p.y_row + col;
     const T* add = p.add ? (const T*)p.add + row * p.add_row + col : nullptr;
     typedef T T4 __attribute__((ext_vector_type(4)));
-    if (p.y_vec >= 4 && col + 3 < p.n) {
+    typedef T4 loose_T4 __attribute__((aligned(2)));
+    if (col + 3 < p.n) {
         if (add) {
-            const T4 a = *(const T4*)add;
+            const T4 a = *(const loose_T4*)add;
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] += (float)a[i];
         }
-        *(T4*)y = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+        *(loose_T4*)y = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -206,18 +208,19 @@ __device__ __forceinline__ void finish(const F8Product& p, int row, int col, f32
 template <typename T>
 __device__ __forceinline__ void finish8(const F8Product& p, int row, int col, f32x4 a, f32x4 b) {
     if (row >= p.m || col >= p.n) return;
-    if (p.y_vec < 8 || col + 7 >= p.n) {
+    if (col + 7 >= p.n) {
         finish<T>(p, row, col, a);
         finish<T>(p, row, col + 4, b);
         return;
     }
     typedef T T8 __attribute__((ext_vector_type(8)));
+    typedef T8 loose_T8 __attribute__((aligned(2)));
     if (p.add) {
-        const T8 v = *(const T8*)((const T*)p.add + row * p.add_row + col);
+        const T8 v = *(const loose_T8*)((const T*)p.add + row * p.add_row + col);
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] += (float)v[i], b[i] += (float)v[i + 4];
     }
-    *(T8*)((T*)p.y + row * p.y_row + col) = T8{(T)a[0], (T)a[1], (T)a[2], (T)a[3], (T)b[0], (T)b[1], (T)b[2], (T)b[3]};
+    *(loose_T8*)((T*)p.y + row * p.y_row + col) = T8{(T)a[0], (T)a[1], (T)a[2], (T)a[3], (T)b[0], (T)b[1], (T)b[2], (T)b[3]};
 }
 
 struct HeldRows {};  // they are in the workspace

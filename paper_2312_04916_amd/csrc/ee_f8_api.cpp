@@ -98,9 +98,6 @@ int ee_f8_matmul(int m, int n, int k, int pair, const void* dev_weight, int x_dt
     p.y = dev_y, p.y_dtype = y_dtype, p.y_row = y_row_stride;
     p.add = dev_add, p.add_row = add_row_stride;
     p.workspace = (char*)dev_workspace;
-    const uintptr_t y_at = (uintptr_t)dev_y | (uintptr_t)dev_add;
-    const int64_t y_rows = y_row_stride | (dev_add ? add_row_stride : 0);
-    p.y_vec = (y_at & (8 * ys - 1)) == 0 && y_rows % 8 == 0 ? 8 : (y_at & (4 * ys - 1)) == 0 && y_rows % 4 == 0 ? 4 : 1;
     return hip_status(launch_f8_matmul(p, (hipStream_t)stream));
 }
 
