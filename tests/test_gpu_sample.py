@@ -261,3 +261,16 @@ def test_two_streams_at_once():
     got = [(call(z, a, stream=s), call(w, b, stream=t)) for _ in range(20)]
     torch.cuda.synchronize()
     assert all(torch.equal(x, want[0]) and torch.equal(y, want[1]) for x, y in got)
+
+
+@pytest.mark.parametrize("rows,vocab", [(127, 16384), (200, 20011), (300, 50304), (700, 16399), (1100, 17000), (2500, 16500)])
+def test_a_row_does_not_depend_on_the_others(rows, vocab):
+    """However many workgroups a row of many candidates gets, which depends on the number of rows, its token stays the same."""
+    z = logits(rows, vocab, "bf16" if rows % 2 else "f32", rows, 1.5)
+    u, t, k, p, m = mixed(rows, vocab)
+    p = torch.where(torch.arange(rows, device="cuda:0") % 3 == 0, 0.97, p)
+    got = ee.sample(z, u, temperature=t, top_k=k, top_p=p, min_p=m)
+    few = [ee.sample(z[i:i + 9], u[i:i + 9], temperature=t[i:i + 9], top_k=k[i:i + 9], top_p=p[i:i + 9], min_p=m[i:i + 9]) for i in range(0, rows, 9)]
+    assert torch.equal(got, torch.cat(few)) and (got >= 0).all()
+    for i in range(0, rows, max(1, rows // 12)):
+        assert int(got[i]) == ref.choose(z[i].double().cpu().numpy(), float(u[i]), float(t[i]), int(k[i]), float(p[i]), float(m[i]))[0], i
