@@ -513,7 +513,7 @@ int ee_f8_pack(int n, int k, int pair, int dtype, const void* dev_w, int64_t w_r
                void* dev_weight, size_t weight_bytes, void* stream);
 /* The values that a packed weight holds (a non-zero pair and up != 0: of the up weight), [n][k] contiguous; exact in either dtype. */
 int ee_f8_unpack(int n, int k, int pair, int up, const void* dev_weight, int dtype, void* dev_w, void* stream);
-/* Workspace of a product of m rows. */
+/* Workspace of a product of m rows, 0 where it needs none (then dev_workspace may be NULL). */
 int ee_f8_matmul_bytes(int m, int n, int k, int pair, int y_dtype, size_t* workspace_bytes);
 /* x [m][k] in x_dtype, y [m][n] in y_dtype; dev_add: NULL, or rows [m][n] in y_dtype that are added before the rounding (y itself, or
  * apart from it).  y must not overlap x (EE_ERR_ARG).  Calls that overlap in time need workspaces of their own; its contents need

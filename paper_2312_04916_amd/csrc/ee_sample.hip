@@ -1077,8 +1077,8 @@ __global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, i
 // 79 with eight, 71 with sixteen; 512 rows 171 with one, 121 with four, 103 with eight.  Where every row has many candidates, 512 rows
 // take 248 with one, 292 with four, 342 with eight.  An element is noted in 16 bits in its part.)
 int sample_parts(int rows, int vocab) {
-    if (vocab < 16384) return 1;
-    return std::max(std::min(MOST_PARTS, std::max(1, 2048 / std::max(rows, 1))), (SampleRow(vocab).runs + 63) / 64);
+    if (vocab < 16384 || rows > 1024) return 1;
+    return std::max(std::min(MOST_PARTS, 2048 / std::max(rows, 1)), (SampleRow(vocab).runs + 63) / 64);
 }
 static size_t bins_at(int rows, int vocab) { return (SampleRow(vocab).bytes() * rows + 255) / 256 * 256; }
 

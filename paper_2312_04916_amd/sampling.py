@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes as C
 from numbers import Real
+from operator import index as index_of
 from typing import Optional, Union
 
 import torch
@@ -30,7 +31,9 @@ def _setting(v, off, dtype, rows: int, index: int, what: str):
     if v is None:
         return None, off
     if isinstance(v, Real):
-        return None, v
+        if dtype is torch.int32:  # (what has no room in it stays as large, or as wrong)
+            return None, max(min(index_of(v), 2 ** 31 - 1), -1)
+        return None, float(v)
     if v.dtype is not dtype or v.get_device() != index or v.shape != (rows,) or not v.is_contiguous():
         raise ValueError(f"{what}: {dtype}[{rows}] on cuda:{index}, contiguous, or a number")
     return v.data_ptr(), off

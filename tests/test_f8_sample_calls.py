@@ -4,6 +4,7 @@ import contextlib
 import ctypes as C
 import types
 
+import numpy as np
 import pytest
 import torch
 
@@ -188,3 +189,19 @@ def test_samples_go_to_the_logits_device(machine, monkeypatch):
         with pytest.raises(ValueError):
             sampling.sample(**{"logits": z, "u": u, **bad})
     assert calls == []
+
+
+def test_numbers_as_settings(machine, monkeypatch):
+    """Whatever kind of number: large top_k is not taken for another one, negative ones stay negative."""
+    current, calls, _ = machine
+    current[0] = 1
+    got = []
+    monkeypatch.setattr(sampling, "_fn", lambda *args: got.append(args[10:14]) or 0)
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **kw: empty(*a, **kw))
+    z, u = Fake(torch.zeros(2, 16)), Fake(torch.zeros(2))
+    for k, want in ((5, 5), (np.int64(7), 7), (2 ** 31, 2 ** 31 - 1), (2 ** 40 + 3, 2 ** 31 - 1), (-1, -1), (-2 ** 32, -1), (True, 1)):
+        sampling.sample(z, u, temperature=np.float32(0.5), top_k=k, top_p=1, min_p=np.float64(0.25))
+        assert got[-1] == (0.5, want, 1.0, 0.25) and [type(v) for v in got[-1]] == [float, int, float, float], got[-1]
+    with pytest.raises(TypeError):
+        sampling.sample(z, u, top_k=5.0)
