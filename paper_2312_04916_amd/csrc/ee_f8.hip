@@ -103,7 +103,8 @@ __device__ __forceinline__ i32x8 load_fragment(const char* f, int lane) {
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// A workgroup packs one block of 128 rows x 128 elements, a wave the 16 rows of a fragment.
+// A workgroup packs one block of 128 rows x 128 elements, a wave the 16 rows of a fragment.  Bound by memory: 50 304 x 4096 in bf16 are
+// packed in 115 us (618 MB, 5.4 TB/s).
 template <typename T>
 __global__ __launch_bounds__(512) void f8_pack_kernel(F8Shape s, const T* w, int64_t w_row, const T* up, int64_t up_row, char* weight) {
     __shared__ uint32_t s_top[8];
@@ -147,7 +148,8 @@ __global__ __launch_bounds__(64) void f8_unpack_kernel(F8Shape s, int up, const 
 }
 
 // ------------------------------------------------------------------------------------------------
-// rows into 8 bits
+// rows into 8 bits: a wave makes the fragment of 16 rows x 128 elements, a group's largest element by two lane swaps.  Bound by memory
+// where there is much (4096 x 4096 in bf16: 11.4 us, 4.4 TB/s), by launch and one load where there is little (61 x 11 008: 3.6).
 // ------------------------------------------------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(256) void f8_rows_kernel(F8Rows r, const T* x, int64_t x_row, int k, char* out) {
@@ -254,6 +256,8 @@ __device__ __forceinline__ void quantise_rows(const F8Product& p, int steps, cha
 // LDS in their order.  T: of the result; float: the held values go through the bf16 instructions, which keep every bit of a
 // product.  X: HeldRows, or the type in which sixteen rows at most come, which every workgroup then
 // quantises for itself, into LDS, while its first loads of the weight are on their way.
+// Bound by the weight's bytes: 1 row by 50 304 x 4096 with fp32 results 38.6 us (5.3 TB/s), 1 row by 6144 x 2048 5.2 us, launch included, 16 rows
+// by a pair of 11 008 x 4096 16.2 (5.6 TB/s), 61 rows by 4096 x 11 008 13.4 (3.4 TB/s: each step's x comes from L2 next to the weight).
 template <typename T, typename X, int MT, int NT, int W, int D>
 __global__ __launch_bounds__(W * 64) void f8_stream_kernel(F8Product p, F8Shape s, F8Rows r, int m_groups, int n_groups) {
     constexpr bool RAW = !__is_same(X, HeldRows);
@@ -383,7 +387,8 @@ __device__ __forceinline__ void wait_copies() {
 
 // Many rows: a workgroup of 2 x 2 waves computes 64 * MI rows of x by 4 * NI tiles of the weight, a wave 32 * MI by 2 * NI tiles in
 // instructions of 32 x 32 x 64.  Both operands come through LDS, copied past the registers in their own order, 64 elements of
-// the contraction at a time, four such stages in turn; the next stage's operands are read while the products of this one run.
+// the contraction at a time, four such stages in turn (three where two workgroups share a CU); the next stage's operands are read while
+// the products of this one run.  Bound by the matrix cores.
 constexpr int XCDS = 8, XCD_CUS = 32, CUS = XCDS * XCD_CUS;
 constexpr int tile_stages(int mi, int ni) { return mi * ni > 8 || mi * ni == 4 ? 4 : 3; }  // (two workgroups share a CU up to 8)
 constexpr int tile_stage_bytes(int mi, int ni) { return 4 * (mi + ni) * 1024 + 1024; }
@@ -559,7 +564,8 @@ __device__ __forceinline__ void f8_tile(const F8Product& p, const F8Shape& s, co
 
 // An XCD takes whole panels of the weight, all rows of one after the other, so that a panel comes from memory once.  What its CUs have
 // left over after whole rounds goes in tiles of half as many rows, if these are one round then (4096 rows by 22 016, 5.5 rounds for 6:
-// 345 -> 320 us).
+// 345 -> 340 us).  4096 rows by a pair of 11 008 x 4096: 335 us, 2.2 PFLOP/s, at which the chip lowers its clock; 1024 rows by
+// 12 288 x 4096: 49 us, 2.1 PFLOP/s.
 template <typename T, int MI, int NI>
 __global__ __launch_bounds__(256, MI * NI <= 8 ? 2 : 1) void f8_tile_kernel(F8Product p, F8Shape s, F8Rows r, int m_groups, int n_groups) {
     constexpr bool HALVES = MI == 4 && NI > 2;
