@@ -950,10 +950,10 @@ __global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, i
         __syncthreads();
     }
     const RowElements<T> row{z, 0, p.vocab, p.vec, top, least_z, g.per_t, left, parts, part_length};
-    const double reach = g.by_m ? -log((double)g.min_p) * (double)g.t : INFINITY;
     u64 whole = note->total;
+    bool intact = true;  // (the bins by distance)
     if (g.by_k) {
-        const bool intact = find_cut<true>(row, s.c, (u64)g.top_k, top, per_bin);
+        intact = find_cut<true>(row, s.c, (u64)g.top_k, top, per_bin);
         whole = s.c.cut.weight;
         if (g.by_p) {
             if (!whole) {  // all are kept
@@ -969,16 +969,34 @@ __global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, i
             }
         }
     }
-    if (g.by_p) find_cut<false>(row, s.c, max(share_of(g.top_p, whole, true), 1ull), top, per_bin);
+    if (g.by_p) intact = find_cut<false>(row, s.c, max(share_of(g.top_p, whole, true), 1ull), top, per_bin);
     __syncthreads();
-    const Cut cut = s.c.cut;
-    auto kept_weight = [&](float v, uint32_t key) { return key >= cut.key && (double)top - (double)v <= reach ? weight_of(v, top, g.per_t) : 0; };
-    const u64 tie = cut.key ? kept_weight(value_of(cut.key), cut.key) : 0;
+    Cut cut = s.c.cut;
+    bool listed = (g.by_k || g.by_p) && s.c.listed;
+    if (g.by_m) {  // cuts below the least key that is within reach
+        const double reach = -log((double)g.min_p) * (double)g.t;
+        auto within = [&](uint32_t key) { return (double)top - (double)value_of(key) <= reach; };
+        uint32_t key = KEY_NINF + 1, high = note->top_key;  // (which is within it)
+        while (key < high) {
+            const uint32_t mid = key + (high - key) / 2;
+            if (within(mid)) high = mid;
+            else key = mid + 1;
+        }
+        if (key - 1 > cut.key) {
+            cut = Cut{key - 1, 0, 1, 0};
+            const int bin = bin_of(cut.key);
+            __syncthreads();  // (the list of another bin is read no more)
+            listed = intact && s.c.bin_count[bin] <= LIST && row.list(s.c, bin);
+            __syncthreads();
+        }
+    }
+    auto kept_weight = [&](float v, uint32_t key) { return key > cut.key ? weight_of(v, top, g.per_t) : 0; };
+    const u64 tie = cut.key && cut.ties ? weight_of(value_of(cut.key), top, g.per_t) : 0;
     // The part: what is kept in the bins before the cut's is all of them, in the cut's bin those of the list that are.  Where there is no
-    // list, or min-p takes some of them (or nothing is cut), all of the row is one part.
+    // list (or nothing is cut), all of the row is one part.
     int first_run = 0, n_runs = at.runs, ties_before = 0;
     u64 target;
-    const bool by_parts = parts > 1 && tie && s.c.listed;
+    const bool by_parts = parts > 1 && cut.key && listed;
     if (by_parts) {
         if (tid < (int)s.c.n_list) {
             const int at_part = (int)s.c.list_index[tid] / part_length;

@@ -274,3 +274,23 @@ def test_a_row_does_not_depend_on_the_others(rows, vocab):
     assert torch.equal(got, torch.cat(few)) and (got >= 0).all()
     for i in range(0, rows, max(1, rows // 12)):
         assert int(got[i]) == ref.choose(z[i].double().cpu().numpy(), float(u[i]), float(t[i]), int(k[i]), float(p[i]), float(m[i]))[0], i
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [5003, 50304])
+def test_min_p_above_the_other_cuts(vocab, dtype):
+    """Many tokens within min-p's reach, which ends above where top-k and top-p cut, below it, exactly on a logit, at 0 and where all logits are
+    equal."""
+    z = logits(12, vocab, dtype, 21, 1.0)
+    z[3] = (z[3] * 4).round() / 4
+    z[4] = 0.0
+    z[5] = z[5].abs().clamp_min(2.0 ** -20)
+    z[5, :9] = 0.0
+    z[6] += 1000
+    z[7] = torch.where(z[7] > 0, 1.0, -1.0)
+    z[8] -= z[8].max() - 2.0
+    z[9, ::3] = -torch.inf
+    u = torch.rand(12, device="cuda:0", generator=gen(8))
+    for t, k, p, m in ((1.0, 0, 1.0, 1e-3), (1.0, 0, 1.0, math.exp(-2.0)), (1.0, 0, 0.999, 0.02), (2.0, vocab // 2, 0.99, 0.05), (0.5, vocab // 2, 1.0, 1e-4), (1.0, 0, 0.6, 1e-9),
+                       (1.0, vocab - 1, 1.0, 1.0), (30.0, 0, 0.9999, 0.8), (1.0, vocab // 3, 1.0, math.exp(-1.5))):
+        check(z, u, t, k, p, m)
