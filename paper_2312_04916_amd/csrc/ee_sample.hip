@@ -499,7 +499,8 @@ __device__ void token_of(const Settings& g, RowShared& s, S& c, const uint32_t (
         part += own.weight[j];
     }
     if (g.by_k || g.by_p) {
-        const float per_bin = fminf((ROW_THREADS - 1) / (top - least_z), 3e38f);
+        // (where there is no floor, what is 32 temperatures below the top and more shares the last bin)
+        const float spread = least_z > -INFINITY ? top - least_z : 32.f * g.t, per_bin = fminf((ROW_THREADS - 1) / spread, 3e38f);
         auto bin_of = [&](uint32_t key) { return bin_at(value_of(key), top, per_bin, ROW_THREADS); };
         empty_bins(c, tid);
         if (tid == 0) c.cut = nothing_cut();
