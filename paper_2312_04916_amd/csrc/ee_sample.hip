@@ -1093,13 +1093,15 @@ __global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, i
 
 }  // namespace
 
-// Rows with many candidates take sixteen workgroups each, or so many fewer that there are 2048.  (50 304 logits, ten sets of rows with settings
+// Rows with many candidates take sixteen workgroups each, or so many fewer that each has two runs and that there are 2048.  (50 304 logits, ten sets of rows with settings
 // of every kind: 1 row 34.1 us with eight of them, 29.5 with sixteen, 28.8 with 32; 64 rows 43.3, 39.2, 39.5.  256 rows 119 us with two,
 // 79 with eight, 71 with sixteen; 512 rows 171 with one, 121 with four, 103 with eight.  Where every row has many candidates, 512 rows
-// take 248 with one, 292 with four, 342 with eight.  An element is noted in 16 bits in its part.)
+// take 248 with one, 292 with four, 342 with eight.  16 rows of 9000 logits: 50.5 with one, 41.5 with five, 40.8 with nine; 64 of 4000 39.8
+// with one, 41.4 with two.  An element is noted in 16 bits in its part.)
 int sample_parts(int rows, int vocab) {
-    if (vocab < 16384 || rows > 1024) return 1;
-    return std::max(std::min(MOST_PARTS, 2048 / std::max(rows, 1)), (SampleRow(vocab).runs + 63) / 64);
+    const int runs = SampleRow(vocab).runs;
+    if (runs <= 4 || rows > 1024) return 1;
+    return std::max(std::min(std::min(MOST_PARTS, (runs + 1) / 2), 2048 / std::max(rows, 1)), (runs + 63) / 64);
 }
 static size_t bins_at(int rows, int vocab) { return (SampleRow(vocab).bytes() * rows + 255) / 256 * 256; }
 
