@@ -312,7 +312,7 @@ __device__ __forceinline__ void empty_bins(CutShared<NT, N_BINS>& s, int tid) {
 // The bins by distance are filled; false: they no longer are.
 template <bool BY_COUNT, int NT, int N_BINS, typename E>
 __device__ bool find_cut(const E& elements, CutShared<NT, N_BINS>& s, u64 limit, float top, float per_bin) {
-    constexpr int PER = N_BINS / NT;
+    constexpr int PER = N_BINS / NT, RANK = NT == 64 ? 64 : LIST;  // (n^2 / NT comparisons: 256 by one wave took 90 us)
     const int tid = threadIdx.x & (NT - 1), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     uint32_t lo = 0, hi = 0;
     int shift = -1;  // -1: bins by distance
@@ -358,7 +358,7 @@ __device__ bool find_cut(const E& elements, CutShared<NT, N_BINS>& s, u64 limit,
         base_count = s.base_count, base_weight = s.base_weight;
         const uint32_t in_bin = s.in_bin;
         uint32_t key_lo = 0xffffffffu, key_hi = 0;
-        if (!(shift < 0 && in_bin <= LIST && elements.list(s, bin))) {
+        if (!(shift < 0 && in_bin <= RANK && elements.list(s, bin))) {
             // (the bin's logits lie between these, and little else)
             const float far = fabsf(top) * 1e-6f + (float)(bin + 1) / per_bin * 1e-5f;
             // (per_bin is 0 where the spread is infinite: fmaxf and fminf drop what is then no number)
@@ -367,16 +367,16 @@ __device__ bool find_cut(const E& elements, CutShared<NT, N_BINS>& s, u64 limit,
             elements.each(z_lo, z_hi, [&](uint32_t key, int index, auto weight) {
                 if (bin_of(key) == bin) {
                     key_lo = min(key_lo, key), key_hi = max(key_hi, key);
-                    if (in_bin <= LIST) {
+                    if (in_bin <= RANK) {
                         const uint32_t at = atomicAdd(&s.n_list, 1u);
                         s.list[at] = key, s.list_index[at] = index, s.list_weight[at] = weight();
                     }
                 }
             });
         }
-        if (in_bin > LIST && key_lo <= key_hi) atomicMin(&s.lo, key_lo), atomicMax(&s.hi, key_hi);
+        if (in_bin > RANK && key_lo <= key_hi) atomicMin(&s.lo, key_lo), atomicMax(&s.hi, key_hi);
         meet<NT>();
-        if (in_bin <= LIST) {
+        if (in_bin <= RANK) {
             const int n = (int)s.n_list;
             if (tid == 0) s.listed = shift < 0;  // (whole)
             // so many lanes for each that all threads have work, 16 at most
@@ -499,8 +499,9 @@ __device__ void token_of(const Settings& g, RowShared& s, S& c, const uint32_t (
         part += own.weight[j];
     }
     if (g.by_k || g.by_p) {
-        // (where there is no floor, what is 32 temperatures below the top and more shares the last bin)
-        const float spread = least_z > -INFINITY ? top - least_z : 32.f * g.t, per_bin = fminf((ROW_THREADS - 1) / spread, 3e38f);
+        // (where there is no floor, what is 64 temperatures below the top and more shares the last bin, in which top-k may cut: with 32, 64 rows
+        // of 600 logits took 28.1 us for 16.8, 16 of 300 24.7 for 17.8)
+        const float spread = least_z > -INFINITY ? top - least_z : 64.f * g.t, per_bin = fminf((ROW_THREADS - 1) / spread, 3e38f);
         auto bin_of = [&](uint32_t key) { return bin_at(value_of(key), top, per_bin, ROW_THREADS); };
         empty_bins(c, tid);
         if (tid == 0) c.cut = nothing_cut();
