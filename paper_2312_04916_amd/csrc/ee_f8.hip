@@ -672,7 +672,13 @@ static void launch_product(const F8Product& p, const F8Shape& s, const F8Rows& r
     // Few tiles: one to a workgroup, so that there are as many as CUs (16 rows by 4096 x 11 008: 11.3 us, two 15); many: two, four.
     if (m_tiles == 1) return pair ? launch_stream<T, H, 1, 2, 4, 4>(p, s, r, st) : tiles >= 1024 ? launch_stream<T, H, 1, 2, 8, 2>(p, s, r, st) : launch_stream<T, H, 1, 1, 4, 4>(p, s, r, st);
     if (m_tiles == 2) return tiles <= 256 && !pair ? launch_stream<T, H, 2, 1, 8, 2>(p, s, r, st) : launch_stream<T, H, 2, 2, 4, 4>(p, s, r, st);
-    if (m_tiles <= 4) return tiles < 512 && !pair ? launch_stream<T, H, 4, 1, 4, 4>(p, s, r, st) : tiles < 512 ? launch_stream<T, H, 4, 2, 4, 2>(p, s, r, st) : launch_stream<T, H, 4, 4, 4, 2>(p, s, r, st);
+    if (m_tiles <= 4) {
+        // as many workgroups as CUs, or a few more (64 rows by 2048 x 5504: two groups of rows 7.5 us, one 10.1; 61 rows by 4096 x 11 008, weights from
+        // memory: one tile 18.7, two 21.6; 50 rows by 6656 x 6656: two 16.8, one 20.8)
+        if (tiles <= 128 && !pair) return launch_stream<T, H, 2, 1, 4, 4>(p, s, r, st);
+        if (tiles <= 256 && !pair) return launch_stream<T, H, 4, 1, 4, 4>(p, s, r, st);
+        return tiles <= 512 ? launch_stream<T, H, 4, 2, 4, 2>(p, s, r, st) : launch_stream<T, H, 4, 4, 4, 2>(p, s, r, st);
+    }
     switch (kind_of(p.m, tiles, pair)) {
         case 0: return launch_tile<T, 4, 4>(p, s, r, st);
         case 1: return launch_tile<T, 4, 3>(p, s, r, st);
