@@ -670,7 +670,9 @@ static void launch_product(const F8Product& p, const F8Shape& s, const F8Rows& r
         return tiles >= 1024 || pair ? launch_stream<T, float, 1, 2, 8, 2>(p, s, r, st) : launch_stream<T, float, 1, 1, 8, 2>(p, s, r, st);
     }
     // Few tiles: one to a workgroup, so that there are as many as CUs (16 rows by 4096 x 11 008: 11.3 us, two 15); many: two, four.
-    if (m_tiles == 1) return pair ? launch_stream<T, H, 1, 2, 4, 4>(p, s, r, st) : tiles >= 1024 ? launch_stream<T, H, 1, 2, 8, 2>(p, s, r, st) : launch_stream<T, H, 1, 1, 4, 4>(p, s, r, st);
+    // Up to 448 tiles, one each would leave many CUs a second workgroup (16 rows by 6656 x 6656, 416 tiles: two 10.6 us, one 12.0; by 7168 x 4096 8.0
+    // and 8.4; by 7680 x 4096, 480 tiles, 9.0 and 8.6).
+    if (m_tiles == 1) return pair || (tiles > 256 && tiles <= 448) ? launch_stream<T, H, 1, 2, 4, 4>(p, s, r, st) : tiles >= 1024 ? launch_stream<T, H, 1, 2, 8, 2>(p, s, r, st) : launch_stream<T, H, 1, 1, 4, 4>(p, s, r, st);
     if (m_tiles == 2) return tiles <= 256 && !pair ? launch_stream<T, H, 2, 1, 8, 2>(p, s, r, st) : launch_stream<T, H, 2, 2, 4, 4>(p, s, r, st);
     if (m_tiles <= 4) {
         // as many workgroups as CUs, or a few more (64 rows by 2048 x 5504: two groups of rows 7.5 us, one 10.1; 61 rows by 4096 x 11 008, weights from
