@@ -984,7 +984,7 @@ __global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, i
             if (within(mid)) high = mid;
             else key = mid + 1;
         }
-        if (key - 1 > cut.key) {
+        if (key > cut.key) {  // (also where the other cut's own elements are the first out of reach)
             cut = Cut{key - 1, 0, 1, 0};
             const int bin = bin_of(cut.key);
             __syncthreads();  // (the list of another bin is read no more)

@@ -1,0 +1,42 @@
+"""Choosing tokens on the GPU where one cut meets another (f8_reference.choose is the plain form in 64 bits)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_sample import DT, MOST_U, check, t32
+
+pytestmark = pytest.mark.gpu
+U = (0.0, 0.01, 0.02, 0.05, 0.3, 0.5, 0.9, 0.999, MOST_U)
+
+
+def groups(vocab, dtype, top, many, far, seed):
+    """Rows of nine equal arrangements, one for each of U: the largest logit once, 50 a quarter above `top - far`, `many` at it, the rest below."""
+    z = torch.full((vocab,), top - far - 1.0)
+    z[:1] = top
+    z[1:51] = top - far + 0.25
+    z[51:51 + many] = top - far
+    z = z[torch.randperm(vocab, generator=torch.Generator().manual_seed(seed))]
+    return z.expand(len(U), vocab).contiguous().cuda().to(DT[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("far", [0.5, 1.0, 1.5, 4.0])
+@pytest.mark.parametrize("vocab,many", [(3001, 1500), (4000, 2400), (5003, 2400), (5003, 200), (50304, 2400), (50304, 30000)])
+def test_min_p_ends_one_step_above_the_other_cut(vocab, many, far, dtype):
+    """min_p = exp(-far) in fp32, for which the group at that distance is out of reach and the next number above it is not, next to a top-k or a
+    top-p that cuts in that very group: 1500 or fewer candidates are cut by the row's own workgroup, more by several or by one."""
+    m = t32(math.exp(-far))
+    reach = -math.log(m)
+    top = 6.0
+    edge = np.float32(top - far)
+    assert top - float(edge) > reach >= top - float(np.nextafter(edge, np.float32(9.0)))
+    z, u = groups(vocab, dtype, top, many, far, vocab + many), torch.tensor(U, device="cuda:0")
+    k = 51 + many // 2
+    below = math.exp(-far - 1.0) * (vocab - 51 - many)
+    above, group = 1 + 50 * math.exp(0.25 - far), many * math.exp(-far)
+    p = (above + group / 2) / (above + group + below)
+    for kk, pp in ((k, 1.0), (0, p), (k, (above + group / 4) / (above + group / 2))):
+        token = check(z, u, 1.0, kk, pp, m)
+        assert (z[torch.arange(len(U)), token.long()] > top - far).all()
