@@ -258,7 +258,8 @@ struct CutShared {
 __device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
 __device__ __forceinline__ u64 of_lane(u64 v, int lane) { return (u64)of_lane((uint32_t)(v >> 32), lane) << 32 | of_lane((uint32_t)v, lane); }
 
-// Sums over the threads: exclusive prefix of each one's value, and the total.  `waves` is free again after the next meeting.
+// Sums over the threads: exclusive prefix of each one's value, and the total.  `waves` is still read here when a thread returns: it may be
+// written again behind the next meeting, not before.
 template <int NT, typename T>
 __device__ __forceinline__ T before_me(T v, T& total, T* waves) {
     const T in = wave_scan(v);
@@ -511,7 +512,10 @@ __device__ void token_of(const Settings& g, RowShared& s, S& c, const uint32_t (
         if (g.by_k) {
             const bool intact = find_cut<true>(own, c, (u64)g.top_k, top, per_bin);
             whole = c.cut.weight;
-            if (g.by_p && !whole) before_me<NT>(part, whole, c.sums);  // (all are kept)
+            if (g.by_p && !whole) {  // all are kept
+                before_me<NT>(part, whole, c.sums);
+                meet<NT>();  // (the waves' sums are written again by the next cut)
+            }
             if (g.by_p && !intact) {
                 meet<NT>();
                 empty_bins(c, tid);
@@ -956,19 +960,14 @@ __global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, i
     bool intact = true;  // (the bins by distance)
     if (g.by_k) {
         intact = find_cut<true>(row, s.c, (u64)g.top_k, top, per_bin);
+        // (with top-p it does cut: the floor is top-k's alone then, and the bins hold what is not below it, top_k tokens at least, or all of
+        // the row, the masked ones too)
         whole = s.c.cut.weight;
-        if (g.by_p) {
-            if (!whole) {  // all are kept
-                u64 w = 0;
-                row.each([&](uint32_t, int, auto weight) { w += weight(); });
-                before_me<NT>(w, whole, s.c.sums);
-            }
-            if (!intact) {
-                __syncthreads();
-                empty_bins(s.c, tid);
-                __syncthreads();
-                fill_bins(row, s.c, bin_of);
-            }
+        if (g.by_p && !intact) {
+            __syncthreads();
+            empty_bins(s.c, tid);
+            __syncthreads();
+            fill_bins(row, s.c, bin_of);
         }
     }
     if (g.by_p) intact = find_cut<false>(row, s.c, max(share_of(g.top_p, whole, true), 1ull), top, per_bin);

@@ -40,3 +40,22 @@ def test_min_p_ends_one_step_above_the_other_cut(vocab, many, far, dtype):
     for kk, pp in ((k, 1.0), (0, p), (k, (above + group / 4) / (above + group / 2))):
         token = check(z, u, 1.0, kk, pp, m)
         assert (z[torch.arange(len(U)), token.long()] > top - far).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("live", [3, 500, 520, 600, 1500, 2040, 2500, 3000])
+@pytest.mark.parametrize("vocab", [3100, 9000, 50304])
+def test_top_k_that_leaves_all_before_top_p(vocab, live, dtype):
+    """A mask leaves no more tokens than top_k, and top-p's share is of all of them: one wave, a workgroup, or the kernel for many candidates."""
+    g = torch.Generator().manual_seed(vocab + live)
+    rows = 12
+    z = torch.full((rows, vocab), -torch.inf)
+    for i in range(rows):
+        at = torch.randperm(vocab, generator=g)[:live]
+        z[i, at] = torch.randn(live, generator=g) * (0.2 + 0.3 * i)
+    z = z.cuda().to(DT[dtype])
+    u = torch.rand(rows, generator=g).cuda()
+    p = (0.05 + 0.94 * torch.rand(rows, generator=g)).cuda()
+    for k in (live, live + 1, min(vocab - 1, 2 * live), vocab - 1):
+        check(z, u, 0.9, k, p, 0.0)
+        check(z, u, 0.9, k, p, 0.02)
