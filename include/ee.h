@@ -531,9 +531,11 @@ int ee_f8_matmul(int m, int n, int k, int pair, const void* dev_weight, int x_dt
  * exp((z - z_max) / temperature).  Kept are the first top_k; of these the shortest run from the start whose weights reach top_p of
  * theirs, one token at least; of these the ones with z_max - z <= -ln(min_p) * temperature.  The token is the first one, by
  * index, at which the running sum of the kept weights exceeds u times their total.  Temperature 0: the first of the order.
- *   Weights are whole multiples of 2^-44 of the largest (where nothing is cut: of the largest of each run of 1024 tokens, whose sum is
- * then rounded to such a multiple) and their sums are exact, so that a row's token depends on nothing but the row and its settings:
- * not on the other rows or their number.
+ *   Weights are whole multiples of 2^-44 of the largest and their sums are exact, so that a row's token depends on nothing but the row and
+ * its settings: not on the other rows or their number.  The sum of all of a row's weights, of which u is the share where nothing is cut
+ * and top_p where top_k cuts nothing, keeps what so small a weight loses: it is formed from runs of 1024 tokens, whose weights are
+ * multiples of 2^-44 of the run's largest (by them the token is found in a run, where nothing is cut) and whose sums are then rounded to
+ * multiples of 2^-44 of the row's.
  *   dev_logprob [rows] (or NULL): the token's log-probability, z - log sum exp, under the logits as they are (temperature 1,
  * nothing cut); dev_confidence [rows] (or NULL): the largest probability under them, which is what the exit rule of Section 5.2
  * compares with its threshold.

@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2312_04916_amd as ee
 from test_gpu_sample import DT, MOST_U, check, t32
 
 pytestmark = pytest.mark.gpu
@@ -59,3 +60,21 @@ def test_top_k_that_leaves_all_before_top_p(vocab, live, dtype):
     for k in (live, live + 1, min(vocab - 1, 2 * live), vocab - 1):
         check(z, u, 0.9, k, p, 0.0)
         check(z, u, 0.9, k, p, 0.02)
+
+
+@pytest.mark.parametrize("vocab,n", [(4096, 2), (8192, 3000), (50304, 3000), (50304, 700)])
+def test_top_p_is_a_share_of_all_that_is_small_too(vocab, n):
+    """n tokens of weight 1 in front, and a tail of exp(-31.5) = 0.367 * 2^-44 each, which is nothing as a multiple of 2^-44 of the largest, but
+    not in all: half of the sum is a little more than n / 2 tokens, of which one more is kept.  With top_k (which takes one token of the
+    tail away) the sum is of what is kept and the tail is nothing."""
+    z = torch.full((2, vocab), -31.5, device="cuda:0")
+    z[:, :n] = 0.0
+    u = torch.full((2,), MOST_U, device="cuda:0")
+    total = n + (vocab - n) * math.exp(-31.5)
+    kept = math.floor(0.5 * total) + 1
+    assert kept == n // 2 + 1 and 0.5 * total - n // 2 > 2.0 ** -44 * 50
+    for dtype in DT.values():
+        assert ee.sample(z.to(dtype), u, top_p=0.5).tolist() == [kept - 1] * 2
+        assert ee.sample(z.to(dtype), u, top_p=0.5, min_p=0.5).tolist() == [kept - 1] * 2
+        assert ee.sample(z.to(dtype), u, top_p=0.5, top_k=vocab - 1).tolist() == [n // 2 - 1] * 2
+        assert ee.sample(z.to(dtype), u, top_p=0.5, top_k=vocab).tolist() == [kept - 1] * 2  # (top_k cuts nothing)
