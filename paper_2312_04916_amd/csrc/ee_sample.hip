@@ -4,6 +4,7 @@
 
 #include <algorithm>
 
+#include "ee_exp.h"
 #include "ee_lanes.h"
 #include "ee_launch.h"
 #include "ee_sample.h"
@@ -210,7 +211,7 @@ __global__ __launch_bounds__(256) void sample_runs_kernel(Sampling p, int each) 
             float part[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                part[j] = (__expf(v[j][0] - ref) + __expf(v[j][1] - ref)) + (__expf(v[j][2] - ref) + __expf(v[j][3] - ref));
+                part[j] = (exp_of(v[j][0] - ref) + exp_of(v[j][1] - ref)) + (exp_of(v[j][2] - ref) + exp_of(v[j][3] - ref));
             const float raw = wave_sum((part[0] + part[1]) + (part[2] + part[3]));
             if (lane == 0) ((float*)(out + at.raws()))[run_now] = raw;
         }
