@@ -506,7 +506,8 @@ int ee_kv4_attend(ee_kv4* c, int layer, const void* dev_q, int64_t q_row_stride,
  * next to the 1.7e-3 of its rounding, and never more than 7 * 2^-13 of sum |x w|.
  *
  * pair: two weights of n rows each, gate and up, packed side by side; y = silu(x Wgate^T) * (x Wup^T).
- * Sizes: 1 <= n <= 2^22, 1 <= k <= 2^18, 0 <= m <= 2^20.  Strides are of rows, in elements; the elements of a row are contiguous. */
+ * Sizes: 1 <= n <= 2^22, 1 <= k <= 2^18, 0 <= m <= 2^20.  Strides are of rows, in elements; the elements of a row are contiguous.
+ * A packed weight and a workspace begin at multiples of 256 bytes, apart from the ranges that rows span. */
 int ee_f8_bytes(int n, int k, int pair, size_t* weight_bytes);
 /* dtype: EE_F32 | EE_BF16, of dev_w [n][k] and, with pair, dev_up [n][k] (else NULL). */
 int ee_f8_pack(int n, int k, int pair, int dtype, const void* dev_w, int64_t w_row_stride, const void* dev_up, int64_t up_row_stride,
@@ -516,8 +517,10 @@ int ee_f8_unpack(int n, int k, int pair, int up, const void* dev_weight, int dty
 /* Workspace of a product of m rows, 0 where it needs none (then dev_workspace may be NULL). */
 int ee_f8_matmul_bytes(int m, int n, int k, int pair, int y_dtype, size_t* workspace_bytes);
 /* x [m][k] in x_dtype, y [m][n] in y_dtype; dev_add: NULL, or rows [m][n] in y_dtype that are added before the rounding (y itself, or
- * apart from it).  y must not overlap x (EE_ERR_ARG).  Calls that overlap in time need workspaces of their own; its contents need
- * not be kept between calls.  The bits of a row of y depend on m, not on the other rows' values. */
+ * apart from it).  y must not overlap x, the weight or other added rows (EE_ERR_ARG): rows of one stride, in bytes, may lie between one
+ * another (columns of one buffer), of others the ranges that they span must be apart.  A single row has no stride.  Calls that
+ * overlap in time need workspaces of their own; its contents need not be kept between calls.  The bits of a row of y depend on m,
+ * not on the other rows' values. */
 int ee_f8_matmul(int m, int n, int k, int pair, const void* dev_weight, int x_dtype, const void* dev_x, int64_t x_row_stride, int y_dtype,
                  void* dev_y, int64_t y_row_stride, const void* dev_add, int64_t add_row_stride, void* dev_workspace,
                  size_t workspace_bytes, void* stream);
@@ -543,7 +546,7 @@ int ee_f8_matmul(int m, int n, int k, int pair, const void* dev_weight, int x_dt
  * -inf, confidence 0. */
 int ee_sample_bytes(int rows, int vocab, size_t* workspace_bytes);
 /* Calls that overlap in time need workspaces of their own; its contents need not be kept between calls.  Results, workspace and what is
- * read must not overlap (EE_ERR_ARG). */
+ * read, with all of the range that the rows of logits span, must not overlap (EE_ERR_ARG). */
 int ee_sample(int rows, int vocab, int dtype, const void* dev_logits, int64_t row_stride, const float* dev_u, const float* dev_temperature,
               const int32_t* dev_top_k, const float* dev_top_p, const float* dev_min_p, float temperature, int32_t top_k, float top_p,
               float min_p, int32_t* dev_token, float* dev_logprob, float* dev_confidence, void* dev_workspace, size_t workspace_bytes,

@@ -1,4 +1,5 @@
-"""Products with weights held in 8 bits on the GPU, form by form: what fp32 results keep of silu."""
+"""Products with weights held in 8 bits on the GPU, form by form: what fp32 results keep of silu, rows of one
+buffer."""
 import pytest
 import torch
 
@@ -24,3 +25,27 @@ def test_silu_keeps_fp32(m):
     assert m < 16 or int((gate[fits] < -40).sum()) > m  # (five rows hold none)
     err = (y.double() - want).abs() / (want.abs() * 2.0 ** -24)
     assert float(err[fits].max()) <= 6.01, float(err[fits].max())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("m", [1, 2, 16, 40, 300, 2000])
+@pytest.mark.parametrize("n,k,apart", [(130, 200, 0), (64, 257, 5), (512, 128, 8)])
+def test_columns_of_one_buffer(m, n, k, apart, dtype):
+    """x, rows to add and the result side by side: the bits that buffers of their own give, and the other columns stay."""
+    g = torch.Generator(device="cuda:0").manual_seed(m + n)
+    w = ee.F8Weight(torch.randn(n, k, device="cuda:0", generator=g).to(dtype))
+    at = k + apart, k + apart + n + apart
+    b = torch.randn(m, at[1] + n + 3, device="cuda:0", generator=g).to(dtype)
+    x, add, y = b[:, :k], b[:, at[0]:at[0] + n], b[:, at[1]:at[1] + n]
+    before = b.clone()
+    want = w.matmul(x.contiguous(), add=add.contiguous())
+    assert w.matmul(x, add=add, out=y) is y and torch.equal(y, want)
+    before[:, at[1]:at[1] + n] = want
+    assert torch.equal(b, before)
+    # onto the added rows themselves
+    w.matmul(x, add=add, out=add)
+    before[:, at[0]:at[0] + n] = want
+    assert torch.equal(b, before)
+    if m > 1:
+        with pytest.raises(RuntimeError):
+            w.matmul(x, out=b[:, k - 1:k - 1 + n])
