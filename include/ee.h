@@ -525,6 +525,11 @@ int ee_f8_matmul(int m, int n, int k, int pair, const void* dev_weight, int x_dt
                  void* dev_y, int64_t y_row_stride, const void* dev_add, int64_t add_row_stride, void* dev_workspace,
                  size_t workspace_bytes, void* stream);
 
+/* Test hook, host only: the launch of a product of m >= 1 rows.  shape[0], [1] = rows of x and of the packed weight (a pair: of both) of a
+ * workgroup, [2] = its waves, [3] = 0 if the operands go straight into registers, 1 if the rows are quantised by the workgroups as
+ * well, 2 if both operands come through LDS (what is left after whole rounds of 256 rows by 192 or more may go in halves). */
+int ee_debug_f8_launch(int m, int n, int k, int pair, int32_t shape[4]);
+
 /* ---------------------------------------------------------------- choosing tokens
  *
  * One token per row of logits [rows][vocab] (dtype EE_F32 | EE_BF16, 1 <= vocab <= 2^18, rows contiguous inside), from random numbers that

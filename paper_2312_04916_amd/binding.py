@@ -25,7 +25,7 @@ EXPORTS = ["ee_strerror", "ee_last_hip_error", "ee_model_bytes", "ee_model_creat
            "ee_kv_cache_flush", "ee_kv_cache_free", "ee_debug_read_hidden", "ee_prefill", "ee_prefill_scored",
            "ee_decode_step", "ee_decode_step_static",
            "ee_kv4_bytes", "ee_kv4_create", "ee_kv4_free", "ee_kv4_get_arrays", "ee_kv4_plan", "ee_kv4_append", "ee_kv4_read", "ee_kv4_attend",
-           "ee_f8_bytes", "ee_f8_pack", "ee_f8_unpack", "ee_f8_matmul_bytes", "ee_f8_matmul", "ee_sample_bytes", "ee_sample"]
+           "ee_f8_bytes", "ee_f8_pack", "ee_f8_unpack", "ee_f8_matmul_bytes", "ee_f8_matmul", "ee_debug_f8_launch", "ee_sample_bytes", "ee_sample"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libee.so")
@@ -126,6 +126,7 @@ def lib():
         L.ee_f8_unpack.argtypes = [i32, i32, i32, i32, vp, i32, vp, vp]
         L.ee_f8_matmul_bytes.argtypes = [i32, i32, i32, i32, i32, C.POINTER(sz)]
         L.ee_f8_matmul.argtypes = [i32, i32, i32, i32, vp, i32, vp, i64, i32, vp, i64, vp, i64, vp, sz, vp]
+        L.ee_debug_f8_launch.argtypes = [i32, i32, i32, i32, i32p]
         f32 = C.c_float
         L.ee_sample_bytes.argtypes = [i32, i32, C.POINTER(sz)]
         L.ee_sample.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, f32, i32, f32, f32, vp, vp, vp, vp, sz, vp]
@@ -374,6 +375,13 @@ def gemm_route(cfg: ee_config, kernel: int, rows: int, prompt: bool = False, max
     r, w = C.c_int32(), C.c_int32()
     _chk(lib().ee_debug_gemm_route(C.byref(cfg), max_rows, max_seqs, kernel, rows, int(prompt), C.byref(r), C.byref(w)), "ee_debug_gemm_route")
     return r.value, w.value
+
+
+def f8_launch(m: int, n: int, k: int, pair: bool = False) -> Tuple[int, int, int, int]:
+    """ee_debug_f8_launch (host only) -> (rows of x and of the packed weight of a workgroup, its waves, 0 registers | 1 own rows | 2 LDS)."""
+    s = (C.c_int32 * 4)()
+    _chk(lib().ee_debug_f8_launch(m, n, k, int(pair), s), "ee_debug_f8_launch")
+    return tuple(s)
 
 
 def rows_launch(cfg: ee_config, kernel: int, rows: int, max_rows: int = EE_MAX_ROWS, max_seqs: int = EE_MAX_SEQS) -> Tuple[int, int, int, int]:

@@ -45,6 +45,7 @@ struct F8Product {
     char* workspace;
 };
 
+void f8_launch_shape(int m, int n, int k, int pair, int32_t shape[4]);
 size_t f8_workspace(int m, int n, int k, int pair, int y_dtype);
 hipError_t launch_f8_pack(const F8Shape& s, int dtype, const void* w, int64_t w_row, const void* up, int64_t up_row, char* weight, hipStream_t st);
 hipError_t launch_f8_unpack(const F8Shape& s, int up, const char* weight, int dtype, void* w, hipStream_t st);

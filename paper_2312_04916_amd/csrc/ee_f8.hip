@@ -664,29 +664,32 @@ static int kind_of(int m, int tiles, bool pair) {
     return best;
 }
 
-template <typename T>
-static void launch_product(const F8Product& p, const F8Shape& s, const F8Rows& r, hipStream_t st) {
-    const int m_tiles = (p.m + 15) / 16, tiles = s.tiles();
-    const bool pair = p.pair;
-    typedef HeldRows H;
-    if (!quantised_first(p.m, s.steps())) {
-        // (all widths of the framework's workloads, 1 row: within 0.4 us of the best of eight kinds)
-        if (p.x_dtype == EE_BF16) return tiles >= 1024 || pair ? launch_stream<T, __bf16, 1, 2, 8, 2>(p, s, r, st) : launch_stream<T, __bf16, 1, 1, 8, 2>(p, s, r, st);
-        return tiles >= 1024 || pair ? launch_stream<T, float, 1, 2, 8, 2>(p, s, r, st) : launch_stream<T, float, 1, 1, 8, 2>(p, s, r, st);
-    }
+// The launch of a product: one of the kinds above, or of what few rows take.
+enum { OWN_2 = N_TILES + N_STREAMS, OWN_1, ROWS16_2, ROWS16_2_WIDE, ROWS16_1, ROWS32_1_WIDE, ROWS32_2, ROWS32_1 };
+static int route_of(int m, int tiles, int steps, bool pair) {
+    const int m_tiles = (m + 15) / 16;
+    // (all widths of the framework's workloads, 1 row: within 0.4 us of the best of eight kinds)
+    if (!quantised_first(m, steps)) return tiles >= 1024 || pair ? OWN_2 : OWN_1;
     // Few tiles: one to a workgroup, so that there are as many as CUs (16 rows by 4096 x 11 008: 11.3 us, two 15); many: two, four.
     // Up to 448 tiles, one each would leave many CUs a second workgroup (16 rows by 6656 x 6656, 416 tiles: two 10.6 us, one 12.0; by 7168 x 4096 8.0
     // and 8.4; by 7680 x 4096, 480 tiles, 9.0 and 8.6).
-    if (m_tiles == 1) return pair || (tiles > 256 && tiles <= 448) ? launch_stream<T, H, 1, 2, 4, 4>(p, s, r, st) : tiles >= 1024 ? launch_stream<T, H, 1, 2, 8, 2>(p, s, r, st) : launch_stream<T, H, 1, 1, 4, 4>(p, s, r, st);
-    if (m_tiles == 2) return tiles <= 256 && !pair ? launch_stream<T, H, 2, 1, 8, 2>(p, s, r, st) : launch_stream<T, H, 2, 2, 4, 4>(p, s, r, st);
+    if (m_tiles == 1) return pair || (tiles > 256 && tiles <= 448) ? ROWS16_2 : tiles >= 1024 ? ROWS16_2_WIDE : ROWS16_1;
+    if (m_tiles == 2) return tiles <= 256 && !pair ? ROWS32_1_WIDE : ROWS32_2;
     if (m_tiles <= 4) {
         // as many workgroups as CUs, or a few more (64 rows by 2048 x 5504: two groups of rows 7.5 us, one 10.1; 61 rows by 4096 x 11 008, weights from
         // memory: one tile 18.7, two 21.6; 50 rows by 6656 x 6656: two 16.8, one 20.8)
-        if (tiles <= 128 && !pair) return launch_stream<T, H, 2, 1, 4, 4>(p, s, r, st);
-        if (tiles <= 256 && !pair) return launch_stream<T, H, 4, 1, 4, 4>(p, s, r, st);
-        return tiles <= 512 ? launch_stream<T, H, 4, 2, 4, 2>(p, s, r, st) : launch_stream<T, H, 4, 4, 4, 2>(p, s, r, st);
+        if (tiles <= 128 && !pair) return ROWS32_1;
+        if (tiles <= 256 && !pair) return N_TILES + 3;
+        return N_TILES + (tiles <= 512 ? 2 : 1);
     }
-    switch (kind_of(p.m, tiles, pair)) {
+    return kind_of(m, tiles, pair);
+}
+
+template <typename T>
+static void launch_product(const F8Product& p, const F8Shape& s, const F8Rows& r, hipStream_t st) {
+    typedef HeldRows H;
+    const bool bf16 = p.x_dtype == EE_BF16;
+    switch (route_of(p.m, s.tiles(), s.steps(), p.pair)) {
         case 0: return launch_tile<T, 4, 4>(p, s, r, st);
         case 1: return launch_tile<T, 4, 3>(p, s, r, st);
         case 2: return launch_tile<T, 3, 3>(p, s, r, st);
@@ -696,8 +699,28 @@ static void launch_product(const F8Product& p, const F8Shape& s, const F8Rows& r
         case 6: return launch_stream<T, H, 8, 4, 4, 2>(p, s, r, st);
         case 7: return launch_stream<T, H, 4, 4, 4, 2>(p, s, r, st);
         case 8: return launch_stream<T, H, 4, 2, 4, 2>(p, s, r, st);
-        default: return launch_stream<T, H, 4, 1, 4, 4>(p, s, r, st);
+        case 9: return launch_stream<T, H, 4, 1, 4, 4>(p, s, r, st);
+        case OWN_2: return bf16 ? launch_stream<T, __bf16, 1, 2, 8, 2>(p, s, r, st) : launch_stream<T, float, 1, 2, 8, 2>(p, s, r, st);
+        case OWN_1: return bf16 ? launch_stream<T, __bf16, 1, 1, 8, 2>(p, s, r, st) : launch_stream<T, float, 1, 1, 8, 2>(p, s, r, st);
+        case ROWS16_2: return launch_stream<T, H, 1, 2, 4, 4>(p, s, r, st);
+        case ROWS16_2_WIDE: return launch_stream<T, H, 1, 2, 8, 2>(p, s, r, st);
+        case ROWS16_1: return launch_stream<T, H, 1, 1, 4, 4>(p, s, r, st);
+        case ROWS32_1_WIDE: return launch_stream<T, H, 2, 1, 8, 2>(p, s, r, st);
+        case ROWS32_2: return launch_stream<T, H, 2, 2, 4, 4>(p, s, r, st);
+        default: return launch_stream<T, H, 2, 1, 4, 4>(p, s, r, st);  // ROWS32_1
     }
+}
+
+void f8_launch_shape(int m, int n, int k, int pair, int32_t shape[4]) {
+    static const int FEW[][3] = {{16, 32, 8}, {16, 16, 8}, {16, 32, 4}, {16, 32, 8}, {16, 16, 4}, {32, 16, 8}, {32, 32, 4}, {32, 16, 4}};
+    const F8Shape s{n, k, pair};
+    const int kind = route_of(m, s.tiles(), s.steps(), pair);
+    const Kind& many = kind < N_TILES ? TILES[kind] : STREAMS[std::min(kind - N_TILES, N_STREAMS - 1)];
+    const bool few = kind >= N_TILES + N_STREAMS;
+    shape[0] = few ? FEW[kind - OWN_2][0] : many.m;
+    shape[1] = few ? FEW[kind - OWN_2][1] : many.n;
+    shape[2] = few ? FEW[kind - OWN_2][2] : 4;
+    shape[3] = kind < N_TILES ? 2 : kind == OWN_1 || kind == OWN_2 ? 1 : 0;
 }
 
 hipError_t launch_f8_matmul(const F8Product& p, hipStream_t st) {

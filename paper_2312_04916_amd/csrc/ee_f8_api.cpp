@@ -80,6 +80,14 @@ int ee_f8_matmul_bytes(int m, int n, int k, int pair, int y_dtype, size_t* works
     return EE_OK;
 }
 
+int ee_debug_f8_launch(int m, int n, int k, int pair, int32_t shape[4]) {
+    if (!shape || m < 1 || m > (1 << 20)) return EE_ERR_ARG;
+    const int rc = check_shape(n, k);
+    if (rc != EE_OK) return rc;
+    f8_launch_shape(m, n, k, pair != 0, shape);
+    return EE_OK;
+}
+
 int ee_f8_matmul(int m, int n, int k, int pair, const void* dev_weight, int x_dtype, const void* dev_x, int64_t x_row_stride, int y_dtype,
                  void* dev_y, int64_t y_row_stride, const void* dev_add, int64_t add_row_stride, void* dev_workspace,
                  size_t workspace_bytes, void* stream) {
