@@ -25,7 +25,7 @@ EXPORTS = ["ee_strerror", "ee_last_hip_error", "ee_model_bytes", "ee_model_creat
            "ee_kv_cache_flush", "ee_kv_cache_free", "ee_debug_read_hidden", "ee_prefill", "ee_prefill_scored",
            "ee_decode_step", "ee_decode_step_static",
            "ee_kv4_bytes", "ee_kv4_create", "ee_kv4_free", "ee_kv4_get_arrays", "ee_kv4_plan", "ee_kv4_append", "ee_kv4_read", "ee_kv4_attend",
-           "ee_f8_bytes", "ee_f8_pack", "ee_f8_unpack", "ee_f8_matmul_bytes", "ee_f8_matmul", "ee_debug_f8_launch", "ee_sample_bytes", "ee_sample"]
+           "ee_f8_bytes", "ee_f8_pack", "ee_f8_unpack", "ee_f8_matmul_bytes", "ee_f8_matmul", "ee_debug_f8_launch", "ee_sample_bytes", "ee_sample_uncut_bytes", "ee_sample"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libee.so")
@@ -129,6 +129,7 @@ def lib():
         L.ee_debug_f8_launch.argtypes = [i32, i32, i32, i32, i32p]
         f32 = C.c_float
         L.ee_sample_bytes.argtypes = [i32, i32, C.POINTER(sz)]
+        L.ee_sample_uncut_bytes.argtypes = [i32, i32, C.POINTER(sz)]
         L.ee_sample.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, f32, i32, f32, f32, vp, vp, vp, vp, sz, vp]
         _lib = L
     return _lib

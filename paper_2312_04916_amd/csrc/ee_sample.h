@@ -21,6 +21,8 @@ struct Sampling {
     float *logprob, *confidence;
     char* workspace;
     int vec;  // rows can be read four elements at a time
+    // whether the settings can cut anything, as far as the host knows
+    bool cuts() const { return top_k || top_p || min_p || (one_top_k > 0 && one_top_k < vocab) || one_top_p < 1.f || one_min_p > 0.f; }
 };
 
 // The workspace of a row.  The first kernel leaves, by index alone, the largest logit of each run of 64 tokens, and of each run of 1024 the
@@ -42,12 +44,12 @@ struct SampleRow {
     constexpr size_t note() const { return (raws() + (size_t)runs * 4 + 15) / 16 * 16; }
     constexpr size_t bytes() const { return note() + (sizeof(SampleNote) + 15) / 16 * 16; }
 };
-// For the third kernel, for each row: a weight and a count for each bin, to which its workgroups add; and what each of these leaves, for
+// For the third kernel, for each row that several of its workgroups share: a weight and a count for each bin, to which they add; and what each of these leaves, for
 // each bin a weight and where its elements begin, and the part's elements.
 constexpr size_t SAMPLE_ROW_BINS = (size_t)SAMPLE_BINS * 12;
 constexpr size_t sample_part_bytes(int part_length) { return (size_t)SAMPLE_BINS * 12 + 16 + (size_t)part_length * 2; }
 int sample_parts(int rows, int vocab);
-size_t sample_workspace(int rows, int vocab);
+size_t sample_workspace(int rows, int vocab, bool cuts);
 
 hipError_t launch_sample(const Sampling& p, hipStream_t st);
 

@@ -565,7 +565,7 @@ __device__ void token_of(const Settings& g, RowShared& s, S& c, const uint32_t (
 // They are few in most rows: read from the runs that have any, in the order of their indices, and held by one wave, or by all if they are
 // more than 512: a wave alone needs no barriers (up to 512 of them: 2 us behind the loads, all eight waves 5).
 template <typename T>
-__global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, char* shared_bins) {
+__global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, int third, char* shared_bins) {
     __shared__ RowShared s;
     constexpr int NT = ROW_THREADS;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x;
@@ -700,7 +700,7 @@ __global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, cha
         __syncthreads();
         // Tokens that lie anywhere leave exp(-n / chunks) of the runs without one: where this says that they are many more than can be
         // held, they are not looked for.
-        bool wide = shared_bins && (float)n_some > (float)n_chunks * (1.f - __expf(-1.25f * CANDIDATES / (float)n_chunks));
+        bool wide = third && (float)n_some > (float)n_chunks * (1.f - __expf(-1.25f * CANDIDATES / (float)n_chunks));
         uint32_t n = 0;
         uint32_t from[ROW_WAVES];
         if (!wide) {
@@ -765,10 +765,12 @@ __global__ __launch_bounds__(ROW_THREADS) void sample_row_kernel(Sampling p, cha
         }
         if (wide) {
             // (not without a third kernel: the host launches one wherever a row can have as many)
-            if (!shared_bins) return;
-            u64* weights = (u64*)(shared_bins + (size_t)r * SAMPLE_ROW_BINS);
-            uint32_t* counts = (uint32_t*)(weights + SAMPLE_BINS);
-            for (int i = tid; i < SAMPLE_BINS; i += NT) weights[i] = 0, counts[i] = 0;
+            if (!third) return;
+            if (shared_bins) {
+                u64* weights = (u64*)(shared_bins + (size_t)r * SAMPLE_ROW_BINS);
+                uint32_t* counts = (uint32_t*)(weights + SAMPLE_BINS);
+                for (int i = tid; i < SAMPLE_BINS; i += NT) weights[i] = 0, counts[i] = 0;
+            }
             if (tid == 0) {
                 note->top_key = top_key, note->least = least, note->arrived = 0, note->total = total, note->raw = raw;
                 note->log_raw = scores ? log(raw) : 0.0;
@@ -1106,10 +1108,13 @@ int sample_parts(int rows, int vocab) {
 }
 static size_t bins_at(int rows, int vocab) { return (SampleRow(vocab).bytes() * rows + 255) / 256 * 256; }
 
-size_t sample_workspace(int rows, int vocab) {
-    const int parts = sample_parts(rows, vocab), runs = SampleRow(vocab).runs;
-    const size_t shared = parts > 1 ? sample_part_bytes((runs + parts - 1) / parts * SAMPLE_RUN) * parts * rows : 0;
-    return bins_at(rows, vocab) + SAMPLE_ROW_BINS * rows + shared;
+// Whether rows may have more candidates than the second kernel takes.
+static bool third_kernel(int vocab, bool cuts) { return cuts && vocab > WAVE_CANDIDATES; }
+
+size_t sample_workspace(int rows, int vocab, bool cuts) {
+    const int parts = third_kernel(vocab, cuts) ? sample_parts(rows, vocab) : 1, runs = SampleRow(vocab).runs;
+    const size_t shared = parts > 1 ? SAMPLE_ROW_BINS + sample_part_bytes((runs + parts - 1) / parts * SAMPLE_RUN) * parts : 0;
+    return bins_at(rows, vocab) + shared * rows;
 }
 
 template <typename T>
@@ -1118,13 +1123,11 @@ static void launch_typed(const Sampling& p, hipStream_t st) {
     // as many waves as the chip holds at once, or so many fewer that all have the same number of runs
     const int64_t runs = (int64_t)p.rows * at.runs, each = (runs + 8191) / 8192, waves = (runs + each - 1) / each;
     EE_LAUNCH(sample_runs_kernel<T>, dim3((int)((waves + 3) / 4)), dim3(256), st, p, (int)each);
-    // what the host knows of the settings and sizes may rule out rows with many candidates
-    const bool cuts = p.top_k || p.top_p || p.min_p || (p.one_top_k > 0 && p.one_top_k < p.vocab) || p.one_top_p < 1.f || p.one_min_p > 0.f;
-    const bool wide = cuts && p.vocab > WAVE_CANDIDATES;
-    char* bins = p.workspace + bins_at(p.rows, p.vocab);
-    EE_LAUNCH(sample_row_kernel<T>, dim3(p.rows), dim3(ROW_THREADS), st, p, wide ? bins : nullptr);
-    if (!wide) return;
+    const bool third = third_kernel(p.vocab, p.cuts());
     const int parts = sample_parts(p.rows, p.vocab);
+    char* bins = p.workspace + bins_at(p.rows, p.vocab);
+    EE_LAUNCH(sample_row_kernel<T>, dim3(p.rows), dim3(ROW_THREADS), st, p, third, third && parts > 1 ? bins : nullptr);
+    if (!third) return;
     EE_LAUNCH(sample_wide_kernel<T>, dim3(p.rows * parts), dim3(WIDE_THREADS), st, p, parts, bins, bins + SAMPLE_ROW_BINS * p.rows);
 }
 

@@ -6,12 +6,15 @@ using namespace ee;
 
 extern "C" {
 
-int ee_sample_bytes(int rows, int vocab, size_t* workspace_bytes) {
+static int workspace_of(int rows, int vocab, bool cuts, size_t* workspace_bytes) {
     if (!workspace_bytes || rows < 0 || rows > (1 << 20)) return EE_ERR_ARG;
     if (vocab < 1 || vocab > (1 << 18)) return EE_ERR_CONFIG;
-    *workspace_bytes = sample_workspace(rows, vocab);
+    *workspace_bytes = sample_workspace(rows, vocab, cuts);
     return EE_OK;
 }
+
+int ee_sample_bytes(int rows, int vocab, size_t* workspace_bytes) { return workspace_of(rows, vocab, true, workspace_bytes); }
+int ee_sample_uncut_bytes(int rows, int vocab, size_t* workspace_bytes) { return workspace_of(rows, vocab, false, workspace_bytes); }
 
 int ee_sample(int rows, int vocab, int dtype, const void* dev_logits, int64_t row_stride, const float* dev_u, const float* dev_temperature,
                          const int32_t* dev_top_k, const float* dev_top_p, const float* dev_min_p, float temperature, int32_t top_k, float top_p,
@@ -28,7 +31,15 @@ int ee_sample(int rows, int vocab, int dtype, const void* dev_logits, int64_t ro
          (uintptr_t)dev_logprob | (uintptr_t)dev_confidence) & 3)
         return EE_ERR_ARG;
     if (!dev_workspace || (uintptr_t)dev_workspace & 255) return EE_ERR_ARG;
-    const size_t need = sample_workspace(rows, vocab);
+    Sampling p;
+    p.rows = rows, p.vocab = vocab, p.dtype = dtype;
+    p.logits = dev_logits, p.row_stride = row_stride;
+    p.u = dev_u, p.temperature = dev_temperature, p.top_k = dev_top_k, p.top_p = dev_top_p, p.min_p = dev_min_p;
+    p.one_temperature = temperature, p.one_top_k = top_k, p.one_top_p = top_p, p.one_min_p = min_p;
+    p.token = dev_token, p.logprob = dev_logprob, p.confidence = dev_confidence;
+    p.workspace = (char*)dev_workspace;
+    p.vec = ((uintptr_t)dev_logits & (4 * es - 1)) == 0 && row_stride % 4 == 0;
+    const size_t need = sample_workspace(rows, vocab, p.cuts());
     if (workspace_bytes < need) return EE_ERR_NOMEM;
     // rows are read while others' results are already written
     const int64_t span = (int64_t)(rows - 1) * row_stride * es;
@@ -48,14 +59,6 @@ int ee_sample(int rows, int vocab, int dtype, const void* dev_logits, int64_t ro
         for (int j = 0; j < i; ++j)
             if (out[j] && meet(out[i], (uintptr_t)out[j], (uintptr_t)out[j] + bytes, bytes)) return EE_ERR_ARG;
     }
-    Sampling p;
-    p.rows = rows, p.vocab = vocab, p.dtype = dtype;
-    p.logits = dev_logits, p.row_stride = row_stride;
-    p.u = dev_u, p.temperature = dev_temperature, p.top_k = dev_top_k, p.top_p = dev_top_p, p.min_p = dev_min_p;
-    p.one_temperature = temperature, p.one_top_k = top_k, p.one_top_p = top_p, p.one_min_p = min_p;
-    p.token = dev_token, p.logprob = dev_logprob, p.confidence = dev_confidence;
-    p.workspace = (char*)dev_workspace;
-    p.vec = ((uintptr_t)dev_logits & (4 * es - 1)) == 0 && row_stride % 4 == 0;
     const hipError_t e = launch_sample(p, (hipStream_t)stream);
     return e == hipSuccess ? EE_OK : note_hip_error((int)e);
 }

@@ -15,14 +15,15 @@ _CODES = {torch.bfloat16: EE_BF16, torch.float32: EE_F32}
 _fn, _sizes = None, {}
 
 
-def _workspace_bytes(rows: int, vocab: int) -> int:
-    size = _sizes.get((rows, vocab))
+def _workspace_bytes(rows: int, vocab: int, cuts: bool) -> int:
+    size = _sizes.get((rows, vocab, cuts))
     if size is None:
         s = C.c_size_t()
-        _chk(lib().ee_sample_bytes(rows, vocab, C.byref(s)), "ee_sample_bytes")
+        query = "ee_sample_bytes" if cuts else "ee_sample_uncut_bytes"
+        _chk(getattr(lib(), query)(rows, vocab, C.byref(s)), query)
         if len(_sizes) >= 4096:
             _sizes.clear()
-        size = _sizes[(rows, vocab)] = s.value
+        size = _sizes[(rows, vocab, cuts)] = s.value
     return size
 
 
@@ -81,7 +82,8 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Union[None, float
     lp, cf = (empty(torch.float32), empty(torch.float32)) if scores else (None, None)
     if _fn is None:
         _fn = lib().ee_sample
-    size = _workspace_bytes(rows, vocab)
+    # (settings that cut nothing, as numbers)
+    size = _workspace_bytes(rows, vocab, not (kp is pp is mp is None and (k == 0 or k >= vocab) and p == 1.0 and m == 0.0))
     work = empty(torch.uint8, size)
     code = _fn(rows, vocab, _CODES[logits.dtype], logits.data_ptr(), logits.stride(0), u.data_ptr(), tp, kp, pp, mp, t, k, p, m, out.data_ptr(),
                lp.data_ptr() if scores else None, cf.data_ptr() if scores else None,
