@@ -550,7 +550,7 @@ int ee_debug_f8_launch(int m, int n, int k, int pair, int32_t shape[4]);
  *   A row without a distribution (nothing above -inf, a NaN, a +inf, or a setting or u out of range): token -1, log-probability
  * -inf, confidence 0. */
 int ee_sample_bytes(int rows, int vocab, size_t* workspace_bytes);
-/* The same for calls whose settings, all given as numbers, cut nothing (top_k 0 or at least vocab, top_p 1, min_p 0): some 130 bytes for each
+/* The same for calls whose settings, all given as numbers, cut nothing (top_k 0 or at least vocab, top_p 1, min_p 0): 77 to 128 bytes for each
  * 1024 tokens of a row.  Where rows may be cut, up to 1024 rows of more than 4096 tokens are shared by several workgroups, whose notes
  * take 2 bytes a token and 36 to 240 KB a row more. */
 int ee_sample_uncut_bytes(int rows, int vocab, size_t* workspace_bytes);

@@ -134,7 +134,9 @@ struct Settings {
     __device__ __forceinline__ bool whole_sum() const { return !bad && !greedy && !by_k && (by_p || !by_m); }
 };
 
-// Four neighbouring elements, -inf behind the row's end
+// Four neighbouring elements, -inf behind the row's end.  (Each lane branches between one load and four: the compiler puts a wait for all loads
+// before the next one of the other arm, so that a wave has one of these on its way, however many are asked for ahead.  Rows that
+// are not aligned are read element by element: 512 rows of 50 257 logits in bf16, temperature alone, take 56 us for 41.)
 template <typename T>
 __device__ __forceinline__ void load4(const T* z, int i, int n, bool vec, float (&v)[4]) {
     if (vec && i + 4 <= n) {
@@ -154,7 +156,8 @@ __device__ __forceinline__ void load4(const T* z, int i, int n, bool vec, float 
 
 // ------------------------------------------------------------------------------------------------
 // the pass over the logits: a wave takes `each` runs of 1024 tokens, one after the other.  512 rows of 50 304 logits in fp32 take 40 us
-// where all weights are summed up, by its 64-bit arithmetic (16 instructions a logit), and 22 where they are not, by memory (4.7 TB/s).
+// where all weights are summed up and 22 where they are not (4.7 TB/s): the 64-bit arithmetic (16 instructions a logit, 18 us) adds to the
+// time of the loads, which do not run ahead of it (load4).
 // ------------------------------------------------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(256) void sample_runs_kernel(Sampling p, int each) {
@@ -436,7 +439,7 @@ constexpr int ROW_THREADS = 512, ROW_WAVES = ROW_THREADS / 64;
 constexpr int CANDIDATES = 2048;        // that the threads hold
 constexpr int WAVE_CANDIDATES = 1024;   // that a wave may find
 constexpr int ONE_WAVE = 512;           // candidates that one wave takes
-constexpr int AT_ONCE = 16;             // runs of 64 tokens that a wave has on their way
+constexpr int AT_ONCE = 16;             // runs of 64 tokens that a wave asks for at once
 
 struct RowShared {
     union {
@@ -898,7 +901,8 @@ struct WideShared {
 // The bins of a row are filled by `parts` workgroups, and whoever is the last goes on: the cuts; the part of the row in which u * total
 // lies, by the weights before the cut's bin in each part and the elements of that bin; the run of 1024 tokens, by the sums of what is
 // kept in the part's runs; the token in it.  All sums are of whole numbers, so that their order does not matter.  One CU reads a
-// row of 50 304 in 10 us, so that nothing but the part's runs is read twice.  22 to 30 us: bins 7, lists 5, cuts 4 each, the token 5.
+// row of 50 304 in 10 us (its loads wait for one another, see load4), so that nothing but the part's runs is read twice: unless the cut's bin has
+// more than 256 elements, of which there is no list, as among many equal logits (4 rows of 200 000 in bf16 with top_k 30 000: 426 us).  22 to 30 us: bins 7, lists 5, cuts 4 each, the token 5.
 template <typename T>
 __global__ __launch_bounds__(WIDE_THREADS) void sample_wide_kernel(Sampling p, int parts, char* shared_bins, char* shared_parts) {
     __shared__ WideShared s;
@@ -1120,7 +1124,7 @@ size_t sample_workspace(int rows, int vocab, bool cuts) {
 template <typename T>
 static void launch_typed(const Sampling& p, hipStream_t st) {
     const SampleRow at(p.vocab);
-    // as many waves as the chip holds at once, or so many fewer that all have the same number of runs
+    // 8192 waves, a few more than the chip holds at once (7 a SIMD), or so many fewer that all have the same number of runs
     const int64_t runs = (int64_t)p.rows * at.runs, each = (runs + 8191) / 8192, waves = (runs + each - 1) / each;
     EE_LAUNCH(sample_runs_kernel<T>, dim3((int)((waves + 3) / 4)), dim3(256), st, p, (int)each);
     const bool third = third_kernel(p.vocab, p.cuts());
